@@ -225,6 +225,68 @@ int vig_gate_prep_bwd_bf16(const void* g_fwd, const void* g_bwd, const void* dlo
 int vig_gate_prep_bwd_f32(const void* g_fwd, const void* g_bwd, const void* dlog_alpha_fwd, const void* dlog_alpha_bwd,
                           void* dg_fwd, void* dg_bwd, int B, int H, int L, int dk, float tau, void* stream);
 
+/* ---- Gated delta rule: the other token mixer with a matrix state ---------------------------------------------------
+ * For every (batch, head) unit, with S a dk x dv state, scalar gates alpha_t = exp(log_alpha_t) and step sizes beta_t,
+ *
+ *     S_t   = alpha_t S_{t-1} + beta_t k_t^T (v_t - alpha_t k_t S_{t-1})        (t = 1 .. L)
+ *     out_t = q_t S_t
+ *
+ * q, k: [B,H,L,dk]; v, out: [B,H,L,dv]; log_alpha, beta: [B,H,L], all of the call's element type (vig_gate_prep_* makes log_alpha
+ * from logits as it does for the mixer above).  Domain: log_alpha <= 0 (-inf forgets the state), beta finite.  For a state that stays
+ * bounded beta_t |k_t|^2 <= 2; nothing is normalised inside.  States are FP32 [B,H,dk,dv] in every call.
+ * state_in: S_0, or NULL for zero.  state_out: receives S_L, or NULL; may be state_in.
+ * reverse != 0: the same from the last token to the first (state_in comes behind token L, state_out is what stands at token 1), the
+ * other direction of a bidirectional mixer over the patch sequence.
+ * bf16: fp32 walks or tensor-core tiles by head size, states and sums in fp32.  f32: fp32 walks.  dk <= 128, dv <= 256.
+ * L == 0 with a state_out copies state_in (or zeros) there; tensors without elements may be NULL.
+ * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
+int vig_gdr_fwd_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
+                     const void* state_in, void* out, void* state_out,
+                     int B, int H, int L, int dk, int dv, int reverse, void* stream);
+int vig_gdr_fwd_f32(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
+                    const void* state_in, void* out, void* state_out,
+                    int B, int H, int L, int dk, int dv, int reverse, void* stream);
+/* Its gradient.  d_out: [B,H,L,dv]; d_state_out: gradient with respect to state_out (fp32) or NULL for zero.  Writes dq, dk_out
+ * [B,H,L,dk], dv_out [B,H,L,dv], dlog_alpha, dbeta [B,H,L] and, unless it is NULL, d_state_in (fp32; may be d_state_out).  Everything is
+ * computed anew from the inputs; scratch comes from the library's pool, stream-ordered.  Outputs must not overlap inputs or one
+ * another.  Errors: as vig_gdr_fwd_*. */
+int vig_gdr_bwd_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
+                     const void* state_in, const void* d_out, const void* d_state_out,
+                     void* dq, void* dk_out, void* dv_out, void* dlog_alpha, void* dbeta, void* d_state_in,
+                     int B, int H, int L, int dk, int dv, int reverse, void* stream);
+int vig_gdr_bwd_f32(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
+                    const void* state_in, const void* d_out, const void* d_state_out,
+                    void* dq, void* dk_out, void* dv_out, void* dlog_alpha, void* dbeta, void* d_state_in,
+                    int B, int H, int L, int dk, int dv, int reverse, void* stream);
+/* One token per unit: q, k [B,H,dk], v, out [B,H,dv], log_alpha, beta [B,H]; state (fp32 [B,H,dk,dv]) is updated in place.
+ * The same arithmetic as a call of L = 1 in fp32.  Errors: as vig_gdr_fwd_*. */
+int vig_gdr_step_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
+                      void* state, void* out, int B, int H, int dk, int dv, void* stream);
+int vig_gdr_step_f32(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
+                     void* state, void* out, int B, int H, int dk, int dv, void* stream);
+
+/* ---- Group norm with an activation, channels last ------------------------------------------------------------------
+ * What follows the depth-wise convolution: for every image and group of C / groups neighbouring channels, with mean and variance (of
+ * the population) over Hh x Ww x C / groups,  out = act((x - mean) / sqrt(var + eps) * weight + bias).
+ * x, out: [B, Hh, Ww, C]; weight, bias: [C] or NULL (1, 0); all of the call's element type.  mean, rstd: FP32 [B, groups], what the
+ * gradient needs, or NULL.  act: a vig_act (GELU is the exact one, by erf).  eps >= 0.  C must be a multiple of 8 (bf16) or 4 (fp32), at
+ * most 2^20, and of groups.  out may be x.  Images too large to stay on chip take scratch from the library's pool, stream-ordered.
+ * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
+typedef enum vig_act { VIG_ACT_NONE = 0, VIG_ACT_SILU = 1, VIG_ACT_GELU = 2 } vig_act;
+int vig_group_norm_bf16(const void* x, const void* weight, const void* bias, void* out, void* mean, void* rstd,
+                        int B, int Hh, int Ww, int C, int groups, float eps, int act, void* stream);
+int vig_group_norm_f32(const void* x, const void* weight, const void* bias, void* out, void* mean, void* rstd,
+                       int B, int Hh, int Ww, int C, int groups, float eps, int act, void* stream);
+/* Its gradient, from mean and rstd as the forward call left them: dx [B,Hh,Ww,C] (may be d_out or x), and dweight, dbias [C] of the
+ * call's type unless NULL (sums over all images, in a fixed order).  An empty call (B, Hh or Ww 0) clears dweight and dbias.
+ * Errors: as vig_group_norm_*. */
+int vig_group_norm_bwd_bf16(const void* x, const void* weight, const void* bias, const void* mean, const void* rstd,
+                            const void* d_out, void* dx, void* dweight, void* dbias,
+                            int B, int Hh, int Ww, int C, int groups, int act, void* stream);
+int vig_group_norm_bwd_f32(const void* x, const void* weight, const void* bias, const void* mean, const void* rstd,
+                           const void* d_out, void* dx, void* dweight, void* dbias,
+                           int B, int Hh, int Ww, int C, int groups, int act, void* stream);
+
 /* ---- Whole path on HOST buffers -------------------------------------------------------------------
  * Gate preparation followed by the BiGLA forward (Eq. 5 line 1 + Eq. 6) for callers whose data
  * lives in host memory.  All seven pointers are HOST pointers (pinned memory makes the copies

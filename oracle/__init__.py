@@ -12,3 +12,5 @@ from .oracle import (  # noqa: F401
 from .backward import bigla_bwd, gate_prep_bwd  # noqa: F401
 from .locality import dwconv3x3, gate_blend  # noqa: F401
 from .quadratic import bigla_quadratic  # noqa: F401
+from .delta_rule import gdr_bwd, gdr_fwd  # noqa: F401
+from .group_norm import group_norm, group_norm_bwd  # noqa: F401

@@ -23,6 +23,7 @@ VIG_DTYPE_BF16 = 1
 _lib = None
 _addr = {}    # of the entry points called through the native module
 _call = None  # its call()
+_native = None
 
 
 class VigError(RuntimeError):
@@ -33,7 +34,7 @@ class VigError(RuntimeError):
 
 def load() -> ctypes.CDLL:
     """Loads the CUDA library (built in-tree by paper_2405_18425_b200.build).  Raises if it is missing."""
-    global _lib, _call
+    global _lib, _call, _native
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise ImportError(
@@ -93,7 +94,16 @@ def load() -> ctypes.CDLL:
                      "vig_gate_prep_f32", "vig_bigla_fwd_gates_bf16", "vig_bigla_fwd_blend_bf16", "vig_dwconv3x3_bf16", "vig_dwconv3x3_f32",
                      "vig_bigla_bwd_bf16", "vig_bigla_bwd_f32", "vig_gate_prep_bwd_bf16", "vig_gate_prep_bwd_f32"):
             _addr[name] = ctypes.cast(getattr(lib, name), vp).value
-        _call = _binding_call.call
+        for stem, ptrs, ints in (("vig_gdr_fwd", 8, 6), ("vig_gdr_bwd", 14, 6), ("vig_gdr_step", 7, 4), ("vig_group_norm_bwd", 9, 6)):
+            for name in (stem + "_bf16", stem + "_f32"):
+                getattr(lib, name).argtypes = [vp] * ptrs + [ci] * ints + [vp]
+        for name in ("vig_group_norm_bf16", "vig_group_norm_f32"):
+            getattr(lib, name).argtypes = [vp] * 6 + [ci] * 5 + [cf, ci, vp]
+        for stem in ("vig_gdr_fwd", "vig_gdr_bwd", "vig_gdr_step", "vig_group_norm", "vig_group_norm_bwd"):
+            for name in (stem + "_bf16", stem + "_f32"):
+                getattr(lib, name).restype = ci
+                _addr[name] = ctypes.cast(getattr(lib, name), vp).value
+        _call, _native = _binding_call.call, _binding_call
         _lib = lib
     return _lib
 
@@ -232,6 +242,63 @@ def vig_gate_blend(o_local, gate2d_logits, o_global, out, stream=None):
     _check(getattr(load(), name)(o_local.data_ptr(), gate2d_logits.data_ptr(), o_global.data_ptr(), out.data_ptr(),
                                  out.numel(), _stream(stream)), name)
     return out
+
+
+# ---- gated delta rule, group norm: every tensor's device, type and shape is checked by the native module -------------------------
+VIG_ACTS = {"none": 0, "silu": 1, "gelu": 2}
+
+
+def _layer_call(name, stream, *args):
+    if _lib is None:
+        load()
+    stem = "vig_" + name
+    status = getattr(_native, name)(_addr[stem + "_bf16"], _addr[stem + "_f32"], None if stream is None else _stream(stream), *args)
+    if status != VIG_OK:
+        raise VigError(status, stem)
+
+
+def _act(act) -> int:
+    if act is None:
+        return 0
+    if isinstance(act, str):
+        if act not in VIG_ACTS:
+            raise ValueError(f"activation {act!r}: one of {sorted(VIG_ACTS)} expected")
+        return VIG_ACTS[act]
+    return int(act)
+
+
+def vig_gdr_fwd(q, k, v, log_alpha, beta, out, state_in=None, state_out=None, reverse=False, stream=None):
+    """Gated delta rule over whole sequences.  q, k: [B,H,L,dk]; v, out: [B,H,L,dv]; log_alpha, beta: [B,H,L]; one dtype (bf16 or
+    fp32).  state_in, state_out: fp32 [B,H,dk,dv] or None.  reverse: from the last token to the first."""
+    _layer_call("gdr_fwd", stream, reverse, q, k, v, log_alpha, beta, state_in, out, state_out)
+    return out
+
+
+def vig_gdr_bwd(q, k, v, log_alpha, beta, d_out, dq, dk, dv, dlog_alpha, dbeta, state_in=None, d_state_out=None, d_state_in=None, reverse=False,
+                stream=None):
+    """Gradient of vig_gdr_fwd for d_out (and d_state_out, of the final state); writes and returns the five gradient tensors, and
+    d_state_in where one is given."""
+    _layer_call("gdr_bwd", stream, reverse, q, k, v, log_alpha, beta, state_in, d_out, d_state_out, dq, dk, dv, dlog_alpha, dbeta, d_state_in)
+    return dq, dk, dv, dlog_alpha, dbeta
+
+
+def vig_gdr_step(q, k, v, log_alpha, beta, state, out, stream=None):
+    """One token of the gated delta rule: q, k [B,H,dk], v, out [B,H,dv], log_alpha, beta [B,H]; state (fp32 [B,H,dk,dv]) in place."""
+    _layer_call("gdr_step", stream, q, k, v, log_alpha, beta, state, out)
+    return out
+
+
+def vig_group_norm(x, weight, bias, out, groups, eps=1e-5, act="none", mean=None, rstd=None, stream=None):
+    """Group norm with an activation ("none", "silu", "gelu") over channels-last images: x, out [B,Hh,Ww,C]; weight, bias [C] or None;
+    mean, rstd: fp32 [B, groups] for the gradient, or None."""
+    _layer_call("group_norm", stream, groups, eps, _act(act), x, weight, bias, out, mean, rstd)
+    return out
+
+
+def vig_group_norm_bwd(x, weight, bias, mean, rstd, d_out, dx, dweight, dbias, groups, act="none", stream=None):
+    """Gradient of vig_group_norm from the mean and rstd it left; dweight, dbias may be None."""
+    _layer_call("group_norm_bwd", stream, groups, _act(act), x, weight, bias, mean, rstd, d_out, dx, dweight, dbias)
+    return dx, dweight, dbias
 
 
 def _host_ptr(a) -> int:

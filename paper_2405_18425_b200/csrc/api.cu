@@ -138,7 +138,7 @@ static cudaMemPool_t device_pool() {
     }
     return pools[dev];
 }
-static cudaError_t pool_alloc(void** p, size_t bytes, cudaStream_t stream) {
+cudaError_t pool_alloc(void** p, size_t bytes, cudaStream_t stream) {
     cudaMemPool_t pool = device_pool();
     return pool ? cudaMallocFromPoolAsync(p, bytes, pool, stream) : cudaErrorMemoryAllocation;
 }

@@ -1,0 +1,171 @@
+// C-ABI entry points of the gated delta rule and of the group norm: argument validation, dispatch, scratch.
+#include <cmath>
+
+#include "gdr.h"
+
+namespace vig {
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }   // (NULL is)
+
+template <typename... P>
+bool any_null(P... p) { return ((p == nullptr) || ...); }
+template <typename... P>
+bool all_aligned(P... p) { return (aligned16(p) && ...); }
+
+int status_of(cudaError_t e) { return e == cudaSuccess ? VIG_OK : VIG_ERR_CUDA; }
+
+// A call without tokens: what comes out is what went in.
+int pass_state(const void* in, void* out, long long units, int dk, int dv, cudaStream_t stream) {
+    const size_t bytes = (size_t)units * dk * dv * sizeof(float);
+    if (!out || out == in || bytes == 0) return VIG_OK;
+    return status_of(in ? cudaMemcpyAsync(out, in, bytes, cudaMemcpyDeviceToDevice, stream) : cudaMemsetAsync(out, 0, bytes, stream));
+}
+
+int check_sizes(int B, int H, int L, int dk, int dv) {
+    if (B < 0 || H < 0 || L < 0 || dk < 1 || dv < 1) return VIG_ERR_BAD_DIM;
+    if (!gdr_supported(dk, dv)) return VIG_ERR_UNSUPPORTED;
+    // grids count units, or units times pieces of 64 tokens
+    if ((long long)B * H * (L / 64 + 1LL) > 0x7fffffffLL) return VIG_ERR_UNSUPPORTED;
+    return VIG_OK;
+}
+
+template <typename T>
+int gdr_fwd_impl(const void* q, const void* k, const void* v, const void* la, const void* beta, const void* state_in, void* out, void* state_out, int B,
+                 int H, int L, int dk, int dv, int reverse, cudaStream_t stream) {
+    if (B != 0 && H != 0 && L != 0 && any_null(q, k, v, la, beta, out)) return VIG_ERR_NULL_POINTER;   // (tensors without elements may have no address)
+    if (B < 0 || H < 0 || L < 0 || dk < 1 || dv < 1) return VIG_ERR_BAD_DIM;
+    if (!all_aligned(q, k, v, la, beta, state_in, out, state_out)) return VIG_ERR_MISALIGNED;
+    const int st = check_sizes(B, H, L, dk, dv);
+    if (st != VIG_OK) return st;
+    const long long units = (long long)B * H;
+    if (units == 0) return VIG_OK;
+    if (L == 0) return pass_state(state_in, state_out, units, dk, dv, stream);
+    Gdr<T> a = {};
+    a.q = (const T*)q; a.k = (const T*)k; a.v = (const T*)v; a.la = (const T*)la; a.beta = (const T*)beta;
+    a.state_in = (const float*)state_in; a.out = (T*)out; a.state_out = (float*)state_out;
+    a.units = units; a.L = L; a.dk = dk; a.dv = dv; a.reverse = reverse != 0;
+    return status_of(launch_gdr_walk_fwd<T>(a, stream));
+}
+
+template <typename T>
+int gdr_bwd_impl(const void* q, const void* k, const void* v, const void* la, const void* beta, const void* state_in, const void* d_out,
+                 const void* d_state_out, void* dq, void* dk_out, void* dv_out, void* dla, void* dbeta, void* d_state_in, int B, int H, int L, int dk,
+                 int dv, int reverse, cudaStream_t stream) {
+    if (B != 0 && H != 0 && L != 0 && (any_null(q, k, v, la, beta, d_out) || any_null(dq, dk_out, dv_out, dla, dbeta))) return VIG_ERR_NULL_POINTER;
+    if (B < 0 || H < 0 || L < 0 || dk < 1 || dv < 1) return VIG_ERR_BAD_DIM;
+    if (!all_aligned(q, k, v, la, beta, state_in, d_out, d_state_out) || !all_aligned(dq, dk_out, dv_out, dla, dbeta, d_state_in)) return VIG_ERR_MISALIGNED;
+    int st = check_sizes(B, H, L, dk, dv);
+    if (st != VIG_OK) return st;
+    const long long units = (long long)B * H;
+    if (units == 0) return VIG_OK;
+    if (L == 0) return pass_state(d_state_out, d_state_in, units, dk, dv, stream);
+    Gdr<T> a = {};
+    a.q = (const T*)q; a.k = (const T*)k; a.v = (const T*)v; a.la = (const T*)la; a.beta = (const T*)beta; a.d_out = (const T*)d_out;
+    a.state_in = (const float*)state_in; a.d_state_out = (const float*)d_state_out;
+    a.dq = (T*)dq; a.dk_out = (T*)dk_out; a.dv_out = (T*)dv_out; a.dla = (T*)dla; a.dbeta = (T*)dbeta; a.d_state_in = (float*)d_state_in;
+    a.units = units; a.L = L; a.dk = dk; a.dv = dv; a.reverse = reverse != 0;
+    void* scratch = nullptr;
+    if (pool_alloc(&scratch, gdr_walk_bwd_scratch_bytes<T>(units, L, dk, dv), stream) != cudaSuccess) return VIG_ERR_CUDA;
+    st = status_of(launch_gdr_walk_bwd<T>(a, scratch, stream));
+    if (cudaFreeAsync(scratch, stream) != cudaSuccess && st == VIG_OK) st = VIG_ERR_CUDA;
+    return st;
+}
+
+template <typename T>
+int gdr_step_impl(const void* q, const void* k, const void* v, const void* la, const void* beta, void* state, void* out, int B, int H, int dk, int dv,
+                  cudaStream_t stream) {
+    if (B != 0 && H != 0 && any_null(q, k, v, la, beta, state, out)) return VIG_ERR_NULL_POINTER;
+    if (B < 0 || H < 0 || dk < 1 || dv < 1) return VIG_ERR_BAD_DIM;
+    if (!all_aligned(q, k, v, la, beta, state, out)) return VIG_ERR_MISALIGNED;
+    const int st = check_sizes(B, H, 1, dk, dv);
+    if (st != VIG_OK) return st;
+    if (B == 0 || H == 0) return VIG_OK;
+    return status_of(launch_gdr_step<T>((const T*)q, (const T*)k, (const T*)v, (const T*)la, (const T*)beta, (float*)state, (T*)out, (long long)B * H,
+                                        dk, dv, stream));
+}
+
+int check_norm(int B, int Hh, int Ww, int C, int groups, int act, size_t elem) {
+    if (B < 0 || Hh < 0 || Ww < 0 || C < 1 || groups < 1) return VIG_ERR_BAD_DIM;
+    if (act != VIG_ACT_NONE && act != VIG_ACT_SILU && act != VIG_ACT_GELU) return VIG_ERR_UNSUPPORTED;
+    if ((long long)Hh * Ww > 0x7fffffffLL || !group_norm_supported(B, Hh * Ww, C, groups, elem)) return VIG_ERR_UNSUPPORTED;
+    return VIG_OK;
+}
+
+template <typename T>
+int group_norm_impl(const void* x, const void* weight, const void* bias, void* out, void* mean, void* rstd, int B, int Hh, int Ww, int C, int groups,
+                    float eps, int act, cudaStream_t stream) {
+    if (B != 0 && Hh != 0 && Ww != 0 && any_null(x, out)) return VIG_ERR_NULL_POINTER;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return VIG_ERR_BAD_DIM;
+    if (B < 0 || Hh < 0 || Ww < 0 || C < 1 || groups < 1) return VIG_ERR_BAD_DIM;
+    if (!all_aligned(x, weight, bias, out, mean, rstd)) return VIG_ERR_MISALIGNED;
+    int st = check_norm(B, Hh, Ww, C, groups, act, sizeof(T));
+    if (st != VIG_OK) return st;
+    const int HW = Hh * Ww;
+    if (B == 0 || HW == 0) return VIG_OK;
+    const size_t need = group_norm_scratch_bytes(B, HW, C, groups, sizeof(T), false);
+    void* scratch = nullptr;
+    if (need > 0 && pool_alloc(&scratch, need, stream) != cudaSuccess) return VIG_ERR_CUDA;
+    st = status_of(launch_group_norm<T>((const T*)x, (const T*)weight, (const T*)bias, (T*)out, (float*)mean, (float*)rstd, B, HW, C, groups, eps, act,
+                                        scratch, stream));
+    if (need > 0 && cudaFreeAsync(scratch, stream) != cudaSuccess && st == VIG_OK) st = VIG_ERR_CUDA;
+    return st;
+}
+
+template <typename T>
+int group_norm_bwd_impl(const void* x, const void* weight, const void* bias, const void* mean, const void* rstd, const void* d_out, void* dx,
+                        void* dweight, void* dbias, int B, int Hh, int Ww, int C, int groups, int act, cudaStream_t stream) {
+    if (B != 0 && Hh != 0 && Ww != 0 && (any_null(x, mean, rstd, d_out) || !dx)) return VIG_ERR_NULL_POINTER;
+    if (B < 0 || Hh < 0 || Ww < 0 || C < 1 || groups < 1) return VIG_ERR_BAD_DIM;
+    if (!all_aligned(x, weight, bias, mean, rstd, d_out) || !all_aligned(dx, dweight, dbias)) return VIG_ERR_MISALIGNED;
+    int st = check_norm(B, Hh, Ww, C, groups, act, sizeof(T));
+    if (st != VIG_OK) return st;
+    const int HW = Hh * Ww;
+    if (B == 0 || HW == 0) {
+        if (dweight && cudaMemsetAsync(dweight, 0, C * sizeof(T), stream) != cudaSuccess) return VIG_ERR_CUDA;
+        if (dbias && cudaMemsetAsync(dbias, 0, C * sizeof(T), stream) != cudaSuccess) return VIG_ERR_CUDA;
+        return VIG_OK;
+    }
+    void* scratch = nullptr;
+    if (pool_alloc(&scratch, group_norm_scratch_bytes(B, HW, C, groups, sizeof(T), true), stream) != cudaSuccess) return VIG_ERR_CUDA;
+    st = status_of(launch_group_norm_bwd<T>((const T*)x, (const T*)weight, (const T*)bias, (const float*)mean, (const float*)rstd, (const T*)d_out,
+                                            (T*)dx, (T*)dweight, (T*)dbias, B, HW, C, groups, act, scratch, stream));
+    if (cudaFreeAsync(scratch, stream) != cudaSuccess && st == VIG_OK) st = VIG_ERR_CUDA;
+    return st;
+}
+
+}  // namespace
+}  // namespace vig
+
+using namespace vig;
+
+extern "C" {
+
+#define VIG_LAYERS(T, NAME)                                                                                                                      \
+    int vig_gdr_fwd_##NAME(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta, const void* state_in, void* out, \
+                           void* state_out, int B, int H, int L, int dk, int dv, int reverse, void* stream) {                                     \
+        return gdr_fwd_impl<T>(q, k, v, log_alpha, beta, state_in, out, state_out, B, H, L, dk, dv, reverse, (cudaStream_t)stream);               \
+    }                                                                                                                                            \
+    int vig_gdr_bwd_##NAME(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta, const void* state_in,            \
+                           const void* d_out, const void* d_state_out, void* dq, void* dk_out, void* dv_out, void* dlog_alpha, void* dbeta,       \
+                           void* d_state_in, int B, int H, int L, int dk, int dv, int reverse, void* stream) {                                    \
+        return gdr_bwd_impl<T>(q, k, v, log_alpha, beta, state_in, d_out, d_state_out, dq, dk_out, dv_out, dlog_alpha, dbeta, d_state_in, B, H, L, \
+                               dk, dv, reverse, (cudaStream_t)stream);                                                                           \
+    }                                                                                                                                            \
+    int vig_gdr_step_##NAME(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta, void* state, void* out, int B,  \
+                            int H, int dk, int dv, void* stream) {                                                                               \
+        return gdr_step_impl<T>(q, k, v, log_alpha, beta, state, out, B, H, dk, dv, (cudaStream_t)stream);                                        \
+    }                                                                                                                                            \
+    int vig_group_norm_##NAME(const void* x, const void* weight, const void* bias, void* out, void* mean, void* rstd, int B, int Hh, int Ww,      \
+                              int C, int groups, float eps, int act, void* stream) {                                                             \
+        return group_norm_impl<T>(x, weight, bias, out, mean, rstd, B, Hh, Ww, C, groups, eps, act, (cudaStream_t)stream);                        \
+    }                                                                                                                                            \
+    int vig_group_norm_bwd_##NAME(const void* x, const void* weight, const void* bias, const void* mean, const void* rstd, const void* d_out,     \
+                                  void* dx, void* dweight, void* dbias, int B, int Hh, int Ww, int C, int groups, int act, void* stream) {        \
+        return group_norm_bwd_impl<T>(x, weight, bias, mean, rstd, d_out, dx, dweight, dbias, B, Hh, Ww, C, groups, act, (cudaStream_t)stream);   \
+    }
+
+VIG_LAYERS(__nv_bfloat16, bf16)
+VIG_LAYERS(float, f32)
+
+}  // extern "C"

@@ -139,6 +139,9 @@ struct HostCopy {
 bool host_copy_usable(const void* host, size_t bytes);   // all of it pinned and mapped, aligned
 cudaError_t launch_host_copy(const HostCopy* copies, int n, int max_blocks, cudaStream_t stream);
 
+// Scratch from the library's own memory pool of the current device, stream-ordered (cudaFreeAsync gives it back).
+cudaError_t pool_alloc(void** p, size_t bytes, cudaStream_t stream);
+
 // Launch with programmatic stream serialization: the kernel's prologue (everything before its pdl_wait) may overlap
 // the tail of the kernel before it in the stream.  cluster: blocks of a cluster (along x; the grid is a multiple of it).
 template <typename... KArgs, typename... Args>
