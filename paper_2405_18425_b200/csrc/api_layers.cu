@@ -2,6 +2,7 @@
 #include <cmath>
 
 #include "gdr.h"
+#include "test_hooks.h"
 
 namespace vig {
 namespace {
@@ -45,6 +46,8 @@ int gdr_fwd_impl(const void* q, const void* k, const void* v, const void* la, co
     a.q = (const T*)q; a.k = (const T*)k; a.v = (const T*)v; a.la = (const T*)la; a.beta = (const T*)beta;
     a.state_in = (const float*)state_in; a.out = (T*)out; a.state_out = (float*)state_out;
     a.units = units; a.L = L; a.dk = dk; a.dv = dv; a.reverse = reverse != 0;
+    if constexpr (sizeof(T) == 2)
+        if (gdr_chunk_supported(dk, dv) && kernel_preference() != VIG_TEST_KERNEL_SIMT) return status_of(launch_gdr_chunk_fwd(a, stream));
     return status_of(launch_gdr_walk_fwd<T>(a, stream));
 }
 

@@ -28,6 +28,10 @@ size_t gdr_walk_bwd_scratch_bytes(long long units, int L, int dk, int dv);
 template <typename T>
 cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t stream);
 
+// ---- forward in chunks on the tensor cores: head sizes that are multiples of eight ----
+bool gdr_chunk_supported(int dk, int dv);
+cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, cudaStream_t stream);
+
 // ---- one token: state updated in place ----
 template <typename T>
 cudaError_t launch_gdr_step(const T* q, const T* k, const T* v, const T* la, const T* beta, float* state, T* out, long long units, int dk, int dv,
