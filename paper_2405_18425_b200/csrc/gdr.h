@@ -1,5 +1,7 @@
 // Internal declarations of the gated delta rule and of the group norm (not part of the C ABI).
 #pragma once
+#include <cuda_fp16.h>
+
 #include "vig_internal.h"
 
 namespace vig {
@@ -31,6 +33,45 @@ cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t str
 // ---- forward in chunks on the tensor cores: head sizes that are multiples of eight ----
 bool gdr_chunk_supported(int dk, int dv);
 cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, cudaStream_t stream);
+
+// What the two walks of the gradient keep, fp16 under powers of two per column; dvp: dv to sixteen, DKP: dk as the kernels pad it.
+struct GdrKept {
+    __half* w;         // [units][chunks][64][dvp]: W = w y; rows behind a call's last sixteen are not written
+    __half* du;        // [units][chunks][64][dvp]: dU = du z 2^e, e of the key's row
+    __half *S, *A;     // transposed, [units][chunks + 1][dvp][DKP] before each chunk (= S y) and behind the last; [units][chunks][dvp][DKP]: what
+                       // arrives behind each chunk (= A z)
+    float *y, *z;      // [units][chunks + 1][dvp], [units][chunks][dvp]
+    int *lost, *lost_grad;   // [units][dvp / 16], [units][chunks]: something left the range of fp16
+    int dvp;
+    // Sixteen columns of a state, as packed for an A operand.
+    template <int DKP>
+    __device__ __forceinline__ void keep_state(__half* to, float* scales, long long at, int col0, const uint32_t (*sa)[4], const float (&back)[2], int g,
+                                               int c) const {
+        __half* const p = to + (at * dvp + col0 + g) * DKP + 2 * c;
+#pragma unroll
+        for (int s = 0; s < DKP / 16; ++s) {
+            *reinterpret_cast<uint32_t*>(p + s * 16) = sa[s][0];
+            *reinterpret_cast<uint32_t*>(p + 8 * DKP + s * 16) = sa[s][1];
+            *reinterpret_cast<uint32_t*>(p + s * 16 + 8) = sa[s][2];
+            *reinterpret_cast<uint32_t*>(p + 8 * DKP + s * 16 + 8) = sa[s][3];
+        }
+        if (c == 0) {
+            scales[at * dvp + col0 + g] = back[0];
+            scales[at * dvp + col0 + g + 8] = back[1];
+        }
+    }
+};
+int gdr_padded_columns(int dv);   // dvp
+int gdr_padded_keys(int dk);      // DKP
+bool gdr_grad_supported(int dk, int dv);
+size_t gdr_grad_scratch_bytes(long long units, int L, int dk, int dv);
+// The whole gradient: both walks, the chunks, and the fp32 walks for units that left the range.
+cudaError_t launch_gdr_chunk_bwd(const Gdr<__nv_bfloat16>& a, void* scratch, cudaStream_t stream);
+cudaError_t launch_gdr_grad(const Gdr<__nv_bfloat16>& a, const GdrKept& kept, cudaStream_t stream);
+// Redoes every unit of which a flag is set (first: `per` flags a unit, second: `chunks`) by the fp32 walks, `slots` at a time.
+size_t gdr_repair_slot_bytes(int L, int dk, int dv);
+cudaError_t launch_gdr_repair(const Gdr<__nv_bfloat16>& a, const int* first, int per, const int* second, int chunks, void* scratch, int slots, cudaStream_t stream);
+cudaError_t launch_gdr_chunk_walks(const Gdr<__nv_bfloat16>& a, const GdrKept& kept, cudaStream_t stream);
 
 // ---- one token: state updated in place ----
 template <typename T>

@@ -317,12 +317,9 @@ __global__ void __launch_bounds__(256) gdr_rows_grad_kernel(Gdr<T> a, Scratch s,
 
 // ---- what is left per token: a block per 64 tokens of a unit -----------------------------------------------------------------
 template <typename T>
-__global__ void __launch_bounds__(256) gdr_finish_kernel(Gdr<T> a, Scratch s) {
+__device__ void finish(const Gdr<T>& a, const Scratch& s, long long unit, int border) {
     __shared__ float E[kBorder], part[8];
-    pdl_wait();
-    pdl_launch_dependents();
-    const long long unit = blockIdx.x / borders(a.L);
-    const int border = blockIdx.x % borders(a.L), t0 = border * kBorder, nt = min(kBorder, a.L - t0);
+    const int t0 = border * kBorder, nt = min(kBorder, a.L - t0);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const long long plane = (long long)a.dk * a.dv, at = (unit * borders(a.L) + border) * plane;
     float sum = 0.f;
@@ -364,6 +361,55 @@ __global__ void __launch_bounds__(256) gdr_finish_kernel(Gdr<T> a, Scratch s) {
             // a gate that leaves nothing (what the sums come to there is rounding), the first of a sequence without an initial state
             run = expf(to_f(a.la[r])) == 0.f || (t0 + t == 0 && !a.state_in) ? 0.f : run + E[t];
             a.dla[r] = from_f<T>(run);
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) gdr_finish_kernel(Gdr<T> a, Scratch s) {
+    pdl_wait();
+    pdl_launch_dependents();
+    finish<T>(a, s, blockIdx.x / borders(a.L), blockIdx.x % borders(a.L));
+}
+
+// Behind the gradient in chunks: units of which something left the range of fp16, whole, a block at a time.  Without any the block ends
+// at once.
+constexpr int kRepairR = 32, kRepairG = 4, kRepairOwners = 64;
+__global__ void __launch_bounds__(256) gdr_repair_kernel(Gdr<__nv_bfloat16> a, Scratch s, const int* first, int per, const int* second, int chunks, int* status) {
+    using T = __nv_bfloat16;
+    extern __shared__ __align__(16) float sm[];
+    pdl_wait();
+    pdl_launch_dependents();
+    auto flagged = [&](long long unit, int from, int step) {
+        int any = 0;
+        for (int i = from; i < per + chunks; i += step) any |= i < per ? first[unit * per + i] : second[unit * chunks + i - per];
+        return any;
+    };
+    int any = 0;
+    for (long long unit = blockIdx.x + (long long)(threadIdx.x >> 5) * gridDim.x; unit < a.units; unit += 8LL * gridDim.x) any |= flagged(unit, threadIdx.x & 31, 32);
+    if (!__syncthreads_or(any)) return;
+    for (long long unit = blockIdx.x; unit < a.units; unit += gridDim.x) {
+        if (!__syncthreads_or(flagged(unit, threadIdx.x, 256))) continue;
+        if (threadIdx.x == 0) atomicAdd(status + 1, 1);
+        // this block's slot, as the walks address it
+        const long long v = ((long long)blockIdx.x - unit) * a.L * a.dv, k = ((long long)blockIdx.x - unit) * a.L * a.dk,
+                        p = ((long long)blockIdx.x - unit) * borders(a.L) * a.dk * a.dv;
+        const Scratch mine = {s.w + v, s.du + v, s.dk1 + k, s.dk2 + k, s.dq + k, s.S + p, s.A + p};
+        for (int j = 0; j < a.dv; j += kRepairOwners) {
+            walk_columns<T, kRepairR, kRepairG, false, true>(a, mine, sm, unit, j, kRepairOwners);
+            __syncthreads();
+            walk_columns<T, kRepairR, kRepairG, true, true>(a, mine, sm, unit, j, kRepairOwners);
+            __syncthreads();
+        }
+        for (int i = 0; i < a.dk; i += kRepairOwners) {
+            walk_rows<T, kRepairR, kRepairG, false>(a, mine, sm, unit, i, kRepairOwners);
+            __syncthreads();
+            walk_rows<T, kRepairR, kRepairG, true>(a, mine, sm, unit, i, kRepairOwners);
+            __syncthreads();
+        }
+        for (int b = 0; b < borders(a.L); ++b) {
+            finish<T>(a, mine, unit, b);
+            __syncthreads();
         }
     }
 }
@@ -466,6 +512,20 @@ cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t str
     if (e != cudaSuccess) return e;
     count_launch(3);
     return launch_pdl(gdr_finish_kernel<T>, dim3((unsigned)(a.units * borders(a.L))), dim3(256), 0, stream, a, s);
+}
+
+size_t gdr_repair_slot_bytes(int L, int dk, int dv) { return gdr_walk_bwd_scratch_bytes<__nv_bfloat16>(1, L, dk, dv); }
+cudaError_t launch_gdr_repair(const Gdr<__nv_bfloat16>& a, const int* first, int per, const int* second, int chunks, void* scratch, int slots, cudaStream_t stream) {
+    int* status = device_status_ptr();
+    if (!status) return cudaErrorUnknown;
+    size_t total;
+    const Scratch s = cut_scratch<__nv_bfloat16>((char*)scratch, &a, slots, a.L, a.dk, a.dv, &total);
+    constexpr int DP = kRepairR * kRepairG;
+    const size_t smem = walk_smem<3, DP>(kRepairOwners);
+    cudaError_t e = allow_smem(gdr_repair_kernel, smem);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    return launch_pdl(gdr_repair_kernel, dim3(slots), dim3(kRepairG * kRepairOwners), smem, stream, a, s, first, per, second, chunks, status);
 }
 
 template cudaError_t launch_gdr_walk_fwd<float>(const Gdr<float>&, cudaStream_t);

@@ -104,6 +104,64 @@ def test_values_of_other_magnitudes(dtype, scale):
     check([("out", out, ref), ("state", last, ref_last)], _terms(150, 32, 64), dtype == "bf16")
 
 
+@pytest.mark.parametrize("parallel", [False, True])
+@pytest.mark.parametrize("size", [(1, 2, 12, 16, 32), (2, 2, 20, 24, 48), (1, 1, 10, 64, 128)], ids=str)
+def test_keys_beyond_unit_length(size, parallel):
+    """beta |k|^2 around 8.  Parallel keys: the state grows about seven times a token, 10^9 and more in all, beyond what fp16 tiles hold; those
+    units are redone in fp32 walks.  Errors grow with the state and stay relative to it; the comparison is token by token (bf16: 2^-7, as
+    everywhere)."""
+    d = gdr_inputs(*size, "bf16", seed=15, states=True)
+    if parallel:
+        d["k"] = torch.nn.functional.normalize(d["k"].float() * 0.1 + d["k"][:, :, :1].float(), dim=-1)
+        d["beta"].fill_(0.5)   # (steps drawn near 1 / 16 would cancel the state instead)
+    d["k"] = (d["k"].float() * 4).bfloat16()
+    torch.cuda.synchronize()
+    vig.vig_test_take_fallback_count()
+    out, last = gdr_forward(d)
+    ref, ref_last = gdr_oracle(d)
+    for t in range(size[2]):
+        assert off(out[:, :, t], ref[:, :, t]) <= 2.0 ** -7, t
+    assert off(last, ref_last) <= 2.0 ** -15
+    taken = vig.vig_test_take_fallback_count()
+    got, want = gdr_gradient(d), gdr_oracle_gradient(d)
+    for name, g, w in zip(("dq", "dk", "dv", "dlog_alpha", "dbeta", "d_state"), got, want):
+        assert off(g, w) <= 2.0 ** -7, name
+    if parallel:
+        assert taken > 0 and vig.vig_test_take_fallback_count() > 0
+
+
+def test_in_range_inputs_stay_on_the_tiles():
+    torch.cuda.synchronize()
+    vig.vig_test_take_fallback_count()
+    for size in SIZES:
+        d = gdr_inputs(*size, "bf16", seed=16, gate_mean=2.0, states=True)
+        gdr_forward(d)
+        gdr_gradient(d)
+    assert vig.vig_test_take_fallback_count() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinities_and_nan_stay_in_their_columns_and_behind_their_tokens(dtype):
+    """A value that is not finite reaches its column from its token on, a key, gate or step the whole unit from its token on (and the
+    token's own read-out), nothing before and no other unit."""
+    for name, at, column in (("v", (0, 0, 37, 5), 5), ("v", (0, 1, 3, 0), 0), ("k", (0, 0, 70, 2), None), ("log_alpha", (0, 1, 20), None), ("beta", (0, 0, 18), None)):
+        for bad in (float("nan"), float("inf")):
+            if name == "log_alpha" and bad > 0:
+                continue
+            d = gdr_inputs(1, 3, 100, 16, 32, dtype, seed=17, gate_mean=2.0)
+            clean, _ = gdr_forward(d)
+            d[name][at] = bad
+            out, _ = gdr_forward(d)
+            same = torch.ones_like(out, dtype=torch.bool)
+            u, t = at[1], at[2]
+            if column is None:
+                same[0, u, t:] = False
+            else:
+                same[0, u, t:, column] = False
+            assert torch.allclose(out[same].float(), clean[same].float(), rtol=2.0 ** -6, atol=2.0 ** -6 * float(clean.float().abs().max())), (name, at, bad)
+            assert not torch.isfinite(out[~same]).any(), (name, at, bad)
+
+
 def test_correlated_keys():
     """Keys that are nearly one another: the triangular systems of a chunk are as ill-conditioned as unit keys make them."""
     for dtype in ("bf16", "f32"):
