@@ -35,39 +35,93 @@ __device__ __forceinline__ void widen16(const uint4& r, float (&f)[8], const __n
         f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ uint4 narrow16(const float (&f)[4], const float*) {
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-}
-__device__ __forceinline__ uint4 narrow16(const float (&f)[8], const __nv_bfloat16*) {
-    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-}
 __device__ __forceinline__ float one(const float* p, long long i, float none) { return p ? p[i] : none; }
 __device__ __forceinline__ float one(const __nv_bfloat16* p, long long i, float none) { return p ? __bfloat162float(p[i]) : none; }
 __device__ __forceinline__ void put(float* p, long long i, float x) { p[i] = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, long long i, float x) { p[i] = __float2bfloat16_rn(x); }
 
-// FAST (results rounded to bf16): e^-z and the quotient from the special-function unit, relative error below 1e-6.
+// The same as pairs of fp32: two values an instruction (all of it is issue-bound otherwise: 42 instructions a value, 94 us for 64 x 56 x 56 x 96).
+__device__ __forceinline__ void widen16(const uint4& r, f32x2 (&f)[2], const float*) {
+    f[0] = pack2(__uint_as_float(r.x), __uint_as_float(r.y));
+    f[1] = pack2(__uint_as_float(r.z), __uint_as_float(r.w));
+}
+__device__ __forceinline__ void widen16(const uint4& r, f32x2 (&f)[4], const __nv_bfloat16*) {
+    const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = pack2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+}
+__device__ __forceinline__ uint4 narrow16(const f32x2 (&f)[2], const float*) {
+    float a, b, c, d;
+    unpack2(f[0], a, b);
+    unpack2(f[1], c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+}
+__device__ __forceinline__ uint4 narrow16(const f32x2 (&f)[4], const __nv_bfloat16*) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a, b;
+        unpack2(f[i], a, b);
+        u[i] = pack_bf16(a, b);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+__device__ __forceinline__ f32x2 both(float x) { return pack2(x, x); }
+__device__ __forceinline__ f32x2 fsub2(f32x2 a, f32x2 b) { return ffma2(b, both(-1.f), a); }
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// FAST (results rounded to bf16): e^-z and the reciprocal from the special-function unit, relative error below 1e-6.
 template <bool FAST>
-__device__ __forceinline__ float sigmoid(float z) {
-    if constexpr (FAST) return __fdividef(1.f, 1.f + ex2(-z * 1.4426950408889634f));   // (1 + inf: 0, as __fdividef has it from 2^126 on)
-    else return 1.f / (1.f + expf(-z));
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 z) {
+    if constexpr (FAST) {
+        float a, b;
+        unpack2(fmul2(z, both(-1.4426950408889634f)), a, b);
+        unpack2(fadd2(pack2(ex2(a), ex2(b)), both(1.f)), a, b);
+        return pack2(rcp_approx(a), rcp_approx(b));   // (of infinity: 0)
+    } else {
+        float a, b;
+        unpack2(z, a, b);
+        return pack2(1.f / (1.f + expf(-a)), 1.f / (1.f + expf(-b)));
+    }
+}
+__device__ __forceinline__ float gelu_cdf(float z) { return 0.5f * erfcf(-0.70710678118654752f * z); }
+template <int ACT, bool FAST>
+__device__ __forceinline__ f32x2 act2(f32x2 z) {
+    if constexpr (ACT == kActSilu) return fmul2(z, sigmoid2<FAST>(z));
+    else if constexpr (ACT == kActGelu) {
+        float a, b;
+        unpack2(z, a, b);
+        return pack2(a * gelu_cdf(a), b * gelu_cdf(b));
+    } else return z;
 }
 template <int ACT, bool FAST>
-__device__ __forceinline__ float act(float z) {
-    if constexpr (ACT == kActSilu) return z * sigmoid<FAST>(z);
-    else if constexpr (ACT == kActGelu) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-    else return z;
-}
-template <int ACT, bool FAST>
-__device__ __forceinline__ float slope(float z) {
+__device__ __forceinline__ f32x2 slope2(f32x2 z) {
     if constexpr (ACT == kActSilu) {
-        const float s = sigmoid<FAST>(z);
-        return s * fmaf(z, 1.f - s, 1.f);
+        const f32x2 s = sigmoid2<FAST>(z);
+        return fmul2(s, ffma2(z, fsub2(both(1.f), s), both(1.f)));
     } else if constexpr (ACT == kActGelu) {
-        const float phi = 0.3989422804014327f * (FAST ? ex2(-0.7213475204444817f * z * z) : expf(-0.5f * z * z));
-        return fmaf(z, phi, 0.5f * erfcf(-0.70710678118654752f * z));
-    } else return 1.f;
+        float a, b;
+        unpack2(z, a, b);
+        auto one_slope = [](float x) {
+            const float phi = 0.3989422804014327f * (FAST ? ex2(-0.7213475204444817f * x * x) : expf(-0.5f * x * x));
+            return fmaf(x, phi, gelu_cdf(x));
+        };
+        return pack2(one_slope(a), one_slope(b));
+    } else return both(1.f);
 }
+
+// x / d without the two dozen instructions of a division: x below 2^16, d from the host.
+struct Div {
+    uint32_t m;
+    int d;
+    Div() = default;
+    explicit Div(int by) : m(by > 1 ? (uint32_t)((1ULL << 32) / by) + 1u : 0u), d(by) {}
+    __device__ __forceinline__ int of(int x) const { return d == 1 ? x : (int)__umulhi((uint32_t)x, m); }
+};
 
 template <typename T>
 struct Norm {
@@ -80,6 +134,9 @@ struct Norm {
     float eps;
     int slab, rows;          // channels of a block; rows of a block
     int blocks;              // of an image (on chip: slabs x blocks of a cluster; else chunks of rows)
+    // on chip: row lanes, groups of the slab, entries of the slab and of a group, threads of an entry; divisors
+    int lanes, groups, entries, width, parts;
+    Div by_vectors, by_entries, by_slab, by_per, by_lanes;
 };
 
 __device__ __forceinline__ float warp_sum(float x) {
@@ -87,53 +144,107 @@ __device__ __forceinline__ float warp_sum(float x) {
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
-__device__ __forceinline__ float peer_f32(const float* p, uint32_t rank) {   // this variable of another block of the cluster
-    float x;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(cluster_peer(smem_u32(p), rank)) : "memory");
+__device__ __forceinline__ float2 peer_f32x2(const float2* p, uint32_t rank) {   // this variable of another block of the cluster
+    float2 x;
+    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(cluster_peer(smem_u32(p), rank)) : "memory");
     return x;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_await() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
-// Shared memory of the forms that stay on chip: a partial sum per thread and channel ([row lane][channel of the slab]), what a group
-// comes to in the block, and what it comes to over the cluster.
-struct Shared {
-    float *red, *own, *all;
-    __device__ Shared(float* base, int lanes, int slab, int groups) {
-        red = base;
-        own = base + lanes * slab;
-        all = own + 2 * groups;
+// A vector of the parameters, or `none` where there are none.
+template <typename T>
+__device__ __forceinline__ void params(const T* p, int c, float none, f32x2 (&f)[Wide<T>::N / 2]) {
+    if (p) widen16(*reinterpret_cast<const uint4*>(p + c), f, p);
+    else
+#pragma unroll
+        for (int e = 0; e < Wide<T>::N / 2; ++e) f[e] = both(none);
+}
+// f(pair, group of its first, group of its second) of a vector's channels c .. c + V - 1
+template <int V, typename F>
+__device__ __forceinline__ void over_pairs(int c, int g, int per, F f) {   // g: the first one's
+    int r = c - g * per;
+#pragma unroll
+    for (int e = 0; e < V; e += 2) {
+        const int g0 = g;
+        if (++r == per) r = 0, ++g;
+        const int g1 = g;
+        if (++r == per) r = 0, ++g;
+        f(e / 2, g0, g1);
     }
-};
-constexpr size_t on_chip_smem(int lanes, int slab, int groups) { return ((size_t)lanes * slab + 4 * groups) * 4; }
+}
+// On chip, threads leave what they have per entry, [row lane][entry of the slab]: an entry is a vector where a vector lies in one group (per a
+// multiple of V), else a channel.  (Sums of an entry over its row lanes by several threads, then a warp per group: each a handful of steps.
+// A warp per group straight away took 3400 cycles of a block's 20000.)
+constexpr size_t on_chip_floats(int lanes, int slab, int groups) { return 2 * ((size_t)lanes * slab + 2 * groups + (slab > kThreads ? slab : kThreads)); }
 
-// Sums of the group over what all threads hold, a warp per group.
-template <typename F>
-__device__ __forceinline__ void over_groups(const float* red, int lanes, int slab, int per, int groups, F f) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    for (int g = warp; g < groups; g += warps) {
-        float s = 0.f;
-        for (int i = lane; i < lanes * per; i += 32) s += red[(i / per) * slab + g * per + i % per];
-        f(g, warp_sum(s));
+// (n values, their mean m, their sum of squares about it q) of all lanes, joined.
+__device__ __forceinline__ void join_warp(float& n, float& m, float& q) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float n2 = __shfl_xor_sync(0xffffffffu, n, o), m2 = __shfl_xor_sync(0xffffffffu, m, o), q2 = __shfl_xor_sync(0xffffffffu, q, o);
+        const float s = n + n2, f = s > 0.f ? n2 / s : 0.f, d = m2 - m;
+        q += fmaf(d * d, n * f, q2);
+        m = fmaf(d, f, m);
+        n = s;
     }
 }
 
+// A vector's channels in the gradient.
+template <typename T>
+struct Channels {
+    static constexpr int V = Wide<T>::N;
+    f32x2 m[V / 2], rs[V / 2], w[V / 2], b[V / 2];
+    // c: the first channel; groups count from group0, whose first channel is c0
+    __device__ __forceinline__ void load(const Norm<T>& a, long long group0, int c0, int c, bool live) {
+        params(a.weight, live ? c0 + c : 0, 1.f, w);
+        params(a.bias, live ? c0 + c : 0, 0.f, b);
+        if (live)
+            over_pairs<V>(c, c < 1 << 16 ? a.by_per.of(c) : c / a.per, a.per, [&](int e, int g0, int g1) {
+                m[e] = pack2(a.cmean[group0 + g0], a.cmean[group0 + g1]);
+                rs[e] = pack2(a.crstd[group0 + g0], a.crstd[group0 + g1]);
+            });
+    }
+    // h = xhat, g = d_out act'(z)
+    template <int ACT>
+    __device__ __forceinline__ void grad(const uint4& x, const uint4& d, f32x2 (&h)[V / 2], f32x2 (&g)[V / 2]) const {
+        f32x2 f[V / 2];
+        widen16(x, f, (const T*)nullptr);
+        widen16(d, g, (const T*)nullptr);
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) {
+            h[e] = fmul2(fsub2(f[e], m[e]), rs[e]);
+            if constexpr (ACT != kActNone) g[e] = fmul2(g[e], slope2<ACT, sizeof(T) == 2>(ffma2(h[e], w[e], b[e])));
+        }
+    }
+    // g <- rstd (g w - m1 - h m2)
+    __device__ __forceinline__ void dx(const f32x2 (&h)[V / 2], f32x2 (&g)[V / 2], const f32x2 (&m1)[V / 2], const f32x2 (&m2)[V / 2]) const {
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) g[e] = fmul2(rs[e], fsub2(fsub2(fmul2(g[e], w[e]), m1[e]), fmul2(h[e], m2[e])));
+    }
+};
+
 // ---- on chip: grid (blocks of a cluster x slabs x B); K vectors of 16 bytes a thread --------------------------------------
 template <typename T, int ACT, int K>
-__global__ void __launch_bounds__(kThreads) norm_kernel(Norm<T> a, int N) {
+__global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_kernel(Norm<T> a, int N) {
     constexpr int V = Wide<T>::N;
     extern __shared__ __align__(16) float smem[];
-    const int nv = a.slab / V, lanes = blockDim.x / nv, tid = threadIdx.x, vc = tid % nv, rl = tid / nv;
-    const int groups = a.slab / a.per;
-    const Shared s(smem, lanes, a.slab, groups);
+    const int lanes = a.lanes, tid = threadIdx.x, rl = a.by_vectors.of(tid), vc = tid - rl * a.by_vectors.d, groups = a.groups;
+    const int entries = a.entries, width = a.width;
+    const bool vectors = entries < a.slab;
+    float2 *const red = reinterpret_cast<float2*>(smem), *const own = red + lanes * entries, *const all = own + groups, *const sums = all + groups;
     const long long image = blockIdx.x / a.blocks;
     const int slab = blockIdx.x % a.blocks / N, rank = blockIdx.x % N;
-    const int c0 = slab * a.slab, row0 = rank * a.rows, rows = min(a.rows, a.HW - row0);   // (may be none)
+    const int c0 = slab * a.slab, row0 = rank * a.rows, rows = max(0, min(a.rows, a.HW - row0));
     const bool live = rl < lanes;
     const long long base = (image * a.HW + row0) * a.C + c0 + vc * V;
     pdl_wait();
     pdl_launch_dependents();
+    f32x2 w[V / 2], b[V / 2];
+    params(a.weight, live ? c0 + vc * V : 0, 1.f, w);
+    params(a.bias, live ? c0 + vc * V : 0, 0.f, b);
     uint4 x[K];
+    x[0] = make_uint4(0u, 0u, 0u, 0u);
     int n = 0;   // vectors of this thread
 #pragma unroll
     for (int i = 0; i < K; ++i) {
@@ -143,110 +254,162 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(Norm<T> a, int N) {
             n = i + 1;
         }
     }
-    float acc[V] = {};
+    // this thread's mean and sum of squares about it per channel, in one pass about its own first value: as that value is one of them, the
+    // sum about it is at most n + 1 times the sum about the mean, and so is what rounding costs
+    const int full = a.by_lanes.of(rows), rest = rows - full * lanes;   // vectors of a row lane: full, or one more
+    const int most = full + (rest > 0);   // the same for the whole block: vectors that no thread has are skipped
+    f32x2 first[V / 2], sum[V / 2], sq[V / 2];
+    widen16(x[0], first, a.x);
 #pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (i < n) {
-            float f[V];
+    for (int e = 0; e < V / 2; ++e) sum[e] = sq[e] = both(0.f);
+#pragma unroll
+    for (int i = 1; i < K; ++i)
+        if (i < most && i < n) {
+            f32x2 f[V / 2];
             widen16(x[i], f, a.x);
 #pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] += f[e];
+            for (int e = 0; e < V / 2; ++e) {
+                const f32x2 d = fsub2(f[e], first[e]);
+                sum[e] = fadd2(sum[e], d);
+                sq[e] = ffma2(d, d, sq[e]);
+            }
         }
-    if (live)
+    if (live) {
+        const float inv = n > 0 ? 1.f / (float)n : 0.f;
+        float mean[V], m2[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) s.red[rl * a.slab + vc * V + e] = acc[e];
-    __syncthreads();
-    const float mine = rows > 0 ? 1.f / ((float)rows * a.per) : 0.f;
-    over_groups(s.red, lanes, a.slab, a.per, groups, [&](int g, float sum) {
-        if ((tid & 31) == 0) s.own[2 * g] = sum * mine;
-    });
-    __syncthreads();
-    int g[V];
-    float m[V];
+        for (int e = 0; e < V / 2; ++e) {
+            float f0, f1, s0, s1, q0, q1;
+            unpack2(first[e], f0, f1);
+            unpack2(sum[e], s0, s1);
+            unpack2(sq[e], q0, q1);
+            mean[2 * e] = fmaf(s0, inv, f0);
+            mean[2 * e + 1] = fmaf(s1, inv, f1);
+            m2[2 * e] = fmaxf(fmaf(-s0 * inv, s0, q0), 0.f);
+            m2[2 * e + 1] = fmaxf(fmaf(-s1 * inv, s1, q1), 0.f);
+        }
+        if (vectors) {
+            float m = 0.f, q = 0.f;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        g[e] = (vc * V + e) / a.per;
-        m[e] = s.own[2 * g[e]];
-        acc[e] = 0.f;
+            for (int e = 0; e < V; ++e) m += mean[e];
+            m *= 1.f / V;
+#pragma unroll
+            for (int e = 0; e < V; ++e) q += fmaf((mean[e] - m) * (float)n, mean[e] - m, m2[e]);
+            red[rl * entries + vc] = make_float2(m, q);
+        } else
+#pragma unroll
+            for (int e = 0; e < V; e += 2) *reinterpret_cast<float4*>(red + rl * entries + vc * V + e) = make_float4(mean[e], m2[e], mean[e + 1], m2[e + 1]);
     }
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (i < n) {
-            float f[V];
-            widen16(x[i], f, a.x);
-#pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] = fmaf(f[e] - m[e], f[e] - m[e], acc[e]);
-        }
-    if (live)
-#pragma unroll
-        for (int e = 0; e < V; ++e) s.red[rl * a.slab + vc * V + e] = acc[e];
     __syncthreads();
-    over_groups(s.red, lanes, a.slab, a.per, groups, [&](int g_, float sum) {
-        if ((tid & 31) == 0) s.own[2 * g_ + 1] = sum;
-    });
+    const float values = vectors ? (float)V : 1.f;               // of an entry and row
+    // an entry over its row lanes, about the first one's mean; then per entry: mean and sum of squares about it
+    const int parts = a.parts;
+    for (int i = tid; i < entries * parts; i += blockDim.x) {
+        const int part = a.by_entries.of(i), c = i - part * entries;
+        const float first_mean = red[c].x;
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll 4
+        for (int r = part; r < lanes; r += parts) {
+            const float2 y = red[r * entries + c];
+            const float k = (float)(full + (r < rest)) * values, d = y.x - first_mean;
+            s1 = fmaf(k, d, s1);
+            s2 += fmaf(k * d, d, y.y);
+        }
+        sums[i] = make_float2(s1, s2);
+    }
+    __syncthreads();
+    const float per_entry = (float)rows * values, of_entry = rows > 0 ? 1.f / per_entry : 0.f, of_group = 1.f / (float)width;
+    for (int j = tid >> 5; j < groups; j += blockDim.x >> 5) {
+        auto entry = [&](int c, float& m, float& q) {
+            float s1 = 0.f, s2 = 0.f;
+#pragma unroll 4
+            for (int p = 0; p < parts; ++p) {
+                const float2 y = sums[p * entries + c];
+                s1 += y.x;
+                s2 += y.y;
+            }
+            m = fmaf(s1, of_entry, red[c].x);
+            q = fmaxf(fmaf(-s1 * of_entry, s1, s2), 0.f);
+        };
+        const int lane = tid & 31;
+        float m = 0.f, q = 0.f;
+        if (width <= 32) {
+            float me = 0.f, qe = 0.f;
+            if (lane < width) entry(j * width + lane, me, qe);
+            m = warp_sum(me) * of_group;
+            q = warp_sum(lane < width ? fmaf(per_entry * (me - m), me - m, qe) : 0.f);
+        } else {
+            for (int c = lane; c < width; c += 32) {
+                float me, qe;
+                entry(j * width + c, me, qe);
+                m += me;
+            }
+            m = warp_sum(m) * of_group;
+            for (int c = lane; c < width; c += 32) {
+                float me, qe;
+                entry(j * width + c, me, qe);
+                q += fmaf(per_entry * (me - m), me - m, qe);
+            }
+            q = warp_sum(q);
+        }
+        if (lane == 0) own[j] = make_float2(m, q);
+    }
     if (N > 1) {
         cluster_arrive();
         cluster_await();
     } else __syncthreads();
     for (int j = tid; j < groups; j += blockDim.x) {
-        float mean = s.own[2 * j], m2 = s.own[2 * j + 1];
+        float m = own[j].x, q = own[j].y;
         if (N > 1) {
-            // blocks' means and sums of squares about them, joined: mean over rows, and every block's sum moved to it
-            float bm[kMostBlocks], bs[kMostBlocks];
-            mean = m2 = 0.f;
+            float2 peer[kMostBlocks];
 #pragma unroll
             for (int p = 0; p < kMostBlocks; ++p)
-                if (p < N) {
-                    bm[p] = peer_f32(s.own + 2 * j, p);
-                    bs[p] = peer_f32(s.own + 2 * j + 1, p);
-                }
+                if (p < N) peer[p] = peer_f32x2(own + j, p);
+            auto share = [&](int p) { return (float)max(0, min(a.rows, a.HW - p * a.rows)); };   // rows of block p
+            m = q = 0.f;
 #pragma unroll
             for (int p = 0; p < kMostBlocks; ++p)
-                if (p < N) mean += bm[p] * ((float)max(0, min(a.rows, a.HW - p * a.rows)) / (float)a.HW);
+                if (p < N) m = fmaf(share(p), peer[p].x, m);
+            m /= (float)a.HW;
 #pragma unroll
             for (int p = 0; p < kMostBlocks; ++p)
-                if (p < N) m2 += bs[p] + (float)max(0, min(a.rows, a.HW - p * a.rows)) * a.per * (bm[p] - mean) * (bm[p] - mean);
+                if (p < N) q += fmaf(share(p) * a.per * (peer[p].x - m), peer[p].x - m, peer[p].y);
         }
-        const float rstd = rsqrtf(m2 / ((float)a.HW * a.per) + a.eps);
-        s.all[2 * j] = mean;
-        s.all[2 * j + 1] = rstd;
+        const float rstd = rsqrtf(q / ((float)a.HW * a.per) + a.eps);
+        all[j] = make_float2(m, rstd);
         if (rank == 0) {
             const long long at = image * (a.C / a.per) + c0 / a.per + j;
-            if (a.mean) a.mean[at] = mean;
+            if (a.mean) a.mean[at] = m;
             if (a.rstd) a.rstd[at] = rstd;
         }
     }
     if (N > 1) cluster_arrive();   // has read the others' shared memory, which they keep until all have
     __syncthreads();
-    float w[V], b[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int c = c0 + vc * V + e;
-        m[e] = live ? s.all[2 * g[e]] : 0.f;
-        w[e] = live ? one(a.weight, c, 1.f) * s.all[2 * g[e] + 1] : 0.f;
-        b[e] = live ? one(a.bias, c, 0.f) : 0.f;
-    }
+    f32x2 m[V / 2];
+    if (live)
+        over_pairs<V>(vc * V, a.by_per.of(vc * V), a.per, [&](int e, int g0, int g1) {
+            const float2 s0 = all[g0], s1 = all[g1];
+            m[e] = pack2(s0.x, s1.x);
+            w[e] = fmul2(w[e], pack2(s0.y, s1.y));
+        });
 #pragma unroll
     for (int i = 0; i < K; ++i)
-        if (i < n) {
-            float f[V];
+        if (i < most && i < n) {
+            f32x2 f[V / 2];
             widen16(x[i], f, a.x);
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[e] = act<ACT, sizeof(T) == 2>(fmaf(f[e] - m[e], w[e], b[e]));
+            for (int e = 0; e < V / 2; ++e) f[e] = act2<ACT, sizeof(T) == 2>(ffma2(fsub2(f[e], m[e]), w[e], b[e]));
             *reinterpret_cast<uint4*>(a.out + base + (long long)(rl + i * lanes) * a.C) = narrow16(f, a.x);
         }
     if (N > 1) cluster_await();
 }
 
 template <typename T, int ACT, int K>
-__global__ void __launch_bounds__(kThreads) norm_grad_kernel(Norm<T> a, int N) {
+__global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_grad_kernel(Norm<T> a, int N) {
     constexpr int V = Wide<T>::N;
-    constexpr bool FAST = sizeof(T) == 2;
     extern __shared__ __align__(16) float smem[];
-    const int nv = a.slab / V, lanes = blockDim.x / nv, tid = threadIdx.x, vc = tid % nv, rl = tid / nv;
-    const int groups = a.slab / a.per;
-    const Shared s(smem, lanes, a.slab, groups);
-    float* const red2 = s.all + 2 * groups;   // [lanes][slab]
+    const int lanes = a.lanes, tid = threadIdx.x, rl = a.by_vectors.of(tid), vc = tid - rl * a.by_vectors.d, groups = a.groups;
+    float2 *const red = reinterpret_cast<float2*>(smem), *const own = red + lanes * a.slab, *const all = own + groups;
     const long long image = blockIdx.x / a.blocks;
     const int slab = blockIdx.x % a.blocks / N, rank = blockIdx.x % N;
     const int c0 = slab * a.slab, row0 = rank * a.rows, rows = min(a.rows, a.HW - row0);
@@ -254,6 +417,8 @@ __global__ void __launch_bounds__(kThreads) norm_grad_kernel(Norm<T> a, int N) {
     const long long base = (image * a.HW + row0) * a.C + c0 + vc * V;
     pdl_wait();
     pdl_launch_dependents();
+    Channels<T> ch;
+    ch.load(a, image * (a.C / a.per) + c0 / a.per, c0, vc * V, live);
     uint4 x[K], d[K];
     int n = 0;
 #pragma unroll
@@ -265,90 +430,100 @@ __global__ void __launch_bounds__(kThreads) norm_grad_kernel(Norm<T> a, int N) {
             n = i + 1;
         }
     }
-    float m[V], rs[V], w[V], b[V], sg[V] = {}, sx[V] = {};
-    const long long at = image * (a.C / a.per) + c0 / a.per;
+    const int most = a.by_lanes.of(rows + lanes - 1);   // the same for the whole block: vectors that no thread has are skipped
+    f32x2 sg[V / 2], sx[V / 2];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int c = vc * V + e;
-        m[e] = live ? a.cmean[at + c / a.per] : 0.f;
-        rs[e] = live ? a.crstd[at + c / a.per] : 0.f;
-        w[e] = live ? one(a.weight, c0 + c, 1.f) : 0.f;
-        b[e] = live ? one(a.bias, c0 + c, 0.f) : 0.f;
-    }
+    for (int e = 0; e < V / 2; ++e) sg[e] = sx[e] = both(0.f);
 #pragma unroll
     for (int i = 0; i < K; ++i)
-        if (i < n) {
-            float f[V], o[V];
-            widen16(x[i], f, a.x);
-            widen16(d[i], o, a.x);
+        if (i < most && i < n) {
+            f32x2 h[V / 2], g[V / 2];
+            ch.template grad<ACT>(x[i], d[i], h, g);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float h = (f[e] - m[e]) * rs[e], g = o[e] * slope<ACT, FAST>(fmaf(h, w[e], b[e]));
-                sg[e] += g;
-                sx[e] = fmaf(g, h, sx[e]);
+            for (int e = 0; e < V / 2; ++e) {
+                sg[e] = fadd2(sg[e], g[e]);
+                sx[e] = ffma2(g[e], h[e], sx[e]);
             }
         }
     if (live)
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            s.red[rl * a.slab + vc * V + e] = sg[e];
-            red2[rl * a.slab + vc * V + e] = sx[e];
+        for (int e = 0; e < V / 2; ++e) {
+            float g0, g1, x0, x1;
+            unpack2(sg[e], g0, g1);
+            unpack2(sx[e], x0, x1);
+            *reinterpret_cast<float4*>(red + rl * a.slab + vc * V + 2 * e) = make_float4(g0, x0, g1, x1);
         }
     __syncthreads();
-    // a channel's sums over the block: what the parameters' gradients and the group's means are made of
-    for (int c = tid; c < a.slab; c += blockDim.x) {
+    // a channel's sums over the block, several threads a channel: what the parameters' gradients and the group's means are made of
+    const int parts = a.parts;
+    for (int i = tid; i < a.slab * parts; i += blockDim.x) {
+        const int part = a.by_slab.of(i), c = i - part * a.slab;
         float u = 0.f, v = 0.f;
-        for (int l = 0; l < lanes; ++l) {
-            u += s.red[l * a.slab + c];
-            v += red2[l * a.slab + c];
+#pragma unroll 4
+        for (int l = part; l < lanes; l += parts) {
+            const float2 y = red[l * a.slab + c];
+            u += y.x;
+            v += y.y;
         }
-        a.part[(image * N + rank) * a.C + c0 + c] = make_float2(u, v);
-        const float wc = one(a.weight, c0 + c, 1.f);
-        s.red[c] = u * wc;    // row lane 0 of this very channel: read above by this thread alone
-        red2[c] = v * wc;
+        red[part * a.slab + c] = make_float2(u, v);   // (row lane `part` of this very channel: read by this thread alone)
     }
     __syncthreads();
-    over_groups(s.red, 1, a.slab, a.per, groups, [&](int g, float sum) {
-        if ((tid & 31) == 0) s.own[2 * g] = sum;
-    });
-    over_groups(red2, 1, a.slab, a.per, groups, [&](int g, float sum) {
-        if ((tid & 31) == 0) s.own[2 * g + 1] = sum;
-    });
+    for (int j = tid >> 5; j < groups; j += blockDim.x >> 5) {
+        float u = 0.f, v = 0.f;
+        for (int c = j * a.per + (tid & 31); c < (j + 1) * a.per; c += 32) {
+            float su = 0.f, sv = 0.f;
+            for (int p = 0; p < parts; ++p) {
+                const float2 y = red[p * a.slab + c];
+                su += y.x;
+                sv += y.y;
+            }
+            a.part[(image * N + rank) * a.C + c0 + c] = make_float2(su, sv);
+            const float wc = one(a.weight, c0 + c, 1.f);
+            u = fmaf(su, wc, u);
+            v = fmaf(sv, wc, v);
+        }
+        u = warp_sum(u);
+        v = warp_sum(v);
+        if ((tid & 31) == 0) own[j] = make_float2(u, v);
+    }
     if (N > 1) {
         cluster_arrive();
         cluster_await();
     } else __syncthreads();
     const float inv = 1.f / ((float)a.HW * a.per);
-    for (int j = tid; j < 2 * groups; j += blockDim.x) {
-        float sum = 0.f;
+    for (int j = tid; j < groups; j += blockDim.x) {
+        float2 sum = own[j];
         if (N > 1) {
+            float2 peer[kMostBlocks];
 #pragma unroll
             for (int p = 0; p < kMostBlocks; ++p)
-                if (p < N) sum += peer_f32(s.own + j, p);
-        } else sum = s.own[j];
-        s.all[j] = sum * inv;
+                if (p < N) peer[p] = peer_f32x2(own + j, p);
+            sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int p = 0; p < kMostBlocks; ++p)
+                if (p < N) {
+                    sum.x += peer[p].x;
+                    sum.y += peer[p].y;
+                }
+        }
+        all[j] = make_float2(sum.x * inv, sum.y * inv);
     }
     if (N > 1) cluster_arrive();
     __syncthreads();
-    float m1[V], m2[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int g = (vc * V + e) / a.per;
-        m1[e] = live ? s.all[2 * g] : 0.f;
-        m2[e] = live ? s.all[2 * g + 1] : 0.f;
-    }
+    f32x2 m1[V / 2], m2[V / 2];
+    if (live)
+        over_pairs<V>(vc * V, a.by_per.of(vc * V), a.per, [&](int e, int g0, int g1) {
+            const float2 s0 = all[g0], s1 = all[g1];
+            m1[e] = pack2(s0.x, s1.x);
+            m2[e] = pack2(s0.y, s1.y);
+        });
 #pragma unroll
     for (int i = 0; i < K; ++i)
-        if (i < n) {
-            float f[V], o[V];
-            widen16(x[i], f, a.x);
-            widen16(d[i], o, a.x);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float h = (f[e] - m[e]) * rs[e], g = o[e] * slope<ACT, FAST>(fmaf(h, w[e], b[e]));
-                f[e] = rs[e] * (fmaf(g, w[e], -m1[e]) - h * m2[e]);
-            }
-            *reinterpret_cast<uint4*>(a.dx + base + (long long)(rl + i * lanes) * a.C) = narrow16(f, a.x);
+        if (i < most && i < n) {
+            f32x2 h[V / 2], g[V / 2];
+            ch.template grad<ACT>(x[i], d[i], h, g);
+            ch.dx(h, g, m1, m2);
+            *reinterpret_cast<uint4*>(a.dx + base + (long long)(rl + i * lanes) * a.C) = narrow16(g, a.x);
         }
     if (N > 1) cluster_await();
 }
@@ -436,14 +611,7 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(Norm<T> a, int chun
         m = fmaf(dm, share, m);
         n += k;
     }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const float n2 = __shfl_xor_sync(0xffffffffu, n, o), m2 = __shfl_xor_sync(0xffffffffu, m, o), q2 = __shfl_xor_sync(0xffffffffu, q, o);
-        const float sum = n + n2, share = sum > 0.f ? n2 / sum : 0.f, dm = m2 - m;
-        q = q + q2 + dm * dm * (share * n);
-        m = fmaf(dm, share, m);
-        n = sum;
-    }
+    join_warp(n, m, q);
     if (lane == 0) {
         a.mean[at] = m;
         a.rstd[at] = rsqrtf(q / n + a.eps);
@@ -461,14 +629,13 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(Norm<T> a) {
     pdl_launch_dependents();
     if (rl >= lanes) return;
     const long long at = image * (a.C / a.per);
-    float m[V], w[V], b[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int c = c0 + vc * V + e;
-        m[e] = a.mean[at + c / a.per];
-        w[e] = one(a.weight, c, 1.f) * a.rstd[at + c / a.per];
-        b[e] = one(a.bias, c, 0.f);
-    }
+    f32x2 m[V / 2], w[V / 2], b[V / 2];
+    params(a.weight, c0 + vc * V, 1.f, w);
+    params(a.bias, c0 + vc * V, 0.f, b);
+    over_pairs<V>(c0 + vc * V, (c0 + vc * V) / a.per, a.per, [&](int e, int g0, int g1) {
+        m[e] = pack2(a.mean[at + g0], a.mean[at + g1]);
+        w[e] = fmul2(w[e], pack2(a.rstd[at + g0], a.rstd[at + g1]));
+    });
     for (int r = rl; r < rows; r += 4 * lanes) {
         uint4 y[4];
 #pragma unroll
@@ -477,10 +644,10 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(Norm<T> a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (r + i * lanes < rows) {
-                float f[V];
+                f32x2 f[V / 2];
                 widen16(y[i], f, a.x);
 #pragma unroll
-                for (int e = 0; e < V; ++e) f[e] = act<ACT, sizeof(T) == 2>(fmaf(f[e] - m[e], w[e], b[e]));
+                for (int e = 0; e < V / 2; ++e) f[e] = act2<ACT, sizeof(T) == 2>(ffma2(fsub2(f[e], m[e]), w[e], b[e]));
                 *reinterpret_cast<uint4*>(a.out + base + (long long)(r + i * lanes) * a.C) = narrow16(f, a.x);
             }
     }
@@ -490,7 +657,6 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(Norm<T> a) {
 template <typename T, int ACT, bool SUMS>
 __global__ void __launch_bounds__(kThreads) norm_grad_chunk_kernel(Norm<T> a, const float2* means) {
     constexpr int V = Wide<T>::N;
-    constexpr bool FAST = sizeof(T) == 2;
     extern __shared__ __align__(16) float smem[];
     const int c0 = blockIdx.z * a.slab, slab = min(a.slab, a.C - c0);
     const int nv = slab / V, lanes = kThreads / nv, tid = threadIdx.x, vc = tid % nv, rl = tid / nv;
@@ -501,18 +667,17 @@ __global__ void __launch_bounds__(kThreads) norm_grad_chunk_kernel(Norm<T> a, co
     pdl_launch_dependents();
     const bool live = rl < lanes;
     const long long at = image * (a.C / a.per);
-    float m[V], rs[V], w[V], b[V], s1[V], s2[V];
+    Channels<T> ch;
+    ch.load(a, at, 0, c0 + vc * V, live);
+    f32x2 s1[V / 2], s2[V / 2];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int c = c0 + vc * V + e;
-        m[e] = live ? a.cmean[at + c / a.per] : 0.f;
-        rs[e] = live ? a.crstd[at + c / a.per] : 0.f;
-        w[e] = live ? one(a.weight, c, 1.f) : 0.f;
-        b[e] = live ? one(a.bias, c, 0.f) : 0.f;
-        const float2 mm = !SUMS && live ? means[at + c / a.per] : make_float2(0.f, 0.f);
-        s1[e] = mm.x;
-        s2[e] = mm.y;
-    }
+    for (int e = 0; e < V / 2; ++e) s1[e] = s2[e] = both(0.f);
+    if (!SUMS && live)
+        over_pairs<V>(c0 + vc * V, (c0 + vc * V) / a.per, a.per, [&](int e, int g0, int g1) {
+            const float2 p = means[at + g0], q = means[at + g1];
+            s1[e] = pack2(p.x, q.x);
+            s2[e] = pack2(p.y, q.y);
+        });
     if (live)
         for (int r = rl; r < rows; r += 2 * lanes) {
             uint4 y[2], d[2];
@@ -525,34 +690,37 @@ __global__ void __launch_bounds__(kThreads) norm_grad_chunk_kernel(Norm<T> a, co
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (r + i * lanes < rows) {
-                    float f[V], o[V];
-                    widen16(y[i], f, a.x);
-                    widen16(d[i], o, a.x);
+                    f32x2 h[V / 2], g[V / 2];
+                    ch.template grad<ACT>(y[i], d[i], h, g);
+                    if constexpr (SUMS) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float h = (f[e] - m[e]) * rs[e], g = o[e] * slope<ACT, FAST>(fmaf(h, w[e], b[e]));
-                        if constexpr (SUMS) {
-                            s1[e] += g;
-                            s2[e] = fmaf(g, h, s2[e]);
-                        } else f[e] = rs[e] * (fmaf(g, w[e], -s1[e]) - h * s2[e]);
+                        for (int e = 0; e < V / 2; ++e) {
+                            s1[e] = fadd2(s1[e], g[e]);
+                            s2[e] = ffma2(g[e], h[e], s2[e]);
+                        }
+                    } else {
+                        ch.dx(h, g, s1, s2);
+                        *reinterpret_cast<uint4*>(a.dx + base + (long long)(r + i * lanes) * a.C) = narrow16(g, a.x);
                     }
-                    if constexpr (!SUMS) *reinterpret_cast<uint4*>(a.dx + base + (long long)(r + i * lanes) * a.C) = narrow16(f, a.x);
                 }
         }
     if constexpr (SUMS) {
-        float *r1 = smem, *r2 = smem + kThreads * V;
+        float2* const red = reinterpret_cast<float2*>(smem);
         if (live)
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                r1[rl * slab + vc * V + e] = s1[e];
-                r2[rl * slab + vc * V + e] = s2[e];
+            for (int e = 0; e < V / 2; ++e) {
+                float g0, g1, x0, x1;
+                unpack2(s1[e], g0, g1);
+                unpack2(s2[e], x0, x1);
+                *reinterpret_cast<float4*>(red + rl * slab + vc * V + 2 * e) = make_float4(g0, x0, g1, x1);
             }
         __syncthreads();
         for (int c = tid; c < slab; c += kThreads) {
             float u = 0.f, v = 0.f;
             for (int l = 0; l < lanes; ++l) {
-                u += r1[l * slab + c];
-                v += r2[l * slab + c];
+                const float2 y = red[l * slab + c];
+                u += y.x;
+                v += y.y;
             }
             a.part[(long long)blockIdx.x * a.C + c0 + c] = make_float2(u, v);
         }
@@ -656,6 +824,26 @@ Plan plan_of(int B, int HW, int C, int groups, int V, bool gradient) {
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
+template <typename T>
+void fill(Norm<T>& a, const Plan& p, int HW, int C, int groups, bool gradient) {
+    constexpr int V = 16 / sizeof(T);
+    a.HW = HW; a.C = C; a.per = C / groups; a.slab = p.slab; a.rows = p.rows;
+    a.blocks = p.on_chip ? p.N * p.slabs : p.chunks;
+    a.by_per = Div(a.per);
+    if (!p.on_chip) return;
+    const bool vectors = !gradient && a.per % V == 0;
+    a.lanes = p.threads / (p.slab / V);
+    a.groups = p.slab / a.per;
+    a.entries = vectors ? p.slab / V : p.slab;
+    a.width = vectors ? a.per / V : a.per;
+    a.parts = p.threads / a.entries;
+    a.parts = a.parts < 1 ? 1 : a.parts > a.lanes ? a.lanes : a.parts;
+    a.by_vectors = Div(p.slab / V);
+    a.by_entries = Div(a.entries);
+    a.by_slab = Div(p.slab);
+    a.by_lanes = Div(a.lanes);
+}
+
 template <typename F>
 cudaError_t with_act(int act, F f) {
     if (act == kActSilu) return f(std::integral_constant<int, kActSilu>());
@@ -667,7 +855,9 @@ cudaError_t with_vectors(int K, F f) {
     if (K <= 1) return f(std::integral_constant<int, 1>());
     if (K <= 2) return f(std::integral_constant<int, 2>());
     if (K <= 4) return f(std::integral_constant<int, 4>());
+    if (K <= 6) return f(std::integral_constant<int, 6>());
     if (K <= 8) return f(std::integral_constant<int, 8>());
+    if (K <= 12) return f(std::integral_constant<int, 12>());
     return f(std::integral_constant<int, 16>());
 }
 
@@ -696,13 +886,14 @@ cudaError_t launch_group_norm(const T* x, const T* weight, const T* bias, T* out
     const Plan p = plan_of(B, HW, C, groups, V, false);
     Norm<T> a = {};
     a.x = x; a.weight = weight; a.bias = bias; a.out = out; a.mean = mean; a.rstd = rstd;
-    a.HW = HW; a.C = C; a.per = C / groups; a.eps = eps; a.slab = p.slab; a.rows = p.rows; a.blocks = p.on_chip ? p.N * p.slabs : p.chunks;
+    a.eps = eps;
+    fill(a, p, HW, C, groups, false);
     if (p.on_chip)
         return with_act(act, [&](auto A) {
             return with_vectors(p.K, [&](auto K) {
                 count_launch();
                 return launch_pdl_cluster(norm_kernel<T, decltype(A)::value, decltype(K)::value>, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads),
-                                          on_chip_smem(p.threads / (p.slab / V), p.slab, p.slab / a.per), p.N, stream, a, p.N);
+                                          on_chip_floats(p.threads / (p.slab / V), p.slab, p.slab / a.per) * 4, p.N, stream, a, p.N);
             });
         });
     a.part = (float2*)scratch;
@@ -726,7 +917,7 @@ cudaError_t launch_group_norm_bwd(const T* x, const T* weight, const T* bias, co
     const Plan p = plan_of(B, HW, C, groups, V, true);
     Norm<T> a = {};
     a.x = x; a.weight = weight; a.bias = bias; a.d_out = d_out; a.dx = dx; a.cmean = mean; a.crstd = rstd;
-    a.HW = HW; a.C = C; a.per = C / groups; a.slab = p.slab; a.rows = p.rows; a.blocks = p.on_chip ? p.N * p.slabs : p.chunks;
+    fill(a, p, HW, C, groups, true);
     a.part = (float2*)scratch;
     cudaError_t e;
     if (p.on_chip)
@@ -738,7 +929,7 @@ cudaError_t launch_group_norm_bwd(const T* x, const T* weight, const T* bias, co
                     const int lanes = p.threads / (p.slab / V);
                     count_launch();
                     return launch_pdl_cluster(norm_grad_kernel<T, decltype(A)::value, k>, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads),
-                                              on_chip_smem(lanes, p.slab, p.slab / a.per) + (size_t)lanes * p.slab * 4, p.N, stream, a, p.N);
+                                              on_chip_floats(lanes, p.slab, p.slab / a.per) * 4, p.N, stream, a, p.N);
                 }
             });
         });
