@@ -38,6 +38,7 @@ constexpr int key_pitch() { return DKP * 2 + 16; }
 // Per token of a chunk, in shared memory: arrays of kChunk floats.
 //   b running sum of log2 alpha; eb 2^b; dl 2^{b_C - b}; gv beta 2^e and gn beta 2^{2e} with 2^e the scale of the key's row (ku); qu the query's
 enum { kB, kEb, kDl, kBeta, kGv, kGn, kKu, kQu, kGateRows };
+__device__ __forceinline__ f32x2 gate_pair(const float* gates, int row, int t) { return *reinterpret_cast<const f32x2*>(gates + row * kChunk + t); }
 
 // Shared memory, in bytes.
 template <int DKP, bool EXACT, Way WAY>
@@ -129,16 +130,12 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
         for (int p = 0; p < kPasses; ++p) {
             const int r = p * kRows + r0, t = r & (kChunk - 1);
             const uint4 x = rows[p];
-            uint32_t m = max(max(max(x.x & 0x7fffu, x.x >> 16 & 0x7fffu), max(x.y & 0x7fffu, x.y >> 16 & 0x7fffu)),
-                             max(max(x.z & 0x7fffu, x.z >> 16 & 0x7fffu), max(x.w & 0x7fffu, x.w >> 16 & 0x7fffu)));
+            uint32_t m = largest_bf16(x);
 #pragma unroll
             for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
             float down, up;
             power_of(m >> 7, down, up);
-            auto half2_of = [&](uint32_t y) { return pack_half(__uint_as_float(y << 16) * down, __uint_as_float(y & 0xffff0000u) * down); };
-            if (e8 < DKP)
-                *reinterpret_cast<uint4*>(smem + (r < kChunk ? lay.k(buf) : lay.q(buf)) + t * KP + e8 * 2) =
-                    make_uint4(half2_of(x.x), half2_of(x.y), half2_of(x.z), half2_of(x.w));
+            if (e8 < DKP) *reinterpret_cast<uint4*>(smem + (r < kChunk ? lay.k(buf) : lay.q(buf)) + t * KP + e8 * 2) = bf16_to_half(x, down);
             if (e8 == 0) gates[(r < kChunk ? kKu : kQu) * kChunk + t] = up;
         }
         named_bar(kBarPrep, kPrep);
@@ -148,14 +145,10 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
             gates[kGn * kChunk + tid] = gv * gates[kKu * kChunk + tid];
         }
         if (it + 1 < chunks) bring(WAY == Way::kBack ? n - 1 : n + 1);
-        // N and P by blocks of sixteen by sixteen; the diagonal ones first, their inverses take longest
+        // N and P by blocks of sixteen by sixteen: two of the diagonal's for each of the first two warps, with their inverses side by side; three
+        // of the others for each of the other two
         const uint32_t kt = base + lay.k(buf), qt = base + lay.q(buf);
-#pragma unroll 1
-        for (int w = warp; w < 10; w += kPrepWarps) {
-            // 0 .. 3: the diagonal; then (1,0) (2,0) (2,1) (3,0) (3,1) (3,2)
-            const int i = w < 4 ? w : w == 4 ? 1 : w < 7 ? 2 : 3, j = w < 4 ? w : w == 4 ? 0 : w < 7 ? w - 5 : w - 7;
-            if (i >= strips) continue;
-            float nn[2][4] = {}, pp[2][4] = {};
+        auto products = [&](int i, int j, float (&nn)[2][4], float (&pp)[2][4]) {
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 uint32_t kb[4], x[4];
@@ -171,59 +164,95 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
                 mma(nn[0], ka, kb[0], kb[1]);
                 mma(nn[1], ka, kb[2], kb[3]);
             }
-            float* const xt = reinterpret_cast<float*>(smem + lay.x) + (w & 3) * 16 * 20;
+        };
+        auto put = [&](int hi_at, int lo_at, bool lo, int at, f32x2 x) {
+            const uint32_t hi = pack_half(x);
+            *reinterpret_cast<uint32_t*>(smem + hi_at + at) = hi;
+            if (lo) {
+                float u, v;
+                unpack2(x, u, v);
+                *reinterpret_cast<uint32_t*>(smem + lo_at + at) = rest_half(u, v, hi);
+            }
+        };
+        if (warp < 2) {
+            float* const xt = reinterpret_cast<float*>(smem + lay.x) + warp * 2 * 16 * 20;
+#pragma unroll 1
+            for (int d = 0; d < 2; ++d) {
+                const int i = 2 * warp + d;
+                if (i >= strips) break;
+                float nn[2][4] = {}, pp[2][4] = {};
+                products(i, i, nn, pp);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {   // rows g, g + 8
-                const int t = i * 16 + g + 8 * h;
-                const float bt = gates[kB * kChunk + t], ku = gates[kKu * kChunk + t], gn = gates[kBeta * kChunk + t] * ku * ku;
+                for (int h = 0; h < 2; ++h) {   // rows g, g + 8
+                    const int tt = g + 8 * h, t = i * 16 + tt;
+                    const float bt = gates[kB * kChunk + t], ku = gates[kKu * kChunk + t], gn = gates[kBeta * kChunk + t] * ku * ku;
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {   // columns 8m + 2c, + 1
-                    const int s = j * 16 + 8 * m + 2 * c, at = block_of(i, j) + (g + 8 * h) * kBlockPitch + (8 * m + 2 * c) * 2;
-                    const float2 bs = *reinterpret_cast<const float2*>(gates + kB * kChunk + s);
-                    const float e0 = s <= t ? ex2(bt - bs.x) : 0.f, e1 = s + 1 <= t ? ex2(bt - bs.y) : 0.f;
-                    if constexpr (Q) {
-                        const float p0 = s <= t ? pp[m][2 * h] * e0 : 0.f, p1 = s + 1 <= t ? pp[m][2 * h + 1] * e1 : 0.f;
-                        const uint32_t hi = pack_half(p0, p1);
-                        *reinterpret_cast<uint32_t*>(smem + lay.p(buf) + at) = hi;
-                        if constexpr (EXACT && WAY == Way::kBack) *reinterpret_cast<uint32_t*>(smem + lay.p_lo(buf) + at) = rest_half(p0, p1, hi);
-                    }
-                    const float n0 = s < t ? nn[m][2 * h] * e0 : 0.f, n1 = s + 1 < t ? nn[m][2 * h + 1] * e1 : 0.f;
-                    const uint32_t hi = pack_half(n0, n1);
-                    *reinterpret_cast<uint32_t*>(smem + lay.n(buf) + at) = hi;
-                    if constexpr (EXACT) *reinterpret_cast<uint32_t*>(smem + lay.n_lo(buf) + at) = rest_half(n0, n1, hi);
-                    if (i == j) {   // beta N, transposed: row s, column t
-                        const int ss = 8 * m + 2 * c, tt = g + 8 * h;
-                        xt[ss * 20 + tt] = n0 * gn;
-                        xt[(ss + 1) * 20 + tt] = n1 * gn;
+                    for (int m = 0; m < 2; ++m) {   // columns 8m + 2c, + 1
+                        const int ss = 8 * m + 2 * c, at = block_of(i, i) + tt * kBlockPitch + ss * 2;
+                        const float2 bs = *reinterpret_cast<const float2*>(gates + kB * kChunk + i * 16 + ss);
+                        const float e0 = ss <= tt ? ex2(bt - bs.x) : 0.f, e1 = ss + 1 <= tt ? ex2(bt - bs.y) : 0.f;
+                        // (selected, not multiplied: what is not finite stays out of earlier tokens)
+                        if constexpr (Q) put(lay.p(buf), lay.p_lo(buf), EXACT && WAY == Way::kBack, at, pack2(ss <= tt ? pp[m][2 * h] * e0 : 0.f, ss + 1 <= tt ? pp[m][2 * h + 1] * e1 : 0.f));
+                        const float n0 = ss < tt ? nn[m][2 * h] * e0 : 0.f, n1 = ss + 1 < tt ? nn[m][2 * h + 1] * e1 : 0.f;
+                        if constexpr (WAY == Way::kKeep) put(lay.n(buf), 0, false, at, pack2(n0, n1));   // (W takes its own strip's off)
+                        xt[(d * 16 + ss) * 20 + tt] = n0 * gn;   // beta N, transposed: row s, column t
+                        xt[(d * 16 + ss + 1) * 20 + tt] = n1 * gn;
                     }
                 }
             }
-            if (i == j) {
-                __syncwarp();
-                // (1 + beta N)^-1, a column a lane: x_t -= (beta N)_ts x_s as soon as x_s is known
-                float x[16];
-                const int cc = lane & 15;
+            __syncwarp();
+            // (1 + beta N)^-1, a column a lane, a block a half warp: x_t -= (beta N)_ts x_s as soon as x_s is known
+            const int cc = lane & 15, i = 2 * warp + (lane >> 4);
+            const float* const own = xt + (lane >> 4) * 16 * 20;
+            float x[16];
 #pragma unroll
-                for (int t = 0; t < 16; ++t) x[t] = t == cc ? 1.f : 0.f;
+            for (int t = 0; t < 16; ++t) x[t] = t == cc ? 1.f : 0.f;
 #pragma unroll
-                for (int s = 0; s < 15; ++s) {
+            for (int s = 0; s < 15; ++s) {
 #pragma unroll
-                    for (int p = (s + 1) / 4; p < 4; ++p) {
-                        const float4 r = *reinterpret_cast<const float4*>(xt + s * 20 + 4 * p);
-                        if (4 * p > s) x[4 * p] = fmaf(-r.x, x[s], x[4 * p]);
-                        if (4 * p + 1 > s) x[4 * p + 1] = fmaf(-r.y, x[s], x[4 * p + 1]);
-                        if (4 * p + 2 > s) x[4 * p + 2] = fmaf(-r.z, x[s], x[4 * p + 2]);
-                        if (4 * p + 3 > s) x[4 * p + 3] = fmaf(-r.w, x[s], x[4 * p + 3]);
+                for (int p = (s + 1) / 4; p < 4; ++p) {
+                    const float4 r = *reinterpret_cast<const float4*>(own + s * 20 + 4 * p);
+                    if (4 * p > s) x[4 * p] = fmaf(-r.x, x[s], x[4 * p]);
+                    if (4 * p + 1 > s) x[4 * p + 1] = fmaf(-r.y, x[s], x[4 * p + 1]);
+                    if (4 * p + 2 > s) x[4 * p + 2] = fmaf(-r.z, x[s], x[4 * p + 2]);
+                    if (4 * p + 3 > s) x[4 * p + 3] = fmaf(-r.w, x[s], x[4 * p + 3]);
+                }
+            }
+            if (i < strips)
+#pragma unroll
+                for (int t = 0; t < 16; ++t) {
+                    const __half hi = __float2half_rn(x[t]);
+                    *reinterpret_cast<__half*>(smem + lay.inv(buf) + i * kBlock + t * kBlockPitch + cc * 2) = hi;
+                    if constexpr (EXACT)
+                        *reinterpret_cast<__half*>(smem + lay.inv_lo(buf) + i * kBlock + t * kBlockPitch + cc * 2) = __float2half_rn(x[t] - __half2float(hi));
+                }
+        } else {
+#pragma unroll 1
+            for (int w = 0; w < 3; ++w) {
+                // (3,0) (3,1) (3,2), (1,0) (2,0) (2,1)
+                const int i = warp == 2 ? 3 : w == 0 ? 1 : 2, j = warp == 2 ? w : w == 2 ? 1 : 0;
+                if (i >= strips) continue;
+                float nn[2][4] = {}, pp[2][4] = {};
+                products(i, j, nn, pp);
+                // e^{b_t - b_s} by way of the last token of s' sixteen: both factors are at most one
+                const float ref = gates[kB * kChunk + j * 16 + 15];
+                f32x2 ec[2];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const float2 bs = *reinterpret_cast<const float2*>(gates + kB * kChunk + j * 16 + 8 * m + 2 * c);
+                    ec[m] = pack2(ex2(ref - bs.x), ex2(ref - bs.y));
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float et = ex2(gates[kB * kChunk + i * 16 + g + 8 * h] - ref);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const int at = block_of(i, j) + (g + 8 * h) * kBlockPitch + (8 * m + 2 * c) * 2;
+                        const f32x2 e = fmul2(ec[m], pack2(et, et));
+                        if constexpr (Q) put(lay.p(buf), lay.p_lo(buf), EXACT && WAY == Way::kBack, at, fmul2(pair(pp[m], h), e));
+                        put(lay.n(buf), lay.n_lo(buf), EXACT, at, fmul2(pair(nn[m], h), e));
                     }
                 }
-                if (lane < 16)
-#pragma unroll
-                    for (int t = 0; t < 16; ++t) {
-                        const __half hi = __float2half_rn(x[t]);
-                        *reinterpret_cast<__half*>(smem + lay.inv(buf) + i * kBlock + t * kBlockPitch + cc * 2) = hi;
-                        if constexpr (EXACT)
-                            *reinterpret_cast<__half*>(smem + lay.inv_lo(buf) + i * kBlock + t * kBlockPitch + cc * 2) = __float2half_rn(x[t] - __half2float(hi));
-                    }
             }
         }
         bar_arrive(kBarFull + buf, threads);
@@ -312,18 +341,19 @@ struct State {
             const float now = __uint_as_float((253u + TOP - ex) << 23), change = now / scale[h];
             back[h] = __uint_as_float((ex + 1u - TOP) << 23);
             scale[h] = now;
+            if (__any_sync(0xffffffffu, change != 1.f)) {
+                const f32x2 cc = pack2(change, change);
 #pragma unroll
-            for (int n = 0; n < DKP / 8; ++n) {
-                x[n][2 * h] *= change;
-                x[n][2 * h + 1] *= change;
+                for (int n = 0; n < DKP / 8; ++n) set_pair(x[n], h, fmul2(pair(x[n], h), cc));
             }
         }
     }
     __device__ __forceinline__ void decay(float s) {
+        const f32x2 ss = pack2(s, s);
 #pragma unroll
         for (int n = 0; n < DKP / 8; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[n][e] *= s;
+            for (int h = 0; h < 2; ++h) set_pair(x[n], h, fmul2(pair(x[n], h), ss));
     }
 };
 
@@ -397,24 +427,26 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, o));
     if constexpr (!OUT) gmax = fmaxf(gmax, 1.f);   // W itself is kept too
-    uint32_t vv[NS][4];   // V transposed: strip i, columns g (0, 2), g + 8 (1, 3) of tokens 2c, 2c + 1 (0, 1), + 8 (2, 3)
+    uint32_t vm[2] = {0u, 0u}, vv[NS][4];   // V transposed: strip i, columns g (0, 2), g + 8 (1, 3) of tokens 2c, 2c + 1 (0, 1), + 8 (2, 3)
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         uint32_t x[4];
         ldsm_trans(vt + (i * 16 + ln.t_row) * kColPitch + ln.t_col * 2, x);
         vv[i][0] = x[0]; vv[i][1] = x[2]; vv[i][2] = x[1]; vv[i][3] = x[3];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            vmax[e & 1] = fmaxf(vmax[e & 1], fmaxf(fabsf(__uint_as_float(vv[i][e] << 16)), fabsf(__uint_as_float(vv[i][e] & 0xffff0000u))));
+        asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(vm[0]) : "r"(vv[i][0]));
+        asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(vm[1]) : "r"(vv[i][1]));
+        asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(vm[0]) : "r"(vv[i][2]));
+        asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(vm[1]) : "r"(vv[i][3]));
     }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) vmax[h] = fmaxf(__uint_as_float((vm[h] & 0x7fffu) << 16), __uint_as_float(vm[h] & 0x7fff0000u));
     vmax[0] *= gmax;
     vmax[1] *= gmax;
     S.template rescale<3>(vmax, back);
     uint32_t sa[KS][4], sl[EXACT ? KS : 1][4];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-        pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);
-        seen.see(sa[s]);
+        pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);   // (what does not fit shows in U)
         if constexpr (EXACT) pack_a_rest(S.x[2 * s], S.x[2 * s + 1], sa[s], sl[s]);
     }
     if constexpr (!OUT) kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + n, col0, sa, back, g, c);
@@ -431,11 +463,11 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
     for (int i = 0; i < NS; ++i)
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const float2 eb = gate2(gates, kEb, i * 16 + 8 * m + 2 * c);
+            const f32x2 eb = gate_pair(gates, kEb, i * 16 + 8 * m + 2 * c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                w[i][m][e] *= e & 1 ? eb.y : eb.x;
-                if constexpr (OUT) o[i][m][e] *= e & 1 ? eb.y : eb.x;
+            for (int h = 0; h < 2; ++h) {
+                set_pair(w[i][m], h, fmul2(pair(w[i][m], h), eb));
+                if constexpr (OUT) set_pair(o[i][m], h, fmul2(pair(o[i][m], h), eb));
             }
         }
 #pragma unroll
@@ -443,19 +475,17 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
         float r[2][4], uu[2][4] = {};
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const float2 ku = gate2(gates, kKu, i * 16 + 8 * m + 2 * c), gv = gate2(gates, kGv, i * 16 + 8 * m + 2 * c);
+            const f32x2 ku = gate_pair(gates, kKu, i * 16 + 8 * m + 2 * c), gv = gate_pair(gates, kGv, i * 16 + 8 * m + 2 * c);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t y = vv[i][2 * m + h];
-                w[i][m][2 * h] = fmaf(__uint_as_float(y << 16), S.scale[h], -ku.x * w[i][m][2 * h]);
-                w[i][m][2 * h + 1] = fmaf(__uint_as_float(y & 0xffff0000u), S.scale[h], -ku.y * w[i][m][2 * h + 1]);
-                r[m][2 * h] = gv.x * w[i][m][2 * h];
-                r[m][2 * h + 1] = gv.y * w[i][m][2 * h + 1];
+                const f32x2 got = fmul2(pair(w[i][m], h), ku);
+                const f32x2 y = ffma2(got, pack2(-1.f, -1.f), fmul2(widen_bf16(vv[i][2 * m + h]), pack2(S.scale[h], S.scale[h])));
+                if constexpr (!OUT) set_pair(w[i][m], h, y);
+                set_pair(r[m], h, fmul2(gv, y));
             }
         }
         uint32_t ra[4], rl[4], u[4], ul[4];
         pack_terms<TERMS>(r, ra, rl);
-        seen.see(ra);
         times_block<false, TERMS>(uu, ra, rl, base + lay.inv(buf) + i * kBlock, base + lay.inv_lo(buf) + i * kBlock, ln);
         pack_terms<TERMS>(uu, u, ul);
         seen.see(u);
@@ -468,9 +498,9 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
         uint32_t ud[4], udl[4];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const float2 dl = gate2(gates, kDl, i * 16 + 8 * m + 2 * c);
+            const f32x2 dl = gate_pair(gates, kDl, i * 16 + 8 * m + 2 * c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) uu[m][e] *= e & 1 ? dl.y : dl.x;
+            for (int h = 0; h < 2; ++h) set_pair(uu[m], h, fmul2(pair(uu[m], h), dl));
         }
         pack_terms<TERMS>(uu, ud, udl);
         rows_into_state<DKP, TERMS>(S, ud, udl, kt, i, ln);
@@ -478,9 +508,13 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
         if constexpr (OUT) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                const float2 qu = gate2(gates, kQu, i * 16 + 8 * m + 2 * c);
+                const f32x2 qu = gate_pair(gates, kQu, i * 16 + 8 * m + 2 * c);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) res[m][h] = pack_bf16(o[i][m][2 * h] * qu.x * back[h], o[i][m][2 * h + 1] * qu.y * back[h]);
+                for (int h = 0; h < 2; ++h) {
+                    float x, y;
+                    unpack2(fmul2(fmul2(pair(o[i][m], h), qu), pack2(back[h], back[h])), x, y);
+                    res[m][h] = pack_bf16(x, y);
+                }
             }
         } else {   // W of the strip: what its own block takes off
             float own[2][4] = {};
@@ -534,8 +568,7 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
     uint32_t aa[KS][4], al[EXACT ? KS : 1][4];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-        pack_a(A.x[2 * s], A.x[2 * s + 1], aa[s]);
-        seen.see(aa[s]);
+        pack_a(A.x[2 * s], A.x[2 * s + 1], aa[s]);   // (what does not fit shows in dU)
         if constexpr (EXACT) pack_a_rest(A.x[2 * s], A.x[2 * s + 1], aa[s], al[s]);
     }
     kept.keep_state<DKP>(kept.A, kept.z, unit * chunks + n, col0, aa, back, g, c);
@@ -543,12 +576,9 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
     auto d_out = [&](int i, float (&x)[2][4]) {   // scaled
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const float2 qu = gate2(gates, kQu, i * 16 + 8 * m + 2 * c);
+            const f32x2 qu = gate_pair(gates, kQu, i * 16 + 8 * m + 2 * c);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                x[m][2 * h] = __uint_as_float(dd[i][2 * m + h] << 16) * qu.x * A.scale[h];
-                x[m][2 * h + 1] = __uint_as_float(dd[i][2 * m + h] & 0xffff0000u) * qu.y * A.scale[h];
-            }
+            for (int h = 0; h < 2; ++h) set_pair(x[m], h, fmul2(fmul2(widen_bf16(dd[i][2 * m + h]), qu), pack2(A.scale[h], A.scale[h])));
         }
     };
     float r[NS][2][4] = {};
@@ -558,9 +588,9 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
     for (int i = 0; i < NS; ++i)
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const float2 dl = gate2(gates, kDl, i * 16 + 8 * m + 2 * c);
+            const f32x2 dl = gate_pair(gates, kDl, i * 16 + 8 * m + 2 * c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r[i][m][e] *= e & 1 ? dl.y : dl.x;
+            for (int h = 0; h < 2; ++h) set_pair(r[i][m], h, fmul2(pair(r[i][m], h), dl));
         }
 #pragma unroll
     for (int j = NS - 1; j >= 0; --j) {
@@ -568,7 +598,6 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
         uint32_t db[4], dbl[4];
         d_out(j, x);
         pack_terms<TERMS>(x, db, dbl);
-        seen.see(db);
 #pragma unroll
         for (int i = j; i >= 0; --i) times_block<true, TERMS>(r[i], db, dbl, base + lay.p(buf) + block_of(j, i), base + lay.p_lo(buf) + block_of(j, i), ln);
     }
@@ -577,18 +606,18 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
         uint32_t pa[4], pl[4];
         float du[2][4] = {}, x[2][4];
         pack_terms<TERMS>(r[i], pa, pl);
-        seen.see(pa);
         times_block<true, TERMS>(du, pa, pl, base + lay.inv(buf) + i * kBlock, base + lay.inv_lo(buf) + i * kBlock, ln);
         uint32_t dv[2][2], dh[2][2];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const float2 gv = gate2(gates, kGv, i * 16 + 8 * m + 2 * c), gn = gate2(gates, kGn, i * 16 + 8 * m + 2 * c);
+            const f32x2 gv = gate_pair(gates, kGv, i * 16 + 8 * m + 2 * c), gn = gate_pair(gates, kGn, i * 16 + 8 * m + 2 * c);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                dv[m][h] = pack_bf16(du[m][2 * h] * gv.x * back[h], du[m][2 * h + 1] * gv.y * back[h]);
+                float p, q;
+                unpack2(fmul2(fmul2(pair(du[m], h), gv), pack2(back[h], back[h])), p, q);
+                dv[m][h] = pack_bf16(p, q);
                 dh[m][h] = pack_half(du[m][2 * h], du[m][2 * h + 1]);
-                x[m][2 * h] = -gn.x * du[m][2 * h];
-                x[m][2 * h + 1] = -gn.y * du[m][2 * h + 1];
+                set_pair(x[m], h, fmul2(fmul2(pair(du[m], h), gn), pack2(-1.f, -1.f)));
             }
         }
         const uint32_t ds[4] = {dh[0][0], dh[0][1], dh[1][0], dh[1][1]};
@@ -604,11 +633,11 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
         d_out(i, y);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const float2 eb = gate2(gates, kEb, i * 16 + 8 * m + 2 * c);
+            const f32x2 eb = gate_pair(gates, kEb, i * 16 + 8 * m + 2 * c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[m][e] *= e & 1 ? eb.y : eb.x;
-                y[m][e] *= e & 1 ? eb.y : eb.x;
+            for (int h = 0; h < 2; ++h) {
+                set_pair(x[m], h, fmul2(pair(x[m], h), eb));
+                set_pair(y[m], h, fmul2(pair(y[m], h), eb));
             }
         }
         pack_terms<TERMS>(x, pe, pel);

@@ -90,13 +90,40 @@ struct Largest {
     __half2 m = __float2half2_rn(0.f);
     __device__ __forceinline__ void see(const uint32_t (&a)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __half2*>(&a[i])));
+        for (int i = 0; i < 4; ++i) {
+            uint32_t& x = *reinterpret_cast<uint32_t*>(&m);
+            asm("max.NaN.xorsign.abs.f16x2 %0, %0, %1;" : "+r"(x) : "r"(a[i]));   // (larger magnitude, the signs' product)
+        }
     }
     __device__ __forceinline__ bool lost() const {   // infinite or not a number
         const float2 f = __half22float2(m);
-        return !(fmaxf(f.x, f.y) <= 65504.f) || f.x != f.x || f.y != f.y;
+        return !(fabsf(f.x) <= 65504.f) || !(fabsf(f.y) <= 65504.f);
     }
 };
+
+// Largest magnitude of eight bf16, as the bits of one.
+__device__ __forceinline__ uint32_t largest_bf16(const uint4& v) {
+    uint32_t m = v.x;
+    asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.y));
+    asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.z));
+    asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.w));
+    m &= 0x7fff7fffu;
+    return max(m & 0xffffu, m >> 16);
+}
+__device__ __forceinline__ f32x2 widen_bf16(uint32_t x) { return pack2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t pack_half(f32x2 x) {
+    float a, b;
+    unpack2(x, a, b);
+    return pack_half(a, b);
+}
+__device__ __forceinline__ uint4 bf16_to_half(const uint4& v, float s) {   // times s
+    const f32x2 ss = pack2(s, s);
+    return make_uint4(pack_half(fmul2(widen_bf16(v.x), ss)), pack_half(fmul2(widen_bf16(v.y), ss)), pack_half(fmul2(widen_bf16(v.z), ss)),
+                      pack_half(fmul2(widen_bf16(v.w), ss)));
+}
+// Two neighbouring values of an accumulator at a time.
+__device__ __forceinline__ f32x2 pair(const float (&t)[4], int h) { return pack2(t[2 * h], t[2 * h + 1]); }
+__device__ __forceinline__ void set_pair(float (&t)[4], int h, f32x2 x) { unpack2(x, t[2 * h], t[2 * h + 1]); }
 
 // 2^-e and 2^e for the exponent e of a positive float's bits (1 and 1 where it has none: zero, subnormal, infinite, NaN).
 __device__ __forceinline__ void power_of(uint32_t exponent, float& down, float& up) {
