@@ -23,7 +23,9 @@ using bf = __nv_bfloat16;
 template <int DKP>
 constexpr int grad_threads() { return DKP > 64 ? 256 : 128; }   // two warps a strip where the key dimensions are many
 
-enum { kB, kEb, kDl, kBeta, kKu, kQu, kH, kHf, kE, kE2, kRows };   // per token; the last two: a strip's first and second warp's part of e
+// Per token, arrays of kChunk floats: running sum of log2 alpha, 2^b, 2^{b_C - b}, beta, scales of the rows of K, Q and dO (2^e, ..), those of dO
+// and Q together over their largest, beta 2^e, beta 2^{2e}, and e of a strip's first and second warp.
+enum { kB, kEb, kDl, kBeta, kKu, kQu, kH, kHf, kGv, kGn, kE, kE2, kRows };
 
 struct GradLayout {
     int kp, vp, k, q, d, r, w, s, a, gates, cols, total;
@@ -40,7 +42,7 @@ struct GradLayout {
         s = take(dvp * kp);
         a = take(dvp * kp);
         gates = take(kChunk * kRows * 4);
-        cols = take(dvp * 2 * 4 + 16 * 4);   // per column: y over its largest, and that times z over its largest; then what is reduced
+        cols = take(dvp * 2 * 4 + 16 * 4);   // per column: y over the largest, and that times z over its largest; then what is reduced
         total = at;
     }
 };
@@ -59,18 +61,22 @@ __device__ __forceinline__ uint4 scale_halves(uint4 x, float s) {
     return x;
 }
 
-// Strip I of the chunk; key dimensions in sixteens s0, s0 + step, ..
-template <int DKP, int I>
-__device__ __forceinline__ void grad_strip(const Gdr<bf>& a, unsigned char* smem, const GradLayout& lay, int dvp, long long unit, int n, float Y, float Z,
-                                           float HF, int s0, int step, int lane, Largest& seen) {
+__device__ __forceinline__ f32x2 row_pair(const float* gates, int row, int t) { return *reinterpret_cast<const f32x2*>(gates + row * kChunk + t); }
+
+// Strip I of the chunk; key dimensions in sixteens s0, s0 + step, ..  (I is a variable and the five blocks' code the same for all warps: with a
+// copy for each strip, fetching instructions was what the warps waited for most, 173 us for 64 x 12 units of 196 tokens, 32 x 64.)
+template <int DKP>
+__device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsigned char* smem, const GradLayout& lay, int dvp, long long unit, int n, float Y,
+                                           float Z, float HF, int s0, int step, int lane, Largest& seen) {
     constexpr int KP = DKP * 2 + 16;
-    const int g = lane >> 2, c = lane & 3, vp = lay.vp;
+    const int g = lane >> 2, c = lane & 3, vp = lay.vp, strips = (min(kChunk, a.L - n * kChunk) + 15) >> 4;
     const Lane ln(lane);
     const uint32_t base = smem_u32(smem), kt = base + lay.k, qt = base + lay.q, dt = base + lay.d, rt = base + lay.r, wt = base + lay.w, st = base + lay.s,
                    at = base + lay.a;
     float* const gates = reinterpret_cast<float*>(smem + lay.gates);
-    auto b_of = [&](uint32_t tile, int row0, int col0) { return tile + (row0 + ln.b_row) * vp + (col0 + ln.b_col) * 2; };
-    // x: dO W^T up to the diagonal (blocks 0 .. I), W dO^T from it on (blocks I .. 3, kept behind them); e: dU W^T, W dU^T
+    const int lane_at = ln.b_row * vp + ln.b_col * 2;
+    auto b_of = [&](uint32_t tile, int row0, int col0) { return tile + lane_at + row0 * vp + col0 * 2; };
+    // Block p: of dO W^T and dU W^T up to the diagonal (p <= I, columns of strip p), of W dO^T and W dU^T from it on (columns of strip p - 1)
     float x[5][2][4] = {}, e[5][2][4] = {};
 #pragma unroll 1
     for (int v = 0; v < dvp; v += 16) {
@@ -79,61 +85,84 @@ __device__ __forceinline__ void grad_strip(const Gdr<bf>& a, unsigned char* smem
         ldsm_a(b_of(rt, I * 16, v), ra);
         ldsm_a(b_of(wt, I * 16, v), wa);
 #pragma unroll
-        for (int j = 0; j <= I; ++j) {
+        for (int p = 0; p < 5; ++p) {
             uint32_t y[4];
-            ldsm(b_of(wt, j * 16, v), y);
-            mma(x[j][0], da, y[0], y[1]);
-            mma(x[j][1], da, y[2], y[3]);
-            mma(e[j][0], ra, y[0], y[1]);
-            mma(e[j][1], ra, y[2], y[3]);
-        }
-#pragma unroll
-        for (int j = I; j < 4; ++j) {
-            uint32_t y[4];
-            ldsm(b_of(dt, j * 16, v), y);
-            mma(x[j + 1][0], wa, y[0], y[1]);
-            mma(x[j + 1][1], wa, y[2], y[3]);
-            ldsm(b_of(rt, j * 16, v), y);
-            mma(e[j + 1][0], wa, y[0], y[1]);
-            mma(e[j + 1][1], wa, y[2], y[3]);
+            if (p <= I) {
+                ldsm(b_of(wt, p * 16, v), y);
+                mma(x[p][0], da, y[0], y[1]);
+                mma(x[p][1], da, y[2], y[3]);
+                mma(e[p][0], ra, y[0], y[1]);
+                mma(e[p][1], ra, y[2], y[3]);
+            } else if (p <= strips) {
+                ldsm(b_of(dt, (p - 1) * 16, v), y);
+                mma(x[p][0], wa, y[0], y[1]);
+                mma(x[p][1], wa, y[2], y[3]);
+                ldsm(b_of(rt, (p - 1) * 16, v), y);
+                mma(e[p][0], wa, y[0], y[1]);
+                mma(e[p][1], wa, y[2], y[3]);
+            }
         }
     }
     const int t0 = I * 16 + g;   // rows t0, t0 + 8
     const float bt[2] = {gates[kB * kChunk + t0], gates[kB * kChunk + t0 + 8]}, beta[2] = {gates[kBeta * kChunk + t0], gates[kBeta * kChunk + t0 + 8]},
                 ku[2] = {gates[kKu * kChunk + t0], gates[kKu * kChunk + t0 + 8]};
-    // dbeta: the diagonal of dU W^T
-    float db[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const float d = g & 1 ? e[I][h][2 * h + 1] : e[I][h][2 * h];   // of row g + 8 h, column the same, in lane c = g / 2
-        db[h] = __shfl_sync(0xffffffffu, d, (lane & 28) | (g >> 1)) * ku[h] * Y * Z;
-    }
-    // to operands
+    const float end = gates[kB * kChunk + I * 16 + 15];
+    float db[2] = {0.f, 0.f};
+    // to operands, e^{b_t - b_s} by way of the last token of s' sixteen off the diagonal (both factors are at most one)
     uint32_t xa[5][4], ea[5][4];
 #pragma unroll
     for (int p = 0; p < 5; ++p) {
         const bool low = p <= I;
         const int j = low ? p : p - 1;
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int col = j * 16 + 8 * m + 2 * c;
-            const float2 bc = row2(gates, kB, col), be = row2(gates, kBeta, col), kc = row2(gates, kKu, col), hf = row2(gates, kHf, col);
+        if (j != I) {
+            const float ref = low ? gates[kB * kChunk + j * 16 + 15] : end;
+            f32x2 er[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int row = t0 + 8 * h;
-                float xx[2], ee[2];
+                const float r = ex2(low ? bt[h] - ref : ref - bt[h]);
+                er[h] = pack2(r, r);
+            }
 #pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    const float b = f ? bc.y : bc.x, bb = f ? be.y : be.x, k = f ? kc.y : kc.x;
-                    const int cc = col + f;
-                    const bool in = low ? cc <= row : cc >= row, strict = low ? cc < row : cc > row;
-                    const float gam = in ? ex2(low ? bt[h] - b : b - bt[h]) : 0.f;
-                    // low: columns s, times 2^e beta_s; else columns t, times the scale of dO's and q's rows, or beta_t 2^{2e}
-                    xx[f] = in ? x[p][m][2 * h + f] * gam * (low ? bb * k : (f ? hf.y : hf.x)) : 0.f;
-                    ee[f] = strict ? e[p][m][2 * h + f] * gam * (low ? bb * k : -bb * k * k) : 0.f;
+            for (int m = 0; m < 2; ++m) {
+                const int col = j * 16 + 8 * m + 2 * c;
+                const float2 bc = row2(gates, kB, col);
+                f32x2 fx = pack2(ex2(low ? ref - bc.x : bc.x - ref), ex2(low ? ref - bc.y : bc.y - ref)), fe = fx;
+                if (low) fe = fx = fmul2(fx, row_pair(gates, kGv, col));   // columns s: times 2^e beta_s
+                else {                                                      // columns t: times the scale of dO's and q's rows, or - beta_t 2^{2e}
+                    fx = fmul2(fx, row_pair(gates, kHf, col));
+                    fe = fmul2(fmul2(fe, row_pair(gates, kGn, col)), pack2(-1.f, -1.f));
                 }
-                xa[p][2 * m + h] = pack_half(xx[0], xx[1]);
-                ea[p][2 * m + h] = pack_half(ee[0], ee[1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    xa[p][2 * m + h] = pack_half(fmul2(pair(x[p][m], h), fmul2(fx, er[h])));
+                    ea[p][2 * m + h] = pack_half(fmul2(pair(e[p][m], h), fmul2(fe, er[h])));
+                }
+            }
+        } else {
+            if (low)   // dbeta: the diagonal of dU W^T, row g + 8 h and the same column: in lane c = g / 2
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float d = g & 1 ? e[p][h][2 * h + 1] : e[p][h][2 * h];
+                    db[h] = __shfl_sync(0xffffffffu, d, (lane & 28) | (g >> 1)) * ku[h] * Y * Z;
+                }
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const int cc = 8 * m + 2 * c, col = I * 16 + cc;
+                const float2 bc = row2(gates, kB, col), fx = row2(gates, low ? kGv : kHf, col), fe = row2(gates, low ? kGv : kGn, col);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = g + 8 * h;
+                    float xx[2], ee[2];
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) {
+                        const bool in = low ? cc + f <= row : cc + f >= row, strict = in && cc + f != row;
+                        const float gam = in ? ex2(low ? bt[h] - (f ? bc.y : bc.x) : (f ? bc.y : bc.x) - bt[h]) : 0.f;
+                        xx[f] = in ? x[p][m][2 * h + f] * gam * (f ? fx.y : fx.x) : 0.f;
+                        ee[f] = strict ? e[p][m][2 * h + f] * gam * (f ? fe.y : fe.x) * (low ? 1.f : -1.f) : 0.f;
+                    }
+                    xa[p][2 * m + h] = pack_half(xx[0], xx[1]);
+                    ea[p][2 * m + h] = pack_half(ee[0], ee[1]);
+                }
             }
         }
         seen.see(xa[p]);
@@ -163,27 +192,27 @@ __device__ __forceinline__ void grad_strip(const Gdr<bf>& a, unsigned char* smem
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
-                hq[m][f] *= eb[f >> 1];
-                h1[m][f] *= eb[f >> 1];
-                h2[m][f] *= dl[f >> 1];
+            for (int h = 0; h < 2; ++h) {
+                set_pair(hq[m], h, fmul2(pair(hq[m], h), pack2(eb[h], eb[h])));
+                set_pair(h1[m], h, fmul2(pair(h1[m], h), pack2(eb[h], eb[h])));
+                set_pair(h2[m], h, fmul2(pair(h2[m], h), pack2(dl[h], dl[h])));
             }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int p = 0; p < 5; ++p) {
             uint32_t y[4];
-            ldsm_trans(at_t<KP>(ln, kt, j * 16, s * 16), y);
-            if (j <= I) {
-                mma(hq[0], xa[j], y[0], y[1]);
-                mma(hq[1], xa[j], y[2], y[3]);
-                mma(h1[0], ea[j], y[0], y[1]);
-                mma(h1[1], ea[j], y[2], y[3]);
-            }
-            if (j >= I) {
-                mma(h2[0], ea[j + 1], y[0], y[1]);
-                mma(h2[1], ea[j + 1], y[2], y[3]);
-                ldsm_trans(at_t<KP>(ln, qt, j * 16, s * 16), y);
-                mma(h3[0], xa[j + 1], y[0], y[1]);
-                mma(h3[1], xa[j + 1], y[2], y[3]);
+            if (p <= I) {
+                ldsm_trans(at_t<KP>(ln, kt, p * 16, s * 16), y);
+                mma(hq[0], xa[p], y[0], y[1]);
+                mma(hq[1], xa[p], y[2], y[3]);
+                mma(h1[0], ea[p], y[0], y[1]);
+                mma(h1[1], ea[p], y[2], y[3]);
+            } else if (p <= strips) {
+                ldsm_trans(at_t<KP>(ln, kt, (p - 1) * 16, s * 16), y);
+                mma(h2[0], ea[p], y[0], y[1]);
+                mma(h2[1], ea[p], y[2], y[3]);
+                ldsm_trans(at_t<KP>(ln, qt, (p - 1) * 16, s * 16), y);
+                mma(h3[0], xa[p], y[0], y[1]);
+                mma(h3[1], xa[p], y[2], y[3]);
             }
         }
 #pragma unroll
@@ -223,7 +252,7 @@ __device__ __forceinline__ void grad_strip(const Gdr<bf>& a, unsigned char* smem
 }
 
 template <int DKP>
-__global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 3 : DKP <= 64 ? 2 : 1) gdr_grad_kernel(Gdr<bf> a, GdrKept kept, int chunks) {
+__global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64 ? 2 : 1) gdr_grad_kernel(Gdr<bf> a, GdrKept kept, int chunks) {
     constexpr int KP = DKP * 2 + 16, kThreads = grad_threads<DKP>();
     constexpr int kLanes = DKP <= 16 ? 2 : DKP <= 32 ? 4 : DKP <= 64 ? 8 : 16;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -236,16 +265,40 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 3 : DKP <= 64
     float *const cy = reinterpret_cast<float*>(smem + lay.cols), *const cyz = cy + dvp, *const red = cyz + dvp;
     pdl_wait();
     pdl_launch_dependents();
+    // everything comes in by asynchronous copies at once, and is turned into operands where it lies
     const uint32_t base = smem_u32(smem);
-    for (int i = tid; i < kChunk * (dvp / 8); i += kThreads) {
-        const int t = i / (dvp / 8), e = i % (dvp / 8) * 8;
-        cp_async16(base + lay.w + t * lay.vp + e * 2, kept.w + (here * kChunk + t) * dvp + e, t < nt);
+    for (int i = tid; i < kChunk * (DKP / 8); i += kThreads) {
+        const int t = i / (DKP / 8), e = i % (DKP / 8) * 8;
+        const bool in = t < nt && e < a.dk;
+        const long long at = in ? a.row(unit, t0 + t) * a.dk + e : 0;
+        cp_async16(base + lay.k + t * KP + e * 2, a.k + at, in);
+        cp_async16(base + lay.q + t * KP + e * 2, a.q + at, in);
     }
+    const int lg = dvp <= 16 ? 1 : dvp <= 32 ? 2 : dvp <= 64 ? 3 : 4, piece = (tid & ((1 << lg) - 1)) * 8;   // lanes of a row of dv columns, and this one's columns
+    if (piece < dvp)
+        for (int t = tid >> lg; t < kChunk; t += kThreads >> lg) {
+            const bool in = t < nt;   // (rows behind the last token were not written)
+            const uint32_t to = t * lay.vp + piece * 2;
+            const long long at = (here * kChunk + t) * dvp + piece;
+            cp_async16(base + lay.w + to, kept.w + at, in);
+            cp_async16(base + lay.r + to, kept.du + at, in);
+            cp_async16(base + lay.d + to, a.d_out + (in && piece < a.dv ? a.row(unit, t0 + t) * a.dv + piece : 0), in && piece < a.dv);
+        }
     for (int i = tid; i < dvp * (DKP / 8); i += kThreads) {
         const int j = i / (DKP / 8), e = i % (DKP / 8) * 8;
         cp_async16(base + lay.s + j * KP + e * 2, kept.S + (states * dvp + j) * DKP + e, true);
+        cp_async16(base + lay.a + j * KP + e * 2, kept.A + (here * dvp + j) * DKP + e, true);
     }
     cp_async_commit();
+    // the state behind the chunk, for the gradient that the next chunk's first gate sees
+    constexpr int kBehind = 128 * (DKP / 8) / kThreads;   // pieces of a thread, at most
+    const bool behind = n + 1 < chunks || a.d_state_out;
+    uint4 next[kBehind];
+#pragma unroll
+    for (int p = 0; p < kBehind; ++p) {
+        const int i = tid + p * kThreads;
+        if (behind && i < dvp * (DKP / 8)) next[p] = *reinterpret_cast<const uint4*>(kept.S + (states + 1) * dvp * DKP + i * 8);
+    }
     // columns: their powers of two over the largest
     float Y = 0.f, Z = 0.f;
     for (int j = lane; j < dvp; j += 32) {
@@ -286,76 +339,84 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 3 : DKP <= 64
         two(kDl, ex2(all - b0), ex2(all - b1));
         two(kBeta, be[0], be[1]);
     }
+    cp_async_wait<0>();
     __syncthreads();
-    // K, Q to fp16 under their rows' powers of two; dO too, a warp a row, and its columns' factors
-    for (int i = tid; i < 2 * kChunk * kLanes; i += kThreads) {
-        const int r = i / kLanes, e8 = i % kLanes * 8, t = r & (kChunk - 1);
+    // K, Q to fp16 under their rows' powers of two
+#pragma unroll
+    for (int p = 0; p < 2 * kChunk * kLanes / kThreads; ++p) {
+        const int i = tid + p * kThreads, r = i / kLanes, e8 = i % kLanes * 8, t = r & (kChunk - 1);
         const bool key = r < kChunk;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (t < nt && e8 < a.dk) x = *reinterpret_cast<const uint4*>((key ? a.k : a.q) + a.row(unit, t0 + t) * a.dk + e8);
-        uint32_t m = max(max(max(x.x & 0x7fffu, x.x >> 16 & 0x7fffu), max(x.y & 0x7fffu, x.y >> 16 & 0x7fffu)),
-                         max(max(x.z & 0x7fffu, x.z >> 16 & 0x7fffu), max(x.w & 0x7fffu, x.w >> 16 & 0x7fffu)));
+        uint4* const at = reinterpret_cast<uint4*>(smem + (key ? lay.k : lay.q) + t * KP + e8 * 2);
+        const uint4 x = e8 < DKP ? *at : make_uint4(0u, 0u, 0u, 0u);
+        uint32_t m = largest_bf16(x);
 #pragma unroll
         for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
         float down, up;
         power_of(m >> 7, down, up);
-        auto half2_of = [&](uint32_t y) { return pack_half(__uint_as_float(y << 16) * down, __uint_as_float(y & 0xffff0000u) * down); };
-        if (e8 < DKP)
-            *reinterpret_cast<uint4*>(smem + (key ? lay.k : lay.q) + t * KP + e8 * 2) = make_uint4(half2_of(x.x), half2_of(x.y), half2_of(x.z), half2_of(x.w));
-        if (e8 == 0) gates[(key ? kKu : kQu) * kChunk + t] = up;
-    }
-    for (int i = tid; i < kChunk * 16; i += kThreads) {   // sixteen lanes a row, pieces of eight columns
-        const int t = i >> 4, e8 = (i & 15) * 8;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (t < nt && e8 < a.dv) x = *reinterpret_cast<const uint4*>(a.d_out + a.row(unit, t0 + t) * a.dv + e8);
-        uint32_t m = max(max(max(x.x & 0x7fffu, x.x >> 16 & 0x7fffu), max(x.y & 0x7fffu, x.y >> 16 & 0x7fffu)),
-                         max(max(x.z & 0x7fffu, x.z >> 16 & 0x7fffu), max(x.w & 0x7fffu, x.w >> 16 & 0x7fffu)));
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        float down, up;
-        power_of(m >> 7, down, up);
-        if (e8 < dvp) {
-            uint32_t h[4];
-            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-                h[p] = pack_half(__uint_as_float(y[p] << 16) * down * cy[e8 + 2 * p], __uint_as_float(y[p] & 0xffff0000u) * down * cy[e8 + 2 * p + 1]);
-            *reinterpret_cast<uint4*>(smem + lay.d + t * lay.vp + e8 * 2) = make_uint4(h[0], h[1], h[2], h[3]);
-        }
-        if (e8 == 0) gates[kH * kChunk + t] = up;
-    }
-    for (int i = tid; i < kChunk * (dvp / 8); i += kThreads) {
-        const int t = i / (dvp / 8), e = i % (dvp / 8) * 8;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);   // (rows behind the last token were not written)
-        if (t < nt) x = *reinterpret_cast<const uint4*>(kept.du + (here * kChunk + t) * dvp + e);
-        __half2* h = reinterpret_cast<__half2*>(&x);
-#pragma unroll
-        for (int p = 0; p < 4; ++p) h[p] = __hmul2(h[p], __floats2half2_rn(cyz[e + 2 * p], cyz[e + 2 * p + 1]));
-        *reinterpret_cast<uint4*>(smem + lay.r + t * lay.vp + e * 2) = x;
-    }
-    // A, and its product with the state behind the chunk: the gradient that the next chunk's first gate sees
-    float anchor = 0.f;
-    const bool behind = n + 1 < chunks || a.d_state_out;
-    for (int i = tid; i < dvp * (DKP / 8); i += kThreads) {
-        const int j = i / (DKP / 8), e = i % (DKP / 8) * 8;
-        const uint4 x = *reinterpret_cast<const uint4*>(kept.A + (here * dvp + j) * DKP + e);
-        *reinterpret_cast<uint4*>(smem + lay.a + j * KP + e * 2) = scale_halves(x, cyz[j]);
-        if (behind) {
-            const uint4 s = *reinterpret_cast<const uint4*>(kept.S + ((states + 1) * dvp + j) * DKP + e);
-            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ss[4] = {s.x, s.y, s.z, s.w};
-            float dot = 0.f;
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const float2 u = unpack_half(xs[p]), v = unpack_half(ss[p]);
-                dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
+        if (e8 < DKP) *at = bf16_to_half(x, down);
+        if (e8 == 0) {
+            gates[(key ? kKu : kQu) * kChunk + t] = up;
+            if (key) {
+                const float gv = gates[kBeta * kChunk + t] * up;
+                gates[kGv * kChunk + t] = gv;
+                gates[kGn * kChunk + t] = gv * up;
             }
-            anchor = fmaf(dot * kept.y[(states + 1) * dvp + j], kept.z[here * dvp + j], anchor);
+        }
+    }
+    // dO under its rows' and its columns' powers of two, dU under its columns'
+    {
+        f32x2 fy[4];
+        __half2 fz[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            fy[p] = piece < dvp ? *reinterpret_cast<const f32x2*>(cy + piece + 2 * p) : 0ull;
+            fz[p] = piece < dvp ? __floats2half2_rn(cyz[piece + 2 * p], cyz[piece + 2 * p + 1]) : __float2half2_rn(0.f);
+        }
+        for (int t = tid >> lg; t < kChunk; t += kThreads >> lg) {
+            uint4* const at = reinterpret_cast<uint4*>(smem + lay.d + t * lay.vp + piece * 2);
+            const uint4 x = piece < dvp ? *at : make_uint4(0u, 0u, 0u, 0u);
+            uint32_t m = largest_bf16(x);
+            for (int o = 1; o < 1 << lg; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+            float down, up;
+            power_of(m >> 7, down, up);
+            if (piece < dvp) {
+                const f32x2 dn = pack2(down, down);
+                *at = make_uint4(pack_half(fmul2(fmul2(widen_bf16(x.x), dn), fy[0])), pack_half(fmul2(fmul2(widen_bf16(x.y), dn), fy[1])),
+                                 pack_half(fmul2(fmul2(widen_bf16(x.z), dn), fy[2])), pack_half(fmul2(fmul2(widen_bf16(x.w), dn), fy[3])));
+                uint4* const ar = reinterpret_cast<uint4*>(smem + lay.r + t * lay.vp + piece * 2);
+                uint4 y = *ar;
+                __half2* const h = reinterpret_cast<__half2*>(&y);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) h[p] = __hmul2(h[p], fz[p]);
+                *ar = y;
+            }
+            if (piece == 0) gates[kH * kChunk + t] = up;
+        }
+    }
+    // A under its columns' powers of two, and its product with the state behind the chunk
+    float anchor = 0.f;
+#pragma unroll
+    for (int p = 0; p < kBehind; ++p) {
+        const int i = tid + p * kThreads, j = i / (DKP / 8), e = i % (DKP / 8) * 8;
+        if (i < dvp * (DKP / 8)) {
+            uint4* const at = reinterpret_cast<uint4*>(smem + lay.a + j * KP + e * 2);
+            const uint4 x = *at;
+            *at = scale_halves(x, cyz[j]);
+            if (behind) {
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ss[4] = {next[p].x, next[p].y, next[p].z, next[p].w};
+                float dot = 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float2 u = unpack_half(xs[q]), v = unpack_half(ss[q]);
+                    dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
+                }
+                anchor = fmaf(dot * kept.y[(states + 1) * dvp + j], kept.z[here * dvp + j], anchor);
+            }
         }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) anchor += __shfl_xor_sync(0xffffffffu, anchor, o);
     if (lane == 0) red[warp] = anchor;
-    cp_async_wait<0>();
     __syncthreads();
     // the scales of dO's and q's rows together, over the largest
     float HF = 0.f;
@@ -372,12 +433,7 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 3 : DKP <= 64
     __syncthreads();
     Largest seen;
     const int strip = warp & 3, half = warp >> 2, step = kThreads / 128;
-    if (strip * 16 < nt) {
-        if (strip == 0) grad_strip<DKP, 0>(a, smem, lay, dvp, unit, n, Y, Z, HF, half, step, lane, seen);
-        else if (strip == 1) grad_strip<DKP, 1>(a, smem, lay, dvp, unit, n, Y, Z, HF, half, step, lane, seen);
-        else if (strip == 2) grad_strip<DKP, 2>(a, smem, lay, dvp, unit, n, Y, Z, HF, half, step, lane, seen);
-        else grad_strip<DKP, 3>(a, smem, lay, dvp, unit, n, Y, Z, HF, half, step, lane, seen);
-    }
+    if (strip * 16 < nt) grad_strip<DKP>(strip, a, smem, lay, dvp, unit, n, Y, Z, HF, half, step, lane, seen);
     const int lost = __syncthreads_or(seen.lost());
     if (tid == 0) kept.lost_grad[here] = lost;
     // dlog_alpha: sums from the chunk's end; a gate that leaves nothing, or has nothing to scale, has none, and the sums start anew there
