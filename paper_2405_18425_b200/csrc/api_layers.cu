@@ -47,7 +47,22 @@ int gdr_fwd_impl(const void* q, const void* k, const void* v, const void* la, co
     a.state_in = (const float*)state_in; a.out = (T*)out; a.state_out = (float*)state_out;
     a.units = units; a.L = L; a.dk = dk; a.dv = dv; a.reverse = reverse != 0;
     if constexpr (sizeof(T) == 2)
-        if (gdr_chunk_supported(dk, dv) && kernel_preference() != VIG_TEST_KERNEL_SIMT) return status_of(launch_gdr_chunk_fwd(a, stream));
+        if (gdr_chunk_supported(dk, dv) && kernel_preference() != VIG_TEST_KERNEL_SIMT) {
+            const size_t need = gdr_chunk_scratch_bytes(units, L, dk, dv);
+            if (need == 0) return status_of(launch_gdr_chunk_fwd(a, nullptr, stream));
+            // segments; an initial state that the call overwrites is put aside, as units that leave the tiles' range start from it again
+            const size_t aside = state_in && state_in == state_out ? (size_t)units * dk * dv * sizeof(float) : 0;
+            char* ws = nullptr;
+            if (pool_alloc((void**)&ws, need + aside, stream) != cudaSuccess) return VIG_ERR_CUDA;
+            cudaError_t e = cudaSuccess;
+            if (aside) {
+                e = cudaMemcpyAsync(ws + need, state_in, aside, cudaMemcpyDeviceToDevice, stream);
+                a.state_in = (const float*)(ws + need);
+            }
+            if (e == cudaSuccess) e = launch_gdr_chunk_fwd(a, ws, stream);
+            const bool freed = cudaFreeAsync(ws, stream) == cudaSuccess;
+            return freed ? status_of(e) : VIG_ERR_CUDA;
+        }
     return status_of(launch_gdr_walk_fwd<T>(a, stream));
 }
 

@@ -32,7 +32,8 @@ cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t str
 
 // ---- forward in chunks on the tensor cores: head sizes that are multiples of eight ----
 bool gdr_chunk_supported(int dk, int dv);
-cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, cudaStream_t stream);
+size_t gdr_chunk_scratch_bytes(long long units, int L, int dk, int dv);   // 0: the call uses no scratch
+cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, void* scratch, cudaStream_t stream);
 
 // What the two walks of the gradient keep, fp16 under powers of two per column; dvp: dv to sixteen, DKP: dk as the kernels pad it.
 struct GdrKept {
@@ -41,7 +42,7 @@ struct GdrKept {
     __half *S, *A;     // transposed, [units][chunks + 1][dvp][DKP] before each chunk (= S y) and behind the last; [units][chunks][dvp][DKP]: what
                        // arrives behind each chunk (= A z)
     float *y, *z;      // [units][chunks + 1][dvp], [units][chunks][dvp]
-    int *lost, *lost_grad;   // [units][dvp / 16], [units][chunks]: something left the range of fp16
+    int* lost_grad;    // [units][chunks]: something left the range of fp16
     int dvp;
     // Sixteen columns of a state, as packed for an A operand.
     template <int DKP>
@@ -71,7 +72,7 @@ cudaError_t launch_gdr_grad(const Gdr<__nv_bfloat16>& a, const GdrKept& kept, cu
 // Redoes every unit of which a flag is set (first: `per` flags a unit, second: `chunks`) by the fp32 walks, `slots` at a time.
 size_t gdr_repair_slot_bytes(int L, int dk, int dv);
 cudaError_t launch_gdr_repair(const Gdr<__nv_bfloat16>& a, const int* first, int per, const int* second, int chunks, void* scratch, int slots, cudaStream_t stream);
-cudaError_t launch_gdr_chunk_walks(const Gdr<__nv_bfloat16>& a, const GdrKept& kept, cudaStream_t stream);
+cudaError_t launch_gdr_repair_fwd(const Gdr<__nv_bfloat16>& a, const int* flags, int per, cudaStream_t stream);
 
 // ---- one token: state updated in place ----
 template <typename T>

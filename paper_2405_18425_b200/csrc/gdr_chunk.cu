@@ -23,6 +23,7 @@ using namespace gdr;
 using bf = __nv_bfloat16;
 
 constexpr int kMostWarps = 4;       // with columns
+constexpr int kMostColumns = 16;    // sixteens of dv
 constexpr int kPrepWarps = 4;
 constexpr int kPrep = 32 * kPrepWarps;
 constexpr int kBlockPitch = 48, kBlock = 16 * kBlockPitch, kColPitch = 48;
@@ -30,7 +31,12 @@ constexpr int kBlockPitch = 48, kBlock = 16 * kBlockPitch, kColPitch = 48;
 __device__ __forceinline__ int block_of(int i, int j) { return (i * (i + 1) / 2 + j) * kBlock; }
 constexpr int kBarFull = 1, kBarEmpty = 3, kBarPrep = 5;   // named barriers: two of the first two
 
-enum class Way { kForward, kKeep, kBack };   // the call's result; the gradient's forward walk, which keeps W and the states; its way back
+// The call's result; the gradient's forward walk, which keeps W and the states; its way back; and what a segment does to a state: where few
+// units leave SMs idle a long sequence is cut into segments that run side by side.  A first launch takes every segment from zero states and, as
+// further columns without values, from the unit vectors (S behind it = T S + B: both are columns of one loop), a small one (gdr_fold_kernel)
+// carries the true states from segment to segment, and the launch proper starts every segment from its own.  Backwards T^T serves.
+enum class Way { kForward, kKeep, kBack, kSum, kBackSum };
+constexpr bool is_back(Way w) { return w == Way::kBack || w == Way::kBackSum; }
 
 template <int DKP>
 constexpr int key_pitch() { return DKP * 2 + 16; }
@@ -44,11 +50,11 @@ __device__ __forceinline__ f32x2 gate_pair(const float* gates, int row, int t) {
 template <int DKP, bool EXACT, Way WAY>
 struct Layout {
     static constexpr int kKeys = kChunk * key_pitch<DKP>(), kMat = 10 * kBlock, kInv = 4 * kBlock, kCols = kChunk * kColPitch;
-    static constexpr bool kQ = WAY != Way::kKeep;   // queries, and P
+    static constexpr bool kQ = WAY == Way::kForward || is_back(WAY);   // queries, and P
     // of a buffer: keys, queries, N, P, inverses, gates, and what their first rounding left
     static constexpr int kQueries = kKeys, kN = kQueries + (kQ ? kKeys : 0), kP = kN + kMat, kInverse = kP + (kQ ? kMat : 0), kGates = kInverse + kInv,
                          kNLo = kGates + kChunk * kGateRows * 4, kPLo = kNLo + (EXACT ? kMat : 0),
-                         kInvLo = kPLo + (EXACT && WAY == Way::kBack ? kMat : 0), kBuffer = kInvLo + (EXACT ? kInv : 0);
+                         kInvLo = kPLo + (EXACT && is_back(WAY) ? kMat : 0), kBuffer = kInvLo + (EXACT ? kInv : 0);
     static constexpr int x = 2 * kBuffer;                  // the diagonal blocks of beta N, transposed, rows of 20 floats
     static constexpr int cols = x + 4 * 16 * 20 * 4;       // a warp's columns of V or dO, two chunks
     static constexpr int k(int buf) { return buf * kBuffer; }
@@ -63,6 +69,14 @@ struct Layout {
     static constexpr int total(int warps) { return cols + 2 * warps * kCols; }
 };
 
+// Segments of a unit: chunks of one; fp32 [units][segs][dk][dv] states before (backwards: behind) each, what they add, and [units][segs][dk][dk].
+struct Segs {
+    int n, per, sums;   // segments, chunks of one, segments that the first launch takes (the last one's transition serves backwards only)
+    float *in, *sum, *trans;
+    int* lost;   // [units][slots]: something left the range of fp16; a slot for every segment and warp of columns
+    int slots;
+};
+
 // What the gradient's walks leave for its last launch, per unit and chunk (see gdr.h).
 using Kept = GdrKept;
 
@@ -70,9 +84,9 @@ __device__ __forceinline__ void bar_arrive(int id, int count) { asm volatile("ba
 
 // ---- the preparing warps ----------------------------------------------------------------------------------------------
 template <int DKP, bool EXACT, Way WAY>
-__device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layout<DKP, EXACT, WAY>& lay, long long unit, int chunks, int threads) {
+__device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layout<DKP, EXACT, WAY>& lay, long long unit, int first, int count, int threads) {
     constexpr int KP = key_pitch<DKP>(), KS = DKP / 16;
-    constexpr bool Q = WAY != Way::kKeep;
+    constexpr bool Q = Layout<DKP, EXACT, WAY>::kQ;
     constexpr int kLanes = DKP <= 16 ? 2 : DKP <= 32 ? 4 : DKP <= 64 ? 8 : 16;   // of a row
     constexpr int kRows = kPrep / kLanes, kPasses = (Q ? 2 : 1) * kChunk / kRows;
     const int tid = threadIdx.x - (blockDim.x - kPrep), lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -97,9 +111,9 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
                 be[h] = t < a.L ? __bfloat162float(a.beta[a.row(unit, t)]) : 0.f;
             }
     };
-    bring(WAY == Way::kBack ? chunks - 1 : 0);
-    for (int it = 0; it < chunks; ++it) {
-        const int n = WAY == Way::kBack ? chunks - 1 - it : it, buf = it & 1, strips = (min(kChunk, a.L - n * kChunk) + 15) >> 4;
+    bring(first);
+    for (int it = 0; it < count; ++it) {
+        const int n = is_back(WAY) ? first - it : first + it, buf = it & 1, strips = (min(kChunk, a.L - n * kChunk) + 15) >> 4;
         if (it >= 2) named_bar(kBarEmpty + buf, threads);
         float* const gates = reinterpret_cast<float*>(smem + lay.gates(buf));
         if (warp == 0) {   // running sum of log2 alpha, two tokens a lane
@@ -144,7 +158,7 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
             gates[kGv * kChunk + tid] = gv;
             gates[kGn * kChunk + tid] = gv * gates[kKu * kChunk + tid];
         }
-        if (it + 1 < chunks) bring(WAY == Way::kBack ? n - 1 : n + 1);
+        if (it + 1 < count) bring(is_back(WAY) ? n - 1 : n + 1);
         // N and P by blocks of sixteen by sixteen: two of the diagonal's for each of the first two warps, with their inverses side by side; three
         // of the others for each of the other two
         const uint32_t kt = base + lay.k(buf), qt = base + lay.q(buf);
@@ -192,7 +206,7 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
                         const float2 bs = *reinterpret_cast<const float2*>(gates + kB * kChunk + i * 16 + ss);
                         const float e0 = ss <= tt ? ex2(bt - bs.x) : 0.f, e1 = ss + 1 <= tt ? ex2(bt - bs.y) : 0.f;
                         // (selected, not multiplied: what is not finite stays out of earlier tokens)
-                        if constexpr (Q) put(lay.p(buf), lay.p_lo(buf), EXACT && WAY == Way::kBack, at, pack2(ss <= tt ? pp[m][2 * h] * e0 : 0.f, ss + 1 <= tt ? pp[m][2 * h + 1] * e1 : 0.f));
+                        if constexpr (Q) put(lay.p(buf), lay.p_lo(buf), EXACT && is_back(WAY), at, pack2(ss <= tt ? pp[m][2 * h] * e0 : 0.f, ss + 1 <= tt ? pp[m][2 * h + 1] * e1 : 0.f));
                         const float n0 = ss < tt ? nn[m][2 * h] * e0 : 0.f, n1 = ss + 1 < tt ? nn[m][2 * h + 1] * e1 : 0.f;
                         if constexpr (WAY == Way::kKeep) put(lay.n(buf), 0, false, at, pack2(n0, n1));   // (W takes its own strip's off)
                         xt[(d * 16 + ss) * 20 + tt] = n0 * gn;   // beta N, transposed: row s, column t
@@ -249,7 +263,7 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
                     for (int m = 0; m < 2; ++m) {
                         const int at = block_of(i, j) + (g + 8 * h) * kBlockPitch + (8 * m + 2 * c) * 2;
                         const f32x2 e = fmul2(ec[m], pack2(et, et));
-                        if constexpr (Q) put(lay.p(buf), lay.p_lo(buf), EXACT && WAY == Way::kBack, at, fmul2(pair(pp[m], h), e));
+                        if constexpr (Q) put(lay.p(buf), lay.p_lo(buf), EXACT && is_back(WAY), at, fmul2(pair(pp[m], h), e));
                         put(lay.n(buf), lay.n_lo(buf), EXACT, at, fmul2(pair(nn[m], h), e));
                     }
                 }
@@ -303,24 +317,29 @@ template <int DKP>
 struct State {
     float x[DKP / 8][4];
     float scale[2] = {1.f, 1.f};
-    __device__ __forceinline__ void load(const float* from, long long unit, const Gdr<bf>& a, int col, int c) {
-        const long long plane = (long long)a.dk * a.dv;
+    // [dk][cols] fp32 at `from` (null: zero)
+    __device__ __forceinline__ void load(const float* from, int dk, int cols, int col, int c) {
 #pragma unroll
         for (int n = 0; n < DKP / 8; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = n * 8 + 2 * c + (e & 1), j = col + (e >> 1) * 8;
-                x[n][e] = from && i < a.dk && j < a.dv ? from[unit * plane + (long long)i * a.dv + j] : 0.f;
+                x[n][e] = from && i < dk && j < cols ? from[(long long)i * cols + j] : 0.f;
             }
     }
-    __device__ __forceinline__ void store(float* to, long long unit, const Gdr<bf>& a, int col, int c) const {
-        const long long plane = (long long)a.dk * a.dv;
+    __device__ __forceinline__ void unit_vectors(int col, int c) {
+#pragma unroll
+        for (int n = 0; n < DKP / 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[n][e] = n * 8 + 2 * c + (e & 1) == col + (e >> 1) * 8 ? 1.f : 0.f;
+    }
+    __device__ __forceinline__ void store(float* to, int dk, int cols, int col, int c) const {
 #pragma unroll
         for (int n = 0; n < DKP / 8; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = n * 8 + 2 * c + (e & 1), j = col + (e >> 1) * 8;
-                if (i < a.dk && j < a.dv) to[unit * plane + (long long)i * a.dv + j] = x[n][e] / scale[e >> 1];
+                if (i < dk && j < cols) to[(long long)i * cols + j] = x[n][e] / scale[e >> 1];
             }
     }
     // New scales: the larger of the state and `outside` (per column) to [2^TOP / 2, 2^TOP).  back: what undoes them.
@@ -419,14 +438,14 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
                                               const Layout<DKP, EXACT, WAY>& lay, int buf, int cols, long long unit, int n, int chunks, int col0, int lane,
                                               const Lane& ln) {
     constexpr int KS = DKP / 16, TERMS = EXACT ? 2 : 1;
-    constexpr bool OUT = WAY == Way::kForward;
+    constexpr bool OUT = WAY == Way::kForward, KEEP = WAY == Way::kKeep;
     const int g = lane >> 2, c = lane & 3;
     const uint32_t base = smem_u32(smem), kt = base + lay.k(buf), qt = base + lay.q(buf), vt = base + cols;
     const float* const gates = reinterpret_cast<const float*>(smem + lay.gates(buf));
     float gmax = fmaxf(fabsf(gates[kGv * kChunk + lane]), fabsf(gates[kGv * kChunk + lane + 32])), vmax[2] = {0.f, 0.f}, back[2];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, o));
-    if constexpr (!OUT) gmax = fmaxf(gmax, 1.f);   // W itself is kept too
+    if constexpr (KEEP) gmax = fmaxf(gmax, 1.f);   // W itself is kept too
     uint32_t vm[2] = {0u, 0u}, vv[NS][4];   // V transposed: strip i, columns g (0, 2), g + 8 (1, 3) of tokens 2c, 2c + 1 (0, 1), + 8 (2, 3)
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
@@ -449,7 +468,7 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
         pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);   // (what does not fit shows in U)
         if constexpr (EXACT) pack_a_rest(S.x[2 * s], S.x[2 * s + 1], sa[s], sl[s]);
     }
-    if constexpr (!OUT) kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + n, col0, sa, back, g, c);
+    if constexpr (KEEP) kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + n, col0, sa, back, g, c);
     S.decay(gates[kEb * kChunk + kChunk - 1]);
     // products with S, of all strips; then strip by strip, what a strip's U means to the strips behind it as soon as it is there: the next
     // strip's chain (N, the step, the inverse) is what bounds a chunk, all else fills its gaps
@@ -480,7 +499,7 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
             for (int h = 0; h < 2; ++h) {
                 const f32x2 got = fmul2(pair(w[i][m], h), ku);
                 const f32x2 y = ffma2(got, pack2(-1.f, -1.f), fmul2(widen_bf16(vv[i][2 * m + h]), pack2(S.scale[h], S.scale[h])));
-                if constexpr (!OUT) set_pair(w[i][m], h, y);
+                if constexpr (KEEP) set_pair(w[i][m], h, y);
                 set_pair(r[m], h, fmul2(gv, y));
             }
         }
@@ -504,7 +523,7 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
         }
         pack_terms<TERMS>(uu, ud, udl);
         rows_into_state<DKP, TERMS>(S, ud, udl, kt, i, ln);
-        uint32_t res[2][2];
+        uint32_t res[2][2] = {};
         if constexpr (OUT) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
@@ -516,7 +535,7 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
                     res[m][h] = pack_bf16(x, y);
                 }
             }
-        } else {   // W of the strip: what its own block takes off
+        } else if constexpr (KEEP) {   // W of the strip: what its own block takes off
             float own[2][4] = {};
             times_block<false, 1>(own, u, ul, base + lay.n(buf) + block_of(i, i), 0, ln);
 #pragma unroll
@@ -528,6 +547,7 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
             const uint32_t ws[4] = {res[0][0], res[0][1], res[1][0], res[1][1]};
             seen.see(ws);
         }
+        if constexpr (!OUT && !KEEP) continue;
         // over the strip's values, and out from there in pieces of sixteen bytes
         stsm_trans(vt + (i * 16 + ln.t_row) * kColPitch + ln.t_col * 2, res[0][0], res[1][0], res[0][1], res[1][1]);
         __syncwarp();
@@ -540,9 +560,9 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
 }
 
 // One chunk of NS strips backwards: S is A, the columns are those of dO.
-template <int DKP, bool EXACT, int NS>
+template <int DKP, bool EXACT, Way WAY, int NS>
 __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, const Gdr<bf>& a, const Kept& kept, unsigned char* smem,
-                                               const Layout<DKP, EXACT, Way::kBack>& lay, int buf, int cols, long long unit, int n, int chunks, int col0,
+                                               const Layout<DKP, EXACT, WAY>& lay, int buf, int cols, long long unit, int n, int chunks, int col0,
                                                int lane, const Lane& ln) {
     constexpr int KS = DKP / 16, TERMS = EXACT ? 2 : 1;
     const int g = lane >> 2, c = lane & 3;
@@ -571,7 +591,7 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
         pack_a(A.x[2 * s], A.x[2 * s + 1], aa[s]);   // (what does not fit shows in dU)
         if constexpr (EXACT) pack_a_rest(A.x[2 * s], A.x[2 * s + 1], aa[s], al[s]);
     }
-    kept.keep_state<DKP>(kept.A, kept.z, unit * chunks + n, col0, aa, back, g, c);
+    if constexpr (WAY == Way::kBack) kept.keep_state<DKP>(kept.A, kept.z, unit * chunks + n, col0, aa, back, g, c);
     A.decay(gates[kEb * kChunk + kChunk - 1]);
     auto d_out = [&](int i, float (&x)[2][4]) {   // scaled
 #pragma unroll
@@ -644,6 +664,7 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
         rows_into_state<DKP, TERMS>(A, pe, pel, kt, i, ln);
         pack_terms<TERMS>(y, pe, pel);
         rows_into_state<DKP, TERMS>(A, pe, pel, qt, i, ln);
+        if constexpr (WAY != Way::kBack) continue;
         // out: dv, then 2^-e dU, through the strip's rows
         const int t = i * 16 + (lane >> 1), e = (lane & 1) * 8;
         const uint32_t at = vt + (i * 16 + ln.t_row) * kColPitch + ln.t_col * 2;
@@ -666,81 +687,144 @@ constexpr bool two_blocks() { return 2 * (Layout<DKP, EXACT, WAY>::total(kMostWa
 // EXACT: states leave the call in fp32, so that what they are made of is taken with 22 bits (two fp16 an operand); otherwise only bf16
 // results do, and eleven bits keep the error below a quarter of their rounding.
 template <int DKP, bool EXACT, Way WAY>
-__global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT, WAY>() ? 2 : 1) gdr_chunk_kernel(Gdr<bf> a, Kept kept, int slabs, int warps, int* status) {
+__global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT, WAY>() ? 2 : 1) gdr_chunk_kernel(Gdr<bf> a, Kept kept, Segs segs, int slabs, int warps, int* status) {
+    constexpr bool BACK = is_back(WAY), PROPER = WAY != Way::kSum && WAY != Way::kBackSum;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, threads = 32 * warps + kPrep;
     const Layout<DKP, EXACT, WAY> lay;
-    const long long unit = blockIdx.x / slabs;
-    const int chunks = (a.L + kChunk - 1) / kChunk;
+    // sums have further slabs for the unit vectors, backwards none, and leave out the first segment
+    const int all = slabs + (WAY == Way::kSum ? (a.dk + warps * 16 - 1) / (warps * 16) : 0), runs = WAY == Way::kSum ? segs.sums : WAY == Way::kBackSum ? segs.n - 1 : segs.n;
+    const int slab = blockIdx.x % all, seg = blockIdx.x / all % runs + (WAY == Way::kBackSum);
+    const long long unit = blockIdx.x / all / runs;
+    const int chunks = (a.L + kChunk - 1) / kChunk, from = seg * segs.per, to = min(chunks, from + segs.per), first = BACK ? to - 1 : from, count = to - from;
+    const bool starts = seg == (BACK ? segs.n - 1 : 0), ends = seg == (BACK ? 0 : segs.n - 1);
     pdl_wait();
     pdl_launch_dependents();
     if (warp >= kMostWarps) {
         if constexpr (two_blocks<DKP, EXACT, WAY>()) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        prepare_chunks<DKP, EXACT, WAY>(a, smem, lay, unit, chunks, threads);
+        prepare_chunks<DKP, EXACT, WAY>(a, smem, lay, unit, first, count, threads);
         return;
     }
     if constexpr (two_blocks<DKP, EXACT, WAY>()) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
     if (warp >= warps) return;   // (four warps split their registers together)
-    const int col0 = (blockIdx.x % slabs * warps + warp) * 16, g = lane >> 2, c = lane & 3;
+    const bool vectors = WAY == Way::kSum && slab >= slabs;   // columns that are unit vectors
+    const int col0 = ((vectors ? slab - slabs : slab) * warps + warp) * 16, g = lane >> 2, c = lane & 3;
     const Lane ln(lane);
     const uint32_t base = smem_u32(smem);
     const int cols0 = lay.cols + warp * 2 * lay.kCols;
     auto cols = [&](int buf) { return cols0 + buf * lay.kCols; };
-    const bf* const from = WAY == Way::kBack ? a.d_out : a.v;
+    const bf* const rows = BACK ? a.d_out : a.v;
     auto fetch = [&](int n, int buf) {   // this warp's columns of the chunk's rows: two pieces of sixteen bytes a row
         const int e = (lane & 1) * 8;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = i * 16 + (lane >> 1);
-            const bool in = n * kChunk + t < a.L && col0 + e < a.dv;
-            cp_async16(base + cols(buf) + t * kColPitch + e * 2, from + (in ? a.row(unit, n * kChunk + t) * a.dv + col0 + e : 0), in);
+            const bool in = n * kChunk + t < a.L && col0 + e < a.dv && !vectors;
+            cp_async16(base + cols(buf) + t * kColPitch + e * 2, rows + (in ? a.row(unit, n * kChunk + t) * a.dv + col0 + e : 0), in);
         }
         cp_async_commit();
     };
+    const long long plane = (long long)a.dk * a.dv, at = unit * segs.n + seg;
     State<DKP> S;
     Largest seen;
-    fetch(WAY == Way::kBack ? chunks - 1 : 0, 0);
-    S.load(WAY == Way::kBack ? a.d_state_out : a.state_in, unit, a, col0 + g, c);
-    for (int it = 0; it < chunks; ++it) {
-        const int n = WAY == Way::kBack ? chunks - 1 - it : it, buf = it & 1, strips = (min(kChunk, a.L - n * kChunk) + 15) >> 4;
-        if (it + 1 < chunks) {
-            fetch(WAY == Way::kBack ? n - 1 : n + 1, buf ^ 1);
+    fetch(first, 0);
+    if (vectors) S.unit_vectors(col0 + g, c);
+    else {
+        const float* const edge = BACK ? a.d_state_out : a.state_in;
+        S.load(!PROPER ? nullptr : !starts ? segs.in + at * plane : edge ? edge + unit * plane : nullptr, a.dk, a.dv, col0 + g, c);
+    }
+    for (int it = 0; it < count; ++it) {
+        const int n = BACK ? first - it : first + it, buf = it & 1, strips = (min(kChunk, a.L - n * kChunk) + 15) >> 4;
+        if (it + 1 < count) {
+            fetch(BACK ? n - 1 : n + 1, buf ^ 1);
             cp_async_wait<1>();
         } else cp_async_wait<0>();
         __syncwarp();
         named_bar(kBarFull + buf, threads);
         auto chunk = [&](auto NS) {
             constexpr int ns = decltype(NS)::value;
-            if constexpr (WAY == Way::kBack) backward_chunk<DKP, EXACT, ns>(S, seen, a, kept, smem, lay, buf, cols(buf), unit, n, chunks, col0, lane, ln);
+            if constexpr (BACK) backward_chunk<DKP, EXACT, WAY, ns>(S, seen, a, kept, smem, lay, buf, cols(buf), unit, n, chunks, col0, lane, ln);
             else forward_chunk<DKP, EXACT, WAY, ns>(S, seen, a, kept, smem, lay, buf, cols(buf), unit, n, chunks, col0, lane, ln);
         };
         if (strips == 4) chunk(std::integral_constant<int, 4>());
         else if (strips == 1) chunk(std::integral_constant<int, 1>());
         else if (strips == 2) chunk(std::integral_constant<int, 2>());
         else chunk(std::integral_constant<int, 3>());
-        if (it + 2 < chunks) bar_arrive(kBarEmpty + buf, threads);
+        if (it + 2 < count) bar_arrive(kBarEmpty + buf, threads);
         __syncwarp();
     }
     const bool lost = __any_sync(0xffffffffu, seen.lost());
     if constexpr (WAY == Way::kForward) {
-        if (lost) {   // (this warp's own stores of its columns come before)
-            __syncwarp();
-            if (lane == 0) atomicAdd(status + 1, 1);
-            walk_sixteen<DKP>(a, unit, col0 + (lane & 15), lane >> 4);
-        } else if (a.state_out) S.store(a.state_out, unit, a, col0 + g, c);
-    } else {
+        if (segs.n == 1) {
+            if (lost) {   // (this warp's own stores of its columns come before)
+                __syncwarp();
+                if (lane == 0) atomicAdd(status + 1, 1);
+                walk_sixteen<DKP>(a, unit, col0 + (lane & 15), lane >> 4);
+                return;
+            }
+        } else if (lost && lane == 0) segs.lost[unit * segs.slots + seg * kMostColumns + col0 / 16] = 1;
+        if (a.state_out && ends) S.store(a.state_out + unit * plane, a.dk, a.dv, col0 + g, c);
+    } else if constexpr (PROPER) {
         if (lane == 0) {
-            int* const flag = kept.lost + unit * (kept.dvp / 16) + col0 / 16;
-            *flag = WAY == Way::kKeep ? lost : lost || *flag;
+            int* const flag = segs.lost + unit * segs.slots + seg * kMostColumns + col0 / 16;
+            if (WAY == Way::kKeep) *flag = lost;
+            else if (lost) *flag = 1;
         }
         if constexpr (WAY == Way::kKeep) {   // the last state, for the gates' gradient
-            float none[2] = {0.f, 0.f}, back[2];
-            uint32_t sa[DKP / 16][4];
-            S.template rescale<3>(none, back);
+            if (ends) {
+                float none[2] = {0.f, 0.f}, back[2];
+                uint32_t sa[DKP / 16][4];
+                S.template rescale<3>(none, back);
 #pragma unroll
-            for (int s = 0; s < DKP / 16; ++s) pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);
-            kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + chunks, col0, sa, back, g, c);
-        } else if (a.d_state_in) S.store(a.d_state_in, unit, a, col0 + g, c);
+                for (int s = 0; s < DKP / 16; ++s) pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);
+                kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + chunks, col0, sa, back, g, c);
+            }
+        } else if (a.d_state_in && ends) S.store(a.d_state_in + unit * plane, a.dk, a.dv, col0 + g, c);
+    } else {
+        if (lost && lane == 0) segs.lost[unit * segs.slots + segs.n * kMostColumns] = 1;   // (whichever warp of the unit's)
+        if (vectors) S.store(segs.trans + at * a.dk * a.dk, a.dk, a.dk, col0 + g, c);
+        else S.store(segs.sum + at * plane, a.dk, a.dv, col0 + g, c);
+    }
+}
+
+// The states between segments: a block takes sixteen columns of a unit.  S before the next = T S + B, backwards A behind the last = T^T A + C,
+// in fp32; T through shared memory, the columns in the other half of it.
+__global__ void __launch_bounds__(256) gdr_fold_kernel(Gdr<bf> a, Segs segs, int slabs, bool back) {
+    extern __shared__ __align__(16) float fold_smem[];
+    const int dk = a.dk, pitch = dk + 1, tid = threadIdx.x, j0 = blockIdx.x % slabs * 16;
+    const long long unit = blockIdx.x / slabs, plane = (long long)dk * a.dv;
+    float *const T = fold_smem, *const X = fold_smem + dk * pitch;   // X: [dk][16]
+    pdl_wait();
+    pdl_launch_dependents();
+    const float* const edge = back ? a.d_state_out : a.state_in;
+    for (int i = tid; i < dk * 16; i += 256) {
+        const int j = j0 + (i & 15);
+        X[i] = edge && j < a.dv ? edge[unit * plane + (long long)(i >> 4) * a.dv + j] : 0.f;
+    }
+    for (int k = 0; k + 1 < segs.n; ++k) {
+        const long long at = unit * segs.n + (back ? segs.n - 1 - k : k), next = back ? at - 1 : at + 1;
+        for (int i = tid; i < dk * dk; i += 256) T[i / dk * pitch + i % dk] = segs.trans[at * dk * dk + i];
+        __syncthreads();
+        float y[8];   // row tid / 2, eight columns
+        const int r = tid >> 1, c0 = (tid & 1) * 8;
+        if (r < dk) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = j0 + c0 + e < a.dv ? segs.sum[at * plane + (long long)r * a.dv + j0 + c0 + e] : 0.f;
+            for (int i = 0; i < dk; ++i) {
+                const float t = back ? T[i * pitch + r] : T[r * pitch + i];
+                const float4 u = *reinterpret_cast<const float4*>(X + i * 16 + c0), v = *reinterpret_cast<const float4*>(X + i * 16 + c0 + 4);
+                y[0] = fmaf(t, u.x, y[0]); y[1] = fmaf(t, u.y, y[1]); y[2] = fmaf(t, u.z, y[2]); y[3] = fmaf(t, u.w, y[3]);
+                y[4] = fmaf(t, v.x, y[4]); y[5] = fmaf(t, v.y, y[5]); y[6] = fmaf(t, v.z, y[6]); y[7] = fmaf(t, v.w, y[7]);
+            }
+        }
+        __syncthreads();
+        if (r < dk)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                X[r * 16 + c0 + e] = y[e];
+                if (j0 + c0 + e < a.dv) segs.in[next * plane + (long long)r * a.dv + j0 + c0 + e] = y[e];
+            }
+        __syncthreads();
     }
 }
 
@@ -756,10 +840,11 @@ cudaError_t with_keys(int dk, F f) {
 }
 
 template <Way WAY>
-cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, bool exact, cudaStream_t stream) {
+cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, const Segs& segs, bool exact, cudaStream_t stream) {
     int* status = device_status_ptr();
     if (!status) return cudaErrorUnknown;
     const int all = (a.dv + 15) / 16, slabs = (all + kMostWarps - 1) / kMostWarps, warps = (all + slabs - 1) / slabs;   // (gdr_padded_columns)
+    const long long blocks = a.units * (WAY == Way::kSum ? segs.sums : WAY == Way::kBackSum ? segs.n - 1 : segs.n) * (slabs + (WAY == Way::kSum ? (a.dk + warps * 16 - 1) / (warps * 16) : 0));
     return with_keys(a.dk, [&](auto D) {
         constexpr int dkp = decltype(D)::value;
         auto go = [&](auto E) {
@@ -769,7 +854,7 @@ cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, bool exact, cudaSt
             cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
             if (e != cudaSuccess) return e;
             count_launch();
-            return launch_pdl(kernel, dim3((unsigned)(a.units * slabs)), dim3(32 * kMostWarps + kPrep), smem, stream, a, kept, slabs, warps, status);
+            return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kMostWarps + kPrep), smem, stream, a, kept, segs, slabs, warps, status);
         };
         if constexpr (WAY != Way::kKeep)
             if (exact) return go(std::true_type());
@@ -777,28 +862,47 @@ cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, bool exact, cudaSt
     });
 }
 
-}  // namespace
-
-bool gdr_chunk_supported(int dk, int dv) { return dk % 8 == 0 && dv % 8 == 0; }
-int gdr_padded_columns(int dv) {
-    const int all = (dv + 15) / 16, slabs = (all + kMostWarps - 1) / kMostWarps;
-    return (all + slabs - 1) / slabs * slabs * 16;
-}
-int gdr_padded_keys(int dk) {
-    int padded = 0;
-    with_keys(dk, [&](auto D) { padded = decltype(D)::value; return cudaSuccess; });
-    return padded;
+cudaError_t launch_fold(const Gdr<bf>& a, const Segs& segs, bool back, cudaStream_t stream) {
+    const int slabs = (a.dv + 15) / 16;
+    const size_t smem = ((size_t)a.dk * (a.dk + 1) + a.dk * 16 + 4) * 4;
+    cudaError_t e = cudaFuncSetAttribute(gdr_fold_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    return launch_pdl(gdr_fold_kernel, dim3((unsigned)(a.units * slabs)), dim3(256), smem, stream, a, segs, slabs, back);
 }
 
-cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, cudaStream_t stream) {
-    return launch_chunks<Way::kForward>(a, Kept{}, a.state_out != nullptr, stream);
+// Segments of a unit: as many as give every SM its two blocks, of four chunks and more, where at least half the chip would be idle otherwise.
+int segments(long long units, int L, int dk, int dv) {
+    if (dk > 64) return 1;   // (one block an SM, and as many columns for the transition as for the state: 2 x 16 units of 4096 tokens, 128 x 128, gain nothing)
+    const long long blocks = units * ((dv + 16 * kMostWarps - 1) / (16 * kMostWarps)), chunks = (L + kChunk - 1) / kChunk;
+    const long long fit = 2LL * 148 / blocks;
+    const long long n = fit < chunks / 4 ? fit : chunks / 4;
+    return n < 3 ? 1 : (int)(n < 32 ? n : 32);
 }
-cudaError_t launch_gdr_chunk_walks(const Gdr<__nv_bfloat16>& a, const GdrKept& kept, cudaStream_t stream) {
-    cudaError_t e = launch_chunks<Way::kKeep>(a, kept, false, stream);
-    return e == cudaSuccess ? launch_chunks<Way::kBack>(a, kept, a.d_state_in != nullptr, stream) : e;
-}
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
-namespace {
+Segs cut_segments(char* base, long long units, int L, int dk, int dv, int n, bool back, size_t* total) {
+    Segs s = {};
+    const int chunks = (L + kChunk - 1) / kChunk;
+    s.per = (chunks + n - 1) / n;
+    s.n = (chunks + s.per - 1) / s.per;
+    s.sums = back ? s.n : s.n - 1;
+    s.slots = s.n > 1 ? s.n * kMostColumns + 1 : gdr_padded_columns(dv) / 16;   // (one segment: all of them are written)
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char* p = base ? base + at : nullptr;
+        at += up(bytes);
+        return p;
+    };
+    s.lost = (int*)take(units * s.slots * 4);
+    if (s.n > 1) {
+        s.in = (float*)take((size_t)units * s.n * dk * dv * 4);
+        s.sum = (float*)take((size_t)units * s.n * dk * dv * 4);
+        s.trans = (float*)take((size_t)units * s.n * dk * dk * 4);
+    }
+    *total = at;
+    return s;
+}
 
 constexpr size_t kRepairBytes = 64u << 20;   // of scratch, unless one unit takes more
 
@@ -806,7 +910,6 @@ int repair_slots(long long units, int L, int dk, int dv) {
     const long long fit = (long long)(kRepairBytes / gdr_repair_slot_bytes(L, dk, dv));
     return (int)(fit < 1 ? 1 : fit > units ? units : fit > 148 ? 148 : fit);
 }
-size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 Kept cut_kept(char* base, long long units, int L, int dk, int dv, size_t* total) {
     Kept k = {};
@@ -824,7 +927,6 @@ Kept cut_kept(char* base, long long units, int L, int dk, int dv, size_t* total)
     k.A = (__half*)take(units * chunks * dvp * dkp * 2);
     k.y = (float*)take(units * (chunks + 1) * dvp * 4);
     k.z = (float*)take(units * chunks * dvp * 4);
-    k.lost = (int*)take(units * (dvp / 16) * 4);
     k.lost_grad = (int*)take(units * chunks * 4);
     *total = at;
     return k;
@@ -832,18 +934,68 @@ Kept cut_kept(char* base, long long units, int L, int dk, int dv, size_t* total)
 
 }  // namespace
 
+bool gdr_chunk_supported(int dk, int dv) { return dk % 8 == 0 && dv % 8 == 0; }
+int gdr_padded_columns(int dv) {
+    const int all = (dv + 15) / 16, slabs = (all + kMostWarps - 1) / kMostWarps;
+    return (all + slabs - 1) / slabs * slabs * 16;
+}
+int gdr_padded_keys(int dk) {
+    int padded = 0;
+    with_keys(dk, [&](auto D) { padded = decltype(D)::value; return cudaSuccess; });
+    return padded;
+}
+
+size_t gdr_chunk_scratch_bytes(long long units, int L, int dk, int dv) {
+    const int n = segments(units, L, dk, dv);
+    size_t total = 0;
+    if (n > 1) cut_segments(nullptr, units, L, dk, dv, n, false, &total);
+    return total;
+}
+cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, void* scratch, cudaStream_t stream) {
+    const bool exact = a.state_out != nullptr;
+    const int n = segments(a.units, a.L, a.dk, a.dv);
+    if (n == 1) {
+        Segs one = {};
+        one.n = 1;
+        one.per = (a.L + kChunk - 1) / kChunk;
+        return launch_chunks<Way::kForward>(a, Kept{}, one, exact, stream);
+    }
+    size_t total;
+    const Segs segs = cut_segments((char*)scratch, a.units, a.L, a.dk, a.dv, n, false, &total);
+    cudaError_t e = cudaMemsetAsync(segs.lost, 0, a.units * segs.slots * 4, stream);
+    if (e == cudaSuccess) e = launch_chunks<Way::kSum>(a, Kept{}, segs, exact, stream);
+    if (e == cudaSuccess) e = launch_fold(a, segs, false, stream);
+    if (e == cudaSuccess) e = launch_chunks<Way::kForward>(a, Kept{}, segs, exact, stream);
+    if (e == cudaSuccess) e = launch_gdr_repair_fwd(a, segs.lost, segs.slots, stream);
+    return e;
+}
+
 size_t gdr_grad_scratch_bytes(long long units, int L, int dk, int dv) {
-    size_t kept;
+    size_t kept, segs;
     cut_kept(nullptr, units, L, dk, dv, &kept);
-    return kept + repair_slots(units, L, dk, dv) * gdr_repair_slot_bytes(L, dk, dv);
+    cut_segments(nullptr, units, L, dk, dv, segments(units, L, dk, dv), true, &segs);
+    return kept + segs + repair_slots(units, L, dk, dv) * gdr_repair_slot_bytes(L, dk, dv);
 }
 cudaError_t launch_gdr_chunk_bwd(const Gdr<__nv_bfloat16>& a, void* scratch, cudaStream_t stream) {
-    size_t used;
+    size_t used, more;
     const Kept kept = cut_kept((char*)scratch, a.units, a.L, a.dk, a.dv, &used);
-    cudaError_t e = launch_gdr_chunk_walks(a, kept, stream);
+    const Segs segs = cut_segments((char*)scratch + used, a.units, a.L, a.dk, a.dv, segments(a.units, a.L, a.dk, a.dv), true, &more);
+    const bool exact = a.d_state_in != nullptr;
+    cudaError_t e = cudaSuccess;
+    if (segs.n > 1) {
+        e = cudaMemsetAsync(segs.lost, 0, a.units * segs.slots * 4, stream);
+        if (e == cudaSuccess) e = launch_chunks<Way::kSum>(a, kept, segs, exact, stream);
+        if (e == cudaSuccess) e = launch_fold(a, segs, false, stream);
+    }
+    if (e == cudaSuccess) e = launch_chunks<Way::kKeep>(a, kept, segs, false, stream);
+    if (segs.n > 1) {
+        if (e == cudaSuccess) e = launch_chunks<Way::kBackSum>(a, kept, segs, exact, stream);
+        if (e == cudaSuccess) e = launch_fold(a, segs, true, stream);
+    }
+    if (e == cudaSuccess) e = launch_chunks<Way::kBack>(a, kept, segs, exact, stream);
     if (e == cudaSuccess) e = launch_gdr_grad(a, kept, stream);
     if (e == cudaSuccess)
-        e = launch_gdr_repair(a, kept.lost, kept.dvp / 16, kept.lost_grad, (a.L + kChunk - 1) / kChunk, (char*)scratch + used,
+        e = launch_gdr_repair(a, segs.lost, segs.slots, kept.lost_grad, (a.L + kChunk - 1) / kChunk, (char*)scratch + used + more,
                               repair_slots(a.units, a.L, a.dk, a.dv), stream);
     return e;
 }

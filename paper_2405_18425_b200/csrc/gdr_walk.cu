@@ -414,6 +414,23 @@ __global__ void __launch_bounds__(256) gdr_repair_kernel(Gdr<__nv_bfloat16> a, S
     }
 }
 
+// The same behind the forward pass in segments.
+__global__ void __launch_bounds__(256) gdr_repair_fwd_kernel(Gdr<__nv_bfloat16> a, const int* flags, int per, int* status) {
+    extern __shared__ __align__(16) float sm[];
+    pdl_wait();
+    pdl_launch_dependents();
+    for (long long unit = blockIdx.x; unit < a.units; unit += gridDim.x) {
+        int any = 0;
+        for (int i = threadIdx.x; i < per; i += 256) any |= flags[unit * per + i];
+        if (!__syncthreads_or(any)) continue;
+        if (threadIdx.x == 0) atomicAdd(status + 1, 1);
+        for (int j = 0; j < a.dv; j += kRepairOwners) {
+            walk_columns<__nv_bfloat16, kRepairR, kRepairG, false, false>(a, Scratch{}, sm, unit, j, kRepairOwners);
+            __syncthreads();
+        }
+    }
+}
+
 // f(R, G) for vectors of d elements
 template <typename F>
 cudaError_t with_vector(int d, F f) {
@@ -526,6 +543,16 @@ cudaError_t launch_gdr_repair(const Gdr<__nv_bfloat16>& a, const int* first, int
     if (e != cudaSuccess) return e;
     count_launch();
     return launch_pdl(gdr_repair_kernel, dim3(slots), dim3(kRepairG * kRepairOwners), smem, stream, a, s, first, per, second, chunks, status);
+}
+
+cudaError_t launch_gdr_repair_fwd(const Gdr<__nv_bfloat16>& a, const int* flags, int per, cudaStream_t stream) {
+    int* status = device_status_ptr();
+    if (!status) return cudaErrorUnknown;
+    const size_t smem = walk_smem<2, kRepairR * kRepairG>(kRepairOwners);
+    cudaError_t e = allow_smem(gdr_repair_fwd_kernel, smem);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    return launch_pdl(gdr_repair_fwd_kernel, dim3((unsigned)(a.units < 148 ? a.units : 148)), dim3(kRepairG * kRepairOwners), smem, stream, a, flags, per, status);
 }
 
 template cudaError_t launch_gdr_walk_fwd<float>(const Gdr<float>&, cudaStream_t);

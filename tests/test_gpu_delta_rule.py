@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 # B, H, L, dk, dv: one token, lengths around 16, 64 and 128, heads of this library and larger ones, odd ones, several blocks of columns
 SIZES = [(1, 1, 1, 16, 32), (2, 3, 2, 24, 48), (3, 1, 16, 8, 8), (2, 3, 17, 24, 48), (1, 2, 64, 32, 64), (2, 2, 65, 128, 128), (1, 3, 130, 20, 17),
          (1, 1, 300, 64, 256), (1, 2, 196, 32, 64), (1, 1, 5, 1, 1), (1, 2, 33, 96, 40), (2, 1, 127, 128, 24), (1, 2, 128, 48, 96), (1, 1, 77, 100, 100),
-         (1, 1, 1100, 24, 48), (2, 1, 515, 64, 64)]
+         (1, 1, 1100, 24, 48), (2, 1, 515, 64, 64), (1, 2, 2049, 16, 40), (1, 1, 1990, 64, 128)]
 
 
 def _terms(L, dk, dv):
