@@ -20,6 +20,28 @@ struct Gdr {
     __host__ __device__ long long row(long long unit, int t) const { return unit * L + (reverse ? L - 1 - t : t); }
 };
 
+#ifdef __CUDACC__
+// Sums from the end of 64 values, two a lane, that start anew at a stop: what the values behind this lane's pair come to, `end` behind the
+// last where nothing stopped it.
+__device__ __forceinline__ float suffix_of_pairs(const float (&x)[2], const bool (&stop)[2], float end) {
+    const int lane = threadIdx.x & 31;
+    float acc = stop[0] ? 0.f : x[0] + (stop[1] ? 0.f : x[1]);
+    bool cut = stop[0] || stop[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float y = __shfl_down_sync(0xffffffffu, acc, o);
+        const int z = __shfl_down_sync(0xffffffffu, (int)cut, o);
+        if (lane + o < 32) {
+            if (!cut) acc += y;
+            cut = cut || z;
+        }
+    }
+    const float later = __shfl_down_sync(0xffffffffu, acc, 1);
+    const int later_cut = __shfl_down_sync(0xffffffffu, (int)cut, 1);
+    return lane == 31 ? end : later + (later_cut ? 0.f : end);
+}
+#endif
+
 bool gdr_supported(int dk, int dv);   // dk <= 128, dv <= 256
 
 // ---- step by step in fp32 on the CUDA cores ----

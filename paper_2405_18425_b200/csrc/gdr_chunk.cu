@@ -376,34 +376,44 @@ struct State {
     }
 };
 
-// acc += A^T-operand x rows of a key tile: D[columns x tokens of the strip]
-template <int DKP, int TERMS>
-__device__ __forceinline__ void state_times_rows(float (&acc)[2][4], const uint32_t (*hi)[4], const uint32_t (*lo)[4], uint32_t tile, int strip, const Lane& ln) {
+// acc of every strip += state operand x the strip's rows of a key tile.  Strips inside, so that a product never waits for the one before it.
+template <int DKP, int TERMS, int NS>
+__device__ __forceinline__ void state_times_rows(float (&acc)[NS][2][4], const uint32_t (&hi)[4], const uint32_t (&lo)[4], uint32_t tile, int s, const Lane& ln) {
+    uint32_t x[NS][4];
 #pragma unroll
-    for (int s = 0; s < DKP / 16; ++s) {
-        uint32_t x[4];
-        ldsm(at_b<key_pitch<DKP>()>(ln, tile, strip * 16, s * 16), x);
-        mma(acc[0], hi[s], x[0], x[1]);
-        mma(acc[1], hi[s], x[2], x[3]);
-        if constexpr (TERMS == 2) {
-            mma(acc[0], lo[s], x[0], x[1]);
-            mma(acc[1], lo[s], x[2], x[3]);
-        }
+    for (int i = 0; i < NS; ++i) ldsm(at_b<key_pitch<DKP>()>(ln, tile, i * 16, s * 16), x[i]);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        mma(acc[i][0], hi, x[i][0], x[i][1]);
+        mma(acc[i][1], hi, x[i][2], x[i][3]);
     }
+    if constexpr (TERMS == 2)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            mma(acc[i][0], lo, x[i][0], x[i][1]);
+            mma(acc[i][1], lo, x[i][2], x[i][3]);
+        }
 }
 // S += (sixteen tokens' operand) x their rows of a key tile
 template <int DKP, int TERMS>
 __device__ __forceinline__ void rows_into_state(State<DKP>& S, const uint32_t (&hi)[4], const uint32_t (&lo)[4], uint32_t tile, int strip, const Lane& ln) {
+    constexpr int KS = DKP / 16, AT = KS % 4 == 0 ? 4 : KS % 2 == 0 ? 2 : 1;   // sixteens of keys at a time
 #pragma unroll
-    for (int s = 0; s < DKP / 16; ++s) {
-        uint32_t y[4];
-        ldsm_trans(at_t<key_pitch<DKP>()>(ln, tile, strip * 16, s * 16), y);
-        mma(S.x[2 * s], hi, y[0], y[1]);
-        mma(S.x[2 * s + 1], hi, y[2], y[3]);
-        if constexpr (TERMS == 2) {
-            mma(S.x[2 * s], lo, y[0], y[1]);
-            mma(S.x[2 * s + 1], lo, y[2], y[3]);
+    for (int s0 = 0; s0 < KS; s0 += AT) {
+        uint32_t y[AT][4];
+#pragma unroll
+        for (int s = 0; s < AT; ++s) ldsm_trans(at_t<key_pitch<DKP>()>(ln, tile, strip * 16, (s0 + s) * 16), y[s]);
+#pragma unroll
+        for (int s = 0; s < AT; ++s) {
+            mma(S.x[2 * (s0 + s)], hi, y[s][0], y[s][1]);
+            mma(S.x[2 * (s0 + s) + 1], hi, y[s][2], y[s][3]);
         }
+        if constexpr (TERMS == 2)
+#pragma unroll
+            for (int s = 0; s < AT; ++s) {
+                mma(S.x[2 * (s0 + s)], lo, y[s][0], y[s][1]);
+                mma(S.x[2 * (s0 + s) + 1], lo, y[s][2], y[s][3]);
+            }
     }
 }
 // acc += operand x a 16 x 16 block of a token-by-token matrix, contracted over its columns, or with TRANS over its rows
@@ -472,11 +482,11 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
     S.decay(gates[kEb * kChunk + kChunk - 1]);
     // products with S, of all strips; then strip by strip, what a strip's U means to the strips behind it as soon as it is there: the next
     // strip's chain (N, the step, the inverse) is what bounds a chunk, all else fills its gaps
-    float w[NS][2][4] = {}, o[OUT ? NS : 1][2][4] = {};
+    float w[NS][2][4] = {}, o[NS][2][4] = {};
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        state_times_rows<DKP, TERMS>(w[i], sa, sl, kt, i, ln);
-        if constexpr (OUT) state_times_rows<DKP, 1>(o[i], sa, sl, qt, i, ln);
+    for (int s = 0; s < KS; ++s) {
+        state_times_rows<DKP, TERMS, NS>(w, sa[s], sl[EXACT ? s : 0], kt, s, ln);
+        if constexpr (OUT) state_times_rows<DKP, 1, NS>(o, sa[s], sa[s], qt, s, ln);
     }
 #pragma unroll
     for (int i = 0; i < NS; ++i)
@@ -603,7 +613,7 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
     };
     float r[NS][2][4] = {};
 #pragma unroll
-    for (int i = 0; i < NS; ++i) state_times_rows<DKP, TERMS>(r[i], aa, al, kt, i, ln);
+    for (int s = 0; s < KS; ++s) state_times_rows<DKP, TERMS, NS>(r, aa[s], al[EXACT ? s : 0], kt, s, ln);
 #pragma unroll
     for (int i = 0; i < NS; ++i)
 #pragma unroll
@@ -788,43 +798,65 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
 }
 
 // The states between segments: a block takes sixteen columns of a unit.  S before the next = T S + B, backwards A behind the last = T^T A + C,
-// in fp32; T through shared memory, the columns in the other half of it.
+// in fp32; transitions and sums come by asynchronous copies a segment ahead.
 __global__ void __launch_bounds__(256) gdr_fold_kernel(Gdr<bf> a, Segs segs, int slabs, bool back) {
     extern __shared__ __align__(16) float fold_smem[];
-    const int dk = a.dk, pitch = dk + 1, tid = threadIdx.x, j0 = blockIdx.x % slabs * 16;
+    const int dk = a.dk, pitch = dk + 4, tid = threadIdx.x, j0 = blockIdx.x % slabs * 16, mine = min(16, a.dv - j0);   // (dk, dv: multiples of eight)
     const long long unit = blockIdx.x / slabs, plane = (long long)dk * a.dv;
-    float *const T = fold_smem, *const X = fold_smem + dk * pitch;   // X: [dk][16]
+    const int size = dk * pitch + dk * 16;
+    float* const X = fold_smem + 2 * size;   // [dk][16]
+    const uint32_t base = smem_u32(fold_smem);
+    auto segment = [&](int k) { return unit * segs.n + (back ? segs.n - 1 - k : k); };
+    auto fetch = [&](int k) {   // [dk][pitch] transition, [dk][16] sum
+        const uint32_t to = base + (k & 1) * size * 4;
+        const float* const t = segs.trans + segment(k) * dk * dk;
+        const int pieces = dk / 4;
+        for (int i = tid; i < dk * pieces; i += 256) {
+            const int r = i / pieces, p = i - r * pieces;
+            cp_async16(to + (r * pitch + p * 4) * 4, t + i * 4, true);
+        }
+        for (int i = tid; i < dk * 4; i += 256) {
+            const int r = i >> 2, p = (i & 3) * 4;
+            cp_async16(to + (dk * pitch + r * 16 + p) * 4, segs.sum + segment(k) * plane + (p < mine ? (long long)r * a.dv + j0 + p : 0), p < mine);
+        }
+        cp_async_commit();
+    };
     pdl_wait();
     pdl_launch_dependents();
+    fetch(0);
     const float* const edge = back ? a.d_state_out : a.state_in;
-    for (int i = tid; i < dk * 16; i += 256) {
-        const int j = j0 + (i & 15);
-        X[i] = edge && j < a.dv ? edge[unit * plane + (long long)(i >> 4) * a.dv + j] : 0.f;
-    }
+    for (int i = tid; i < dk * 16; i += 256) X[i] = edge && (i & 15) < mine ? edge[unit * plane + (long long)(i >> 4) * a.dv + j0 + (i & 15)] : 0.f;
     for (int k = 0; k + 1 < segs.n; ++k) {
-        const long long at = unit * segs.n + (back ? segs.n - 1 - k : k), next = back ? at - 1 : at + 1;
-        for (int i = tid; i < dk * dk; i += 256) T[i / dk * pitch + i % dk] = segs.trans[at * dk * dk + i];
+        if (k + 2 < segs.n) {
+            fetch(k + 1);
+            cp_async_wait<1>();
+        } else cp_async_wait<0>();
         __syncthreads();
-        float y[8];   // row tid / 2, eight columns
-        const int r = tid >> 1, c0 = (tid & 1) * 8;
-        if (r < dk) {
+        const float *const T = fold_smem + (k & 1) * size, *const B = T + dk * pitch;
+        const long long next = segment(k + 1);
+        // row tid / 4, four columns; rows of 64 and more a second time
+        float4 y[2];
+        const int c0 = (tid & 3) * 4;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = j0 + c0 + e < a.dv ? segs.sum[at * plane + (long long)r * a.dv + j0 + c0 + e] : 0.f;
+        for (int h = 0; h < 2; ++h) {
+            const int r = (tid >> 2) + 64 * h;
+            if (r >= dk) break;
+            y[h] = *reinterpret_cast<const float4*>(B + r * 16 + c0);
+#pragma unroll 4
             for (int i = 0; i < dk; ++i) {
                 const float t = back ? T[i * pitch + r] : T[r * pitch + i];
-                const float4 u = *reinterpret_cast<const float4*>(X + i * 16 + c0), v = *reinterpret_cast<const float4*>(X + i * 16 + c0 + 4);
-                y[0] = fmaf(t, u.x, y[0]); y[1] = fmaf(t, u.y, y[1]); y[2] = fmaf(t, u.z, y[2]); y[3] = fmaf(t, u.w, y[3]);
-                y[4] = fmaf(t, v.x, y[4]); y[5] = fmaf(t, v.y, y[5]); y[6] = fmaf(t, v.z, y[6]); y[7] = fmaf(t, v.w, y[7]);
+                const float4 u = *reinterpret_cast<const float4*>(X + i * 16 + c0);
+                y[h].x = fmaf(t, u.x, y[h].x); y[h].y = fmaf(t, u.y, y[h].y); y[h].z = fmaf(t, u.z, y[h].z); y[h].w = fmaf(t, u.w, y[h].w);
             }
         }
         __syncthreads();
-        if (r < dk)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                X[r * 16 + c0 + e] = y[e];
-                if (j0 + c0 + e < a.dv) segs.in[next * plane + (long long)r * a.dv + j0 + c0 + e] = y[e];
-            }
-        __syncthreads();
+        for (int h = 0; h < 2; ++h) {
+            const int r = (tid >> 2) + 64 * h;
+            if (r >= dk) break;
+            *reinterpret_cast<float4*>(X + r * 16 + c0) = y[h];
+            if (c0 < mine) *reinterpret_cast<float4*>(segs.in + next * plane + (long long)r * a.dv + j0 + c0) = y[h];
+        }
     }
 }
 
@@ -864,19 +896,20 @@ cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, const Segs& segs, 
 
 cudaError_t launch_fold(const Gdr<bf>& a, const Segs& segs, bool back, cudaStream_t stream) {
     const int slabs = (a.dv + 15) / 16;
-    const size_t smem = ((size_t)a.dk * (a.dk + 1) + a.dk * 16 + 4) * 4;
+    const size_t smem = ((size_t)2 * (a.dk * (a.dk + 4) + a.dk * 16) + a.dk * 16) * 4;
     cudaError_t e = cudaFuncSetAttribute(gdr_fold_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     count_launch();
     return launch_pdl(gdr_fold_kernel, dim3((unsigned)(a.units * slabs)), dim3(256), smem, stream, a, segs, slabs, back);
 }
 
-// Segments of a unit: as many as give every SM its two blocks, of four chunks and more, where at least half the chip would be idle otherwise.
+// Segments of a unit: as many as let the blocks of the launch proper run at once (two an SM), of four chunks and more, from three segments on:
+// below, what the first launch adds is what the second saves.  (A block's time is its chunks' in a row, whether or not another shares its SM:
+// 32 units of 4096 tokens, 24 x 48, 8 segments 49 + 39 us for the two launches, 5 segments, with which the first fits the chip too, 40 + 57.)
 int segments(long long units, int L, int dk, int dv) {
     if (dk > 64) return 1;   // (one block an SM, and as many columns for the transition as for the state: 2 x 16 units of 4096 tokens, 128 x 128, gain nothing)
     const long long blocks = units * ((dv + 16 * kMostWarps - 1) / (16 * kMostWarps)), chunks = (L + kChunk - 1) / kChunk;
-    const long long fit = 2LL * 148 / blocks;
-    const long long n = fit < chunks / 4 ? fit : chunks / 4;
+    const long long fit = 2LL * 148 / blocks, n = fit < chunks / 4 ? fit : chunks / 4;
     return n < 3 ? 1 : (int)(n < 32 ? n : 32);
 }
 size_t up(size_t n) { return (n + 255) / 256 * 256; }

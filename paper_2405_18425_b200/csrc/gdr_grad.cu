@@ -450,21 +450,7 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
             stop[h] = t < nt && (expf(__bfloat162float(a.la[a.row(unit, t0 + t)])) == 0.f || (t0 + t == 0 && !a.state_in));
             if (stop[h]) sum[h] = 0.f;
         }
-        // suffix sums of pairs: (sum, whether something stopped it)
-        float acc = stop[0] ? 0.f : sum[0] + (stop[1] ? 0.f : sum[1]);
-        bool cut = stop[0] || stop[1];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const float y = __shfl_down_sync(0xffffffffu, acc, o);
-            const int z = __shfl_down_sync(0xffffffffu, (int)cut, o);
-            if (lane + o < 32) {
-                if (!cut) acc += y;
-                cut = cut || z;
-            }
-        }
-        float later = __shfl_down_sync(0xffffffffu, acc, 1);   // what the pairs behind come to, with the anchor where nothing stopped it
-        const int later_cut = __shfl_down_sync(0xffffffffu, (int)cut, 1);
-        later = lane == 31 ? run : later + (later_cut ? 0.f : run);
+        const float later = suffix_of_pairs(sum, stop, run);
         const float d1 = stop[1] ? 0.f : sum[1] + later, d0 = stop[0] ? 0.f : sum[0] + d1;
         if (2 * lane < nt) a.dla[a.row(unit, t0 + 2 * lane)] = __float2bfloat16_rn(d0);
         if (2 * lane + 1 < nt) a.dla[a.row(unit, t0 + 2 * lane + 1)] = __float2bfloat16_rn(d1);

@@ -21,8 +21,54 @@
 namespace vig {
 namespace {
 
-constexpr int kTile = 16;     // tokens staged at a time
+template <int DP>
+constexpr int tile_tokens() { return DP <= 64 ? 32 : 16; }   // staged at a time, a tile ahead of the walk
 constexpr int kBorder = 64;   // tokens between the states that the gradient keeps
+
+__device__ __forceinline__ float to_f(float x);
+__device__ __forceinline__ float to_f(__nv_bfloat16 x);
+__device__ __forceinline__ void cp_async4(float* dst, const float* src, bool in) {   // zero where !in
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async16(float* dst, const float* src, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+// Rows of a tile to shared memory as fp32: n rows (of kTile) of `cols` values at src(row), part of rows of `ld` values from a multiple of eight on;
+// zeros up to `width` and kTile.  fp32 by asynchronous copies, which the walk of the tile before hides; bf16 through registers, four values at a time.
+template <typename T, int kTile, typename F>
+__device__ __forceinline__ void stage_rows(float* dst, int n, int cols, int ld, int width, F src) {
+    const int tid = threadIdx.x, nth = blockDim.x;
+    if constexpr (sizeof(T) == 4) {
+        const float* const any = (const float*)src(0);
+        if (((cols | ld | width) & 3) == 0) {   // (rows then start on sixteen bytes: so do the tensors)
+            const int w = width >> 2;
+            for (int i = tid; i < kTile * w; i += nth) {
+                const int t = i / w, e = (i - t * w) * 4;
+                const bool in = t < n && e < cols;
+                cp_async16(dst + t * width + e, in ? (const float*)src(t) + e : any, in);
+            }
+        } else
+            for (int i = tid; i < kTile * width; i += nth) {
+                const int t = i / width, e = i - t * width;
+                const bool in = t < n && e < cols;
+                cp_async4(dst + i, in ? (const float*)src(t) + e : any, in);
+            }
+    } else
+        for (int i0 = tid; i0 < kTile * width; i0 += 4 * nth) {
+            T x[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const int i = i0 + h * nth, t = i / width, e = i - t * width;
+                x[h] = i < kTile * width && t < n && e < cols ? src(t)[e] : T(0.f);
+            }
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                if (i0 + h * nth < kTile * width) dst[i0 + h * nth] = to_f(x[h]);
+        }
+}
+__device__ __forceinline__ void stage_one(float* dst, const float* src) { cp_async4(dst, src, true); }
+__device__ __forceinline__ void stage_one(float* dst, const __nv_bfloat16* src) { *dst = to_f(*src); }
+__device__ __forceinline__ void staged() { asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory"); }
 
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -99,41 +145,32 @@ struct Vec {
 // Shared memory of a walk, in floats: two buffers of N vectors of kTile tokens, a scalar per owner (column or row) and token, the two
 // gates; one buffer of results.
 template <int N, int DP>
-__host__ __device__ constexpr int buffer_floats(int owners) { return kTile * (N * DP + 2 * owners + 2); }
+__host__ __device__ constexpr int buffer_floats(int owners) { return tile_tokens<DP>() * (N * DP + 2 * owners + 2); }
 template <int N, int DP>
-constexpr size_t walk_smem(int owners) { return (size_t)(2 * buffer_floats<N, DP>(owners) + 2 * kTile * owners) * 4; }
+constexpr size_t walk_smem(int owners) { return (size_t)(2 * buffer_floats<N, DP>(owners) + 2 * tile_tokens<DP>() * owners) * 4; }
 
 // ---- columns: owners are columns of S, vectors of dk ------------------------------------------------------------------
 // BACK: the walk of A.  KEEP (the gradient's walks): states at the borders.
 template <typename T, int R, int G, bool BACK, bool KEEP>
 __device__ void walk_columns(const Gdr<T>& a, const Scratch& s, float* sm, long long unit, int j0, int owners) {
-    constexpr int DP = R * G;
+    constexpr int DP = R * G, kTile = tile_tokens<DP>();
     const int tid = threadIdx.x, nth = blockDim.x, l = tid % G, col = tid / G, j = j0 + col;
     const int mine = min(owners, a.dv - j0);
     const bool valid = col < mine;
     const int bf = buffer_floats<2, DP>(owners);
     float* const res = sm + 2 * bf;
-    const int tiles = (a.L + kTile - 1) / kTile;
+    const int tiles = (a.L + kTile - 1) / kTile, lg = 31 - __clz(owners);   // (owners: a power of two)
     const T* const scalar = BACK ? a.d_out : a.v;
     auto stage = [&](int tile, int b) {
         float *kk = sm + b * bf, *qq = kk + kTile * DP, *sc = qq + kTile * DP, *al = sc + 2 * kTile * owners, *be = al + kTile;
-        const int t0 = tile * kTile;
-        for (int i = tid; i < kTile * DP; i += nth) {
-            const int t = i / DP, e = i % DP;
-            const bool in = t0 + t < a.L && e < a.dk;
-            const long long at = in ? a.row(unit, t0 + t) * a.dk + e : 0;
-            kk[i] = in ? to_f(a.k[at]) : 0.f;
-            qq[i] = in ? to_f(a.q[at]) : 0.f;
-        }
-        for (int i = tid; i < kTile * owners; i += nth) {
-            const int t = i / owners, c = i % owners;
-            if (t0 + t < a.L && c < mine) sc[i] = to_f(scalar[a.row(unit, t0 + t) * a.dv + j0 + c]);
-            else sc[i] = 0.f;
-        }
-        if (tid < kTile && t0 + tid < a.L) {
+        const int t0 = tile * kTile, n = min(kTile, a.L - t0);
+        stage_rows<T, kTile>(kk, n, a.dk, a.dk, DP, [&](int t) { return a.k + a.row(unit, t0 + t) * a.dk; });
+        stage_rows<T, kTile>(qq, n, a.dk, a.dk, DP, [&](int t) { return a.q + a.row(unit, t0 + t) * a.dk; });
+        stage_rows<T, kTile>(sc, n, mine, a.dv, owners, [&](int t) { return scalar + a.row(unit, t0 + t) * a.dv + j0; });
+        if (tid < n) {
             const long long r = a.row(unit, t0 + tid);
-            al[tid] = expf(to_f(a.la[r]));
-            be[tid] = to_f(a.beta[r]);
+            stage_one(al + tid, a.la + r);
+            stage_one(be + tid, a.beta + r);
         }
     };
     Vec<R, G> x;
@@ -151,18 +188,25 @@ __device__ void walk_columns(const Gdr<T>& a, const Scratch& s, float* sm, long 
             });
     };
     stage(BACK ? tiles - 1 : 0, 0);
+    staged();
     __syncthreads();
     for (int n = 0; n < tiles; ++n) {
         const int tile = BACK ? tiles - 1 - n : n, t0 = tile * kTile, nt = min(kTile, a.L - t0), b = n & 1;
         if (n + 1 < tiles) stage(BACK ? tile - 1 : tile + 1, b ^ 1);
         const float *kk = sm + b * bf, *qq = kk + kTile * DP, *sc = qq + kTile * DP, *al = sc + 2 * kTile * owners, *be = al + kTile;
         if (KEEP && BACK && ((t0 + nt) % kBorder == 0 || t0 + nt == a.L)) keep(s.A, (t0 + nt - 1) / kBorder);
+        // (a token's vectors are read while the one before it is walked)
+        Vec<R, G> k, q;
+        const int at0 = BACK ? nt - 1 : 0;
+        k.load(kk + at0 * DP, l);
+        q.load(qq + at0 * DP, l);
+        float alpha = expf(al[at0]), beta = be[at0], y = sc[at0 * owners + col];
         for (int i = 0; i < nt; ++i) {
-            const int t = BACK ? nt - 1 - i : i;
-            Vec<R, G> k, q;
-            k.load(kk + t * DP, l);
-            q.load(qq + t * DP, l);
-            const float alpha = al[t], beta = be[t], y = sc[t * owners + col];
+            const int t = BACK ? nt - 1 - i : i, t1 = i + 1 < nt ? (BACK ? t - 1 : t + 1) : t;
+            Vec<R, G> k1, q1;
+            k1.load(kk + t1 * DP, l);
+            q1.load(qq + t1 * DP, l);
+            const float alpha1 = expf(al[t1]), beta1 = be[t1], y1 = sc[t1 * owners + col];
             if (BACK) {
                 x.add(q, y);
                 const float du = x.dot(k);
@@ -180,11 +224,17 @@ __device__ void walk_columns(const Gdr<T>& a, const Scratch& s, float* sm, long 
                     if (l == 0) res[t * owners + col] = o;
                 }
             }
+            k = k1;
+            q = q1;
+            alpha = alpha1;
+            beta = beta1;
+            y = y1;
         }
         if (KEEP && !BACK && ((t0 + nt) % kBorder == 0 || t0 + nt == a.L)) keep(s.S, (t0 + nt - 1) / kBorder);
+        staged();   // the next tile
         __syncthreads();
         for (int i = tid; i < nt * owners; i += nth) {
-            const int t = i / owners, c = i % owners;
+            const int t = i >> lg, c = i & (owners - 1);
             if (c >= mine) continue;
             const long long at = a.row(unit, t0 + t) * a.dv + j0 + c;
             if (BACK) {
@@ -221,36 +271,26 @@ __global__ void __launch_bounds__(256) gdr_columns_grad_kernel(Gdr<T> a, Scratch
 // ---- rows: owners are rows of S, vectors of dv ---------------------------------------------------------------------------
 template <typename T, int R, int G, bool BACK>
 __device__ void walk_rows(const Gdr<T>& a, const Scratch& s, float* sm, long long unit, int i0, int owners) {
-    constexpr int DP = R * G;
+    constexpr int DP = R * G, kTile = tile_tokens<DP>();
     const int tid = threadIdx.x, nth = blockDim.x, l = tid % G, own = tid / G, row = i0 + own;
     const int mine = min(owners, a.dk - i0);
     const bool valid = own < mine;
     const int bf = buffer_floats<3, DP>(owners);
     float* const res = sm + 2 * bf;
-    const int tiles = (a.L + kTile - 1) / kTile;
+    const int tiles = (a.L + kTile - 1) / kTile, lg = 31 - __clz(owners);   // (owners: a power of two)
     auto stage = [&](int tile, int b) {
         float *uu = sm + b * bf, *dd = uu + kTile * DP, *oo = dd + kTile * DP, *kk = oo + kTile * DP, *qq = kk + kTile * owners,
               *al = qq + kTile * owners, *be = al + kTile;
-        const int t0 = tile * kTile;
-        for (int i = tid; i < kTile * DP; i += nth) {
-            const int t = i / DP, e = i % DP;
-            const bool in = t0 + t < a.L && e < a.dv;
-            const long long r = in ? a.row(unit, t0 + t) : 0, at = r * a.dv + (in ? e : 0);
-            uu[i] = in ? to_f(a.beta[r]) * s.w[at] : 0.f;
-            dd[i] = in ? s.du[at] : 0.f;
-            oo[i] = in ? to_f(a.d_out[at]) : 0.f;
-        }
-        for (int i = tid; i < kTile * owners; i += nth) {
-            const int t = i / owners, c = i % owners;
-            const bool in = t0 + t < a.L && c < mine;
-            const long long at = in ? a.row(unit, t0 + t) * a.dk + i0 + c : 0;
-            kk[i] = in ? to_f(a.k[at]) : 0.f;
-            qq[i] = in ? to_f(a.q[at]) : 0.f;
-        }
-        if (tid < kTile && t0 + tid < a.L) {
+        const int t0 = tile * kTile, n = min(kTile, a.L - t0);
+        stage_rows<float, kTile>(uu, n, a.dv, a.dv, DP, [&](int t) { return s.w + a.row(unit, t0 + t) * a.dv; });
+        stage_rows<float, kTile>(dd, n, a.dv, a.dv, DP, [&](int t) { return s.du + a.row(unit, t0 + t) * a.dv; });
+        stage_rows<T, kTile>(oo, n, a.dv, a.dv, DP, [&](int t) { return a.d_out + a.row(unit, t0 + t) * a.dv; });
+        stage_rows<T, kTile>(kk, n, mine, a.dk, owners, [&](int t) { return a.k + a.row(unit, t0 + t) * a.dk + i0; });
+        stage_rows<T, kTile>(qq, n, mine, a.dk, owners, [&](int t) { return a.q + a.row(unit, t0 + t) * a.dk + i0; });
+        if (tid < n) {
             const long long r = a.row(unit, t0 + tid);
-            al[tid] = expf(to_f(a.la[r]));
-            be[tid] = to_f(a.beta[r]);
+            stage_one(al + tid, a.la + r);
+            stage_one(be + tid, a.beta + r);
         }
     };
     Vec<R, G> x;
@@ -261,39 +301,59 @@ __device__ void walk_rows(const Gdr<T>& a, const Scratch& s, float* sm, long lon
             if (e < a.dv) y = first[(unit * a.dk + row) * a.dv + e];
         });
     stage(BACK ? tiles - 1 : 0, 0);
+    staged();
     __syncthreads();
     for (int n = 0; n < tiles; ++n) {
         const int tile = BACK ? tiles - 1 - n : n, t0 = tile * kTile, nt = min(kTile, a.L - t0), b = n & 1;
         if (n + 1 < tiles) stage(BACK ? tile - 1 : tile + 1, b ^ 1);
         const float *uu = sm + b * bf, *dd = uu + kTile * DP, *oo = dd + kTile * DP, *kk = oo + kTile * DP, *qq = kk + kTile * owners,
                     *al = qq + kTile * owners, *be = al + kTile;
-        for (int i = 0; i < nt; ++i) {
-            const int t = BACK ? nt - 1 - i : i;
-            Vec<R, G> u, du, dout;
-            u.load(uu + t * DP, l);
+        auto token = [&](int t, Vec<R, G>& w, Vec<R, G>& du, Vec<R, G>& dout, float& alpha, float& beta, float& k, float& q) {
+            w.load(uu + t * DP, l);
             du.load(dd + t * DP, l);
             dout.load(oo + t * DP, l);
-            const float alpha = al[t], beta = be[t], k = kk[t * owners + own], q = qq[t * owners + own];
+            alpha = expf(al[t]);
+            beta = be[t];
+            k = kk[t * owners + own];
+            q = qq[t * owners + own];
+        };
+        constexpr bool AHEAD = R <= 16;   // read a token's vectors while the one before it is walked: registers permitting
+        Vec<R, G> w, du, dout, w1, du1, dout1;
+        float alpha, beta, k, q, alpha1, beta1, k1, q1;
+        token(BACK ? nt - 1 : 0, w, du, dout, alpha, beta, k, q);
+        for (int i = 0; i < nt; ++i) {
+            const int t = BACK ? nt - 1 - i : i, t1 = i + 1 < nt ? (BACK ? t - 1 : t + 1) : t;
+            if (AHEAD) token(t1, w1, du1, dout1, alpha1, beta1, k1, q1);
             if (BACK) {
                 x.add(dout, q);
-                const float g = x.dot(u);
+                const float g = beta * x.dot(w);
                 x.add(du, -beta * k);
                 x.scale(alpha);
                 if (l == 0) res[t * owners + own] = g;
             } else {
                 x.scale(alpha);
                 const float g = -beta * x.dot(du);
-                x.add(u, k);
+                x.add(w, beta * k);
                 const float dq = x.dot(dout);
                 if (l == 0) {
                     res[t * owners + own] = g;
                     res[(kTile + t) * owners + own] = dq;
                 }
             }
+            if (AHEAD) {
+                w = w1;
+                du = du1;
+                dout = dout1;
+                alpha = alpha1;
+                beta = beta1;
+                k = k1;
+                q = q1;
+            } else token(t1, w, du, dout, alpha, beta, k, q);
         }
+        staged();   // the next tile
         __syncthreads();
         for (int i = tid; i < nt * owners; i += nth) {
-            const int t = i / owners, c = i % owners;
+            const int t = i >> lg, c = i & (owners - 1);
             if (c >= mine) continue;
             const long long at = a.row(unit, t0 + t) * a.dk + i0 + c;
             if (BACK) s.dk1[at] = res[i];
@@ -318,16 +378,19 @@ __global__ void __launch_bounds__(256) gdr_rows_grad_kernel(Gdr<T> a, Scratch s,
 // ---- what is left per token: a block per 64 tokens of a unit -----------------------------------------------------------------
 template <typename T>
 __device__ void finish(const Gdr<T>& a, const Scratch& s, long long unit, int border) {
-    __shared__ float E[kBorder], part[8];
+    __shared__ float E[kBorder], part[16];
+    const int threads = blockDim.x, warps = threads >> 5;
     const int t0 = border * kBorder, nt = min(kBorder, a.L - t0);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const long long plane = (long long)a.dk * a.dv, at = (unit * borders(a.L) + border) * plane;
     float sum = 0.f;
-    for (int i = tid; i < plane; i += 256) sum = fmaf(s.S[at + i], s.A[at + i], sum);
+#pragma unroll 8
+    for (int i = tid; i < plane; i += threads) sum = fmaf(s.S[at + i], s.A[at + i], sum);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) part[warp] = sum;
-    for (int t = warp; t < nt; t += 8) {
+#pragma unroll 2
+    for (int t = warp; t < nt; t += warps) {
         const long long r = a.row(unit, t0 + t);
         const float beta = to_f(a.beta[r]);
         float e = 0.f, db = 0.f;
@@ -353,20 +416,27 @@ __device__ void finish(const Gdr<T>& a, const Scratch& s, long long unit, int bo
         }
     }
     __syncthreads();
-    if (tid == 0) {
+    // sums from the border; a gate that leaves nothing (what the sums come to there is rounding), or that has nothing to scale (the first of a
+    // sequence without an initial state), has none, and they start anew there
+    if (warp == 0) {
         float run = 0.f;
-        for (int w = 0; w < 8; ++w) run += part[w];
-        for (int t = nt - 1; t >= 0; --t) {
-            const long long r = a.row(unit, t0 + t);
-            // a gate that leaves nothing (what the sums come to there is rounding), the first of a sequence without an initial state
-            run = expf(to_f(a.la[r])) == 0.f || (t0 + t == 0 && !a.state_in) ? 0.f : run + E[t];
-            a.dla[r] = from_f<T>(run);
+        for (int w = 0; w < warps; ++w) run += part[w];
+        float mine[2];
+        bool stop[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int t = 2 * lane + h;
+            stop[h] = t < nt && (expf(to_f(a.la[a.row(unit, t0 + t)])) == 0.f || (t0 + t == 0 && !a.state_in));
+            mine[h] = t < nt && !stop[h] ? E[t] : 0.f;
         }
+        run = suffix_of_pairs(mine, stop, run);
+        if (2 * lane + 1 < nt) a.dla[a.row(unit, t0 + 2 * lane + 1)] = from_f<T>(run = stop[1] ? 0.f : mine[1] + run);
+        if (2 * lane < nt) a.dla[a.row(unit, t0 + 2 * lane)] = from_f<T>(stop[0] ? 0.f : mine[0] + run);
     }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) gdr_finish_kernel(Gdr<T> a, Scratch s) {
+__global__ void __launch_bounds__(512) gdr_finish_kernel(Gdr<T> a, Scratch s) {
     pdl_wait();
     pdl_launch_dependents();
     finish<T>(a, s, blockIdx.x / borders(a.L), blockIdx.x % borders(a.L));
@@ -443,10 +513,13 @@ cudaError_t with_vector(int d, F f) {
     return f(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
 }
 
-// Owners a block holds: at most 256 threads, whole warps.
-int owners_of(int n, int G) {
-    const int most = 256 / G, slabs = (n + most - 1) / most, per = (n + slabs - 1) / slabs, warp = 32 / G;
-    return (per + warp - 1) / warp * warp;
+// Owners a block holds: whole warps, a power of two, at most 256 threads; fewer where that gives every SM a block (48 units of 196 tokens, 32 x 64
+// fp32: one block a unit 47 us).
+int owners_of(int n, int G, long long walks) {
+    const int most = 256 / G;
+    int owners = 32 / G;
+    while (owners < most && owners < n && walks * ((n + 2 * owners - 1) / (2 * owners)) >= 148) owners *= 2;
+    return owners;
 }
 
 template <typename K>
@@ -486,7 +559,7 @@ template <typename T>
 cudaError_t launch_gdr_walk_fwd(const Gdr<T>& a, cudaStream_t stream) {
     return with_vector(a.dk, [&](auto R, auto G) {
         constexpr int r = decltype(R)::value, g = decltype(G)::value;
-        const int owners = owners_of(a.dv, g);
+        const int owners = owners_of(a.dv, g, a.units);
         const size_t smem = walk_smem<2, r * g>(owners);
         auto kernel = gdr_columns_kernel<T, r, g>;
         cudaError_t e = allow_smem(kernel, smem);
@@ -509,7 +582,7 @@ cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t str
     const Scratch s = cut_scratch<T>((char*)scratch, &a, a.units, a.L, a.dk, a.dv, &total);
     cudaError_t e = with_vector(a.dk, [&](auto R, auto G) {
         constexpr int r = decltype(R)::value, g = decltype(G)::value;
-        const int owners = owners_of(a.dv, g);
+        const int owners = owners_of(a.dv, g, 2 * a.units);
         const size_t smem = walk_smem<2, r * g>(owners);
         auto kernel = gdr_columns_grad_kernel<T, r, g>;
         cudaError_t e = allow_smem(kernel, smem);
@@ -519,7 +592,7 @@ cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t str
     if (e != cudaSuccess) return e;
     e = with_vector(a.dv, [&](auto R, auto G) {
         constexpr int r = decltype(R)::value, g = decltype(G)::value;
-        const int owners = owners_of(a.dk, g);
+        const int owners = owners_of(a.dk, g, 2 * a.units);
         const size_t smem = walk_smem<3, r * g>(owners);
         auto kernel = gdr_rows_grad_kernel<T, r, g>;
         cudaError_t e = allow_smem(kernel, smem);
@@ -528,7 +601,7 @@ cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t str
     });
     if (e != cudaSuccess) return e;
     count_launch(3);
-    return launch_pdl(gdr_finish_kernel<T>, dim3((unsigned)(a.units * borders(a.L))), dim3(256), 0, stream, a, s);
+    return launch_pdl(gdr_finish_kernel<T>, dim3((unsigned)(a.units * borders(a.L))), dim3(512), 0, stream, a, s);
 }
 
 size_t gdr_repair_slot_bytes(int L, int dk, int dv) { return gdr_walk_bwd_scratch_bytes<__nv_bfloat16>(1, L, dk, dv); }

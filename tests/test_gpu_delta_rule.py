@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 # B, H, L, dk, dv: one token, lengths around 16, 64 and 128, heads of this library and larger ones, odd ones, several blocks of columns
 SIZES = [(1, 1, 1, 16, 32), (2, 3, 2, 24, 48), (3, 1, 16, 8, 8), (2, 3, 17, 24, 48), (1, 2, 64, 32, 64), (2, 2, 65, 128, 128), (1, 3, 130, 20, 17),
          (1, 1, 300, 64, 256), (1, 2, 196, 32, 64), (1, 1, 5, 1, 1), (1, 2, 33, 96, 40), (2, 1, 127, 128, 24), (1, 2, 128, 48, 96), (1, 1, 77, 100, 100),
-         (1, 1, 1100, 24, 48), (2, 1, 515, 64, 64), (1, 2, 2049, 16, 40), (1, 1, 1990, 64, 128)]
+         (1, 1, 1100, 24, 48), (2, 1, 515, 64, 64), (1, 2, 2049, 16, 40), (1, 1, 1990, 64, 128), (1, 2, 40, 70, 70), (1, 1, 50, 12, 130)]
 
 
 def _terms(L, dk, dv):
@@ -128,6 +128,31 @@ def test_keys_beyond_unit_length(size, parallel):
         assert off(g, w) <= 2.0 ** -7, name
     if parallel:
         assert taken > 0 and vig.vig_test_take_fallback_count() > 0
+
+
+def test_one_unit_of_a_long_call_beyond_the_range():
+    """Segments side by side: a dozen parallel keys beyond unit length in the middle of one unit (10^9), forgotten soon after; that unit is redone
+    whole, the others are not."""
+    for size in ((1, 2, 1100, 24, 48), (2, 1, 400, 32, 64)):
+        d = gdr_inputs(*size, "bf16", seed=18, gate_mean=1.0, states=True)
+        mid = size[2] // 2
+        d["k"][0, 0, mid:mid + 12] = d["k"][0, 0, mid] * 4
+        d["beta"][0, 0, mid:mid + 12] = 0.5
+        d["log_alpha"][0, 0, mid + 15] = float("-inf")
+        torch.cuda.synchronize()
+        vig.vig_test_take_fallback_count()
+        out, last = gdr_forward(d)
+        taken = vig.vig_test_take_fallback_count()
+        ref, ref_last = gdr_oracle(d)
+        for u in range(size[0] * size[1]):
+            for part in (slice(0, mid), slice(mid, mid + 15), slice(mid + 15, None)):
+                assert off(out.flatten(0, 1)[u, part], ref.reshape(-1, *ref.shape[2:])[u, part]) <= 2.0 ** -7
+        check([("state", last, ref_last)], sum(size[2:]), True)
+        got, want = gdr_gradient(d), gdr_oracle_gradient(d)
+        assert taken > 0 and vig.vig_test_take_fallback_count() == 1
+        for name, g, w in zip(("dq", "dk", "dv", "dlog_alpha", "dbeta", "d_state"), got, want):
+            for u in range(size[0] * size[1]):
+                assert off(g.flatten(0, 1)[u], w.reshape(-1, *w.shape[2:])[u]) <= 2.0 ** -7, (name, u)
 
 
 def test_in_range_inputs_stay_on_the_tiles():
