@@ -201,6 +201,7 @@ __device__ void walk_columns(const Gdr<T>& a, const Scratch& s, float* sm, long 
         k.load(kk + at0 * DP, l);
         q.load(qq + at0 * DP, l);
         float alpha = expf(al[at0]), beta = be[at0], y = sc[at0 * owners + col];
+#pragma unroll 2
         for (int i = 0; i < nt; ++i) {
             const int t = BACK ? nt - 1 - i : i, t1 = i + 1 < nt ? (BACK ? t - 1 : t + 1) : t;
             Vec<R, G> k1, q1;
@@ -321,6 +322,7 @@ __device__ void walk_rows(const Gdr<T>& a, const Scratch& s, float* sm, long lon
         Vec<R, G> w, du, dout, w1, du1, dout1;
         float alpha, beta, k, q, alpha1, beta1, k1, q1;
         token(BACK ? nt - 1 : 0, w, du, dout, alpha, beta, k, q);
+#pragma unroll 2
         for (int i = 0; i < nt; ++i) {
             const int t = BACK ? nt - 1 - i : i, t1 = i + 1 < nt ? (BACK ? t - 1 : t + 1) : t;
             if (AHEAD) token(t1, w1, du1, dout1, alpha1, beta1, k1, q1);

@@ -431,6 +431,7 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
         }
     }
     const int most = a.by_lanes.of(rows + lanes - 1);   // the same for the whole block: vectors that no thread has are skipped
+    constexpr bool kKeepG = sizeof(T) == 4;   // g takes d_out's registers where it fits them: no second pass through the activation
     f32x2 sg[V / 2], sx[V / 2];
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) sg[e] = sx[e] = both(0.f);
@@ -444,6 +445,7 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
                 sg[e] = fadd2(sg[e], g[e]);
                 sx[e] = ffma2(g[e], h[e], sx[e]);
             }
+            if constexpr (kKeepG) d[i] = narrow16(g, a.x);
         }
     if (live)
 #pragma unroll
@@ -521,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
     for (int i = 0; i < K; ++i)
         if (i < most && i < n) {
             f32x2 h[V / 2], g[V / 2];
-            ch.template grad<ACT>(x[i], d[i], h, g);
+            ch.template grad<kKeepG ? kActNone : ACT>(x[i], d[i], h, g);
             ch.dx(h, g, m1, m2);
             *reinterpret_cast<uint4*>(a.dx + base + (long long)(rl + i * lanes) * a.C) = narrow16(g, a.x);
         }
