@@ -689,8 +689,8 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
     }
 }
 
-// Whether two blocks share an SM: their shared memory must.  Each then has 128 registers a thread, of which the preparing warps leave the
-// others 48 (128 x (176 + 80) = 256 x 128).
+// Whether two blocks share an SM: their shared memory must.  Each then has 128 registers a thread.  (Unequal shares, 80 to 104 for the preparing
+// warps and 176 to 152 for the others: 53 to 47 us for 64 x 12 units of 196 tokens, 32 x 64, against 46.)
 template <int DKP, bool EXACT, Way WAY>
 constexpr bool two_blocks() { return 2 * (Layout<DKP, EXACT, WAY>::total(kMostWarps) + 1024) <= 228 * 1024; }
 
@@ -710,13 +710,10 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
     const bool starts = seg == (BACK ? segs.n - 1 : 0), ends = seg == (BACK ? 0 : segs.n - 1);
     pdl_wait();
     pdl_launch_dependents();
-    if (warp >= kMostWarps) {
-        if constexpr (two_blocks<DKP, EXACT, WAY>()) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp >= warps) {
         prepare_chunks<DKP, EXACT, WAY>(a, smem, lay, unit, first, count, threads);
         return;
     }
-    if constexpr (two_blocks<DKP, EXACT, WAY>()) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-    if (warp >= warps) return;   // (four warps split their registers together)
     const bool vectors = WAY == Way::kSum && slab >= slabs;   // columns that are unit vectors
     const int col0 = ((vectors ? slab - slabs : slab) * warps + warp) * 16, g = lane >> 2, c = lane & 3;
     const Lane ln(lane);
@@ -875,7 +872,8 @@ template <Way WAY>
 cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, const Segs& segs, bool exact, cudaStream_t stream) {
     int* status = device_status_ptr();
     if (!status) return cudaErrorUnknown;
-    const int all = (a.dv + 15) / 16, slabs = (all + kMostWarps - 1) / kMostWarps, warps = (all + slabs - 1) / slabs;   // (gdr_padded_columns)
+    const int sixteens = gdr_padded_columns(a.dv) / 16;
+    const int slabs = (sixteens + kMostWarps - 1) / kMostWarps, warps = sixteens / slabs;   // (narrower blocks for few units: 332 -> 414 us for 2 x 16 x 4096, 128 x 128)
     const long long blocks = a.units * (WAY == Way::kSum ? segs.sums : WAY == Way::kBackSum ? segs.n - 1 : segs.n) * (slabs + (WAY == Way::kSum ? (a.dk + warps * 16 - 1) / (warps * 16) : 0));
     return with_keys(a.dk, [&](auto D) {
         constexpr int dkp = decltype(D)::value;
@@ -886,7 +884,7 @@ cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, const Segs& segs, 
             cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
             if (e != cudaSuccess) return e;
             count_launch();
-            return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kMostWarps + kPrep), smem, stream, a, kept, segs, slabs, warps, status);
+            return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * warps + kPrep), smem, stream, a, kept, segs, slabs, warps, status);
         };
         if constexpr (WAY != Way::kKeep)
             if (exact) return go(std::true_type());

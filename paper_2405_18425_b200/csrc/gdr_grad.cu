@@ -114,7 +114,10 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
     for (int p = 0; p < 5; ++p) {
         const bool low = p <= I;
         const int j = low ? p : p - 1;
-        if (j != I) {
+        if (j >= strips) {   // (no tokens there, and nothing in shared memory)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) xa[p][h] = ea[p][h] = 0u;
+        } else if (j != I) {
             const float ref = low ? gates[kB * kChunk + j * 16 + 15] : end;
             f32x2 er[2];
 #pragma unroll
@@ -265,9 +268,10 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
     float *const cy = reinterpret_cast<float*>(smem + lay.cols), *const cyz = cy + dvp, *const red = cyz + dvp;
     pdl_wait();
     pdl_launch_dependents();
-    // everything comes in by asynchronous copies at once, and is turned into operands where it lies
+    // everything comes in by asynchronous copies at once, and is turned into operands where it lies; rows up to the last strip with tokens
     const uint32_t base = smem_u32(smem);
-    for (int i = tid; i < kChunk * (DKP / 8); i += kThreads) {
+    const int rows = (nt + 15) & ~15;
+    for (int i = tid; i < rows * (DKP / 8); i += kThreads) {
         const int t = i / (DKP / 8), e = i % (DKP / 8) * 8;
         const bool in = t < nt && e < a.dk;
         const long long at = in ? a.row(unit, t0 + t) * a.dk + e : 0;
@@ -276,7 +280,7 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
     }
     const int lg = dvp <= 16 ? 1 : dvp <= 32 ? 2 : dvp <= 64 ? 3 : 4, piece = (tid & ((1 << lg) - 1)) * 8;   // lanes of a row of dv columns, and this one's columns
     if (piece < dvp)
-        for (int t = tid >> lg; t < kChunk; t += kThreads >> lg) {
+        for (int t = tid >> lg; t < rows; t += kThreads >> lg) {
             const bool in = t < nt;   // (rows behind the last token were not written)
             const uint32_t to = t * lay.vp + piece * 2;
             const long long at = (here * kChunk + t) * dvp + piece;
@@ -346,14 +350,15 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
     for (int p = 0; p < 2 * kChunk * kLanes / kThreads; ++p) {
         const int i = tid + p * kThreads, r = i / kLanes, e8 = i % kLanes * 8, t = r & (kChunk - 1);
         const bool key = r < kChunk;
+        if (p * kThreads / kLanes % kChunk >= rows) continue;   // the first of the pass's rows
         uint4* const at = reinterpret_cast<uint4*>(smem + (key ? lay.k : lay.q) + t * KP + e8 * 2);
-        const uint4 x = e8 < DKP ? *at : make_uint4(0u, 0u, 0u, 0u);
+        const uint4 x = e8 < DKP && t < rows ? *at : make_uint4(0u, 0u, 0u, 0u);
         uint32_t m = largest_bf16(x);
 #pragma unroll
         for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
         float down, up;
         power_of(m >> 7, down, up);
-        if (e8 < DKP) *at = bf16_to_half(x, down);
+        if (e8 < DKP && t < rows) *at = bf16_to_half(x, down);
         if (e8 == 0) {
             gates[(key ? kKu : kQu) * kChunk + t] = up;
             if (key) {
@@ -372,7 +377,8 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
             fy[p] = piece < dvp ? *reinterpret_cast<const f32x2*>(cy + piece + 2 * p) : 0ull;
             fz[p] = piece < dvp ? __floats2half2_rn(cyz[piece + 2 * p], cyz[piece + 2 * p + 1]) : __float2half2_rn(0.f);
         }
-        for (int t = tid >> lg; t < kChunk; t += kThreads >> lg) {
+        // (whole warps: a warp's rows, at most sixteen, are either all there or all not)
+        for (int t = tid >> lg; t < rows; t += kThreads >> lg) {
             uint4* const at = reinterpret_cast<uint4*>(smem + lay.d + t * lay.vp + piece * 2);
             const uint4 x = piece < dvp ? *at : make_uint4(0u, 0u, 0u, 0u);
             uint32_t m = largest_bf16(x);
@@ -421,7 +427,8 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
     // the scales of dO's and q's rows together, over the largest
     float HF = 0.f;
     {
-        const float p = gates[kH * kChunk + lane] * gates[kQu * kChunk + lane], q = gates[kH * kChunk + lane + 32] * gates[kQu * kChunk + lane + 32];
+        const float p = lane < rows ? gates[kH * kChunk + lane] * gates[kQu * kChunk + lane] : 0.f,
+                    q = lane + 32 < rows ? gates[kH * kChunk + lane + 32] * gates[kQu * kChunk + lane + 32] : 0.f;
         HF = fmaxf(p, q);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) HF = fmaxf(HF, __shfl_xor_sync(0xffffffffu, HF, o));
