@@ -9,8 +9,9 @@
 //
 // A block runs through the chunks of a unit for up to 64 columns.  Four of its warps prepare: they bring the rows of K and Q, scale them and
 // make N, P and the inverses of the next chunk while the others, a warp for every sixteen columns (gdr_tile.cuh), work on this one.  Two
-// buffers, handed over by named barriers.  (All warps doing both in turn: 64 x 12 units of 196 tokens, 32 x 64, 70 us, 32 units of 4096, 24 x
-// 48, 448 us: a chunk took 7 us from start to end.)
+// buffers, handed over by named barriers.  64 x 12 units of 196 tokens, 32 x 64 (58 MB): 48 us, 0.19 of the rate of a copy, bound by instruction issue
+// (8400 warp instructions a chunk, 430 of them products) and a chunk's chain with two blocks an SM.  (All warps doing both in turn: 70 us; 32 units of
+// 4096 tokens, 24 x 48, 448 us, 7 us a chunk; now 86 in segments, 2.4 us a chunk.)
 #include <type_traits>
 
 #include "gdr.h"

@@ -8,7 +8,8 @@
 // (E K's part of dK and e: replacing S by its decayed form shows e_t = q.dq - v.dv, and v = w + what k retrieves.)
 // A block takes a chunk, a warp sixteen of its tokens as rows: the blocks of X and E up to the diagonal and those of their transposes from it
 // on, five of each for every warp, so that no warp needs another's.  Sums over dv run in fp32 over fp16 operands that are scaled by powers of
-// two: rows of K, Q and dO by their largest element, columns by what the walks kept them under.
+// two: rows of K, Q and dO by their largest element, columns by what the walks kept them under.  64 x 12 units of 196 tokens, 32 x 64: 91 us for 112 MB, bound by
+// instruction issue (3400 a warp, 160 of them products).
 #include <type_traits>
 
 #include "gdr.h"

@@ -3,7 +3,8 @@
 //   S~_t = alpha_t S_{t-1};  w_t = v_t - S~_t^T k_t;  u_t = beta_t w_t;  S_t = S~_t + k_t u_t^T;  out_t = S_t^T q_t
 //
 // The columns of S never meet: column j needs v_tj and the vectors k_t, q_t that all columns share.  A column is held in the registers
-// of four lanes (eight for vectors of more than 128), the shared vectors come through shared memory, sixteen tokens at a time.
+// of four lanes (eight for vectors of more than 128), the shared vectors come through shared memory, 16 or 32 tokens at a time.  A step's chain bounds
+// it (two exchanges between lanes, two passes over the column): 48 units of 196 tokens, 32 x 64 fp32, 35 us, 340 cycles a token.
 // The gradient is four such walks and nothing else:
 //   columns forwards   w, and S at the end of every 64 tokens
 //   columns backwards  A = what arrives at S_t from behind;  D = A + q do^T;  du = D^T k;  dv = beta du;  A <- alpha (D - beta k du^T);
@@ -642,7 +643,8 @@ template cudaError_t launch_gdr_walk_bwd<__nv_bfloat16>(const Gdr<__nv_bfloat16>
 // A block takes 32 columns of a unit's state: sixteen groups of rows, a thread four columns (or one) of every sixteenth row, all of
 // them in registers at once.  Retrieval and read-out are summed in one pass over the state as it was:
 //   S^T k and S^T q;   w = v - alpha S^T k;   out = alpha S^T q + (q . k) u;   S <- alpha S + k u^T
-// Bound by the state's way in and out.
+// Bound by the state's way in and out: 4096 states of 128 x 128, 541 MB, 92 us, 0.90 of the rate of a copy.  (Blocks of 32 columns: a row's piece is
+// one line of 128 bytes, and sixteen blocks fit an SM.)
 namespace {
 
 template <typename T, int V>

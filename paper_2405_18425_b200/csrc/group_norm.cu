@@ -8,6 +8,8 @@
 // are exchanged through distributed shared memory, and every value crosses memory once in and once out.  Larger images go through
 // it twice, in launches of their own.  Variances are sums of squares about a mean that is known: a block's own first, moved to the
 // image's when blocks are joined, so that a mean far from zero costs no digits.  All sums run in a fixed order.
+// 64 x 56 x 56 x 96 bf16 with SiLU (77 MB): 40 us, 0.30 of the rate of a copy: a block's phases follow one another (load, sums, cluster, results: 7.6 us), two
+// blocks an SM.  64 x 14 x 14 x 768: 18 us, its gradient 30 us and 4 for the parameters.
 #include <type_traits>
 
 #include "gdr.h"
