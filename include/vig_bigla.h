@@ -234,7 +234,7 @@ int vig_gate_prep_bwd_f32(const void* g_fwd, const void* g_bwd, const void* dlog
  * q, k: [B,H,L,dk]; v, out: [B,H,L,dv]; log_alpha, beta: [B,H,L], all of the call's element type (vig_gate_prep_* makes log_alpha
  * from logits as it does for the mixer above).  Domain: log_alpha <= 0 (-inf forgets the state), beta finite.  For a state that stays
  * bounded beta_t |k_t|^2 <= 2; nothing is normalised inside.  States are FP32 [B,H,dk,dv] in every call.
- * state_in: S_0, or NULL for zero.  state_out: receives S_L, or NULL; may be state_in.
+ * out must not overlap an input.  state_in: S_0, or NULL for zero.  state_out: receives S_L, or NULL; may be state_in.
  * reverse != 0: the same from the last token to the first (state_in comes behind token L, state_out is what stands at token 1), the
  * other direction of a bidirectional mixer over the patch sequence.
  * bf16: dk and dv multiples of eight run in chunks of 64 tokens on the tensor cores (operands of eleven significant bits under powers of two, 22

@@ -83,27 +83,27 @@ int gdr_bwd_impl(const void* q, const void* k, const void* v, const void* la, co
     a.state_in = (const float*)state_in; a.d_state_out = (const float*)d_state_out;
     a.dq = (T*)dq; a.dk_out = (T*)dk_out; a.dv_out = (T*)dv_out; a.dla = (T*)dla; a.dbeta = (T*)dbeta; a.d_state_in = (float*)d_state_in;
     a.units = units; a.L = L; a.dk = dk; a.dv = dv; a.reverse = reverse != 0;
+    size_t need = 0;
+    bool chunks = false;
+    if constexpr (sizeof(T) == 2) {
+        chunks = gdr_grad_supported(dk, dv) && kernel_preference() != VIG_TEST_KERNEL_SIMT;
+        if (chunks) need = gdr_grad_scratch_bytes(units, L, dk, dv);
+    }
+    if (!chunks) need = gdr_walk_bwd_scratch_bytes<T>(units, L, dk, dv);
+    // a final state's gradient that the call overwrites is put aside: later launches start from it again
+    const size_t aside = d_state_in && d_state_in == d_state_out ? (size_t)units * dk * dv * sizeof(float) : 0;
+    char* ws = nullptr;
+    if (pool_alloc((void**)&ws, need + aside, stream) != cudaSuccess) return VIG_ERR_CUDA;
+    cudaError_t e = cudaSuccess;
+    if (aside) {
+        e = cudaMemcpyAsync(ws + need, d_state_out, aside, cudaMemcpyDeviceToDevice, stream);
+        a.d_state_out = (const float*)(ws + need);
+    }
     if constexpr (sizeof(T) == 2)
-        if (gdr_grad_supported(dk, dv) && kernel_preference() != VIG_TEST_KERNEL_SIMT) {
-            // a final state's gradient that the call overwrites is put aside: units that leave the tiles' range start from it again
-            const size_t aside = d_state_in && d_state_in == d_state_out ? (size_t)units * dk * dv * sizeof(float) : 0;
-            const size_t need = gdr_grad_scratch_bytes(units, L, dk, dv);
-            char* ws = nullptr;
-            if (pool_alloc((void**)&ws, need + aside, stream) != cudaSuccess) return VIG_ERR_CUDA;
-            cudaError_t e = cudaSuccess;
-            if (aside) {
-                e = cudaMemcpyAsync(ws + need, d_state_out, aside, cudaMemcpyDeviceToDevice, stream);
-                a.d_state_out = (const float*)(ws + need);
-            }
-            if (e == cudaSuccess) e = launch_gdr_chunk_bwd(a, ws, stream);
-            st = status_of(e);
-            if (cudaFreeAsync(ws, stream) != cudaSuccess && st == VIG_OK) st = VIG_ERR_CUDA;
-            return st;
-        }
-    void* scratch = nullptr;
-    if (pool_alloc(&scratch, gdr_walk_bwd_scratch_bytes<T>(units, L, dk, dv), stream) != cudaSuccess) return VIG_ERR_CUDA;
-    st = status_of(launch_gdr_walk_bwd<T>(a, scratch, stream));
-    if (cudaFreeAsync(scratch, stream) != cudaSuccess && st == VIG_OK) st = VIG_ERR_CUDA;
+        if (chunks && e == cudaSuccess) e = launch_gdr_chunk_bwd(a, ws, stream);
+    if (!chunks && e == cudaSuccess) e = launch_gdr_walk_bwd<T>(a, ws, stream);
+    st = status_of(e);
+    if (cudaFreeAsync(ws, stream) != cudaSuccess && st == VIG_OK) st = VIG_ERR_CUDA;
     return st;
 }
 

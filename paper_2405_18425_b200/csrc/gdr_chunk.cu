@@ -358,7 +358,7 @@ struct State {
 #pragma unroll
             for (int o = 1; o < 4; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
             const uint32_t ex = min(max(__float_as_uint(m) >> 23, 10u), 244u);
-            const float now = __uint_as_float((253u + TOP - ex) << 23), change = now / scale[h];
+            const float now = __uint_as_float((253u + TOP - ex) << 23), change = fminf(now / scale[h], 0x1p126f);   // (more only where the state is nothing beside either)
             back[h] = __uint_as_float((ex + 1u - TOP) << 23);
             scale[h] = now;
             if (__any_sync(0xffffffffu, change != 1.f)) {

@@ -281,9 +281,49 @@ def test_same_bits_again_and_alone(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_other_stream_and_captured_graphs(dtype):
+@pytest.mark.parametrize("size", [(2, 2, 140, 32, 64), (1, 2, 900, 24, 48), (2, 2, 50, 20, 30)], ids=str)
+def test_states_in_place(size, dtype):
+    """The final state over the initial one, the initial state's gradient over the final one's, and a call whose units are redone."""
+    for beyond in (False, True):
+        d = gdr_inputs(*size, dtype, seed=19, states=True)
+        if beyond:
+            d["k"][0, 0, 20:30] = d["k"][0, 0, 20] * 4
+            d["beta"][0, 0, 20:30] = 0.5
+            d["log_alpha"][0, 0, 33] = float("-inf")
+        want, want_last = gdr_forward(d)
+        want_grads = gdr_gradient(d)
+        state, d_state = d["state"].clone(), d["d_state"].clone()
+        out = torch.empty_like(want)
+        vig.vig_gdr_fwd(*(d[n] for n in NAMES), out, state_in=state, state_out=state)
+        assert torch.equal(out, want) and torch.equal(state, want_last)
+        grads = [torch.empty_like(g) for g in want_grads[:5]]
+        vig.vig_gdr_bwd(*(d[n] for n in NAMES), d["d_out"], *grads, state_in=d["state"], d_state_out=d_state, d_state_in=d_state)
+        for a, b in zip(grads + [d_state], want_grads):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_state_after_values_of_very_different_size(dtype):
+    """A chunk of values of 1e9, forgotten, then nothing at all, then values of 1e-9: scales of the columns jump both ways."""
+    d = gdr_inputs(1, 2, 260, 16, 32, dtype, seed=20)
+    d["v"][:, :, :64] *= 1e9
+    d["log_alpha"][:, :, 64] = float("-inf")
+    d["v"][:, :, 64:128] = 0
+    d["v"][:, :, 128:] *= 1e-9
+    torch.cuda.synchronize()
+    vig.vig_test_take_fallback_count()
+    out, last = gdr_forward(d)
+    ref, ref_last = gdr_oracle(d)
+    for part in (slice(0, 64), slice(128, None)):
+        assert off(out[:, :, part], ref[:, :, part]) <= bound(out, 300)
+    assert (out[:, :, 64:128] == 0).all() and off(last, ref_last) <= 2.0 ** -15
+    assert vig.vig_test_take_fallback_count() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(2, 2, 140, 32, 64), (1, 2, 1100, 24, 48)], ids=str)
+def test_other_stream_and_captured_graphs(size, dtype):
     """On a side stream; captured twice, replayed in turn on new inputs beside a call outside any graph."""
-    size = (2, 2, 140, 32, 64)
     sets = [gdr_inputs(*size, dtype, seed=s, states=True) for s in (12, 13, 14)]
     want = [gdr_forward(d) + tuple(gdr_gradient(d)) for d in sets]
     side = torch.cuda.Stream()
