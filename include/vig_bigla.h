@@ -237,10 +237,11 @@ int vig_gate_prep_bwd_f32(const void* g_fwd, const void* g_bwd, const void* dlog
  * out must not overlap an input.  state_in: S_0, or NULL for zero.  state_out: receives S_L, or NULL; may be state_in.
  * reverse != 0: the same from the last token to the first (state_in comes behind token L, state_out is what stands at token 1), the
  * other direction of a bidirectional mixer over the patch sequence.
- * bf16: dk and dv multiples of eight run in chunks of 64 tokens on the tensor cores (operands of eleven significant bits under powers of two, 22
- *       where a final state is asked for; sums and states fp32), every other size as fp32 walks on the CUDA cores.  Columns of the state that
- *       leave the range of the chunks' operands, which needs beta_t |k_t|^2 > 2, are computed by fp32 walks inside the call.  Long sequences of
- *       few units are cut into segments that run side by side, with scratch from the library's pool.
+ * bf16: chunks of 64 tokens on the tensor cores (operands of eleven significant bits under powers of two, 22 where a final state is
+ *       asked for; sums and states fp32); a handful of tokens, and the gradient of more than 128 value columns, as fp32 walks on the CUDA cores.
+ *       Sizes that are no multiples of eight are laid out again in scratch on the way in and out.  Columns of the state
+ *       that leave the range of the chunks' operands, which needs beta_t |k_t|^2 > 2, are computed by fp32 walks inside the call.  Long
+ *       sequences of few units are cut into segments that run side by side, with scratch from the library's pool.
  * f32:  fp32 walks on the CUDA cores.  dk <= 128, dv <= 256 for either type.
  * L == 0 with a state_out copies state_in (or zeros) there; tensors without elements may be NULL.
  * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */

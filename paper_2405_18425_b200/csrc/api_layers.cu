@@ -31,6 +31,40 @@ int check_sizes(int B, int H, int L, int dk, int dv) {
     return VIG_OK;
 }
 
+// bf16: chunks on the tensor cores, or walks.  A chunk costs its set-up whatever it holds, a walk its tokens: 1500 units of 64 x 64, forward, tiles and walks
+// us: 2 tokens 29, 21; 8 tokens 29, 33; 128 x 128: 8 tokens 112, 79, 16 tokens 113, about 125; gradient of 150 units of 64 x 64: 4 tokens 40, 33; 8 tokens
+// 40, 40; of 1500: 2 tokens 148, 143; 4 tokens 149, 162.
+template <typename T>
+bool takes_tiles(long long units, int L, int dk, int dv, bool gradient) {
+    if (sizeof(T) != 2 || (gradient && !gdr_grad_supported(dk, dv))) return false;
+    const int pref = kernel_preference();
+    if (pref == VIG_TEST_KERNEL_SIMT || pref == VIG_TEST_KERNEL_WARP_TILES) return pref == VIG_TEST_KERNEL_WARP_TILES;
+    return L > (gradient ? (units <= 600 ? 4 : 2) : 8);
+}
+
+// Copies of a call's rows with zeros up to multiples of eight, where the sizes are none.
+struct Padded {
+    int dk, dv, dk0, dv0;
+    size_t keys, values;   // bytes of a copy; 0: no copies
+    Padded(int dk_, int dv_, size_t rows) : dk((dk_ + 7) & ~7), dv((dv_ + 7) & ~7), dk0(dk_), dv0(dv_) {
+        const bool any = dk != dk0 || dv != dv0;
+        keys = any ? (rows * dk * 2 + 255) / 256 * 256 : 0;
+        values = any ? (rows * dv * 2 + 255) / 256 * 256 : 0;
+    }
+    template <typename T>
+    void key(const T*& t, RowCopy& c, char*& at) const {
+        c = {t, at, dk0, dk};
+        t = (const T*)at;
+        at += keys;
+    }
+    template <typename T>
+    void value(const T*& t, RowCopy& c, char*& at) const {
+        c = {t, at, dv0, dv};
+        t = (const T*)at;
+        at += values;
+    }
+};
+
 template <typename T>
 int gdr_fwd_impl(const void* q, const void* k, const void* v, const void* la, const void* beta, const void* state_in, void* out, void* state_out, int B,
                  int H, int L, int dk, int dv, int reverse, cudaStream_t stream) {
@@ -45,21 +79,39 @@ int gdr_fwd_impl(const void* q, const void* k, const void* v, const void* la, co
     Gdr<T> a = {};
     a.q = (const T*)q; a.k = (const T*)k; a.v = (const T*)v; a.la = (const T*)la; a.beta = (const T*)beta;
     a.state_in = (const float*)state_in; a.out = (T*)out; a.state_out = (float*)state_out;
-    a.units = units; a.L = L; a.dk = dk; a.dv = dv; a.reverse = reverse != 0;
+    a.units = units; a.L = L; a.dk = a.ldk = dk; a.dv = a.ldv = dv; a.reverse = reverse != 0;
     if constexpr (sizeof(T) == 2)
-        if (gdr_chunk_supported(dk, dv) && kernel_preference() != VIG_TEST_KERNEL_SIMT) {
-            const size_t need = gdr_chunk_scratch_bytes(units, L, dk, dv);
-            if (need == 0) return status_of(launch_gdr_chunk_fwd(a, nullptr, stream));
-            // segments; an initial state that the call overwrites is put aside, as units that leave the tiles' range start from it again
-            const size_t aside = state_in && state_in == state_out ? (size_t)units * dk * dv * sizeof(float) : 0;
+        if (takes_tiles<T>(units, L, dk, dv, false)) {
+            const size_t rows = (size_t)units * L;
+            const Padded pad(dk, dv, rows);
+            const size_t need = (gdr_chunk_scratch_bytes(units, L, dk, dv) + 255) / 256 * 256, copies = 2 * pad.keys + 2 * pad.values;
+            // an initial state that the call overwrites is put aside where segments' units that leave the tiles' range start from it again
+            const size_t aside = need > 0 && state_in && state_in == state_out ? (size_t)units * dk * dv * sizeof(float) : 0;
+            if (need + aside + copies == 0) return status_of(launch_gdr_chunk_fwd(a, nullptr, stream));
             char* ws = nullptr;
-            if (pool_alloc((void**)&ws, need + aside, stream) != cudaSuccess) return VIG_ERR_CUDA;
+            if (pool_alloc((void**)&ws, need + aside + copies, stream) != cudaSuccess) return VIG_ERR_CUDA;
             cudaError_t e = cudaSuccess;
             if (aside) {
-                e = cudaMemcpyAsync(ws + need, state_in, aside, cudaMemcpyDeviceToDevice, stream);
-                a.state_in = (const float*)(ws + need);
+                e = cudaMemcpyAsync(ws + need + copies, state_in, aside, cudaMemcpyDeviceToDevice, stream);
+                a.state_in = (const float*)(ws + need + copies);
+            }
+            if (copies && e == cudaSuccess) {
+                char* p = ws + need;
+                RowCopy in[kRowCopies];
+                int n = 0;
+                pad.key(a.q, in[n++], p);
+                pad.key(a.k, in[n++], p);
+                pad.value(a.v, in[n++], p);
+                e = launch_copy_rows(in, n, rows, stream);
+                a.out = (T*)p;
+                a.ldk = pad.dk;
+                a.ldv = pad.dv;
             }
             if (e == cudaSuccess) e = launch_gdr_chunk_fwd(a, ws, stream);
+            if (copies && e == cudaSuccess) {
+                const RowCopy back = {a.out, out, pad.dv, dv};
+                e = launch_copy_rows(&back, 1, rows, stream);
+            }
             const bool freed = cudaFreeAsync(ws, stream) == cudaSuccess;
             return freed ? status_of(e) : VIG_ERR_CUDA;
         }
@@ -82,25 +134,50 @@ int gdr_bwd_impl(const void* q, const void* k, const void* v, const void* la, co
     a.q = (const T*)q; a.k = (const T*)k; a.v = (const T*)v; a.la = (const T*)la; a.beta = (const T*)beta; a.d_out = (const T*)d_out;
     a.state_in = (const float*)state_in; a.d_state_out = (const float*)d_state_out;
     a.dq = (T*)dq; a.dk_out = (T*)dk_out; a.dv_out = (T*)dv_out; a.dla = (T*)dla; a.dbeta = (T*)dbeta; a.d_state_in = (float*)d_state_in;
-    a.units = units; a.L = L; a.dk = dk; a.dv = dv; a.reverse = reverse != 0;
+    a.units = units; a.L = L; a.dk = a.ldk = dk; a.dv = a.ldv = dv; a.reverse = reverse != 0;
     size_t need = 0;
     bool chunks = false;
     if constexpr (sizeof(T) == 2) {
-        chunks = gdr_grad_supported(dk, dv) && kernel_preference() != VIG_TEST_KERNEL_SIMT;
+        chunks = takes_tiles<T>(units, L, dk, dv, true);
         if (chunks) need = gdr_grad_scratch_bytes(units, L, dk, dv);
     }
     if (!chunks) need = gdr_walk_bwd_scratch_bytes<T>(units, L, dk, dv);
     // a final state's gradient that the call overwrites is put aside: later launches start from it again
     const size_t aside = d_state_in && d_state_in == d_state_out ? (size_t)units * dk * dv * sizeof(float) : 0;
+    const size_t rows = (size_t)units * L;
+    const Padded pad(dk, dv, rows);
+    const size_t copies = chunks ? 4 * pad.keys + 3 * pad.values : 0;
+    need = (need + 255) / 256 * 256;
+    const size_t put = (aside + 255) / 256 * 256;
     char* ws = nullptr;
-    if (pool_alloc((void**)&ws, need + aside, stream) != cudaSuccess) return VIG_ERR_CUDA;
+    if (pool_alloc((void**)&ws, need + put + copies, stream) != cudaSuccess) return VIG_ERR_CUDA;
     cudaError_t e = cudaSuccess;
     if (aside) {
         e = cudaMemcpyAsync(ws + need, d_state_out, aside, cudaMemcpyDeviceToDevice, stream);
         a.d_state_out = (const float*)(ws + need);
     }
     if constexpr (sizeof(T) == 2)
-        if (chunks && e == cudaSuccess) e = launch_gdr_chunk_bwd(a, ws, stream);
+        if (chunks && e == cudaSuccess) {
+            if (copies) {
+                char* p = ws + need + put;
+                RowCopy in[kRowCopies];
+                pad.key(a.q, in[0], p);
+                pad.key(a.k, in[1], p);
+                pad.value(a.v, in[2], p);
+                pad.value(a.d_out, in[3], p);
+                e = launch_copy_rows(in, 4, rows, stream);
+                a.dq = (T*)p;
+                a.dk_out = (T*)(p + pad.keys);
+                a.dv_out = (T*)(p + 2 * pad.keys);
+                a.ldk = pad.dk;
+                a.ldv = pad.dv;
+            }
+            if (e == cudaSuccess) e = launch_gdr_chunk_bwd(a, ws, stream);
+            if (copies && e == cudaSuccess) {
+                const RowCopy back[3] = {{a.dq, dq, pad.dk, dk}, {a.dk_out, dk_out, pad.dk, dk}, {a.dv_out, dv_out, pad.dv, dv}};
+                e = launch_copy_rows(back, 3, rows, stream);
+            }
+        }
     if (!chunks && e == cudaSuccess) e = launch_gdr_walk_bwd<T>(a, ws, stream);
     st = status_of(e);
     if (cudaFreeAsync(ws, stream) != cudaSuccess && st == VIG_OK) st = VIG_ERR_CUDA;

@@ -16,6 +16,7 @@ struct Gdr {
     float *state_out, *d_state_in;
     long long units;
     int L, dk, dv;
+    int ldk, ldv;   // values of a row of q, k, dq, dk and of v, d_out, out, dv in memory: dk and dv, or those to a multiple of eight (gdr_pad.cu)
     bool reverse;
     __host__ __device__ long long row(long long unit, int t) const { return unit * L + (reverse ? L - 1 - t : t); }
 };
@@ -52,8 +53,17 @@ size_t gdr_walk_bwd_scratch_bytes(long long units, int L, int dk, int dv);
 template <typename T>
 cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t stream);
 
-// ---- forward in chunks on the tensor cores: head sizes that are multiples of eight ----
-bool gdr_chunk_supported(int dk, int dv);
+// ---- rows of other sizes than multiples of eight: laid out again with zeros behind them for the forms that take pieces of sixteen bytes ----
+struct RowCopy {
+    const void* src;
+    void* dst;
+    int from, to;   // values of a row there and here
+};
+constexpr int kRowCopies = 4;
+// rows x n copies of bf16 rows; zeros behind the source's values.
+cudaError_t launch_copy_rows(const RowCopy* copies, int n, long long rows, cudaStream_t stream);
+
+// ---- forward in chunks on the tensor cores: ldk and ldv multiples of eight ----
 size_t gdr_chunk_scratch_bytes(long long units, int L, int dk, int dv);   // 0: the call uses no scratch
 cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, void* scratch, cudaStream_t stream);
 
@@ -61,16 +71,18 @@ cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, void* scratch, cud
 struct GdrKept {
     __half* w;         // [units][chunks][64][dvp]: W = w y; rows behind a call's last sixteen are not written
     __half* du;        // [units][chunks][64][dvp]: dU = du z 2^e, e of the key's row
-    __half *S, *A;     // transposed, [units][chunks + 1][dvp][DKP] before each chunk (= S y) and behind the last; [units][chunks][dvp][DKP]: what
+    __half *S, *A;     // transposed, [units][chunks + 1][dvp][DKP] before each chunk (= S y) and, where its gradient is given, behind the
+                       // last; [units][chunks][dvp][DKP]: what
                        // arrives behind each chunk (= A z)
     float *y, *z;      // [units][chunks + 1][dvp], [units][chunks][dvp]
     int* lost_grad;    // [units][chunks]: something left the range of fp16
     int dvp;
-    // Sixteen columns of a state, as packed for an A operand.
+    // Sixteen columns of a state, as packed for an A operand; not `there`: a state of zeros, of which only the scales are wanted (W and dU have them too).
     template <int DKP>
     __device__ __forceinline__ void keep_state(__half* to, float* scales, long long at, int col0, const uint32_t (*sa)[4], const float (&back)[2], int g,
-                                               int c) const {
+                                               int c, bool there) const {
         __half* const p = to + (at * dvp + col0 + g) * DKP + 2 * c;
+        if (there)
 #pragma unroll
         for (int s = 0; s < DKP / 16; ++s) {
             *reinterpret_cast<uint32_t*>(p + s * 16) = sa[s][0];

@@ -102,7 +102,7 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
         for (int p = 0; p < kPasses; ++p) {
             const int r = p * kRows + r0, t = r & (kChunk - 1);
             rows[p] = make_uint4(0u, 0u, 0u, 0u);
-            if (t0 + t < a.L && e8 < a.dk) rows[p] = *reinterpret_cast<const uint4*>((r < kChunk ? a.k : a.q) + a.row(unit, t0 + t) * a.dk + e8);
+            if (t0 + t < a.L && e8 < a.ldk) rows[p] = *reinterpret_cast<const uint4*>((r < kChunk ? a.k : a.q) + a.row(unit, t0 + t) * a.ldk + e8);
         }
         if (warp == 0)
 #pragma unroll
@@ -295,17 +295,17 @@ __device__ __noinline__ void walk_sixteen(const Gdr<bf>& a, long long unit, int 
 #pragma unroll 1
         for (int i = 0; 2 * i + half < a.dk; ++i) {
             S[i] *= alpha;
-            s = fmaf(__bfloat162float(a.k[r * a.dk + 2 * i + half]), S[i], s);
+            s = fmaf(__bfloat162float(a.k[r * a.ldk + 2 * i + half]), S[i], s);
         }
         s += __shfl_xor_sync(0xffffffffu, s, 16);
-        const float u = valid ? beta * (__bfloat162float(a.v[r * a.dv + j]) - s) : 0.f;
+        const float u = valid ? beta * (__bfloat162float(a.v[r * a.ldv + j]) - s) : 0.f;
 #pragma unroll 1
         for (int i = 0; 2 * i + half < a.dk; ++i) {
-            S[i] = fmaf(__bfloat162float(a.k[r * a.dk + 2 * i + half]), u, S[i]);
-            o = fmaf(__bfloat162float(a.q[r * a.dk + 2 * i + half]), S[i], o);
+            S[i] = fmaf(__bfloat162float(a.k[r * a.ldk + 2 * i + half]), u, S[i]);
+            o = fmaf(__bfloat162float(a.q[r * a.ldk + 2 * i + half]), S[i], o);
         }
         o += __shfl_xor_sync(0xffffffffu, o, 16);
-        if (valid && half == 0) a.out[r * a.dv + j] = __float2bfloat16_rn(o);
+        if (valid && half == 0) a.out[r * a.ldv + j] = __float2bfloat16_rn(o);
     }
     if (a.state_out && valid)
 #pragma unroll 1
@@ -479,7 +479,7 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
         pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);   // (what does not fit shows in U)
         if constexpr (EXACT) pack_a_rest(S.x[2 * s], S.x[2 * s + 1], sa[s], sl[s]);
     }
-    if constexpr (KEEP) kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + n, col0, sa, back, g, c);
+    if constexpr (KEEP) kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + n, col0, sa, back, g, c, n > 0 || a.state_in);
     S.decay(gates[kEb * kChunk + kChunk - 1]);
     // products with S, of all strips; then strip by strip, what a strip's U means to the strips behind it as soon as it is there: the next
     // strip's chain (N, the step, the inverse) is what bounds a chunk, all else fills its gaps
@@ -565,7 +565,7 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
         const int t = i * 16 + (lane >> 1), e = (lane & 1) * 8;
         const uint4 piece = *reinterpret_cast<const uint4*>(smem + cols + t * kColPitch + e * 2);
         if constexpr (OUT) {
-            if (n * kChunk + t < a.L && col0 + e < a.dv) *reinterpret_cast<uint4*>(a.out + a.row(unit, n * kChunk + t) * a.dv + col0 + e) = piece;
+            if (n * kChunk + t < a.L && col0 + e < a.ldv) *reinterpret_cast<uint4*>(a.out + a.row(unit, n * kChunk + t) * a.ldv + col0 + e) = piece;
         } else *reinterpret_cast<uint4*>(kept.w + ((unit * chunks + n) * kChunk + t) * kept.dvp + col0 + e) = piece;
     }
 }
@@ -602,7 +602,7 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
         pack_a(A.x[2 * s], A.x[2 * s + 1], aa[s]);   // (what does not fit shows in dU)
         if constexpr (EXACT) pack_a_rest(A.x[2 * s], A.x[2 * s + 1], aa[s], al[s]);
     }
-    if constexpr (WAY == Way::kBack) kept.keep_state<DKP>(kept.A, kept.z, unit * chunks + n, col0, aa, back, g, c);
+    if constexpr (WAY == Way::kBack) kept.keep_state<DKP>(kept.A, kept.z, unit * chunks + n, col0, aa, back, g, c, n + 1 < chunks || a.d_state_out);
     A.decay(gates[kEb * kChunk + kChunk - 1]);
     auto d_out = [&](int i, float (&x)[2][4]) {   // scaled
 #pragma unroll
@@ -682,7 +682,7 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
         const uint4* const piece = reinterpret_cast<const uint4*>(smem + cols + t * kColPitch + e * 2);
         stsm_trans(at, dv[0][0], dv[1][0], dv[0][1], dv[1][1]);
         __syncwarp();
-        if (n * kChunk + t < a.L && col0 + e < a.dv) *reinterpret_cast<uint4*>(a.dv_out + a.row(unit, n * kChunk + t) * a.dv + col0 + e) = *piece;
+        if (n * kChunk + t < a.L && col0 + e < a.ldv) *reinterpret_cast<uint4*>(a.dv_out + a.row(unit, n * kChunk + t) * a.ldv + col0 + e) = *piece;
         __syncwarp();
         stsm_trans(at, dh[0][0], dh[1][0], dh[0][1], dh[1][1]);
         __syncwarp();
@@ -727,8 +727,8 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = i * 16 + (lane >> 1);
-            const bool in = n * kChunk + t < a.L && col0 + e < a.dv && !vectors;
-            cp_async16(base + cols(buf) + t * kColPitch + e * 2, rows + (in ? a.row(unit, n * kChunk + t) * a.dv + col0 + e : 0), in);
+            const bool in = n * kChunk + t < a.L && col0 + e < a.ldv && !vectors;
+            cp_async16(base + cols(buf) + t * kColPitch + e * 2, rows + (in ? a.row(unit, n * kChunk + t) * a.ldv + col0 + e : 0), in);
         }
         cp_async_commit();
     };
@@ -779,13 +779,13 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
             else if (lost) *flag = 1;
         }
         if constexpr (WAY == Way::kKeep) {   // the last state, for the gates' gradient
-            if (ends) {
+            if (ends && a.d_state_out) {
                 float none[2] = {0.f, 0.f}, back[2];
                 uint32_t sa[DKP / 16][4];
                 S.template rescale<3>(none, back);
 #pragma unroll
                 for (int s = 0; s < DKP / 16; ++s) pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);
-                kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + chunks, col0, sa, back, g, c);
+                kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + chunks, col0, sa, back, g, c, true);
             }
         } else if (a.d_state_in && ends) S.store(a.d_state_in + unit * plane, a.dk, a.dv, col0 + g, c);
     } else {
@@ -906,6 +906,7 @@ cudaError_t launch_fold(const Gdr<bf>& a, const Segs& segs, bool back, cudaStrea
 // below, what the first launch adds is what the second saves.  (A block's time is its chunks' in a row, whether or not another shares its SM:
 // 32 units of 4096 tokens, 24 x 48, 8 segments 49 + 39 us for the two launches, 5 segments, with which the first fits the chip too, 40 + 57.)
 int segments(long long units, int L, int dk, int dv) {
+    if (dk % 8 || dv % 8) return 1;   // (the states' copies between segments are whole pieces of sixteen bytes)
     if (dk > 64) return 1;   // (one block an SM, and as many columns for the transition as for the state: 2 x 16 units of 4096 tokens, 128 x 128, gain nothing)
     const long long blocks = units * ((dv + 16 * kMostWarps - 1) / (16 * kMostWarps)), chunks = (L + kChunk - 1) / kChunk;
     const long long fit = 2LL * 148 / blocks, n = fit < chunks / 4 ? fit : chunks / 4;
@@ -966,7 +967,6 @@ Kept cut_kept(char* base, long long units, int L, int dk, int dv, size_t* total)
 
 }  // namespace
 
-bool gdr_chunk_supported(int dk, int dv) { return dk % 8 == 0 && dv % 8 == 0; }
 int gdr_padded_columns(int dv) {
     const int all = (dv + 15) / 16, slabs = (all + kMostWarps - 1) / kMostWarps;
     return (all + slabs - 1) / slabs * slabs * 16;

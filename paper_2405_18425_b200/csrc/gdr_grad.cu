@@ -68,7 +68,7 @@ __device__ __forceinline__ f32x2 row_pair(const float* gates, int row, int t) { 
 // copy for each strip, fetching instructions was what the warps waited for most, 173 us for 64 x 12 units of 196 tokens, 32 x 64.)
 template <int DKP>
 __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsigned char* smem, const GradLayout& lay, int dvp, long long unit, int n, float Y,
-                                           float Z, float HF, int s0, int step, int lane, Largest& seen) {
+                                           float Z, float HF, bool before, bool behind, int s0, int step, int lane, Largest& seen) {
     constexpr int KP = DKP * 2 + 16;
     const int g = lane >> 2, c = lane & 3, vp = lay.vp, strips = (min(kChunk, a.L - n * kChunk) + 15) >> 4;
     const Lane ln(lane);
@@ -178,21 +178,27 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
 #pragma unroll 1
     for (int s = s0; s < DKP / 16; s += step) {
         float hq[2][4] = {}, h1[2][4] = {}, h2[2][4] = {}, h3[2][4] = {};
+        if (before)
 #pragma unroll 2
-        for (int v = 0; v < dvp; v += 16) {
-            uint32_t da[4], ra[4], wa[4], y[4];
-            ldsm_a(b_of(dt, I * 16, v), da);
-            ldsm_a(b_of(rt, I * 16, v), ra);
-            ldsm_a(b_of(wt, I * 16, v), wa);
-            ldsm_trans(at_t<KP>(ln, st, v, s * 16), y);
-            mma(hq[0], da, y[0], y[1]);
-            mma(hq[1], da, y[2], y[3]);
-            mma(h1[0], ra, y[0], y[1]);
-            mma(h1[1], ra, y[2], y[3]);
-            ldsm_trans(at_t<KP>(ln, at, v, s * 16), y);
-            mma(h2[0], wa, y[0], y[1]);
-            mma(h2[1], wa, y[2], y[3]);
-        }
+            for (int v = 0; v < dvp; v += 16) {
+                uint32_t da[4], ra[4], y[4];
+                ldsm_a(b_of(dt, I * 16, v), da);
+                ldsm_a(b_of(rt, I * 16, v), ra);
+                ldsm_trans(at_t<KP>(ln, st, v, s * 16), y);
+                mma(hq[0], da, y[0], y[1]);
+                mma(hq[1], da, y[2], y[3]);
+                mma(h1[0], ra, y[0], y[1]);
+                mma(h1[1], ra, y[2], y[3]);
+            }
+        if (behind)
+#pragma unroll 2
+            for (int v = 0; v < dvp; v += 16) {
+                uint32_t wa[4], y[4];
+                ldsm_a(b_of(wt, I * 16, v), wa);
+                ldsm_trans(at_t<KP>(ln, at, v, s * 16), y);
+                mma(h2[0], wa, y[0], y[1]);
+                mma(h2[1], wa, y[2], y[3]);
+            }
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -223,7 +229,7 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
         for (int h = 0; h < 2; ++h) {
             const int t = t0 + 8 * h;
             const bool in = n * kChunk + t < a.L;
-            const long long r = in ? a.row(unit, n * kChunk + t) * a.dk : 0;
+            const long long r = in ? a.row(unit, n * kChunk + t) * a.ldk : 0;
             const float step1 = -beta[h] * ku[h] * Y, qu = gates[kQu * kChunk + t];
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
@@ -233,7 +239,7 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
                 const float q0 = qs[h] * hq[m][2 * h], q1 = qs[h] * hq[m][2 * h + 1], o0 = step1 * h1[m][2 * h] * Z, o1 = step1 * h1[m][2 * h + 1] * Z;
                 const float k0 = o0 + beta[h] * Y * (h2[m][2 * h] * Z + h3[m][2 * h] * HF), k1 = o1 + beta[h] * Y * (h2[m][2 * h + 1] * Z + h3[m][2 * h + 1] * HF);
                 sum[h] += qu * (qq.x * q0 + qq.y * q1) + ku[h] * (kk.x * o0 + kk.y * o1);
-                if (in && col < a.dk) {
+                if (in && col < a.ldk) {
                     *reinterpret_cast<uint32_t*>(a.dq + r + col) = pack_bf16(q0, q1);
                     *reinterpret_cast<uint32_t*>(a.dk_out + r + col) = pack_bf16(k0, k1);
                 }
@@ -272,10 +278,11 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
     // everything comes in by asynchronous copies at once, and is turned into operands where it lies; rows up to the last strip with tokens
     const uint32_t base = smem_u32(smem);
     const int rows = (nt + 15) & ~15;
+    const bool before = n > 0 || a.state_in, behind = n + 1 < chunks || a.d_state_out;   // (zeros otherwise, which nothing is read of)
     for (int i = tid; i < rows * (DKP / 8); i += kThreads) {
         const int t = i / (DKP / 8), e = i % (DKP / 8) * 8;
-        const bool in = t < nt && e < a.dk;
-        const long long at = in ? a.row(unit, t0 + t) * a.dk + e : 0;
+        const bool in = t < nt && e < a.ldk;
+        const long long at = in ? a.row(unit, t0 + t) * a.ldk + e : 0;
         cp_async16(base + lay.k + t * KP + e * 2, a.k + at, in);
         cp_async16(base + lay.q + t * KP + e * 2, a.q + at, in);
     }
@@ -287,17 +294,17 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
             const long long at = (here * kChunk + t) * dvp + piece;
             cp_async16(base + lay.w + to, kept.w + at, in);
             cp_async16(base + lay.r + to, kept.du + at, in);
-            cp_async16(base + lay.d + to, a.d_out + (in && piece < a.dv ? a.row(unit, t0 + t) * a.dv + piece : 0), in && piece < a.dv);
+            const bool values = in && piece < a.ldv;
+            cp_async16(base + lay.d + to, a.d_out + (values ? a.row(unit, t0 + t) * a.ldv + piece : 0), values);
         }
     for (int i = tid; i < dvp * (DKP / 8); i += kThreads) {
         const int j = i / (DKP / 8), e = i % (DKP / 8) * 8;
-        cp_async16(base + lay.s + j * KP + e * 2, kept.S + (states * dvp + j) * DKP + e, true);
-        cp_async16(base + lay.a + j * KP + e * 2, kept.A + (here * dvp + j) * DKP + e, true);
+        if (before) cp_async16(base + lay.s + j * KP + e * 2, kept.S + (states * dvp + j) * DKP + e, true);
+        if (behind) cp_async16(base + lay.a + j * KP + e * 2, kept.A + (here * dvp + j) * DKP + e, true);
     }
     cp_async_commit();
     // the state behind the chunk, for the gradient that the next chunk's first gate sees
     constexpr int kBehind = 128 * (DKP / 8) / kThreads;   // pieces of a thread, at most
-    const bool behind = n + 1 < chunks || a.d_state_out;
     uint4 next[kBehind];
 #pragma unroll
     for (int p = 0; p < kBehind; ++p) {
@@ -405,11 +412,11 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
 #pragma unroll
     for (int p = 0; p < kBehind; ++p) {
         const int i = tid + p * kThreads, j = i / (DKP / 8), e = i % (DKP / 8) * 8;
-        if (i < dvp * (DKP / 8)) {
+        if (behind && i < dvp * (DKP / 8)) {
             uint4* const at = reinterpret_cast<uint4*>(smem + lay.a + j * KP + e * 2);
             const uint4 x = *at;
             *at = scale_halves(x, cyz[j]);
-            if (behind) {
+            {
                 const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ss[4] = {next[p].x, next[p].y, next[p].z, next[p].w};
                 float dot = 0.f;
 #pragma unroll
@@ -441,7 +448,7 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
     __syncthreads();
     Largest seen;
     const int strip = warp & 3, half = warp >> 2, step = kThreads / 128;
-    if (strip * 16 < nt) grad_strip<DKP>(strip, a, smem, lay, dvp, unit, n, Y, Z, HF, half, step, lane, seen);
+    if (strip * 16 < nt) grad_strip<DKP>(strip, a, smem, lay, dvp, unit, n, Y, Z, HF, before, behind, half, step, lane, seen);
     const int lost = __syncthreads_or(seen.lost());
     if (tid == 0) kept.lost_grad[here] = lost;
     // dlog_alpha: sums from the chunk's end; a gate that leaves nothing, or has nothing to scale, has none, and the sums start anew there
@@ -467,7 +474,7 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
 
 }  // namespace
 
-bool gdr_grad_supported(int dk, int dv) { return gdr_chunk_supported(dk, dv) && dv <= 128; }
+bool gdr_grad_supported(int dk, int dv) { return dk <= 128 && dv <= 128; }
 
 cudaError_t launch_gdr_grad(const Gdr<__nv_bfloat16>& a, const GdrKept& kept, cudaStream_t stream) {
     const int chunks = (a.L + kChunk - 1) / kChunk;

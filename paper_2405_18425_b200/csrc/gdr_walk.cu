@@ -6,7 +6,7 @@
 // of four lanes (eight for vectors of more than 128), the shared vectors come through shared memory, 16 or 32 tokens at a time.  A step's chain bounds
 // it (two exchanges between lanes, two passes over the column): 48 units of 196 tokens, 32 x 64 fp32, 35 us, 340 cycles a token.
 // The gradient is four such walks and nothing else:
-//   columns forwards   w, and S at the end of every 64 tokens
+//   columns forwards   w, and S at the end of every 64 tokens (of the last ones where d_state_out meets it)
 //   columns backwards  A = what arrives at S_t from behind;  D = A + q do^T;  du = D^T k;  dv = beta du;  A <- alpha (D - beta k du^T);
 //                      and A at the end of every 64 tokens
 //   rows forwards      dq = S do,  dk'' = - beta S~ du     (S from w: u = beta w)
@@ -165,9 +165,9 @@ __device__ void walk_columns(const Gdr<T>& a, const Scratch& s, float* sm, long 
     auto stage = [&](int tile, int b) {
         float *kk = sm + b * bf, *qq = kk + kTile * DP, *sc = qq + kTile * DP, *al = sc + 2 * kTile * owners, *be = al + kTile;
         const int t0 = tile * kTile, n = min(kTile, a.L - t0);
-        stage_rows<T, kTile>(kk, n, a.dk, a.dk, DP, [&](int t) { return a.k + a.row(unit, t0 + t) * a.dk; });
-        stage_rows<T, kTile>(qq, n, a.dk, a.dk, DP, [&](int t) { return a.q + a.row(unit, t0 + t) * a.dk; });
-        stage_rows<T, kTile>(sc, n, mine, a.dv, owners, [&](int t) { return scalar + a.row(unit, t0 + t) * a.dv + j0; });
+        stage_rows<T, kTile>(kk, n, a.dk, a.ldk, DP, [&](int t) { return a.k + a.row(unit, t0 + t) * a.ldk; });
+        stage_rows<T, kTile>(qq, n, a.dk, a.ldk, DP, [&](int t) { return a.q + a.row(unit, t0 + t) * a.ldk; });
+        stage_rows<T, kTile>(sc, n, mine, a.ldv, owners, [&](int t) { return scalar + a.row(unit, t0 + t) * a.ldv + j0; });
         if (tid < n) {
             const long long r = a.row(unit, t0 + tid);
             stage_one(al + tid, a.la + r);
@@ -195,7 +195,7 @@ __device__ void walk_columns(const Gdr<T>& a, const Scratch& s, float* sm, long 
         const int tile = BACK ? tiles - 1 - n : n, t0 = tile * kTile, nt = min(kTile, a.L - t0), b = n & 1;
         if (n + 1 < tiles) stage(BACK ? tile - 1 : tile + 1, b ^ 1);
         const float *kk = sm + b * bf, *qq = kk + kTile * DP, *sc = qq + kTile * DP, *al = sc + 2 * kTile * owners, *be = al + kTile;
-        if (KEEP && BACK && ((t0 + nt) % kBorder == 0 || t0 + nt == a.L)) keep(s.A, (t0 + nt - 1) / kBorder);
+        if (KEEP && BACK && (t0 + nt) % kBorder == 0 && t0 + nt < a.L) keep(s.A, (t0 + nt - 1) / kBorder);   // (behind the last token: d_state_out)
         // (a token's vectors are read while the one before it is walked)
         Vec<R, G> k, q;
         const int at0 = BACK ? nt - 1 : 0;
@@ -232,18 +232,18 @@ __device__ void walk_columns(const Gdr<T>& a, const Scratch& s, float* sm, long 
             beta = beta1;
             y = y1;
         }
-        if (KEEP && !BACK && ((t0 + nt) % kBorder == 0 || t0 + nt == a.L)) keep(s.S, (t0 + nt - 1) / kBorder);
+        if (KEEP && !BACK && (t0 + nt == a.L ? a.d_state_out != nullptr : (t0 + nt) % kBorder == 0)) keep(s.S, (t0 + nt - 1) / kBorder);
         staged();   // the next tile
         __syncthreads();
         for (int i = tid; i < nt * owners; i += nth) {
             const int t = i >> lg, c = i & (owners - 1);
             if (c >= mine) continue;
-            const long long at = a.row(unit, t0 + t) * a.dv + j0 + c;
+            const long long r = a.row(unit, t0 + t), at = r * a.dv + j0 + c;
             if (BACK) {
                 s.du[at] = res[i];
-                a.dv_out[at] = from_f<T>(be[t] * res[i]);
+                a.dv_out[r * a.ldv + j0 + c] = from_f<T>(be[t] * res[i]);
             } else if (KEEP) s.w[at] = res[i];
-            else a.out[at] = from_f<T>(res[i]);
+            else a.out[r * a.ldv + j0 + c] = from_f<T>(res[i]);
         }
         __syncthreads();
     }
@@ -286,9 +286,9 @@ __device__ void walk_rows(const Gdr<T>& a, const Scratch& s, float* sm, long lon
         const int t0 = tile * kTile, n = min(kTile, a.L - t0);
         stage_rows<float, kTile>(uu, n, a.dv, a.dv, DP, [&](int t) { return s.w + a.row(unit, t0 + t) * a.dv; });
         stage_rows<float, kTile>(dd, n, a.dv, a.dv, DP, [&](int t) { return s.du + a.row(unit, t0 + t) * a.dv; });
-        stage_rows<T, kTile>(oo, n, a.dv, a.dv, DP, [&](int t) { return a.d_out + a.row(unit, t0 + t) * a.dv; });
-        stage_rows<T, kTile>(kk, n, mine, a.dk, owners, [&](int t) { return a.k + a.row(unit, t0 + t) * a.dk + i0; });
-        stage_rows<T, kTile>(qq, n, mine, a.dk, owners, [&](int t) { return a.q + a.row(unit, t0 + t) * a.dk + i0; });
+        stage_rows<T, kTile>(oo, n, a.dv, a.ldv, DP, [&](int t) { return a.d_out + a.row(unit, t0 + t) * a.ldv; });
+        stage_rows<T, kTile>(kk, n, mine, a.ldk, owners, [&](int t) { return a.k + a.row(unit, t0 + t) * a.ldk + i0; });
+        stage_rows<T, kTile>(qq, n, mine, a.ldk, owners, [&](int t) { return a.q + a.row(unit, t0 + t) * a.ldk + i0; });
         if (tid < n) {
             const long long r = a.row(unit, t0 + tid);
             stage_one(al + tid, a.la + r);
@@ -387,8 +387,11 @@ __device__ void finish(const Gdr<T>& a, const Scratch& s, long long unit, int bo
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const long long plane = (long long)a.dk * a.dv, at = (unit * borders(a.L) + border) * plane;
     float sum = 0.f;
+    const bool last = t0 + nt == a.L;
+    const float* const behind = last ? a.d_state_out ? a.d_state_out + unit * plane : nullptr : s.A + at;
+    if (behind)
 #pragma unroll 8
-    for (int i = tid; i < plane; i += threads) sum = fmaf(s.S[at + i], s.A[at + i], sum);
+        for (int i = tid; i < plane; i += threads) sum = fmaf(s.S[at + i], behind[i], sum);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) part[warp] = sum;
@@ -399,14 +402,14 @@ __device__ void finish(const Gdr<T>& a, const Scratch& s, long long unit, int bo
         float e = 0.f, db = 0.f;
         for (int i = lane; i < a.dk; i += 32) {
             const float dq = s.dq[r * a.dk + i];
-            e = fmaf(to_f(a.q[r * a.dk + i]), dq, e);
-            if constexpr (sizeof(T) == 2) a.dq[r * a.dk + i] = from_f<T>(dq);
-            a.dk_out[r * a.dk + i] = from_f<T>(s.dk1[r * a.dk + i] + s.dk2[r * a.dk + i]);
+            e = fmaf(to_f(a.q[r * a.ldk + i]), dq, e);
+            if constexpr (sizeof(T) == 2) a.dq[r * a.ldk + i] = from_f<T>(dq);
+            a.dk_out[r * a.ldk + i] = from_f<T>(s.dk1[r * a.dk + i] + s.dk2[r * a.dk + i]);
         }
         for (int i = lane; i < a.dv; i += 32) {
             const float du = s.du[r * a.dv + i];
             db = fmaf(du, s.w[r * a.dv + i], db);
-            e = fmaf(-beta * du, to_f(a.v[r * a.dv + i]), e);
+            e = fmaf(-beta * du, to_f(a.v[r * a.ldv + i]), e);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {

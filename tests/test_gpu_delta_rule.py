@@ -41,6 +41,23 @@ def test_gradient(size, dtype, states):
     check(list(zip(("dq", "dk", "dv", "dlog_alpha", "dbeta", "d_state"), got, ref)), _terms(*size[2:]), dtype == "bf16")
 
 
+@pytest.mark.parametrize("preference", [vig.VIG_TEST_KERNEL_SIMT, vig.VIG_TEST_KERNEL_WARP_TILES], ids=["walks", "tiles"])
+@pytest.mark.parametrize("size", [(2, 3, 1, 24, 48), (1, 2, 3, 17, 33), (2, 1, 5, 128, 128), (1, 2, 8, 64, 16), (1, 1, 12, 9, 100), (3, 1, 70, 40, 72), (1, 2, 131, 33, 65)], ids=str)
+@pytest.mark.parametrize("states", [False, True])
+def test_either_form_of_bf16(size, states, preference):
+    """Sizes of either side of the line between walks and tiles, by the form that the library would not choose as well."""
+    d = gdr_inputs(*size, "bf16", seed=21, gate_mean=1.0, states=states)
+    vig.vig_test_set_kernel_preference(preference)
+    try:
+        out, last = gdr_forward(d, reverse=states)
+        got = gdr_gradient(d, reverse=states)
+    finally:
+        vig.vig_test_set_kernel_preference(vig.VIG_TEST_KERNEL_AUTO)
+    ref, ref_last = gdr_oracle(d, reverse=states)
+    check([("out", out, ref), ("state", last, ref_last)], _terms(*size[2:]), True)
+    check(list(zip(("dq", "dk", "dv", "dlog_alpha", "dbeta", "d_state"), got, gdr_oracle_gradient(d, reverse=states))), _terms(*size[2:]), True)
+
+
 def test_gradient_against_differences():
     """Of the GPU's own fp32 forward call along random directions.  Central differences: third derivatives h^2 / 6 and rounding
     2^-24 sqrt(values) / h; h = 2^-6 and a loss of ~700 values leave 1e-4 of either."""
