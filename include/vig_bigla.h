@@ -253,8 +253,9 @@ int vig_gdr_fwd_f32(const void* q, const void* k, const void* v, const void* log
                     int B, int H, int L, int dk, int dv, int reverse, void* stream);
 /* Its gradient.  d_out: [B,H,L,dv]; d_state_out: gradient with respect to state_out (fp32) or NULL for zero.  Writes dq, dk_out
  * [B,H,L,dk], dv_out [B,H,L,dv], dlog_alpha, dbeta [B,H,L] and, unless it is NULL, d_state_in (fp32; may be d_state_out).  Everything is
- * computed anew from the inputs; scratch comes from the library's pool, stream-ordered.  Outputs must not overlap inputs or one
- * another.  Errors: as vig_gdr_fwd_*. */
+ * computed anew from the inputs; scratch comes from the library's pool, stream-ordered: about 4 dv + dk dv / 8 bytes a token and head in chunks,
+ * 8 dv + 12 dk + dk dv / 8 as walks, and up to 64 MB (or one unit's walks) for units that leave the chunks' range.  Outputs must not
+ * overlap inputs or one another.  Errors: as vig_gdr_fwd_*. */
 int vig_gdr_bwd_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
                      const void* state_in, const void* d_out, const void* d_state_out,
                      void* dq, void* dk_out, void* dv_out, void* dlog_alpha, void* dbeta, void* d_state_in,

@@ -3,7 +3,7 @@
 //   S~_t = alpha_t S_{t-1};  w_t = v_t - S~_t^T k_t;  u_t = beta_t w_t;  S_t = S~_t + k_t u_t^T;  out_t = S_t^T q_t
 //
 // The columns of S never meet: column j needs v_tj and the vectors k_t, q_t that all columns share.  A column is held in the registers
-// of four lanes (eight for vectors of more than 128), the shared vectors come through shared memory, 16 or 32 tokens at a time.  A step's chain bounds
+// of four lanes (eight for vectors of more than 64), the shared vectors come through shared memory, 16 or 32 tokens at a time.  A step's chain bounds
 // it (two exchanges between lanes, two passes over the column): 48 units of 196 tokens, 32 x 64 fp32, 35 us, 340 cycles a token.
 // The gradient is four such walks and nothing else:
 //   columns forwards   w, and S at the end of every 64 tokens (of the last ones where d_state_out meets it)
@@ -507,16 +507,16 @@ __global__ void __launch_bounds__(256) gdr_repair_fwd_kernel(Gdr<__nv_bfloat16> 
     }
 }
 
-// f(R, G) for vectors of d elements.  (Eight lanes a vector where SMs have few warps: 48 units of 196 tokens, 32 x 64 fp32, columns 35 and 51 -> 36 and
-// 55 us, rows 71 -> 64: a step's chain is what counts, and it has one more exchange.)
+// f(R, G) for vectors of d elements: four lanes, eight beyond 64 elements (48 units of 196 tokens, 128 x 128 fp32, a training step 560 -> 497 us; of 32 x 64
+// it would be 150 -> 162: a step's chain is what counts there, and it has one more exchange).
 template <typename F>
 cudaError_t with_vector(int d, F f) {
     if (d <= 16) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
     if (d <= 32) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
     if (d <= 48) return f(std::integral_constant<int, 12>(), std::integral_constant<int, 4>());
     if (d <= 64) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
-    if (d <= 96) return f(std::integral_constant<int, 24>(), std::integral_constant<int, 4>());
-    if (d <= 128) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 4>());
+    if (d <= 96) return f(std::integral_constant<int, 12>(), std::integral_constant<int, 8>());
+    if (d <= 128) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
     return f(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
 }
 
