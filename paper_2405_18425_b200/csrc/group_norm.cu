@@ -146,10 +146,10 @@ __device__ __forceinline__ float warp_sum(float x) {
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
-__device__ __forceinline__ float2 peer_f32x2(const float2* p, uint32_t rank) {   // this variable of another block of the cluster
-    float2 x;
-    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(cluster_peer(smem_u32(p), rank)) : "memory");
-    return x;
+// This variable of another block of the cluster.  Blocks write what they have into each other's memory ahead of the one barrier that they then meet at
+// (reading it from there behind the barrier, with another one before the end, was as fast: 40 us for 64 x 56 x 56 x 96).
+__device__ __forceinline__ void put_peer(float2* p, uint32_t rank, float2 x) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(cluster_peer(smem_u32(p), rank)), "f"(x.x), "f"(x.y) : "memory");
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_await() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
@@ -178,7 +178,7 @@ __device__ __forceinline__ void over_pairs(int c, int g, int per, F f) {   // g:
 // On chip, threads leave what they have per entry, [row lane][entry of the slab]: an entry is a vector where a vector lies in one group (per a
 // multiple of V), else a channel.  (Sums of an entry over its row lanes by several threads, then a warp per group: each a handful of steps.
 // A warp per group straight away took 3400 cycles of a block's 20000.)
-constexpr size_t on_chip_floats(int lanes, int slab, int groups) { return 2 * ((size_t)lanes * slab + 2 * groups + (slab > kThreads ? slab : kThreads)); }
+constexpr size_t on_chip_floats(int lanes, int slab, int groups) { return 2 * ((size_t)lanes * slab + (1 + kMostBlocks) * groups + (slab > kThreads ? slab : kThreads)); }
 
 // (n values, their mean m, their sum of squares about it q) of all lanes, joined.
 __device__ __forceinline__ void join_warp(float& n, float& m, float& q) {
@@ -234,12 +234,13 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_ke
     const int lanes = a.lanes, tid = threadIdx.x, rl = a.by_vectors.of(tid), vc = tid - rl * a.by_vectors.d, groups = a.groups;
     const int entries = a.entries, width = a.width;
     const bool vectors = entries < a.slab;
-    float2 *const red = reinterpret_cast<float2*>(smem), *const own = red + lanes * entries, *const all = own + groups, *const sums = all + groups;
+    float2 *const red = reinterpret_cast<float2*>(smem), *const own = red + lanes * entries, *const all = own + kMostBlocks * groups, *const sums = all + groups;   // own: of every block of the cluster
     const long long image = blockIdx.x / a.blocks;
     const int slab = blockIdx.x % a.blocks / N, rank = blockIdx.x % N;
     const int c0 = slab * a.slab, row0 = rank * a.rows, rows = max(0, min(a.rows, a.HW - row0));
     const bool live = rl < lanes;
     const long long base = (image * a.HW + row0) * a.C + c0 + vc * V;
+    if (N > 1) cluster_arrive();   // (the others may write here from then on)
     pdl_wait();
     pdl_launch_dependents();
     f32x2 w[V / 2], b[V / 2];
@@ -320,6 +321,7 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_ke
         sums[i] = make_float2(s1, s2);
     }
     __syncthreads();
+    if (N > 1) cluster_await();
     const float per_entry = (float)rows * values, of_entry = rows > 0 ? 1.f / per_entry : 0.f, of_group = 1.f / (float)width;
     for (int j = tid >> 5; j < groups; j += blockDim.x >> 5) {
         auto entry = [&](int c, float& m, float& q) {
@@ -354,7 +356,9 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_ke
             }
             q = warp_sum(q);
         }
-        if (lane == 0) own[j] = make_float2(m, q);
+        if (N > 1) {
+            if (lane < N) put_peer(own + rank * groups + j, lane, make_float2(m, q));
+        } else if (lane == 0) own[j] = make_float2(m, q);
     }
     if (N > 1) {
         cluster_arrive();
@@ -366,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_ke
             float2 peer[kMostBlocks];
 #pragma unroll
             for (int p = 0; p < kMostBlocks; ++p)
-                if (p < N) peer[p] = peer_f32x2(own + j, p);
+                if (p < N) peer[p] = own[p * groups + j];
             auto share = [&](int p) { return (float)max(0, min(a.rows, a.HW - p * a.rows)); };   // rows of block p
             m = q = 0.f;
 #pragma unroll
@@ -385,7 +389,6 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_ke
             if (a.rstd) a.rstd[at] = rstd;
         }
     }
-    if (N > 1) cluster_arrive();   // has read the others' shared memory, which they keep until all have
     __syncthreads();
     f32x2 m[V / 2];
     if (live)
@@ -403,7 +406,6 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_ke
             for (int e = 0; e < V / 2; ++e) f[e] = act2<ACT, sizeof(T) == 2>(ffma2(fsub2(f[e], m[e]), w[e], b[e]));
             *reinterpret_cast<uint4*>(a.out + base + (long long)(rl + i * lanes) * a.C) = narrow16(f, a.x);
         }
-    if (N > 1) cluster_await();
 }
 
 template <typename T, int ACT, int K>
@@ -411,12 +413,13 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
     constexpr int V = Wide<T>::N;
     extern __shared__ __align__(16) float smem[];
     const int lanes = a.lanes, tid = threadIdx.x, rl = a.by_vectors.of(tid), vc = tid - rl * a.by_vectors.d, groups = a.groups;
-    float2 *const red = reinterpret_cast<float2*>(smem), *const own = red + lanes * a.slab, *const all = own + groups;
+    float2 *const red = reinterpret_cast<float2*>(smem), *const own = red + lanes * a.slab, *const all = own + kMostBlocks * groups;   // own: of every block of the cluster
     const long long image = blockIdx.x / a.blocks;
     const int slab = blockIdx.x % a.blocks / N, rank = blockIdx.x % N;
     const int c0 = slab * a.slab, row0 = rank * a.rows, rows = min(a.rows, a.HW - row0);
     const bool live = rl < lanes;
     const long long base = (image * a.HW + row0) * a.C + c0 + vc * V;
+    if (N > 1) cluster_arrive();   // (the others may write here from then on)
     pdl_wait();
     pdl_launch_dependents();
     Channels<T> ch;
@@ -472,6 +475,7 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
         red[part * a.slab + c] = make_float2(u, v);   // (row lane `part` of this very channel: read by this thread alone)
     }
     __syncthreads();
+    if (N > 1) cluster_await();
     for (int j = tid >> 5; j < groups; j += blockDim.x >> 5) {
         float u = 0.f, v = 0.f;
         for (int c = j * a.per + (tid & 31); c < (j + 1) * a.per; c += 32) {
@@ -488,7 +492,9 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
         }
         u = warp_sum(u);
         v = warp_sum(v);
-        if ((tid & 31) == 0) own[j] = make_float2(u, v);
+        if (N > 1) {
+            if ((tid & 31) < N) put_peer(own + rank * groups + j, tid & 31, make_float2(u, v));
+        } else if ((tid & 31) == 0) own[j] = make_float2(u, v);
     }
     if (N > 1) {
         cluster_arrive();
@@ -498,21 +504,17 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
     for (int j = tid; j < groups; j += blockDim.x) {
         float2 sum = own[j];
         if (N > 1) {
-            float2 peer[kMostBlocks];
-#pragma unroll
-            for (int p = 0; p < kMostBlocks; ++p)
-                if (p < N) peer[p] = peer_f32x2(own + j, p);
             sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int p = 0; p < kMostBlocks; ++p)
                 if (p < N) {
-                    sum.x += peer[p].x;
-                    sum.y += peer[p].y;
+                    const float2 y = own[p * groups + j];
+                    sum.x += y.x;
+                    sum.y += y.y;
                 }
         }
         all[j] = make_float2(sum.x * inv, sum.y * inv);
     }
-    if (N > 1) cluster_arrive();
     __syncthreads();
     f32x2 m1[V / 2], m2[V / 2];
     if (live)
@@ -529,7 +531,6 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
             ch.dx(h, g, m1, m2);
             *reinterpret_cast<uint4*>(a.dx + base + (long long)(rl + i * lanes) * a.C) = narrow16(g, a.x);
         }
-    if (N > 1) cluster_await();
 }
 
 // ---- larger images: three launches.  Grid (chunks of rows x B, 1, slabs of at most 256 vectors) ------------------------------------
@@ -799,7 +800,8 @@ Plan plan_of(int B, int HW, int C, int groups, int V, bool gradient) {
         const int threads = kThreads / nv * nv, lanes = threads / nv;
         for (int N = 1; N <= kMostBlocks; N *= 2) {
             const int rows = (HW + N - 1) / N, K = (rows + lanes - 1) / lanes;
-            if (K > most) continue;
+            // (no more shared memory than a block has without asking: slabs of many groups)
+            if (K > most || on_chip_floats((threads + 31) / 32 * 32 / nv, slab, slab / per) * 4 > 48 * 1024) continue;
             p = {true, N, slab, units / m, rows, (threads + 31) / 32 * 32, K, 0};
             break;
         }
