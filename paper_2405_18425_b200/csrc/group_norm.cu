@@ -4,11 +4,11 @@
 //   g = d_out act'(z);  dbias_c = sum g;  dweight_c = sum g xhat;  dx = rstd (g w - mean(g w) - xhat mean(g w xhat))
 //
 // Memory bounds all of it, so an image's groups stay on chip between the statistics and their use wherever they fit: a cluster of up to
-// eight blocks holds all rows of a slab of whole groups in registers (16-byte vectors, a thread's vectors all of the same channels), sums
+// eight blocks holds all rows of a slab of whole groups in shared memory (16-byte vectors, a thread's vectors all of the same channels), sums
 // are exchanged through distributed shared memory, and every value crosses memory once in and once out.  Larger images go through
 // it twice, in launches of their own.  Variances are sums of squares about a mean that is known: a block's own first, moved to the
 // image's when blocks are joined, so that a mean far from zero costs no digits.  All sums run in a fixed order.
-// 64 x 56 x 56 x 96 bf16 with SiLU (77 MB): 40 us, 0.30 of the rate of a copy: a block's phases follow one another (load, sums, cluster, results: 7.6 us), two
+// 64 x 56 x 56 x 96 bf16 with SiLU (77 MB): 31 us, 0.38 of the rate of a copy: a block's phases follow one another (load, sums, cluster, results), two
 // blocks an SM.  64 x 14 x 14 x 768: 18 us, its gradient 30 us and 4 for the parameters.
 #include <type_traits>
 
@@ -138,6 +138,7 @@ struct Norm {
     int blocks;              // of an image (on chip: slabs x blocks of a cluster; else chunks of rows)
     // on chip: row lanes, groups of the slab, entries of the slab and of a group, threads of an entry; divisors
     int lanes, groups, entries, width, parts;
+    int held;                // floats of shared memory in front of the vectors
     Div by_vectors, by_entries, by_slab, by_per, by_lanes;
 };
 
@@ -226,9 +227,16 @@ struct Channels {
     }
 };
 
-// ---- on chip: grid (blocks of a cluster x slabs x B); K vectors of 16 bytes a thread --------------------------------------
-template <typename T, int ACT, int K>
-__global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_kernel(Norm<T> a, int N) {
+__device__ __forceinline__ void cp_async16(uint4* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_all() { asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory"); }
+
+// ---- on chip: grid (blocks of a cluster x slabs x B) --------------------------------------------------------------------------
+// A thread's vectors lie in shared memory, brought there by its own asynchronous copies and read by nobody else.  (In registers, 16 of them a thread: 40 us
+// where this takes 35 with 16 and 31 with 24.)
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kThreads, 4) norm_kernel(Norm<T> a, int N) {
     constexpr int V = Wide<T>::N;
     extern __shared__ __align__(16) float smem[];
     const int lanes = a.lanes, tid = threadIdx.x, rl = a.by_vectors.of(tid), vc = tid - rl * a.by_vectors.d, groups = a.groups;
@@ -243,40 +251,30 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_ke
     if (N > 1) cluster_arrive();   // (the others may write here from then on)
     pdl_wait();
     pdl_launch_dependents();
-    f32x2 w[V / 2], b[V / 2];
-    params(a.weight, live ? c0 + vc * V : 0, 1.f, w);
-    params(a.bias, live ? c0 + vc * V : 0, 0.f, b);
-    uint4 x[K];
-    x[0] = make_uint4(0u, 0u, 0u, 0u);
-    int n = 0;   // vectors of this thread
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-        const int r = rl + i * lanes;
-        if (live && r < rows) {
-            x[i] = *reinterpret_cast<const uint4*>(a.x + base + (long long)r * a.C);
-            n = i + 1;
-        }
-    }
+    uint4* const x = reinterpret_cast<uint4*>(smem + a.held) + tid;   // every kThreads-th
+    const int full = a.by_lanes.of(rows), rest = rows - full * lanes;   // vectors of a row lane: full, or one more
+    const int n = live ? full + (rl < rest) : 0;
+    for (int i = 0; i < n; ++i) cp_async16(x + i * kThreads, a.x + base + (long long)(rl + i * lanes) * a.C);
     // this thread's mean and sum of squares about it per channel, in one pass about its own first value: as that value is one of them, the
     // sum about it is at most n + 1 times the sum about the mean, and so is what rounding costs
-    const int full = a.by_lanes.of(rows), rest = rows - full * lanes;   // vectors of a row lane: full, or one more
-    const int most = full + (rest > 0);   // the same for the whole block: vectors that no thread has are skipped
-    f32x2 first[V / 2], sum[V / 2], sq[V / 2];
-    widen16(x[0], first, a.x);
+    f32x2 w[V / 2], b[V / 2], first[V / 2], sum[V / 2], sq[V / 2];
+    params(a.weight, live ? c0 + vc * V : 0, 1.f, w);
+    params(a.bias, live ? c0 + vc * V : 0, 0.f, b);
+    cp_async_all();
+    widen16(n > 0 ? x[0] : make_uint4(0u, 0u, 0u, 0u), first, a.x);
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) sum[e] = sq[e] = both(0.f);
+#pragma unroll 2
+    for (int i = 1; i < n; ++i) {
+        f32x2 f[V / 2];
+        widen16(x[i * kThreads], f, a.x);
 #pragma unroll
-    for (int i = 1; i < K; ++i)
-        if (i < most && i < n) {
-            f32x2 f[V / 2];
-            widen16(x[i], f, a.x);
-#pragma unroll
-            for (int e = 0; e < V / 2; ++e) {
-                const f32x2 d = fsub2(f[e], first[e]);
-                sum[e] = fadd2(sum[e], d);
-                sq[e] = ffma2(d, d, sq[e]);
-            }
+        for (int e = 0; e < V / 2; ++e) {
+            const f32x2 d = fsub2(f[e], first[e]);
+            sum[e] = fadd2(sum[e], d);
+            sq[e] = ffma2(d, d, sq[e]);
         }
+    }
     if (live) {
         const float inv = n > 0 ? 1.f / (float)n : 0.f;
         float mean[V], m2[V];
@@ -397,61 +395,54 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 4 : K <= 8 ? 3 : 2) norm_ke
             m[e] = pack2(s0.x, s1.x);
             w[e] = fmul2(w[e], pack2(s0.y, s1.y));
         });
+#pragma unroll 2
+    for (int i = 0; i < n; ++i) {
+        f32x2 f[V / 2];
+        widen16(x[i * kThreads], f, a.x);
 #pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (i < most && i < n) {
-            f32x2 f[V / 2];
-            widen16(x[i], f, a.x);
-#pragma unroll
-            for (int e = 0; e < V / 2; ++e) f[e] = act2<ACT, sizeof(T) == 2>(ffma2(fsub2(f[e], m[e]), w[e], b[e]));
-            *reinterpret_cast<uint4*>(a.out + base + (long long)(rl + i * lanes) * a.C) = narrow16(f, a.x);
-        }
+        for (int e = 0; e < V / 2; ++e) f[e] = act2<ACT, sizeof(T) == 2>(ffma2(fsub2(f[e], m[e]), w[e], b[e]));
+        *reinterpret_cast<uint4*>(a.out + base + (long long)(rl + i * lanes) * a.C) = narrow16(f, a.x);
+    }
 }
 
-template <typename T, int ACT, int K>
-__global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_grad_kernel(Norm<T> a, int N) {
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kThreads, 3) norm_grad_kernel(Norm<T> a, int N, int K) {   // K: vectors of a thread, at most
     constexpr int V = Wide<T>::N;
     extern __shared__ __align__(16) float smem[];
     const int lanes = a.lanes, tid = threadIdx.x, rl = a.by_vectors.of(tid), vc = tid - rl * a.by_vectors.d, groups = a.groups;
     float2 *const red = reinterpret_cast<float2*>(smem), *const own = red + lanes * a.slab, *const all = own + kMostBlocks * groups;   // own: of every block of the cluster
     const long long image = blockIdx.x / a.blocks;
     const int slab = blockIdx.x % a.blocks / N, rank = blockIdx.x % N;
-    const int c0 = slab * a.slab, row0 = rank * a.rows, rows = min(a.rows, a.HW - row0);
+    const int c0 = slab * a.slab, row0 = rank * a.rows, rows = max(0, min(a.rows, a.HW - row0));
     const bool live = rl < lanes;
     const long long base = (image * a.HW + row0) * a.C + c0 + vc * V;
     if (N > 1) cluster_arrive();   // (the others may write here from then on)
     pdl_wait();
     pdl_launch_dependents();
+    uint4 *const x = reinterpret_cast<uint4*>(smem + a.held) + tid, *const d = x + K * kThreads;
+    const int full = a.by_lanes.of(rows), n = live ? full + (rl < rows - full * lanes) : 0;
+    for (int i = 0; i < n; ++i) {
+        const long long at = base + (long long)(rl + i * lanes) * a.C;
+        cp_async16(x + i * kThreads, a.x + at);
+        cp_async16(d + i * kThreads, a.d_out + at);
+    }
     Channels<T> ch;
     ch.load(a, image * (a.C / a.per) + c0 / a.per, c0, vc * V, live);
-    uint4 x[K], d[K];
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-        const int r = rl + i * lanes;
-        if (live && r < rows) {
-            x[i] = *reinterpret_cast<const uint4*>(a.x + base + (long long)r * a.C);
-            d[i] = *reinterpret_cast<const uint4*>(a.d_out + base + (long long)r * a.C);
-            n = i + 1;
-        }
-    }
-    const int most = a.by_lanes.of(rows + lanes - 1);   // the same for the whole block: vectors that no thread has are skipped
-    constexpr bool kKeepG = sizeof(T) == 4;   // g takes d_out's registers where it fits them: no second pass through the activation
+    cp_async_all();
+    constexpr bool kKeepG = sizeof(T) == 4;   // g takes d_out's place where it fits: no second pass through the activation
     f32x2 sg[V / 2], sx[V / 2];
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) sg[e] = sx[e] = both(0.f);
+    for (int i = 0; i < n; ++i) {
+        f32x2 h[V / 2], g[V / 2];
+        ch.template grad<ACT>(x[i * kThreads], d[i * kThreads], h, g);
 #pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (i < most && i < n) {
-            f32x2 h[V / 2], g[V / 2];
-            ch.template grad<ACT>(x[i], d[i], h, g);
-#pragma unroll
-            for (int e = 0; e < V / 2; ++e) {
-                sg[e] = fadd2(sg[e], g[e]);
-                sx[e] = ffma2(g[e], h[e], sx[e]);
-            }
-            if constexpr (kKeepG) d[i] = narrow16(g, a.x);
+        for (int e = 0; e < V / 2; ++e) {
+            sg[e] = fadd2(sg[e], g[e]);
+            sx[e] = ffma2(g[e], h[e], sx[e]);
         }
+        if constexpr (kKeepG) d[i * kThreads] = narrow16(g, a.x);
+    }
     if (live)
 #pragma unroll
         for (int e = 0; e < V / 2; ++e) {
@@ -523,14 +514,12 @@ __global__ void __launch_bounds__(kThreads, K <= 2 ? 4 : K <= 4 ? 3 : 2) norm_gr
             m1[e] = pack2(s0.x, s1.x);
             m2[e] = pack2(s0.y, s1.y);
         });
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (i < most && i < n) {
-            f32x2 h[V / 2], g[V / 2];
-            ch.template grad<kKeepG ? kActNone : ACT>(x[i], d[i], h, g);
-            ch.dx(h, g, m1, m2);
-            *reinterpret_cast<uint4*>(a.dx + base + (long long)(rl + i * lanes) * a.C) = narrow16(g, a.x);
-        }
+    for (int i = 0; i < n; ++i) {
+        f32x2 h[V / 2], g[V / 2];
+        ch.template grad<kKeepG ? kActNone : ACT>(x[i * kThreads], d[i * kThreads], h, g);
+        ch.dx(h, g, m1, m2);
+        *reinterpret_cast<uint4*>(a.dx + base + (long long)(rl + i * lanes) * a.C) = narrow16(g, a.x);
+    }
 }
 
 // ---- larger images: three launches.  Grid (chunks of rows x B, 1, slabs of at most 256 vectors) ------------------------------------
@@ -792,11 +781,13 @@ int gcd(int a, int b) { return b == 0 ? a : gcd(b, a % b); }
 
 Plan plan_of(int B, int HW, int C, int groups, int V, bool gradient) {
     Plan p = {};
-    const int per = C / groups, base = per / gcd(per, V) * V, units = C / base, most = gradient ? 8 : 16;
+    const int per = C / groups, base = per / gcd(per, V) * V, units = C / base, most = gradient ? 12 : 24;   // 96 KB of a block's shared memory, two blocks an SM (64 KB: 35 us where this takes 31, fp32 57 and 49)
     for (int m = 1; m <= units; ++m) {
         if (units % m) continue;
         const int slab = base * m, nv = slab / V;
         if (nv > kThreads) break;
+        // few images: not wider where that leaves SMs without a block (1 x 64 x 64 x 192: 6.7 us against 7.8)
+        if (p.on_chip && (long long)B * (units / m) * kMostBlocks < 148) break;
         const int threads = kThreads / nv * nv, lanes = threads / nv;
         for (int N = 1; N <= kMostBlocks; N *= 2) {
             const int rows = (HW + N - 1) / N, K = (rows + lanes - 1) / lanes;
@@ -848,6 +839,7 @@ void fill(Norm<T>& a, const Plan& p, int HW, int C, int groups, bool gradient) {
     a.by_entries = Div(a.entries);
     a.by_slab = Div(p.slab);
     a.by_lanes = Div(a.lanes);
+    a.held = (int)((on_chip_floats(a.lanes, p.slab, a.groups) + 3) / 4 * 4);
 }
 
 template <typename F>
@@ -856,17 +848,6 @@ cudaError_t with_act(int act, F f) {
     if (act == kActGelu) return f(std::integral_constant<int, kActGelu>());
     return f(std::integral_constant<int, kActNone>());
 }
-template <typename F>
-cudaError_t with_vectors(int K, F f) {
-    if (K <= 1) return f(std::integral_constant<int, 1>());
-    if (K <= 2) return f(std::integral_constant<int, 2>());
-    if (K <= 4) return f(std::integral_constant<int, 4>());
-    if (K <= 6) return f(std::integral_constant<int, 6>());
-    if (K <= 8) return f(std::integral_constant<int, 8>());
-    if (K <= 12) return f(std::integral_constant<int, 12>());
-    return f(std::integral_constant<int, 16>());
-}
-
 }  // namespace
 
 bool group_norm_supported(int B, int HW, int C, int groups, size_t elem) {
@@ -896,11 +877,12 @@ cudaError_t launch_group_norm(const T* x, const T* weight, const T* bias, T* out
     fill(a, p, HW, C, groups, false);
     if (p.on_chip)
         return with_act(act, [&](auto A) {
-            return with_vectors(p.K, [&](auto K) {
-                count_launch();
-                return launch_pdl_cluster(norm_kernel<T, decltype(A)::value, decltype(K)::value>, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads),
-                                          on_chip_floats(p.threads / (p.slab / V), p.slab, p.slab / a.per) * 4, p.N, stream, a, p.N);
-            });
+            const size_t smem = (size_t)a.held * 4 + (size_t)p.K * kThreads * 16;
+            auto kernel = norm_kernel<T, decltype(A)::value>;
+            cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return e;
+            count_launch();
+            return launch_pdl_cluster(kernel, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads), smem, p.N, stream, a, p.N);
         });
     a.part = (float2*)scratch;
     float* stats = (float*)((char*)scratch + up((size_t)B * p.chunks * C * sizeof(float2)));
@@ -928,16 +910,12 @@ cudaError_t launch_group_norm_bwd(const T* x, const T* weight, const T* bias, co
     cudaError_t e;
     if (p.on_chip)
         e = with_act(act, [&](auto A) {
-            return with_vectors(p.K, [&](auto K) -> cudaError_t {
-                constexpr int k = decltype(K)::value;
-                if constexpr (k > 8) return cudaErrorInvalidValue;   // (plans of the gradient stop at eight)
-                else {
-                    const int lanes = p.threads / (p.slab / V);
-                    count_launch();
-                    return launch_pdl_cluster(norm_grad_kernel<T, decltype(A)::value, k>, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads),
-                                              on_chip_floats(lanes, p.slab, p.slab / a.per) * 4, p.N, stream, a, p.N);
-                }
-            });
+            const size_t smem = (size_t)a.held * 4 + (size_t)2 * p.K * kThreads * 16;
+            auto kernel = norm_grad_kernel<T, decltype(A)::value>;
+            cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (r != cudaSuccess) return r;
+            count_launch();
+            return launch_pdl_cluster(kernel, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads), smem, p.N, stream, a, p.N, p.K);
         });
     else {
         float2* means = (float2*)((char*)scratch + up((size_t)B * p.chunks * C * sizeof(float2)));

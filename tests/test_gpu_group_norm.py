@@ -13,7 +13,8 @@ pytestmark = pytest.mark.gpu
 # last, images that stay on chip and images that do not
 SIZES = [(1, 1, 1, 32, 2), (3, 7, 5, 96, 32), (2, 14, 14, 768, 32), (1, 64, 64, 192, 8), (2, 9, 11, 40, 8), (2, 56, 56, 96, 32), (1, 3, 3, 64, 64),
          (2, 13, 17, 256, 1), (1, 112, 112, 64, 16), (1, 160, 200, 48, 3), (2, 31, 33, 2304, 1), (300, 4, 4, 16, 2), (1, 1, 200, 8, 1), (1, 230, 230, 8, 2),
-         (2, 3, 5, 2008, 2008), (1, 5, 5, 2008, 8), (2, 20, 20, 1048, 131), (1, 9, 9, 4096, 4096), (1, 6, 6, 2056, 8)]
+         (2, 3, 5, 2008, 2008), (1, 5, 5, 2008, 8), (2, 20, 20, 1048, 131), (1, 9, 9, 4096, 4096), (1, 6, 6, 2056, 8),
+         (1, 192, 256, 8, 2), (1, 1, 49153, 8, 2), (1, 96, 256, 8, 2), (1, 1, 24577, 8, 2)]
 
 
 def _inputs(B, Hh, Ww, C, dtype, seed, mean=0.3):
