@@ -2,9 +2,26 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "vig_internal.h"
 
 namespace vig {
+
+// Lets a kernel have up to `most` bytes of dynamic shared memory, the largest that any call of it takes: set once per device.  (The limit belongs to the
+// process: set to each call's own size, another thread's smaller one could come between it and the launch.)
+template <auto Kernel>
+cudaError_t allow_smem(size_t most) {
+    static std::atomic<bool> done[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (most <= 48 * 1024 || done[dev].load(std::memory_order_acquire)) return cudaSuccess;
+    if ((e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most)) != cudaSuccess) return e;
+    done[dev].store(true, std::memory_order_release);
+    return cudaSuccess;
+}
 
 // A call of the gated delta rule.  Row t of a unit in walking order is token t, or L - 1 - t in a reverse call.  Null pointers:
 // state_in, state_out, d_state_out, d_state_in where the caller has none; out in the gradient, d_out and the gradients forward.

@@ -25,6 +25,7 @@ using bf = __nv_bfloat16;
 
 constexpr int kMostWarps = 4;       // with columns
 constexpr int kMostColumns = 16;    // sixteens of dv
+constexpr int kMostSegmentKeys = 64;   // key dimensions of sequences in segments
 constexpr int kPrepWarps = 4;
 constexpr int kPrep = 32 * kPrepWarps;
 constexpr int kBlockPitch = 48, kBlock = 16 * kBlockPitch, kColPitch = 48;
@@ -881,11 +882,10 @@ cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, const Segs& segs, 
         auto go = [&](auto E) {
             constexpr bool ex = decltype(E)::value;
             const int smem = Layout<dkp, ex, WAY>::total(warps);
-            auto kernel = gdr_chunk_kernel<dkp, ex, WAY>;
-            cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+            cudaError_t e = allow_smem<gdr_chunk_kernel<dkp, ex, WAY>>(Layout<dkp, ex, WAY>::total(kMostWarps));
             if (e != cudaSuccess) return e;
             count_launch();
-            return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * warps + kPrep), smem, stream, a, kept, segs, slabs, warps, status);
+            return launch_pdl(gdr_chunk_kernel<dkp, ex, WAY>, dim3((unsigned)blocks), dim3(32 * warps + kPrep), smem, stream, a, kept, segs, slabs, warps, status);
         };
         if constexpr (WAY != Way::kKeep)
             if (exact) return go(std::true_type());
@@ -895,8 +895,9 @@ cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, const Segs& segs, 
 
 cudaError_t launch_fold(const Gdr<bf>& a, const Segs& segs, bool back, cudaStream_t stream) {
     const int slabs = (a.dv + 15) / 16;
-    const size_t smem = ((size_t)2 * (a.dk * (a.dk + 4) + a.dk * 16) + a.dk * 16) * 4;
-    cudaError_t e = cudaFuncSetAttribute(gdr_fold_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    auto bytes = [](int dk) { return ((size_t)2 * (dk * (dk + 4) + dk * 16) + dk * 16) * 4; };
+    const size_t smem = bytes(a.dk);
+    cudaError_t e = allow_smem<gdr_fold_kernel>(bytes(kMostSegmentKeys));
     if (e != cudaSuccess) return e;
     count_launch();
     return launch_pdl(gdr_fold_kernel, dim3((unsigned)(a.units * slabs)), dim3(256), smem, stream, a, segs, slabs, back);
@@ -907,7 +908,7 @@ cudaError_t launch_fold(const Gdr<bf>& a, const Segs& segs, bool back, cudaStrea
 // 32 units of 4096 tokens, 24 x 48, 8 segments 49 + 39 us for the two launches, 5 segments, with which the first fits the chip too, 40 + 57.)
 int segments(long long units, int L, int dk, int dv) {
     if (dk % 8 || dv % 8) return 1;   // (the states' copies between segments are whole pieces of sixteen bytes)
-    if (dk > 64) return 1;   // (one block an SM, and as many columns for the transition as for the state: 2 x 16 units of 4096 tokens, 128 x 128, gain nothing)
+    if (dk > kMostSegmentKeys) return 1;   // (one block an SM, and as many columns for the transition as for the state: 2 x 16 units of 4096 tokens, 128 x 128, gain nothing)
     const long long blocks = units * ((dv + 16 * kMostWarps - 1) / (16 * kMostWarps)), chunks = (L + kChunk - 1) / kChunk;
     const long long fit = 2LL * 148 / blocks, n = fit < chunks / 4 ? fit : chunks / 4;
     return n < 3 ? 1 : (int)(n < 32 ? n : 32);

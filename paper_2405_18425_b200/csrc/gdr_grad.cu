@@ -21,6 +21,7 @@ namespace {
 using namespace gdr;
 using bf = __nv_bfloat16;
 
+constexpr int kMostColumns = 128;
 template <int DKP>
 constexpr int grad_threads() { return DKP > 64 ? 256 : 128; }   // two warps a strip where the key dimensions are many
 
@@ -474,18 +475,17 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
 
 }  // namespace
 
-bool gdr_grad_supported(int dk, int dv) { return dk <= 128 && dv <= 128; }
+bool gdr_grad_supported(int dk, int dv) { return dk <= 128 && dv <= kMostColumns; }
 
 cudaError_t launch_gdr_grad(const Gdr<__nv_bfloat16>& a, const GdrKept& kept, cudaStream_t stream) {
     const int chunks = (a.L + kChunk - 1) / kChunk;
     auto launch = [&](auto D) {
         constexpr int dkp = decltype(D)::value;
         const int smem = GradLayout(dkp, kept.dvp).total;
-        auto kernel = gdr_grad_kernel<dkp>;
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        cudaError_t e = allow_smem<gdr_grad_kernel<dkp>>(GradLayout(dkp, kMostColumns).total);
         if (e != cudaSuccess) return e;
         count_launch();
-        return launch_pdl(kernel, dim3((unsigned)(a.units * chunks)), dim3(grad_threads<dkp>()), smem, stream, a, kept, chunks);
+        return launch_pdl(gdr_grad_kernel<dkp>, dim3((unsigned)(a.units * chunks)), dim3(grad_threads<dkp>()), smem, stream, a, kept, chunks);
     };
     if (a.dk <= 16) return launch(std::integral_constant<int, 16>());
     if (a.dk <= 32) return launch(std::integral_constant<int, 32>());

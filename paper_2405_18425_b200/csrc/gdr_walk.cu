@@ -529,11 +529,6 @@ int owners_of(int n, int G, long long walks) {
     return owners;
 }
 
-template <typename K>
-cudaError_t allow_smem(K kernel, size_t bytes) {
-    return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : cudaSuccess;
-}
-
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T>
@@ -568,11 +563,10 @@ cudaError_t launch_gdr_walk_fwd(const Gdr<T>& a, cudaStream_t stream) {
         constexpr int r = decltype(R)::value, g = decltype(G)::value;
         const int owners = owners_of(a.dv, g, a.units);
         const size_t smem = walk_smem<2, r * g>(owners);
-        auto kernel = gdr_columns_kernel<T, r, g>;
-        cudaError_t e = allow_smem(kernel, smem);
+        cudaError_t e = allow_smem<gdr_columns_kernel<T, r, g>>(walk_smem<2, r * g>(256 / g));
         if (e != cudaSuccess) return e;
         count_launch();
-        return launch_pdl(kernel, dim3((unsigned)a.units, (a.dv + owners - 1) / owners), dim3(owners * g), smem, stream, a, owners);
+        return launch_pdl(gdr_columns_kernel<T, r, g>, dim3((unsigned)a.units, (a.dv + owners - 1) / owners), dim3(owners * g), smem, stream, a, owners);
     });
 }
 
@@ -591,20 +585,18 @@ cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t str
         constexpr int r = decltype(R)::value, g = decltype(G)::value;
         const int owners = owners_of(a.dv, g, 2 * a.units);
         const size_t smem = walk_smem<2, r * g>(owners);
-        auto kernel = gdr_columns_grad_kernel<T, r, g>;
-        cudaError_t e = allow_smem(kernel, smem);
+        cudaError_t e = allow_smem<gdr_columns_grad_kernel<T, r, g>>(walk_smem<2, r * g>(256 / g));
         if (e != cudaSuccess) return e;
-        return launch_pdl(kernel, dim3((unsigned)a.units, (a.dv + owners - 1) / owners, 2), dim3(owners * g), smem, stream, a, s, owners);
+        return launch_pdl(gdr_columns_grad_kernel<T, r, g>, dim3((unsigned)a.units, (a.dv + owners - 1) / owners, 2), dim3(owners * g), smem, stream, a, s, owners);
     });
     if (e != cudaSuccess) return e;
     e = with_vector(a.dv, [&](auto R, auto G) {
         constexpr int r = decltype(R)::value, g = decltype(G)::value;
         const int owners = owners_of(a.dk, g, 2 * a.units);
         const size_t smem = walk_smem<3, r * g>(owners);
-        auto kernel = gdr_rows_grad_kernel<T, r, g>;
-        cudaError_t e = allow_smem(kernel, smem);
+        cudaError_t e = allow_smem<gdr_rows_grad_kernel<T, r, g>>(walk_smem<3, r * g>(256 / g));
         if (e != cudaSuccess) return e;
-        return launch_pdl(kernel, dim3((unsigned)a.units, (a.dk + owners - 1) / owners, 2), dim3(owners * g), smem, stream, a, s, owners);
+        return launch_pdl(gdr_rows_grad_kernel<T, r, g>, dim3((unsigned)a.units, (a.dk + owners - 1) / owners, 2), dim3(owners * g), smem, stream, a, s, owners);
     });
     if (e != cudaSuccess) return e;
     count_launch(3);
@@ -619,7 +611,7 @@ cudaError_t launch_gdr_repair(const Gdr<__nv_bfloat16>& a, const int* first, int
     const Scratch s = cut_scratch<__nv_bfloat16>((char*)scratch, &a, slots, a.L, a.dk, a.dv, &total);
     constexpr int DP = kRepairR * kRepairG;
     const size_t smem = walk_smem<3, DP>(kRepairOwners);
-    cudaError_t e = allow_smem(gdr_repair_kernel, smem);
+    cudaError_t e = allow_smem<gdr_repair_kernel>(smem);
     if (e != cudaSuccess) return e;
     count_launch();
     return launch_pdl(gdr_repair_kernel, dim3(slots), dim3(kRepairG * kRepairOwners), smem, stream, a, s, first, per, second, chunks, status);
@@ -629,7 +621,7 @@ cudaError_t launch_gdr_repair_fwd(const Gdr<__nv_bfloat16>& a, const int* flags,
     int* status = device_status_ptr();
     if (!status) return cudaErrorUnknown;
     const size_t smem = walk_smem<2, kRepairR * kRepairG>(kRepairOwners);
-    cudaError_t e = allow_smem(gdr_repair_fwd_kernel, smem);
+    cudaError_t e = allow_smem<gdr_repair_fwd_kernel>(smem);
     if (e != cudaSuccess) return e;
     count_launch();
     return launch_pdl(gdr_repair_fwd_kernel, dim3((unsigned)(a.units < 148 ? a.units : 148)), dim3(kRepairG * kRepairOwners), smem, stream, a, flags, per, status);

@@ -777,11 +777,14 @@ struct Plan {
     int chunks;                             // else
 };
 
+constexpr int kMostHeld = 48 * 1024, kMostVectors = 24;   // a block's shared memory: in front of the vectors; vectors of a thread, of all inputs together
+constexpr size_t kMostSmem = kMostHeld + (size_t)kMostVectors * kThreads * 16;
+
 int gcd(int a, int b) { return b == 0 ? a : gcd(b, a % b); }
 
 Plan plan_of(int B, int HW, int C, int groups, int V, bool gradient) {
     Plan p = {};
-    const int per = C / groups, base = per / gcd(per, V) * V, units = C / base, most = gradient ? 12 : 24;   // 96 KB of a block's shared memory, two blocks an SM (64 KB: 35 us where this takes 31, fp32 57 and 49)
+    const int per = C / groups, base = per / gcd(per, V) * V, units = C / base, most = gradient ? kMostVectors / 2 : kMostVectors;   // 96 KB of a block's shared memory, two blocks an SM (64 KB: 35 us where this takes 31, fp32 57 and 49)
     for (int m = 1; m <= units; ++m) {
         if (units % m) continue;
         const int slab = base * m, nv = slab / V;
@@ -792,7 +795,7 @@ Plan plan_of(int B, int HW, int C, int groups, int V, bool gradient) {
         for (int N = 1; N <= kMostBlocks; N *= 2) {
             const int rows = (HW + N - 1) / N, K = (rows + lanes - 1) / lanes;
             // (no more shared memory than a block has without asking: slabs of many groups)
-            if (K > most || on_chip_floats((threads + 31) / 32 * 32 / nv, slab, slab / per) * 4 > 48 * 1024) continue;
+            if (K > most || on_chip_floats((threads + 31) / 32 * 32 / nv, slab, slab / per) * 4 > kMostHeld) continue;
             p = {true, N, slab, units / m, rows, (threads + 31) / 32 * 32, K, 0};
             break;
         }
@@ -878,11 +881,10 @@ cudaError_t launch_group_norm(const T* x, const T* weight, const T* bias, T* out
     if (p.on_chip)
         return with_act(act, [&](auto A) {
             const size_t smem = (size_t)a.held * 4 + (size_t)p.K * kThreads * 16;
-            auto kernel = norm_kernel<T, decltype(A)::value>;
-            cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            cudaError_t e = allow_smem<norm_kernel<T, decltype(A)::value>>(kMostSmem);
             if (e != cudaSuccess) return e;
             count_launch();
-            return launch_pdl_cluster(kernel, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads), smem, p.N, stream, a, p.N);
+            return launch_pdl_cluster(norm_kernel<T, decltype(A)::value>, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads), smem, p.N, stream, a, p.N);
         });
     a.part = (float2*)scratch;
     float* stats = (float*)((char*)scratch + up((size_t)B * p.chunks * C * sizeof(float2)));
@@ -911,11 +913,10 @@ cudaError_t launch_group_norm_bwd(const T* x, const T* weight, const T* bias, co
     if (p.on_chip)
         e = with_act(act, [&](auto A) {
             const size_t smem = (size_t)a.held * 4 + (size_t)2 * p.K * kThreads * 16;
-            auto kernel = norm_grad_kernel<T, decltype(A)::value>;
-            cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            cudaError_t r = allow_smem<norm_grad_kernel<T, decltype(A)::value>>(kMostSmem);
             if (r != cudaSuccess) return r;
             count_launch();
-            return launch_pdl_cluster(kernel, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads), smem, p.N, stream, a, p.N, p.K);
+            return launch_pdl_cluster(norm_grad_kernel<T, decltype(A)::value>, dim3((unsigned)((long long)a.blocks * B)), dim3(p.threads), smem, p.N, stream, a, p.N, p.K);
         });
     else {
         float2* means = (float2*)((char*)scratch + up((size_t)B * p.chunks * C * sizeof(float2)));
