@@ -237,10 +237,10 @@ int vig_gate_prep_bwd_f32(const void* g_fwd, const void* g_bwd, const void* dlog
  * out must not overlap an input.  state_in: S_0, or NULL for zero.  state_out: receives S_L, or NULL; may be state_in.
  * reverse != 0: the same from the last token to the first (state_in comes behind token L, state_out is what stands at token 1), the
  * other direction of a bidirectional mixer over the patch sequence.
- * bf16: chunks of 64 tokens on the tensor cores (operands of eleven significant bits under powers of two, 22 where a final state is
- *       asked for; sums and states fp32); a handful of tokens, and the gradient of more than 128 value columns, as fp32 walks on the CUDA cores.
+ * bf16: chunks of 64 tokens on the tensor cores (what is computed enters products as sums of bf16 terms: sixteen significant bits, 24 where a final
+ *       state is asked for, with the range of fp32; sums and states fp32); a handful of tokens, and the gradient of more than 128 value columns, as fp32 walks on the CUDA cores.
  *       Sizes that are no multiples of eight are laid out again in scratch on the way in and out.  Columns of the state
- *       that leave the range of the chunks' operands, which needs beta_t |k_t|^2 > 2, are computed by fp32 walks inside the call.  Long
+ *       that grow 2^15-fold within a chunk, which needs beta_t |k_t|^2 > 2, or are not finite are computed by fp32 walks inside the call.  Long
  *       sequences of few units are cut into segments that run side by side, with scratch from the library's pool.
  * f32:  fp32 walks on the CUDA cores.  dk <= 128, dv <= 256 for either type.
  * L == 0 with a state_out copies state_in (or zeros) there; tensors without elements may be NULL.
@@ -253,8 +253,8 @@ int vig_gdr_fwd_f32(const void* q, const void* k, const void* v, const void* log
                     int B, int H, int L, int dk, int dv, int reverse, void* stream);
 /* Its gradient.  d_out: [B,H,L,dv]; d_state_out: gradient with respect to state_out (fp32) or NULL for zero.  Writes dq, dk_out
  * [B,H,L,dk], dv_out [B,H,L,dv], dlog_alpha, dbeta [B,H,L] and, unless it is NULL, d_state_in (fp32; may be d_state_out).  Everything is
- * computed anew from the inputs; scratch comes from the library's pool, stream-ordered: about 4 dv + dk dv / 8 bytes a token and head in chunks,
- * 8 dv + 12 dk + dk dv / 8 as walks, and up to 64 MB (or one unit's walks) for units that leave the chunks' range.  Outputs must not
+ * computed anew from the inputs; scratch comes from the library's pool, stream-ordered: about 8 dv + dk dv / 8 bytes a token and head in chunks
+ * (sizes to multiples of sixteen; 8 dk + 6 dv more where they are no multiples of eight, and the segments' states), 8 dv + 12 dk + dk dv / 8 as walks, and up to 64 MB (or one unit's walks) for units that the chunks leave to them.  Outputs must not
  * overlap inputs or one another.  Errors: as vig_gdr_fwd_*. */
 int vig_gdr_bwd_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
                      const void* state_in, const void* d_out, const void* d_state_out,

@@ -1,7 +1,5 @@
 // Internal declarations of the gated delta rule and of the group norm (not part of the C ABI).
 #pragma once
-#include <cuda_fp16.h>
-
 #include <atomic>
 
 #include "vig_internal.h"
@@ -84,32 +82,28 @@ cudaError_t launch_copy_rows(const RowCopy* copies, int n, long long rows, cudaS
 size_t gdr_chunk_scratch_bytes(long long units, int L, int dk, int dv);   // 0: the call uses no scratch
 cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, void* scratch, cudaStream_t stream);
 
-// What the two walks of the gradient keep, fp16 under powers of two per column; dvp: dv to sixteen, DKP: dk as the kernels pad it.
+// What the two walks of the gradient keep, two bf16 terms each (the second `.._term` values behind the first; sixteen significant bits, at two bytes a
+// term what fp32 would take, and ready to be an operand); dvp: dv to sixteen, DKP: dk as the kernels pad it.
 struct GdrKept {
-    __half* w;         // [units][chunks][64][dvp]: W = w y; rows behind a call's last sixteen are not written
-    __half* du;        // [units][chunks][64][dvp]: dU = du z 2^e, e of the key's row
-    __half *S, *A;     // transposed, [units][chunks + 1][dvp][DKP] before each chunk (= S y) and, where its gradient is given, behind the
-                       // last; [units][chunks][dvp][DKP]: what
-                       // arrives behind each chunk (= A z)
-    float *y, *z;      // [units][chunks + 1][dvp], [units][chunks][dvp]
-    int* lost_grad;    // [units][chunks]: something left the range of fp16
+    __nv_bfloat16* w;      // [2][units][chunks][64][dvp]: W; rows behind a call's last sixteen are not written
+    __nv_bfloat16* du;     // [2][units][chunks][64][dvp]: dU
+    __nv_bfloat16 *S, *A;  // transposed, [2][units][chunks + 1][dvp][DKP] before each chunk and, where its gradient is given, behind the
+                           // last; [2][units][chunks][dvp][DKP]: what arrives behind each chunk
+    long long row_term, S_term, A_term;
+    int* lost_grad;        // [units][chunks]: something is not finite
     int dvp;
-    // Sixteen columns of a state, as packed for an A operand; not `there`: a state of zeros, of which only the scales are wanted (W and dU have them too).
-    template <int DKP>
-    __device__ __forceinline__ void keep_state(__half* to, float* scales, long long at, int col0, const uint32_t (*sa)[4], const float (&back)[2], int g,
-                                               int c, bool there) const {
-        __half* const p = to + (at * dvp + col0 + g) * DKP + 2 * c;
-        if (there)
+    // Sixteen columns and sixteen key dimensions of a state, as packed for an A operand; not `there`: a state of zeros, which nothing is read of.
+    template <int DKP, int N>
+    __device__ __forceinline__ void keep_state(__nv_bfloat16* to, long long term, long long at, int col0, int s, const uint32_t (&sa)[N][4], int g, int c,
+                                               bool there) const {
+        if (!there) return;
 #pragma unroll
-        for (int s = 0; s < DKP / 16; ++s) {
-            *reinterpret_cast<uint32_t*>(p + s * 16) = sa[s][0];
-            *reinterpret_cast<uint32_t*>(p + 8 * DKP + s * 16) = sa[s][1];
-            *reinterpret_cast<uint32_t*>(p + s * 16 + 8) = sa[s][2];
-            *reinterpret_cast<uint32_t*>(p + 8 * DKP + s * 16 + 8) = sa[s][3];
-        }
-        if (c == 0) {
-            scales[at * dvp + col0 + g] = back[0];
-            scales[at * dvp + col0 + g + 8] = back[1];
+        for (int m = 0; m < 2; ++m) {
+            __nv_bfloat16* const p = to + m * term + (at * dvp + col0 + g) * DKP + s * 16 + 2 * c;
+            *reinterpret_cast<uint32_t*>(p) = sa[m][0];
+            *reinterpret_cast<uint32_t*>(p + 8 * DKP) = sa[m][1];
+            *reinterpret_cast<uint32_t*>(p + 8) = sa[m][2];
+            *reinterpret_cast<uint32_t*>(p + 8 * DKP + 8) = sa[m][3];
         }
     }
 };

@@ -7,11 +7,11 @@
 // one another a product with the inverse of 1 + beta N of their own 16 x 16 block, which one warp computes by substitution in fp32.
 // e^{b_t - b_s} is taken of the difference, never of its parts, so that no gate is out of range.
 //
-// A block runs through the chunks of a unit for up to 64 columns.  Four of its warps prepare: they bring the rows of K and Q, scale them and
-// make N, P and the inverses of the next chunk while the others, a warp for every sixteen columns (gdr_tile.cuh), work on this one.  Two
-// buffers, handed over by named barriers.  64 x 12 units of 196 tokens, 32 x 64 (58 MB): 48 us, 0.19 of the rate of a copy, bound by instruction issue
-// (8400 warp instructions a chunk, 430 of them products) and a chunk's chain with two blocks an SM.  (All warps doing both in turn: 70 us; 32 units of
-// 4096 tokens, 24 x 48, 448 us, 7 us a chunk; now 86 in segments, 2.4 us a chunk.)
+// A block runs through the chunks of a unit for up to 64 columns.  Four of its warps prepare: they bring the rows of K and Q and make N, P and the
+// inverses of the next chunk while the others, a warp for every sixteen columns (gdr_tile.cuh), work on this one.  Two buffers, handed over by
+// named barriers.  64 x 12 units of 196 tokens, 32 x 64 (58 MB): 55 us, 0.16 of the rate of a copy, bound by instruction issue and a chunk's chain with two
+// blocks an SM.  (One term of fp16 an operand under powers of two: 50 us, but see gdr_tile.cuh.  32 units of 4096 tokens, 24 x 48, without segments 448 us,
+// 7 us a chunk.)
 #include <type_traits>
 
 #include "gdr.h"
@@ -28,7 +28,6 @@ constexpr int kMostColumns = 16;    // sixteens of dv
 constexpr int kMostSegmentKeys = 64;   // key dimensions of sequences in segments
 constexpr int kPrepWarps = 4;
 constexpr int kPrep = 32 * kPrepWarps;
-constexpr int kBlockPitch = 48, kBlock = 16 * kBlockPitch, kColPitch = 48;
 // Token-by-token matrices are kept as their lower triangle of 16 x 16 blocks.
 __device__ __forceinline__ int block_of(int i, int j) { return (i * (i + 1) / 2 + j) * kBlock; }
 constexpr int kBarFull = 1, kBarEmpty = 3, kBarPrep = 5;   // named barriers: two of the first two
@@ -44,19 +43,24 @@ template <int DKP>
 constexpr int key_pitch() { return DKP * 2 + 16; }
 
 // Per token of a chunk, in shared memory: arrays of kChunk floats.
-//   b running sum of log2 alpha; eb 2^b; dl 2^{b_C - b}; gv beta 2^e and gn beta 2^{2e} with 2^e the scale of the key's row (ku); qu the query's
-enum { kB, kEb, kDl, kBeta, kGv, kGn, kKu, kQu, kGateRows };
+//   b running sum of log2 alpha; eb 2^b; dl 2^{b_C - b}; beta; and of the whole chunk the largest of K and of Q that each preparing warp met (at 0 and
+//   4), and of beta (at 8)
+enum { kB, kEb, kDl, kBeta, kMost, kGateRows };
 __device__ __forceinline__ f32x2 gate_pair(const float* gates, int row, int t) { return *reinterpret_cast<const f32x2*>(gates + row * kChunk + t); }
+
+// Terms of what is computed: states that leave the call in fp32 are made of three, bf16 results of two.
+template <bool EXACT>
+constexpr int terms() { return EXACT ? 3 : 2; }
 
 // Shared memory, in bytes.
 template <int DKP, bool EXACT, Way WAY>
 struct Layout {
-    static constexpr int kKeys = kChunk * key_pitch<DKP>(), kMat = 10 * kBlock, kInv = 4 * kBlock, kCols = kChunk * kColPitch;
+    static constexpr int kKeys = kChunk * key_pitch<DKP>(), kMat = 10 * kBlock, kInv = 4 * kBlock, kCols = kChunk * 32;
     static constexpr bool kQ = WAY == Way::kForward || is_back(WAY);   // queries, and P
-    // of a buffer: keys, queries, N, P, inverses, gates, and what their first rounding left
-    static constexpr int kQueries = kKeys, kN = kQueries + (kQ ? kKeys : 0), kP = kN + kMat, kInverse = kP + (kQ ? kMat : 0), kGates = kInverse + kInv,
-                         kNLo = kGates + kChunk * kGateRows * 4, kPLo = kNLo + (EXACT ? kMat : 0),
-                         kInvLo = kPLo + (EXACT && is_back(WAY) ? kMat : 0), kBuffer = kInvLo + (EXACT ? kInv : 0);
+    static constexpr int kTerms = terms<EXACT>(), kPTerms = is_back(WAY) ? kTerms : 2;   // (forwards P makes bf16 results only)
+    // of a buffer: keys, queries, the terms of N, P and the inverses, gates
+    static constexpr int kQueries = kKeys, kN = kQueries + (kQ ? kKeys : 0), kP = kN + kTerms * kMat, kInverse = kP + (kQ ? kPTerms * kMat : 0),
+                         kGates = kInverse + kTerms * kInv, kBuffer = kGates + kChunk * kGateRows * 4;
     static constexpr int x = 2 * kBuffer;                  // the diagonal blocks of beta N, transposed, rows of 20 floats
     static constexpr int cols = x + 4 * 16 * 20 * 4;       // a warp's columns of V or dO, two chunks
     static constexpr int k(int buf) { return buf * kBuffer; }
@@ -65,9 +69,6 @@ struct Layout {
     static constexpr int p(int buf) { return buf * kBuffer + kP; }
     static constexpr int inv(int buf) { return buf * kBuffer + kInverse; }
     static constexpr int gates(int buf) { return buf * kBuffer + kGates; }
-    static constexpr int n_lo(int buf) { return buf * kBuffer + kNLo; }
-    static constexpr int p_lo(int buf) { return buf * kBuffer + kPLo; }
-    static constexpr int inv_lo(int buf) { return buf * kBuffer + kInvLo; }
     static constexpr int total(int warps) { return cols + 2 * warps * kCols; }
 };
 
@@ -75,7 +76,7 @@ struct Layout {
 struct Segs {
     int n, per, sums;   // segments, chunks of one, segments that the first launch takes (the last one's transition serves backwards only)
     float *in, *sum, *trans;
-    int* lost;   // [units][slots]: something left the range of fp16; a slot for every segment and warp of columns
+    int* lost;   // [units][slots]: something grew beyond the loop's digits or is not finite; a slot for every segment and warp of columns
     int slots;
 };
 
@@ -87,8 +88,9 @@ __device__ __forceinline__ void bar_arrive(int id, int count) { asm volatile("ba
 // ---- the preparing warps ----------------------------------------------------------------------------------------------
 template <int DKP, bool EXACT, Way WAY>
 __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layout<DKP, EXACT, WAY>& lay, long long unit, int first, int count, int threads) {
-    constexpr int KP = key_pitch<DKP>(), KS = DKP / 16;
-    constexpr bool Q = Layout<DKP, EXACT, WAY>::kQ;
+    using Lay = Layout<DKP, EXACT, WAY>;
+    constexpr int KP = key_pitch<DKP>(), KS = DKP / 16, TERMS = Lay::kTerms, PT = Lay::kPTerms;
+    constexpr bool Q = Lay::kQ;
     constexpr int kLanes = DKP <= 16 ? 2 : DKP <= 32 ? 4 : DKP <= 64 ? 8 : 16;   // of a row
     constexpr int kRows = kPrep / kLanes, kPasses = (Q ? 2 : 1) * kChunk / kRows;
     const int tid = threadIdx.x - (blockDim.x - kPrep), lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -128,11 +130,12 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
             }
             s[0] = l[0];
             s[1] = l[0] + l[1];
-            float run = s[1];
+            float run = s[1], step = fmaxf(fabsf(be[0]), fabsf(be[1]));
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const float y = __shfl_up_sync(0xffffffffu, run, o);
                 if (lane >= o) run += y;
+                step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, o));
             }
             const float before = run - s[1], all = __shfl_sync(0xffffffffu, run, 31), b0 = before + s[0], b1 = before + s[1];
             auto two = [&](int row, float x, float y) { *reinterpret_cast<float2*>(gates + row * kChunk + 2 * lane) = make_float2(x, y); };
@@ -140,26 +143,24 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
             two(kEb, ex2(b0), ex2(b1));
             two(kDl, ex2(all - b0), ex2(all - b1));
             two(kBeta, be[0], be[1]);
+            if (lane == 0) gates[kMost * kChunk + 8] = step;
         }
-        // K and Q to fp16, each row over its largest element's power of two
+        // K and Q as they come, and the largest of each
+        uint32_t most[2] = {0u, 0u};
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
             const int r = p * kRows + r0, t = r & (kChunk - 1);
-            const uint4 x = rows[p];
-            uint32_t m = largest_bf16(x);
+            larger(most[p * kRows >= kChunk], rows[p]);
+            if (e8 < DKP) *reinterpret_cast<uint4*>(smem + (r < kChunk ? lay.k(buf) : lay.q(buf)) + t * KP + e8 * 2) = rows[p];
+        }
 #pragma unroll
-            for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-            float down, up;
-            power_of(m >> 7, down, up);
-            if (e8 < DKP) *reinterpret_cast<uint4*>(smem + (r < kChunk ? lay.k(buf) : lay.q(buf)) + t * KP + e8 * 2) = bf16_to_half(x, down);
-            if (e8 == 0) gates[(r < kChunk ? kKu : kQu) * kChunk + t] = up;
+        for (int m = 0; m < (Q ? 2 : 1); ++m) {
+            float x = largest_of(most[m]);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+            if (lane == 0) gates[kMost * kChunk + 4 * m + warp] = x;
         }
         named_bar(kBarPrep, kPrep);
-        if (tid < kChunk) {
-            const float gv = gates[kBeta * kChunk + tid] * gates[kKu * kChunk + tid];
-            gates[kGv * kChunk + tid] = gv;
-            gates[kGn * kChunk + tid] = gv * gates[kKu * kChunk + tid];
-        }
         if (it + 1 < count) bring(is_back(WAY) ? n - 1 : n + 1);
         // N and P by blocks of sixteen by sixteen: two of the diagonal's for each of the first two warps, with their inverses side by side; three
         // of the others for each of the other two
@@ -181,15 +182,15 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
                 mma(nn[1], ka, kb[2], kb[3]);
             }
         };
-        auto put = [&](int hi_at, int lo_at, bool lo, int at, f32x2 x) {
-            const uint32_t hi = pack_half(x);
-            *reinterpret_cast<uint32_t*>(smem + hi_at + at) = hi;
-            if (lo) {
-                float u, v;
-                unpack2(x, u, v);
-                *reinterpret_cast<uint32_t*>(smem + lo_at + at) = rest_half(u, v, hi);
-            }
+        auto put = [&](auto N, int matrix, int at, f32x2 x) {   // its terms, a matrix each
+            constexpr int kN = decltype(N)::value;
+            uint32_t t[kN];
+            split<kN>(x, t);
+#pragma unroll
+            for (int m = 0; m < kN; ++m) *reinterpret_cast<uint32_t*>(smem + matrix + m * Lay::kMat + at) = t[m];
         };
+        const std::integral_constant<int, TERMS> terms_n;
+        const std::integral_constant<int, PT> terms_p;
         if (warp < 2) {
             float* const xt = reinterpret_cast<float*>(smem + lay.x) + warp * 2 * 16 * 20;
 #pragma unroll 1
@@ -201,18 +202,18 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {   // rows g, g + 8
                     const int tt = g + 8 * h, t = i * 16 + tt;
-                    const float bt = gates[kB * kChunk + t], ku = gates[kKu * kChunk + t], gn = gates[kBeta * kChunk + t] * ku * ku;
+                    const float bt = gates[kB * kChunk + t], beta = gates[kBeta * kChunk + t];
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {   // columns 8m + 2c, + 1
-                        const int ss = 8 * m + 2 * c, at = block_of(i, i) + tt * kBlockPitch + ss * 2;
+                        const int ss = 8 * m + 2 * c, at = block_of(i, i) + in_block(tt, m) + 4 * c;
                         const float2 bs = *reinterpret_cast<const float2*>(gates + kB * kChunk + i * 16 + ss);
                         const float e0 = ss <= tt ? ex2(bt - bs.x) : 0.f, e1 = ss + 1 <= tt ? ex2(bt - bs.y) : 0.f;
                         // (selected, not multiplied: what is not finite stays out of earlier tokens)
-                        if constexpr (Q) put(lay.p(buf), lay.p_lo(buf), EXACT && is_back(WAY), at, pack2(ss <= tt ? pp[m][2 * h] * e0 : 0.f, ss + 1 <= tt ? pp[m][2 * h + 1] * e1 : 0.f));
+                        if constexpr (Q) put(terms_p, lay.p(buf), at, pack2(ss <= tt ? pp[m][2 * h] * e0 : 0.f, ss + 1 <= tt ? pp[m][2 * h + 1] * e1 : 0.f));
                         const float n0 = ss < tt ? nn[m][2 * h] * e0 : 0.f, n1 = ss + 1 < tt ? nn[m][2 * h + 1] * e1 : 0.f;
-                        if constexpr (WAY == Way::kKeep) put(lay.n(buf), 0, false, at, pack2(n0, n1));   // (W takes its own strip's off)
-                        xt[(d * 16 + ss) * 20 + tt] = n0 * gn;   // beta N, transposed: row s, column t
-                        xt[(d * 16 + ss + 1) * 20 + tt] = n1 * gn;
+                        if constexpr (WAY == Way::kKeep) put(terms_n, lay.n(buf), at, pack2(n0, n1));   // (W takes its own strip's off)
+                        xt[(d * 16 + ss) * 20 + tt] = n0 * beta;   // beta N, transposed: row s, column t
+                        xt[(d * 16 + ss + 1) * 20 + tt] = n1 * beta;
                     }
                 }
             }
@@ -236,11 +237,15 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
             }
             if (i < strips)
 #pragma unroll
-                for (int t = 0; t < 16; ++t) {
-                    const __half hi = __float2half_rn(x[t]);
-                    *reinterpret_cast<__half*>(smem + lay.inv(buf) + i * kBlock + t * kBlockPitch + cc * 2) = hi;
-                    if constexpr (EXACT)
-                        *reinterpret_cast<__half*>(smem + lay.inv_lo(buf) + i * kBlock + t * kBlockPitch + cc * 2) = __float2half_rn(x[t] - __half2float(hi));
+                for (int t = 0; t < 16; t += 2) {
+                    uint32_t y[TERMS];
+                    split<TERMS>(pack2(x[t], x[t + 1]), y);
+#pragma unroll
+                    for (int m = 0; m < TERMS; ++m) {
+                        unsigned char* const at = smem + lay.inv(buf) + m * Lay::kInv + i * kBlock + (cc & 7) * 2;
+                        *reinterpret_cast<unsigned short*>(at + in_block(t, cc >> 3)) = (unsigned short)y[m];
+                        *reinterpret_cast<unsigned short*>(at + in_block(t + 1, cc >> 3)) = (unsigned short)(y[m] >> 16);
+                    }
                 }
         } else {
 #pragma unroll 1
@@ -263,10 +268,10 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
                     const float et = ex2(gates[kB * kChunk + i * 16 + g + 8 * h] - ref);
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
-                        const int at = block_of(i, j) + (g + 8 * h) * kBlockPitch + (8 * m + 2 * c) * 2;
+                        const int at = block_of(i, j) + in_block(g + 8 * h, m) + 4 * c;
                         const f32x2 e = fmul2(ec[m], pack2(et, et));
-                        if constexpr (Q) put(lay.p(buf), lay.p_lo(buf), EXACT && is_back(WAY), at, fmul2(pair(pp[m], h), e));
-                        put(lay.n(buf), lay.n_lo(buf), EXACT, at, fmul2(pair(nn[m], h), e));
+                        if constexpr (Q) put(terms_p, lay.p(buf), at, fmul2(pair(pp[m], h), e));
+                        put(terms_n, lay.n(buf), at, fmul2(pair(nn[m], h), e));
                     }
                 }
             }
@@ -277,7 +282,7 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
 
 // ---- the warps with columns ---------------------------------------------------------------------------------------------
 
-// Columns of a warp step by step in fp32, two lanes a column: what leaves the range of the tiles.
+// Columns of a warp step by step in fp32, two lanes a column: what grows too far for the chunks or is not finite.
 template <int DKP>
 __device__ __noinline__ void walk_sixteen(const Gdr<bf>& a, long long unit, int j, int half) {
     const bool valid = j < a.dv;
@@ -313,12 +318,10 @@ __device__ __noinline__ void walk_sixteen(const Gdr<bf>& a, long long unit, int 
         for (int i = 0; 2 * i + half < a.dk; ++i) a.state_out[unit * plane + (long long)(2 * i + half) * a.dv + j] = S[i];
 }
 
-// The state of sixteen columns, transposed: tile n holds key dimensions 8n + 2c, + 1 of columns g (0, 1) and g + 8 (2, 3), times `scale`, a
-// power of two per column.
+// The state of sixteen columns, transposed: tile n holds key dimensions 8n + 2c, + 1 of columns g (0, 1) and g + 8 (2, 3).
 template <int DKP>
 struct State {
     float x[DKP / 8][4];
-    float scale[2] = {1.f, 1.f};
     // [dk][cols] fp32 at `from` (null: zero)
     __device__ __forceinline__ void load(const float* from, int dk, int cols, int col, int c) {
 #pragma unroll
@@ -341,33 +344,8 @@ struct State {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = n * 8 + 2 * c + (e & 1), j = col + (e >> 1) * 8;
-                if (i < dk && j < cols) to[(long long)i * cols + j] = x[n][e] / scale[e >> 1];
+                if (i < dk && j < cols) to[(long long)i * cols + j] = x[n][e];
             }
-    }
-    // New scales: the larger of the state and `outside` (per column) to [2^TOP / 2, 2^TOP).  back: what undoes them.
-    template <int TOP>
-    __device__ __forceinline__ void rescale(const float (&outside)[2], float (&back)[2]) {
-        float most[2] = {0.f, 0.f};
-#pragma unroll
-        for (int m = 0; m < DKP / 8; ++m) {
-            most[0] = fmaxf(most[0], fmaxf(fabsf(x[m][0]), fabsf(x[m][1])));
-            most[1] = fmaxf(most[1], fmaxf(fabsf(x[m][2]), fabsf(x[m][3])));
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float m = fmaxf(outside[h], most[h] / scale[h]);   // (a power of two: exact)
-#pragma unroll
-            for (int o = 1; o < 4; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            const uint32_t ex = min(max(__float_as_uint(m) >> 23, 10u), 244u);
-            const float now = __uint_as_float((253u + TOP - ex) << 23), change = fminf(now / scale[h], 0x1p126f);   // (more only where the state is nothing beside either)
-            back[h] = __uint_as_float((ex + 1u - TOP) << 23);
-            scale[h] = now;
-            if (__any_sync(0xffffffffu, change != 1.f)) {
-                const f32x2 cc = pack2(change, change);
-#pragma unroll
-                for (int n = 0; n < DKP / 8; ++n) set_pair(x[n], h, fmul2(pair(x[n], h), cc));
-            }
-        }
     }
     __device__ __forceinline__ void decay(float s) {
         const f32x2 ss = pack2(s, s);
@@ -379,26 +357,22 @@ struct State {
 };
 
 // acc of every strip += state operand x the strip's rows of a key tile.  Strips inside, so that a product never waits for the one before it.
-template <int DKP, int TERMS, int NS>
-__device__ __forceinline__ void state_times_rows(float (&acc)[NS][2][4], const uint32_t (&hi)[4], const uint32_t (&lo)[4], uint32_t tile, int s, const Lane& ln) {
+template <int DKP, int N, int NS, int M>
+__device__ __forceinline__ void state_times_rows(float (&acc)[NS][2][4], const uint32_t (&op)[M][4], uint32_t tile, int s, const Lane& ln) {
     uint32_t x[NS][4];
 #pragma unroll
     for (int i = 0; i < NS; ++i) ldsm(at_b<key_pitch<DKP>()>(ln, tile, i * 16, s * 16), x[i]);
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        mma(acc[i][0], hi, x[i][0], x[i][1]);
-        mma(acc[i][1], hi, x[i][2], x[i][3]);
-    }
-    if constexpr (TERMS == 2)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            mma(acc[i][0], lo, x[i][0], x[i][1]);
-            mma(acc[i][1], lo, x[i][2], x[i][3]);
+            mma(acc[i][0], op[n], x[i][0], x[i][1]);
+            mma(acc[i][1], op[n], x[i][2], x[i][3]);
         }
 }
 // S += (sixteen tokens' operand) x their rows of a key tile
-template <int DKP, int TERMS>
-__device__ __forceinline__ void rows_into_state(State<DKP>& S, const uint32_t (&hi)[4], const uint32_t (&lo)[4], uint32_t tile, int strip, const Lane& ln) {
+template <int DKP, int N>
+__device__ __forceinline__ void rows_into_state(State<DKP>& S, const uint32_t (&op)[N][4], uint32_t tile, int strip, const Lane& ln) {
     constexpr int KS = DKP / 16, AT = KS % 4 == 0 ? 4 : KS % 2 == 0 ? 2 : 1;   // sixteens of keys at a time
 #pragma unroll
     for (int s0 = 0; s0 < KS; s0 += AT) {
@@ -406,90 +380,85 @@ __device__ __forceinline__ void rows_into_state(State<DKP>& S, const uint32_t (&
 #pragma unroll
         for (int s = 0; s < AT; ++s) ldsm_trans(at_t<key_pitch<DKP>()>(ln, tile, strip * 16, (s0 + s) * 16), y[s]);
 #pragma unroll
-        for (int s = 0; s < AT; ++s) {
-            mma(S.x[2 * (s0 + s)], hi, y[s][0], y[s][1]);
-            mma(S.x[2 * (s0 + s) + 1], hi, y[s][2], y[s][3]);
-        }
-        if constexpr (TERMS == 2)
+        for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int s = 0; s < AT; ++s) {
-                mma(S.x[2 * (s0 + s)], lo, y[s][0], y[s][1]);
-                mma(S.x[2 * (s0 + s) + 1], lo, y[s][2], y[s][3]);
+                mma(S.x[2 * (s0 + s)], op[n], y[s][0], y[s][1]);
+                mma(S.x[2 * (s0 + s) + 1], op[n], y[s][2], y[s][3]);
             }
     }
 }
-// acc += operand x a 16 x 16 block of a token-by-token matrix, contracted over its columns, or with TRANS over its rows
-template <bool TRANS, int TERMS>
-__device__ __forceinline__ void times_block(float (&acc)[2][4], const uint32_t (&hi)[4], const uint32_t (&lo)[4], uint32_t block, uint32_t block_lo,
-                                            const Lane& ln) {
-    uint32_t x[4];
-    if constexpr (TRANS) ldsm_trans(at_t<kBlockPitch>(ln, block, 0, 0), x);
-    else ldsm(at_b<kBlockPitch>(ln, block, 0, 0), x);
-    mma(acc[0], hi, x[0], x[1]);
-    mma(acc[1], hi, x[2], x[3]);
-    if constexpr (TERMS == 2) {
-        mma(acc[0], lo, x[0], x[1]);
-        mma(acc[1], lo, x[2], x[3]);
-        uint32_t y[4];
-        if constexpr (TRANS) ldsm_trans(at_t<kBlockPitch>(ln, block_lo, 0, 0), y);
-        else ldsm(at_b<kBlockPitch>(ln, block_lo, 0, 0), y);
-        mma(acc[0], hi, y[0], y[1]);
-        mma(acc[1], hi, y[2], y[3]);
+// acc += operand (A terms) x a 16 x 16 block of a token-by-token matrix (B terms, `stride` apart), contracted over its columns, or with TRANS over
+// its rows.  Products of terms that are smaller than the last of either are left out.
+template <bool TRANS, int A, int B, int M>
+__device__ __forceinline__ void times_block(float (&acc)[2][4], const uint32_t (&op)[M][4], uint32_t block, int stride, const Lane& ln) {
+    constexpr int kMost = A > B ? A : B;
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        uint32_t x[4];
+        if constexpr (TRANS) ldsm_trans(block + b * stride + ln.t_block, x);
+        else ldsm(block + b * stride + ln.b_block, x);
+#pragma unroll
+        for (int n = 0; n < A; ++n)
+            if (n + b < kMost) {
+                mma(acc[0], op[n], x[0], x[1]);
+                mma(acc[1], op[n], x[2], x[3]);
+            }
     }
 }
-template <int TERMS>
-__device__ __forceinline__ void pack_terms(const float (&t)[2][4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
-    pack_a(t[0], t[1], hi);
-    if constexpr (TERMS == 2) pack_a_rest(t[0], t[1], hi, lo);
-}
-__device__ __forceinline__ float2 gate2(const float* gates, int row, int t) { return *reinterpret_cast<const float2*>(gates + row * kChunk + t); }
 
-// One chunk of NS strips forwards.
+// How far a column's U (backwards dU) may outgrow what goes into the chunk before it is walked step by step instead.  With beta |k|^2 <= 2 a token's
+// transition has norm at most one, which bounds a column's |u| by (129 + dk) beta (|v| + |k| |S|) and its |du| by dk |k| (|A| + 64 |q| |do|), with the chunk's
+// largest elements of each; beyond, the chunk's triangular systems cancel digits that the steps keep.
+constexpr float kGrowth = 32768.f;
+
+// One chunk of NS strips forwards.  False where a column of this lane grew too far or is not finite.
 template <int DKP, bool EXACT, Way WAY, int NS>
-__device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, const Gdr<bf>& a, const Kept& kept, unsigned char* smem,
+__device__ __forceinline__ bool forward_chunk(State<DKP>& S, const Gdr<bf>& a, const Kept& kept, unsigned char* smem,
                                               const Layout<DKP, EXACT, WAY>& lay, int buf, int cols, long long unit, int n, int chunks, int col0, int lane,
                                               const Lane& ln) {
-    constexpr int KS = DKP / 16, TERMS = EXACT ? 2 : 1;
+    using Lay = Layout<DKP, EXACT, WAY>;
+    constexpr int KS = DKP / 16, TERMS = Lay::kTerms;
     constexpr bool OUT = WAY == Way::kForward, KEEP = WAY == Way::kKeep;
     const int g = lane >> 2, c = lane & 3;
     const uint32_t base = smem_u32(smem), kt = base + lay.k(buf), qt = base + lay.q(buf), vt = base + cols;
     const float* const gates = reinterpret_cast<const float*>(smem + lay.gates(buf));
-    float gmax = fmaxf(fabsf(gates[kGv * kChunk + lane]), fabsf(gates[kGv * kChunk + lane + 32])), vmax[2] = {0.f, 0.f}, back[2];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, o));
-    if constexpr (KEEP) gmax = fmaxf(gmax, 1.f);   // W itself is kept too
-    uint32_t vm[2] = {0u, 0u}, vv[NS][4];   // V transposed: strip i, columns g (0, 2), g + 8 (1, 3) of tokens 2c, 2c + 1 (0, 1), + 8 (2, 3)
+    uint32_t vm[2] = {0u, 0u}, sm[2] = {0u, 0u}, vv[NS][4];   // V transposed: strip i, columns g (0, 2), g + 8 (1, 3) of tokens 2c, 2c + 1 (0, 1), + 8 (2, 3)
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         uint32_t x[4];
-        ldsm_trans(vt + (i * 16 + ln.t_row) * kColPitch + ln.t_col * 2, x);
+        ldsm_trans(vt + i * kBlock + ln.t_block, x);
         vv[i][0] = x[0]; vv[i][1] = x[2]; vv[i][2] = x[1]; vv[i][3] = x[3];
-        asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(vm[0]) : "r"(vv[i][0]));
-        asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(vm[1]) : "r"(vv[i][1]));
-        asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(vm[0]) : "r"(vv[i][2]));
-        asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(vm[1]) : "r"(vv[i][3]));
-    }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) vmax[h] = fmaxf(__uint_as_float((vm[h] & 0x7fffu) << 16), __uint_as_float(vm[h] & 0x7fff0000u));
-    vmax[0] *= gmax;
-    vmax[1] *= gmax;
-    S.template rescale<3>(vmax, back);
-    uint32_t sa[KS][4], sl[EXACT ? KS : 1][4];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);   // (what does not fit shows in U)
-        if constexpr (EXACT) pack_a_rest(S.x[2 * s], S.x[2 * s + 1], sa[s], sl[s]);
+        for (int e = 0; e < 4; ++e) larger(vm[e & 1], vv[i][e]);
     }
-    if constexpr (KEEP) kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + n, col0, sa, back, g, c, n > 0 || a.state_in);
-    S.decay(gates[kEb * kChunk + kChunk - 1]);
     // products with S, of all strips; then strip by strip, what a strip's U means to the strips behind it as soon as it is there: the next
     // strip's chain (N, the step, the inverse) is what bounds a chunk, all else fills its gaps
     float w[NS][2][4] = {}, o[NS][2][4] = {};
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-        state_times_rows<DKP, TERMS, NS>(w, sa[s], sl[EXACT ? s : 0], kt, s, ln);
-        if constexpr (OUT) state_times_rows<DKP, 1, NS>(o, sa[s], sa[s], qt, s, ln);
+        uint32_t sa[TERMS][4];
+        pack_a<TERMS>(S.x[2 * s], S.x[2 * s + 1], sa);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) larger(sm[e & 1], sa[0][e]);
+        if constexpr (KEEP) kept.keep_state<DKP>(kept.S, kept.S_term, unit * (chunks + 1) + n, col0, s, sa, g, c, n > 0 || a.state_in);
+        state_times_rows<DKP, TERMS, NS>(w, sa, kt, s, ln);
+        if constexpr (OUT) state_times_rows<DKP, 2, NS>(o, sa, qt, s, ln);
     }
+    S.decay(gates[kEb * kChunk + kChunk - 1]);
+    float limit[2];
+    {
+        const float4 k4 = *reinterpret_cast<const float4*>(gates + kMost * kChunk);
+        const float k = fmaxf(fmaxf(k4.x, k4.y), fmaxf(k4.z, k4.w)), step = gates[kMost * kChunk + 8] * kGrowth;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float x = fmaf(k, largest_of(sm[h]), largest_of(vm[h]));
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+            limit[h] = x * step;
+        }
+    }
+    uint32_t um[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < NS; ++i)
 #pragma unroll
@@ -506,116 +475,110 @@ __device__ __forceinline__ void forward_chunk(State<DKP>& S, Largest& seen, cons
         float r[2][4], uu[2][4] = {};
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const f32x2 ku = gate_pair(gates, kKu, i * 16 + 8 * m + 2 * c), gv = gate_pair(gates, kGv, i * 16 + 8 * m + 2 * c);
+            const f32x2 beta = gate_pair(gates, kBeta, i * 16 + 8 * m + 2 * c);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const f32x2 got = fmul2(pair(w[i][m], h), ku);
-                const f32x2 y = ffma2(got, pack2(-1.f, -1.f), fmul2(widen_bf16(vv[i][2 * m + h]), pack2(S.scale[h], S.scale[h])));
+                const f32x2 y = ffma2(pair(w[i][m], h), pack2(-1.f, -1.f), widen_bf16(vv[i][2 * m + h]));
                 if constexpr (KEEP) set_pair(w[i][m], h, y);
-                set_pair(r[m], h, fmul2(gv, y));
+                set_pair(r[m], h, fmul2(beta, y));
             }
         }
-        uint32_t ra[4], rl[4], u[4], ul[4];
-        pack_terms<TERMS>(r, ra, rl);
-        times_block<false, TERMS>(uu, ra, rl, base + lay.inv(buf) + i * kBlock, base + lay.inv_lo(buf) + i * kBlock, ln);
-        pack_terms<TERMS>(uu, u, ul);
-        seen.see(u);
+        uint32_t ra[TERMS][4], u[TERMS][4];
+        pack_a<TERMS>(r[0], r[1], ra);
+        times_block<false, TERMS, TERMS>(uu, ra, base + lay.inv(buf) + i * kBlock, Lay::kInv, ln);
+        pack_a<TERMS>(uu[0], uu[1], u);
 #pragma unroll
-        for (int j = i + 1; j < NS; ++j) times_block<false, TERMS>(w[j], u, ul, base + lay.n(buf) + block_of(j, i), base + lay.n_lo(buf) + block_of(j, i), ln);
+        for (int e = 0; e < 4; ++e) see(um[e & 1], u[0][e]);
+#pragma unroll
+        for (int j = i + 1; j < NS; ++j) times_block<false, TERMS, TERMS>(w[j], u, base + lay.n(buf) + block_of(j, i), Lay::kMat, ln);
         if constexpr (OUT)
 #pragma unroll
-            for (int j = i; j < NS; ++j) times_block<false, 1>(o[j], u, ul, base + lay.p(buf) + block_of(j, i), 0, ln);
+            for (int j = i; j < NS; ++j) times_block<false, 2, 2>(o[j], u, base + lay.p(buf) + block_of(j, i), Lay::kMat, ln);
         // S += (e^{b_C - b} U)^T K
-        uint32_t ud[4], udl[4];
+        uint32_t ud[TERMS][4];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             const f32x2 dl = gate_pair(gates, kDl, i * 16 + 8 * m + 2 * c);
 #pragma unroll
             for (int h = 0; h < 2; ++h) set_pair(uu[m], h, fmul2(pair(uu[m], h), dl));
         }
-        pack_terms<TERMS>(uu, ud, udl);
-        rows_into_state<DKP, TERMS>(S, ud, udl, kt, i, ln);
-        uint32_t res[2][2] = {};
-        if constexpr (OUT) {
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const f32x2 qu = gate_pair(gates, kQu, i * 16 + 8 * m + 2 * c);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x, y;
-                    unpack2(fmul2(fmul2(pair(o[i][m], h), qu), pack2(back[h], back[h])), x, y);
-                    res[m][h] = pack_bf16(x, y);
-                }
-            }
-        } else if constexpr (KEEP) {   // W of the strip: what its own block takes off
-            float own[2][4] = {};
-            times_block<false, 1>(own, u, ul, base + lay.n(buf) + block_of(i, i), 0, ln);
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const float2 ku = gate2(gates, kKu, i * 16 + 8 * m + 2 * c);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) res[m][h] = pack_half(fmaf(-ku.x, own[m][2 * h], w[i][m][2 * h]), fmaf(-ku.y, own[m][2 * h + 1], w[i][m][2 * h + 1]));
-            }
-            const uint32_t ws[4] = {res[0][0], res[0][1], res[1][0], res[1][1]};
-            seen.see(ws);
-        }
+        pack_a<TERMS>(uu[0], uu[1], ud);
+        rows_into_state<DKP, TERMS>(S, ud, kt, i, ln);
         if constexpr (!OUT && !KEEP) continue;
         // over the strip's values, and out from there in pieces of sixteen bytes
-        stsm_trans(vt + (i * 16 + ln.t_row) * kColPitch + ln.t_col * 2, res[0][0], res[1][0], res[0][1], res[1][1]);
-        __syncwarp();
-        const int t = i * 16 + (lane >> 1), e = (lane & 1) * 8;
-        const uint4 piece = *reinterpret_cast<const uint4*>(smem + cols + t * kColPitch + e * 2);
-        if constexpr (OUT) {
-            if (n * kChunk + t < a.L && col0 + e < a.ldv) *reinterpret_cast<uint4*>(a.out + a.row(unit, n * kChunk + t) * a.ldv + col0 + e) = piece;
-        } else *reinterpret_cast<uint4*>(kept.w + ((unit * chunks + n) * kChunk + t) * kept.dvp + col0 + e) = piece;
+        constexpr int kOut = OUT ? 1 : 2;
+        uint32_t res[2][2][kOut];
+        if constexpr (KEEP) {   // W of the strip: what its own block takes off
+            float own[2][4] = {};
+            times_block<false, 2, 2>(own, u, base + lay.n(buf) + block_of(i, i), Lay::kMat, ln);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) split<kOut>(ffma2(pair(own[m], h), pack2(-1.f, -1.f), pair(w[i][m], h)), res[m][h]);
+        } else {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) split<kOut>(pair(o[i][m], h), res[m][h]);
+        }
+        const int t = n * kChunk + i * 16 + (lane >> 1), e = (lane & 1) * 8;
+        const uint4* const piece = reinterpret_cast<const uint4*>(smem + cols + i * kBlock + in_block(lane >> 1, lane & 1));
+#pragma unroll
+        for (int m = 0; m < kOut; ++m) {
+            if (m > 0) __syncwarp();
+            stsm_trans(vt + i * kBlock + ln.t_block, res[0][0][m], res[1][0][m], res[0][1][m], res[1][1][m]);
+            __syncwarp();
+            if constexpr (OUT) {
+                if (t < a.L && col0 + e < a.ldv) *reinterpret_cast<uint4*>(a.out + a.row(unit, t) * a.ldv + col0 + e) = *piece;
+            } else *reinterpret_cast<uint4*>(kept.w + m * kept.row_term + (unit * chunks * kChunk + t) * kept.dvp + col0 + e) = *piece;
+        }
     }
+    return within(um[0], limit[0]) && within(um[1], limit[1]);
 }
 
 // One chunk of NS strips backwards: S is A, the columns are those of dO.
 template <int DKP, bool EXACT, Way WAY, int NS>
-__device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, const Gdr<bf>& a, const Kept& kept, unsigned char* smem,
+__device__ __forceinline__ bool backward_chunk(State<DKP>& A, const Gdr<bf>& a, const Kept& kept, unsigned char* smem,
                                                const Layout<DKP, EXACT, WAY>& lay, int buf, int cols, long long unit, int n, int chunks, int col0,
                                                int lane, const Lane& ln) {
-    constexpr int KS = DKP / 16, TERMS = EXACT ? 2 : 1;
+    using Lay = Layout<DKP, EXACT, WAY>;
+    constexpr int KS = DKP / 16, TERMS = Lay::kTerms;
     const int g = lane >> 2, c = lane & 3;
     const uint32_t base = smem_u32(smem), kt = base + lay.k(buf), qt = base + lay.q(buf), vt = base + cols;
     const float* const gates = reinterpret_cast<const float*>(smem + lay.gates(buf));
-    // dO, times the scale of its query's row: everything it meets is a product with that row
-    float most[2] = {0.f, 0.f}, back[2];
-    uint32_t dd[NS][4];
+    uint32_t dm[2] = {0u, 0u}, am[2] = {0u, 0u}, dd[NS][1][4];   // dO, an operand as it is
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         uint32_t x[4];
-        ldsm_trans(vt + (i * 16 + ln.t_row) * kColPitch + ln.t_col * 2, x);
-        dd[i][0] = x[0]; dd[i][1] = x[2]; dd[i][2] = x[1]; dd[i][3] = x[3];
+        ldsm_trans(vt + i * kBlock + ln.t_block, x);
+        dd[i][0][0] = x[0]; dd[i][0][1] = x[2]; dd[i][0][2] = x[1]; dd[i][0][3] = x[3];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const float2 qu = gate2(gates, kQu, i * 16 + 8 * m + 2 * c);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                most[h] = fmaxf(most[h], fmaxf(fabsf(__uint_as_float(dd[i][2 * m + h] << 16)) * qu.x, fabsf(__uint_as_float(dd[i][2 * m + h] & 0xffff0000u)) * qu.y));
-        }
+        for (int e = 0; e < 4; ++e) larger(dm[e & 1], dd[i][0][e]);
     }
-    A.template rescale<0>(most, back);
-    uint32_t aa[KS][4], al[EXACT ? KS : 1][4];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        pack_a(A.x[2 * s], A.x[2 * s + 1], aa[s]);   // (what does not fit shows in dU)
-        if constexpr (EXACT) pack_a_rest(A.x[2 * s], A.x[2 * s + 1], aa[s], al[s]);
-    }
-    if constexpr (WAY == Way::kBack) kept.keep_state<DKP>(kept.A, kept.z, unit * chunks + n, col0, aa, back, g, c, n + 1 < chunks || a.d_state_out);
-    A.decay(gates[kEb * kChunk + kChunk - 1]);
-    auto d_out = [&](int i, float (&x)[2][4]) {   // scaled
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const f32x2 qu = gate_pair(gates, kQu, i * 16 + 8 * m + 2 * c);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) set_pair(x[m], h, fmul2(fmul2(widen_bf16(dd[i][2 * m + h]), qu), pack2(A.scale[h], A.scale[h])));
-        }
-    };
     float r[NS][2][4] = {};
 #pragma unroll
-    for (int s = 0; s < KS; ++s) state_times_rows<DKP, TERMS, NS>(r, aa[s], al[EXACT ? s : 0], kt, s, ln);
+    for (int s = 0; s < KS; ++s) {
+        uint32_t aa[TERMS][4];
+        pack_a<TERMS>(A.x[2 * s], A.x[2 * s + 1], aa);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) larger(am[e & 1], aa[0][e]);
+        if constexpr (WAY == Way::kBack) kept.keep_state<DKP>(kept.A, kept.A_term, unit * chunks + n, col0, s, aa, g, c, n + 1 < chunks || a.d_state_out);
+        state_times_rows<DKP, TERMS, NS>(r, aa, kt, s, ln);
+    }
+    A.decay(gates[kEb * kChunk + kChunk - 1]);
+    float limit[2];
+    {
+        const float4 k4 = *reinterpret_cast<const float4*>(gates + kMost * kChunk), q4 = *reinterpret_cast<const float4*>(gates + kMost * kChunk + 4);
+        const float k = fmaxf(fmaxf(k4.x, k4.y), fmaxf(k4.z, k4.w)), q = fmaxf(fmaxf(q4.x, q4.y), fmaxf(q4.z, q4.w));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float x = fmaf(q, largest_of(dm[h]), largest_of(am[h]));
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+            limit[h] = x * k * kGrowth;
+        }
+    }
+    uint32_t um[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < NS; ++i)
 #pragma unroll
@@ -625,70 +588,67 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
             for (int h = 0; h < 2; ++h) set_pair(r[i][m], h, fmul2(pair(r[i][m], h), dl));
         }
 #pragma unroll
-    for (int j = NS - 1; j >= 0; --j) {
-        float x[2][4];
-        uint32_t db[4], dbl[4];
-        d_out(j, x);
-        pack_terms<TERMS>(x, db, dbl);
+    for (int j = NS - 1; j >= 0; --j)
 #pragma unroll
-        for (int i = j; i >= 0; --i) times_block<true, TERMS>(r[i], db, dbl, base + lay.p(buf) + block_of(j, i), base + lay.p_lo(buf) + block_of(j, i), ln);
-    }
+        for (int i = j; i >= 0; --i) times_block<true, 1, TERMS>(r[i], dd[j], base + lay.p(buf) + block_of(j, i), Lay::kMat, ln);
 #pragma unroll
     for (int i = NS - 1; i >= 0; --i) {
-        uint32_t pa[4], pl[4];
+        uint32_t pa[TERMS][4];
         float du[2][4] = {}, x[2][4];
-        pack_terms<TERMS>(r[i], pa, pl);
-        times_block<true, TERMS>(du, pa, pl, base + lay.inv(buf) + i * kBlock, base + lay.inv_lo(buf) + i * kBlock, ln);
-        uint32_t dv[2][2], dh[2][2];
+        pack_a<TERMS>(r[i][0], r[i][1], pa);
+        times_block<true, TERMS, TERMS>(du, pa, base + lay.inv(buf) + i * kBlock, Lay::kInv, ln);
+        uint32_t dv[2][2], dh[2][2][2];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const f32x2 gv = gate_pair(gates, kGv, i * 16 + 8 * m + 2 * c), gn = gate_pair(gates, kGn, i * 16 + 8 * m + 2 * c);
+            const f32x2 beta = gate_pair(gates, kBeta, i * 16 + 8 * m + 2 * c);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                const f32x2 y = fmul2(pair(du[m], h), beta);
                 float p, q;
-                unpack2(fmul2(fmul2(pair(du[m], h), gv), pack2(back[h], back[h])), p, q);
+                unpack2(y, p, q);
                 dv[m][h] = pack_bf16(p, q);
-                dh[m][h] = pack_half(du[m][2 * h], du[m][2 * h + 1]);
-                set_pair(x[m], h, fmul2(fmul2(pair(du[m], h), gn), pack2(-1.f, -1.f)));
+                split<2>(pair(du[m], h), dh[m][h]);
+                see(um[h], dh[m][h][0]);
+                set_pair(x[m], h, fmul2(y, pack2(-1.f, -1.f)));
             }
         }
-        const uint32_t ds[4] = {dh[0][0], dh[0][1], dh[1][0], dh[1][1]};
-        seen.see(ds);
-        uint32_t ra[4], rl[4];   // - 2^e R
-        pack_terms<TERMS>(x, ra, rl);
-        seen.see(ra);
+        uint32_t ra[TERMS][4];   // - R
+        pack_a<TERMS>(x[0], x[1], ra);
 #pragma unroll
-        for (int j = i - 1; j >= 0; --j) times_block<true, TERMS>(r[j], ra, rl, base + lay.n(buf) + block_of(i, j), base + lay.n_lo(buf) + block_of(i, j), ln);
+        for (int j = i - 1; j >= 0; --j) times_block<true, TERMS, TERMS>(r[j], ra, base + lay.n(buf) + block_of(i, j), Lay::kMat, ln);
         // A += (e^b dO)^T Q - (e^b R)^T K
-        uint32_t pe[4], pel[4];
+        uint32_t pe[TERMS][4];
         float y[2][4];
-        d_out(i, y);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             const f32x2 eb = gate_pair(gates, kEb, i * 16 + 8 * m + 2 * c);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 set_pair(x[m], h, fmul2(pair(x[m], h), eb));
-                set_pair(y[m], h, fmul2(pair(y[m], h), eb));
+                set_pair(y[m], h, fmul2(widen_bf16(dd[i][0][2 * m + h]), eb));
             }
         }
-        pack_terms<TERMS>(x, pe, pel);
-        rows_into_state<DKP, TERMS>(A, pe, pel, kt, i, ln);
-        pack_terms<TERMS>(y, pe, pel);
-        rows_into_state<DKP, TERMS>(A, pe, pel, qt, i, ln);
+        pack_a<TERMS>(x[0], x[1], pe);
+        rows_into_state<DKP, TERMS>(A, pe, kt, i, ln);
+        pack_a<TERMS>(y[0], y[1], pe);
+        rows_into_state<DKP, TERMS>(A, pe, qt, i, ln);
         if constexpr (WAY != Way::kBack) continue;
-        // out: dv, then 2^-e dU, through the strip's rows
-        const int t = i * 16 + (lane >> 1), e = (lane & 1) * 8;
-        const uint32_t at = vt + (i * 16 + ln.t_row) * kColPitch + ln.t_col * 2;
-        const uint4* const piece = reinterpret_cast<const uint4*>(smem + cols + t * kColPitch + e * 2);
+        // out: dv, then the terms of dU, through the strip's rows
+        const int t = n * kChunk + i * 16 + (lane >> 1), e = (lane & 1) * 8;
+        const uint32_t at = vt + i * kBlock + ln.t_block;
+        const uint4* const piece = reinterpret_cast<const uint4*>(smem + cols + i * kBlock + in_block(lane >> 1, lane & 1));
         stsm_trans(at, dv[0][0], dv[1][0], dv[0][1], dv[1][1]);
         __syncwarp();
-        if (n * kChunk + t < a.L && col0 + e < a.ldv) *reinterpret_cast<uint4*>(a.dv_out + a.row(unit, n * kChunk + t) * a.ldv + col0 + e) = *piece;
-        __syncwarp();
-        stsm_trans(at, dh[0][0], dh[1][0], dh[0][1], dh[1][1]);
-        __syncwarp();
-        *reinterpret_cast<uint4*>(kept.du + ((unit * chunks + n) * kChunk + t) * kept.dvp + col0 + e) = *piece;
+        if (t < a.L && col0 + e < a.ldv) *reinterpret_cast<uint4*>(a.dv_out + a.row(unit, t) * a.ldv + col0 + e) = *piece;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            __syncwarp();
+            stsm_trans(at, dh[0][0][m], dh[1][0][m], dh[0][1][m], dh[1][1][m]);
+            __syncwarp();
+            *reinterpret_cast<uint4*>(kept.du + m * kept.row_term + (unit * chunks * kChunk + t) * kept.dvp + col0 + e) = *piece;
+        }
     }
+    return within(um[0], limit[0]) && within(um[1], limit[1]);
 }
 
 // Whether two blocks share an SM: their shared memory must.  Each then has 128 registers a thread.  (Unequal shares, 80 to 104 for the preparing
@@ -696,8 +656,8 @@ __device__ __forceinline__ void backward_chunk(State<DKP>& A, Largest& seen, con
 template <int DKP, bool EXACT, Way WAY>
 constexpr bool two_blocks() { return 2 * (Layout<DKP, EXACT, WAY>::total(kMostWarps) + 1024) <= 228 * 1024; }
 
-// EXACT: states leave the call in fp32, so that what they are made of is taken with 22 bits (two fp16 an operand); otherwise only bf16
-// results do, and eleven bits keep the error below a quarter of their rounding.
+// EXACT: states leave the call in fp32, so that what they are made of is taken with 24 bits (three terms an operand); otherwise only bf16
+// results do, and sixteen bits keep a rounding of the loop's own below a hundredth of theirs.
 template <int DKP, bool EXACT, Way WAY>
 __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT, WAY>() ? 2 : 1) gdr_chunk_kernel(Gdr<bf> a, Kept kept, Segs segs, int slabs, int warps, int* status) {
     constexpr bool BACK = is_back(WAY), PROPER = WAY != Way::kSum && WAY != Way::kBackSum;
@@ -729,13 +689,13 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
         for (int i = 0; i < 4; ++i) {
             const int t = i * 16 + (lane >> 1);
             const bool in = n * kChunk + t < a.L && col0 + e < a.ldv && !vectors;
-            cp_async16(base + cols(buf) + t * kColPitch + e * 2, rows + (in ? a.row(unit, n * kChunk + t) * a.ldv + col0 + e : 0), in);
+            cp_async16(base + cols(buf) + i * kBlock + in_block(lane >> 1, lane & 1), rows + (in ? a.row(unit, n * kChunk + t) * a.ldv + col0 + e : 0), in);
         }
         cp_async_commit();
     };
     const long long plane = (long long)a.dk * a.dv, at = unit * segs.n + seg;
     State<DKP> S;
-    Largest seen;
+    bool lost = false;
     fetch(first, 0);
     if (vectors) S.unit_vectors(col0 + g, c);
     else {
@@ -752,8 +712,8 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
         named_bar(kBarFull + buf, threads);
         auto chunk = [&](auto NS) {
             constexpr int ns = decltype(NS)::value;
-            if constexpr (BACK) backward_chunk<DKP, EXACT, WAY, ns>(S, seen, a, kept, smem, lay, buf, cols(buf), unit, n, chunks, col0, lane, ln);
-            else forward_chunk<DKP, EXACT, WAY, ns>(S, seen, a, kept, smem, lay, buf, cols(buf), unit, n, chunks, col0, lane, ln);
+            if constexpr (BACK) lost |= !backward_chunk<DKP, EXACT, WAY, ns>(S, a, kept, smem, lay, buf, cols(buf), unit, n, chunks, col0, lane, ln);
+            else lost |= !forward_chunk<DKP, EXACT, WAY, ns>(S, a, kept, smem, lay, buf, cols(buf), unit, n, chunks, col0, lane, ln);
         };
         if (strips == 4) chunk(std::integral_constant<int, 4>());
         else if (strips == 1) chunk(std::integral_constant<int, 1>());
@@ -762,7 +722,7 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
         if (it + 2 < count) bar_arrive(kBarEmpty + buf, threads);
         __syncwarp();
     }
-    const bool lost = __any_sync(0xffffffffu, seen.lost());
+    lost = __any_sync(0xffffffffu, lost);
     if constexpr (WAY == Way::kForward) {
         if (segs.n == 1) {
             if (lost) {   // (this warp's own stores of its columns come before)
@@ -781,12 +741,12 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
         }
         if constexpr (WAY == Way::kKeep) {   // the last state, for the gates' gradient
             if (ends && a.d_state_out) {
-                float none[2] = {0.f, 0.f}, back[2];
-                uint32_t sa[DKP / 16][4];
-                S.template rescale<3>(none, back);
 #pragma unroll
-                for (int s = 0; s < DKP / 16; ++s) pack_a(S.x[2 * s], S.x[2 * s + 1], sa[s]);
-                kept.keep_state<DKP>(kept.S, kept.y, unit * (chunks + 1) + chunks, col0, sa, back, g, c, true);
+                for (int s = 0; s < DKP / 16; ++s) {
+                    uint32_t sa[2][4];
+                    pack_a<2>(S.x[2 * s], S.x[2 * s + 1], sa);
+                    kept.keep_state<DKP>(kept.S, kept.S_term, unit * (chunks + 1) + chunks, col0, s, sa, g, c, true);
+                }
             }
         } else if (a.d_state_in && ends) S.store(a.d_state_in + unit * plane, a.dk, a.dv, col0 + g, c);
     } else {
@@ -955,12 +915,13 @@ Kept cut_kept(char* base, long long units, int L, int dk, int dv, size_t* total)
         return p;
     };
     k.dvp = (int)dvp;
-    k.w = (__half*)take(units * chunks * kChunk * dvp * 2);
-    k.du = (__half*)take(units * chunks * kChunk * dvp * 2);
-    k.S = (__half*)take(units * (chunks + 1) * dvp * dkp * 2);
-    k.A = (__half*)take(units * chunks * dvp * dkp * 2);
-    k.y = (float*)take(units * (chunks + 1) * dvp * 4);
-    k.z = (float*)take(units * chunks * dvp * 4);
+    k.row_term = (long long)(units * chunks * kChunk * dvp);
+    k.S_term = (long long)(units * (chunks + 1) * dvp * dkp);
+    k.A_term = (long long)(units * chunks * dvp * dkp);
+    k.w = (bf*)take(2 * k.row_term * 2);
+    k.du = (bf*)take(2 * k.row_term * 2);
+    k.S = (bf*)take(2 * k.S_term * 2);
+    k.A = (bf*)take(2 * k.A_term * 2);
     k.lost_grad = (int*)take(units * chunks * 4);
     *total = at;
     return k;

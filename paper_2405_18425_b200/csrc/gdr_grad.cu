@@ -7,9 +7,8 @@
 //
 // (E K's part of dK and e: replacing S by its decayed form shows e_t = q.dq - v.dv, and v = w + what k retrieves.)
 // A block takes a chunk, a warp sixteen of its tokens as rows: the blocks of X and E up to the diagonal and those of their transposes from it
-// on, five of each for every warp, so that no warp needs another's.  Sums over dv run in fp32 over fp16 operands that are scaled by powers of
-// two: rows of K, Q and dO by their largest element, columns by what the walks kept them under.  64 x 12 units of 196 tokens, 32 x 64: 91 us for 112 MB, bound by
-// instruction issue (3400 a warp, 160 of them products).
+// on, five of each for every warp, so that no warp needs another's.  K, Q and dO are bf16 as they come, all else is two bf16 terms an operand (gdr_tile.cuh):
+// what the walks kept, and X and E.  Bound by instruction issue and shared memory (two blocks an SM for 32 x 64).
 #include <type_traits>
 
 #include "gdr.h"
@@ -25,26 +24,31 @@ constexpr int kMostColumns = 128;
 template <int DKP>
 constexpr int grad_threads() { return DKP > 64 ? 256 : 128; }   // two warps a strip where the key dimensions are many
 
-// Per token, arrays of kChunk floats: running sum of log2 alpha, 2^b, 2^{b_C - b}, beta, scales of the rows of K, Q and dO (2^e, ..), those of dO
-// and Q together over their largest, beta 2^e, beta 2^{2e}, and e of a strip's first and second warp.
-enum { kB, kEb, kDl, kBeta, kKu, kQu, kH, kHf, kGv, kGn, kE, kE2, kRows };
+// Whether A takes the place of S in shared memory once nothing more is read of S: where both do not fit (128 x 128: 255 KB).
+template <int DKP>
+constexpr bool grad_shares() { return DKP > 96; }
 
-struct GradLayout {
-    int kp, vp, k, q, d, r, w, s, a, gates, cols, total;
-    __host__ __device__ GradLayout(int dkp, int dvp) {
+// Per token, arrays of kChunk floats: running sum of log2 alpha, 2^b, 2^{b_C - b}, beta, and e of a strip's first and second warp.
+enum { kB, kEb, kDl, kBeta, kE, kE2, kRows };
+
+struct GradLayout {   // W, dU, S and A: two terms, row_term and state_term bytes apart
+    int kp, vp, row_term, state_term, k, q, d, r, w, s, a, gates, red, total;
+    __host__ __device__ GradLayout(int dkp, int dvp, bool shares) {
         kp = dkp * 2 + 16;
         vp = dvp * 2 + 16;
+        row_term = kChunk * vp;
+        state_term = dvp * kp;
         int at = 0;
         auto take = [&](int bytes) { const int o = at; at += bytes; return o; };
         k = take(kChunk * kp);
         q = take(kChunk * kp);
-        d = take(kChunk * vp);
-        r = take(kChunk * vp);
-        w = take(kChunk * vp);
-        s = take(dvp * kp);
-        a = take(dvp * kp);
+        d = take(row_term);
+        r = take(2 * row_term);
+        w = take(2 * row_term);
+        s = take(2 * state_term);
+        a = shares ? s : take(2 * state_term);
         gates = take(kChunk * kRows * 4);
-        cols = take(dvp * 2 * 4 + 16 * 4);   // per column: y over the largest, and that times z over its largest; then what is reduced
+        red = take(16 * 4);
         total = at;
     }
 };
@@ -55,21 +59,27 @@ __device__ __forceinline__ void ldsm_a(uint32_t addr, uint32_t (&a)[4]) {
     a[0] = x[0]; a[1] = x[2]; a[2] = x[1]; a[3] = x[3];
 }
 __device__ __forceinline__ float2 row2(const float* gates, int row, int t) { return *reinterpret_cast<const float2*>(gates + row * kChunk + t); }
-__device__ __forceinline__ uint4 scale_halves(uint4 x, float s) {
-    const __half2 f = __float2half2_rn(s);   // a power of two of at most one (zero below 2^-24: nothing is left of such a column beside the largest)
-    __half2* h = reinterpret_cast<__half2*>(&x);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __hmul2(h[i], f);
-    return x;
-}
-
 __device__ __forceinline__ f32x2 row_pair(const float* gates, int row, int t) { return *reinterpret_cast<const f32x2*>(gates + row * kChunk + t); }
+
+// acc += a (A terms) x y (B terms), without the product of second terms.
+template <int A, int B>
+__device__ __forceinline__ void add_products(float (&acc)[2][4], const uint32_t (&a)[A][4], const uint32_t (&y)[B][4]) {
+#pragma unroll
+    for (int i = 0; i < A; ++i)
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+            if (i + j < 2) {
+                mma(acc[0], a[i], y[j][0], y[j][1]);
+                mma(acc[1], a[i], y[j][2], y[j][3]);
+            }
+}
 
 // Strip I of the chunk; key dimensions in sixteens s0, s0 + step, ..  (I is a variable and the five blocks' code the same for all warps: with a
 // copy for each strip, fetching instructions was what the warps waited for most, 173 us for 64 x 12 units of 196 tokens, 32 x 64.)
-template <int DKP>
-__device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsigned char* smem, const GradLayout& lay, int dvp, long long unit, int n, float Y,
-                                           float Z, float HF, bool before, bool behind, int s0, int step, int lane, Largest& seen) {
+// bring_a: called by all threads of the block between the products with S and those with A.
+template <int DKP, typename F>
+__device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsigned char* smem, const GradLayout& lay, int dvp, long long unit, int n,
+                                           bool before, bool behind, int s0, int step, int lane, uint32_t& seen, F bring_a) {
     constexpr int KP = DKP * 2 + 16;
     const int g = lane >> 2, c = lane & 3, vp = lay.vp, strips = (min(kChunk, a.L - n * kChunk) + 15) >> 4;
     const Lane ln(lane);
@@ -78,47 +88,57 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
     float* const gates = reinterpret_cast<float*>(smem + lay.gates);
     const int lane_at = ln.b_row * vp + ln.b_col * 2;
     auto b_of = [&](uint32_t tile, int row0, int col0) { return tile + lane_at + row0 * vp + col0 * 2; };
+    auto both_a = [&](uint32_t tile, int row0, int col0, uint32_t (&x)[2][4]) {
+        ldsm_a(b_of(tile, row0, col0), x[0]);
+        ldsm_a(b_of(tile + lay.row_term, row0, col0), x[1]);
+    };
+    auto both_b = [&](uint32_t tile, int row0, int col0, uint32_t (&x)[2][4]) {
+        ldsm(b_of(tile, row0, col0), x[0]);
+        ldsm(b_of(tile + lay.row_term, row0, col0), x[1]);
+    };
     // Block p: of dO W^T and dU W^T up to the diagonal (p <= I, columns of strip p), of W dO^T and W dU^T from it on (columns of strip p - 1)
     float x[5][2][4] = {}, e[5][2][4] = {};
 #pragma unroll 1
-    for (int v = 0; v < dvp; v += 16) {
-        uint32_t da[4], ra[4], wa[4];
-        ldsm_a(b_of(dt, I * 16, v), da);
-        ldsm_a(b_of(rt, I * 16, v), ra);
-        ldsm_a(b_of(wt, I * 16, v), wa);
+    for (int v = I < strips ? 0 : dvp; v < dvp; v += 16) {
+        uint32_t da[1][4], ra[2][4], wa[2][4];
+        ldsm_a(b_of(dt, I * 16, v), da[0]);
+        both_a(rt, I * 16, v, ra);
+        both_a(wt, I * 16, v, wa);
 #pragma unroll
         for (int p = 0; p < 5; ++p) {
-            uint32_t y[4];
+            uint32_t y[2][4];
             if (p <= I) {
-                ldsm(b_of(wt, p * 16, v), y);
-                mma(x[p][0], da, y[0], y[1]);
-                mma(x[p][1], da, y[2], y[3]);
-                mma(e[p][0], ra, y[0], y[1]);
-                mma(e[p][1], ra, y[2], y[3]);
+                both_b(wt, p * 16, v, y);
+                add_products(x[p], da, y);
+                add_products(e[p], ra, y);
             } else if (p <= strips) {
-                ldsm(b_of(dt, (p - 1) * 16, v), y);
-                mma(x[p][0], wa, y[0], y[1]);
-                mma(x[p][1], wa, y[2], y[3]);
-                ldsm(b_of(rt, (p - 1) * 16, v), y);
-                mma(e[p][0], wa, y[0], y[1]);
-                mma(e[p][1], wa, y[2], y[3]);
+                uint32_t z[1][4];
+                ldsm(b_of(dt, (p - 1) * 16, v), z[0]);
+                add_products(x[p], wa, z);
+                both_b(rt, (p - 1) * 16, v, y);
+                add_products(e[p], wa, y);
             }
         }
     }
     const int t0 = I * 16 + g;   // rows t0, t0 + 8
-    const float bt[2] = {gates[kB * kChunk + t0], gates[kB * kChunk + t0 + 8]}, beta[2] = {gates[kBeta * kChunk + t0], gates[kBeta * kChunk + t0 + 8]},
-                ku[2] = {gates[kKu * kChunk + t0], gates[kKu * kChunk + t0 + 8]};
+    const float bt[2] = {gates[kB * kChunk + t0], gates[kB * kChunk + t0 + 8]}, beta[2] = {gates[kBeta * kChunk + t0], gates[kBeta * kChunk + t0 + 8]};
     const float end = gates[kB * kChunk + I * 16 + 15];
     float db[2] = {0.f, 0.f};
-    // to operands, e^{b_t - b_s} by way of the last token of s' sixteen off the diagonal (both factors are at most one)
-    uint32_t xa[5][4], ea[5][4];
+    // to operands of two terms, e^{b_t - b_s} by way of the last token of s' sixteen off the diagonal (both factors are at most one)
+    uint32_t xa[5][2][4], ea[5][2][4];
+    auto put = [&](uint32_t (&to)[2][4], int i, f32x2 v) {
+        uint32_t t[2];
+        split<2>(v, t);
+        to[0][i] = t[0];
+        to[1][i] = t[1];
+    };
 #pragma unroll
     for (int p = 0; p < 5; ++p) {
         const bool low = p <= I;
         const int j = low ? p : p - 1;
         if (j >= strips) {   // (no tokens there, and nothing in shared memory)
 #pragma unroll
-            for (int h = 0; h < 4; ++h) xa[p][h] = ea[p][h] = 0u;
+            for (int h = 0; h < 4; ++h) xa[p][0][h] = xa[p][1][h] = ea[p][0][h] = ea[p][1][h] = 0u;
         } else if (j != I) {
             const float ref = low ? gates[kB * kChunk + j * 16 + 15] : end;
             f32x2 er[2];
@@ -131,16 +151,13 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
             for (int m = 0; m < 2; ++m) {
                 const int col = j * 16 + 8 * m + 2 * c;
                 const float2 bc = row2(gates, kB, col);
-                f32x2 fx = pack2(ex2(low ? ref - bc.x : bc.x - ref), ex2(low ? ref - bc.y : bc.y - ref)), fe = fx;
-                if (low) fe = fx = fmul2(fx, row_pair(gates, kGv, col));   // columns s: times 2^e beta_s
-                else {                                                      // columns t: times the scale of dO's and q's rows, or - beta_t 2^{2e}
-                    fx = fmul2(fx, row_pair(gates, kHf, col));
-                    fe = fmul2(fmul2(fe, row_pair(gates, kGn, col)), pack2(-1.f, -1.f));
-                }
+                f32x2 fx = pack2(ex2(low ? ref - bc.x : bc.x - ref), ex2(low ? ref - bc.y : bc.y - ref)), fe = fmul2(fx, row_pair(gates, kBeta, col));
+                if (low) fx = fe;                          // columns s: times beta_s
+                else fe = fmul2(fe, pack2(-1.f, -1.f));    // columns t: times - beta_t, X as it is
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    xa[p][2 * m + h] = pack_half(fmul2(pair(x[p][m], h), fmul2(fx, er[h])));
-                    ea[p][2 * m + h] = pack_half(fmul2(pair(e[p][m], h), fmul2(fe, er[h])));
+                    put(xa[p], 2 * m + h, fmul2(pair(x[p][m], h), fmul2(fx, er[h])));
+                    put(ea[p], 2 * m + h, fmul2(pair(e[p][m], h), fmul2(fe, er[h])));
                 }
             }
         } else {
@@ -148,12 +165,12 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float d = g & 1 ? e[p][h][2 * h + 1] : e[p][h][2 * h];
-                    db[h] = __shfl_sync(0xffffffffu, d, (lane & 28) | (g >> 1)) * ku[h] * Y * Z;
+                    db[h] = __shfl_sync(0xffffffffu, d, (lane & 28) | (g >> 1));
                 }
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
                 const int cc = 8 * m + 2 * c, col = I * 16 + cc;
-                const float2 bc = row2(gates, kB, col), fx = row2(gates, low ? kGv : kHf, col), fe = row2(gates, low ? kGv : kGn, col);
+                const float2 bc = row2(gates, kB, col), be = row2(gates, kBeta, col);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int row = g + 8 * h;
@@ -161,44 +178,39 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
 #pragma unroll
                     for (int f = 0; f < 2; ++f) {
                         const bool in = low ? cc + f <= row : cc + f >= row, strict = in && cc + f != row;
-                        const float gam = in ? ex2(low ? bt[h] - (f ? bc.y : bc.x) : (f ? bc.y : bc.x) - bt[h]) : 0.f;
-                        xx[f] = in ? x[p][m][2 * h + f] * gam * (f ? fx.y : fx.x) : 0.f;
-                        ee[f] = strict ? e[p][m][2 * h + f] * gam * (f ? fe.y : fe.x) * (low ? 1.f : -1.f) : 0.f;
+                        const float gam = in ? ex2(low ? bt[h] - (f ? bc.y : bc.x) : (f ? bc.y : bc.x) - bt[h]) : 0.f, step = f ? be.y : be.x;
+                        xx[f] = in ? x[p][m][2 * h + f] * gam * (low ? step : 1.f) : 0.f;
+                        ee[f] = strict ? e[p][m][2 * h + f] * gam * (low ? step : -step) : 0.f;
                     }
-                    xa[p][2 * m + h] = pack_half(xx[0], xx[1]);
-                    ea[p][2 * m + h] = pack_half(ee[0], ee[1]);
+                    put(xa[p], 2 * m + h, pack2(xx[0], xx[1]));
+                    put(ea[p], 2 * m + h, pack2(ee[0], ee[1]));
                 }
             }
         }
-        seen.see(xa[p]);
-        seen.see(ea[p]);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            see(seen, xa[p][0][h]);
+            see(seen, ea[p][0][h]);
+        }
     }
     const float eb[2] = {gates[kEb * kChunk + t0], gates[kEb * kChunk + t0 + 8]}, dl[2] = {gates[kDl * kChunk + t0], gates[kDl * kChunk + t0 + 8]};
-    const float qs[2] = {gates[kH * kChunk + t0] * Y, gates[kH * kChunk + t0 + 8] * Y};
     float sum[2] = {0.f, 0.f};
-#pragma unroll 1
-    for (int s = s0; s < DKP / 16; s += step) {
-        float hq[2][4] = {}, h1[2][4] = {}, h2[2][4] = {}, h3[2][4] = {};
+    auto state = [&](uint32_t tile, int s, int v, uint32_t (&y)[2][4]) {
+        ldsm_trans(at_t<KP>(ln, tile, v, s * 16), y[0]);
+        ldsm_trans(at_t<KP>(ln, tile + lay.state_term, v, s * 16), y[1]);
+    };
+    // sixteen key dimensions of dq, and o: the first bracket of dK (with its sign)
+    auto with_s = [&](int s, float (&o)[2][4]) {
+        float hq[2][4] = {}, h1[2][4] = {};
         if (before)
 #pragma unroll 2
             for (int v = 0; v < dvp; v += 16) {
-                uint32_t da[4], ra[4], y[4];
-                ldsm_a(b_of(dt, I * 16, v), da);
-                ldsm_a(b_of(rt, I * 16, v), ra);
-                ldsm_trans(at_t<KP>(ln, st, v, s * 16), y);
-                mma(hq[0], da, y[0], y[1]);
-                mma(hq[1], da, y[2], y[3]);
-                mma(h1[0], ra, y[0], y[1]);
-                mma(h1[1], ra, y[2], y[3]);
-            }
-        if (behind)
-#pragma unroll 2
-            for (int v = 0; v < dvp; v += 16) {
-                uint32_t wa[4], y[4];
-                ldsm_a(b_of(wt, I * 16, v), wa);
-                ldsm_trans(at_t<KP>(ln, at, v, s * 16), y);
-                mma(h2[0], wa, y[0], y[1]);
-                mma(h2[1], wa, y[2], y[3]);
+                uint32_t da[1][4], ra[2][4], y[2][4];
+                ldsm_a(b_of(dt, I * 16, v), da[0]);
+                both_a(rt, I * 16, v, ra);
+                state(st, s, v, y);
+                add_products(hq, da, y);
+                add_products(h1, ra, y);
             }
 #pragma unroll
         for (int m = 0; m < 2; ++m)
@@ -206,47 +218,87 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
             for (int h = 0; h < 2; ++h) {
                 set_pair(hq[m], h, fmul2(pair(hq[m], h), pack2(eb[h], eb[h])));
                 set_pair(h1[m], h, fmul2(pair(h1[m], h), pack2(eb[h], eb[h])));
-                set_pair(h2[m], h, fmul2(pair(h2[m], h), pack2(dl[h], dl[h])));
             }
 #pragma unroll
-        for (int p = 0; p < 5; ++p) {
-            uint32_t y[4];
+        for (int p = 0; p < 4; ++p)
             if (p <= I) {
-                ldsm_trans(at_t<KP>(ln, kt, p * 16, s * 16), y);
-                mma(hq[0], xa[p], y[0], y[1]);
-                mma(hq[1], xa[p], y[2], y[3]);
-                mma(h1[0], ea[p], y[0], y[1]);
-                mma(h1[1], ea[p], y[2], y[3]);
-            } else if (p <= strips) {
-                ldsm_trans(at_t<KP>(ln, kt, (p - 1) * 16, s * 16), y);
-                mma(h2[0], ea[p], y[0], y[1]);
-                mma(h2[1], ea[p], y[2], y[3]);
-                ldsm_trans(at_t<KP>(ln, qt, (p - 1) * 16, s * 16), y);
-                mma(h3[0], xa[p], y[0], y[1]);
-                mma(h3[1], xa[p], y[2], y[3]);
+                uint32_t y[1][4];
+                ldsm_trans(at_t<KP>(ln, kt, p * 16, s * 16), y[0]);
+                add_products(hq, xa[p], y);
+                add_products(h1, ea[p], y);
             }
-        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int t = t0 + 8 * h;
             const bool in = n * kChunk + t < a.L;
             const long long r = in ? a.row(unit, n * kChunk + t) * a.ldk : 0;
-            const float step1 = -beta[h] * ku[h] * Y, qu = gates[kQu * kChunk + t];
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
                 const int col = s * 16 + 8 * m + 2 * c;
-                const float2 kk = unpack_half(*reinterpret_cast<const uint32_t*>(smem + lay.k + t * KP + col * 2)),
-                             qq = unpack_half(*reinterpret_cast<const uint32_t*>(smem + lay.q + t * KP + col * 2));
-                const float q0 = qs[h] * hq[m][2 * h], q1 = qs[h] * hq[m][2 * h + 1], o0 = step1 * h1[m][2 * h] * Z, o1 = step1 * h1[m][2 * h + 1] * Z;
-                const float k0 = o0 + beta[h] * Y * (h2[m][2 * h] * Z + h3[m][2 * h] * HF), k1 = o1 + beta[h] * Y * (h2[m][2 * h + 1] * Z + h3[m][2 * h + 1] * HF);
-                sum[h] += qu * (qq.x * q0 + qq.y * q1) + ku[h] * (kk.x * o0 + kk.y * o1);
-                if (in && col < a.ldk) {
-                    *reinterpret_cast<uint32_t*>(a.dq + r + col) = pack_bf16(q0, q1);
-                    *reinterpret_cast<uint32_t*>(a.dk_out + r + col) = pack_bf16(k0, k1);
-                }
+                const float2 kk = unpack_bf16(*reinterpret_cast<const uint32_t*>(smem + lay.k + t * KP + col * 2)),
+                             qq = unpack_bf16(*reinterpret_cast<const uint32_t*>(smem + lay.q + t * KP + col * 2));
+                o[m][2 * h] = -beta[h] * h1[m][2 * h];
+                o[m][2 * h + 1] = -beta[h] * h1[m][2 * h + 1];
+                sum[h] += qq.x * hq[m][2 * h] + qq.y * hq[m][2 * h + 1] + kk.x * o[m][2 * h] + kk.y * o[m][2 * h + 1];
+                if (in && col < a.ldk) *reinterpret_cast<uint32_t*>(a.dq + r + col) = pack_bf16(hq[m][2 * h], hq[m][2 * h + 1]);
             }
         }
+    };
+    // the other two, and dk
+    auto with_a = [&](int s, const float (&o)[2][4]) {
+        float h2[2][4] = {};
+        if (behind)
+#pragma unroll 2
+            for (int v = 0; v < dvp; v += 16) {
+                uint32_t wa[2][4], y[2][4];
+                both_a(wt, I * 16, v, wa);
+                state(at, s, v, y);
+                add_products(h2, wa, y);
+            }
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) set_pair(h2[m], h, fmul2(pair(h2[m], h), pack2(dl[h], dl[h])));
+#pragma unroll
+        for (int p = 1; p < 5; ++p)
+            if (p > I && p <= strips) {
+                uint32_t y[1][4];
+                ldsm_trans(at_t<KP>(ln, kt, (p - 1) * 16, s * 16), y[0]);
+                add_products(h2, ea[p], y);
+                ldsm_trans(at_t<KP>(ln, qt, (p - 1) * 16, s * 16), y[0]);
+                add_products(h2, xa[p], y);
+            }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int t = t0 + 8 * h;
+            if (n * kChunk + t >= a.L) continue;
+            bf* const r = a.dk_out + a.row(unit, n * kChunk + t) * a.ldk;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const int col = s * 16 + 8 * m + 2 * c;
+                if (col < a.ldk)
+                    *reinterpret_cast<uint32_t*>(r + col) = pack_bf16(fmaf(beta[h], h2[m][2 * h], o[m][2 * h]), fmaf(beta[h], h2[m][2 * h + 1], o[m][2 * h + 1]));
+            }
+        }
+    };
+    if constexpr (grad_shares<DKP>()) {
+        float o[DKP / 32][2][4];   // (two warps a strip)
+        if (I < strips)
+#pragma unroll
+            for (int i = 0; i < DKP / 32; ++i) with_s(s0 + i * step, o[i]);
+        bring_a();
+        if (I < strips)
+#pragma unroll
+            for (int i = 0; i < DKP / 32; ++i) with_a(s0 + i * step, o[i]);
+    } else {
+#pragma unroll 1
+        for (int s = s0; s < DKP / 16; s += step) {
+            float o[2][4];
+            with_s(s, o);
+            with_a(s, o);
+        }
     }
+    if (I >= strips) return;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 1);
@@ -263,20 +315,19 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
 }
 
 template <int DKP>
-__global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64 ? 2 : 1) gdr_grad_kernel(Gdr<bf> a, GdrKept kept, int chunks) {
+__global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 3 : DKP <= 64 ? 2 : 1) gdr_grad_kernel(Gdr<bf> a, GdrKept kept, int chunks) {
     constexpr int KP = DKP * 2 + 16, kThreads = grad_threads<DKP>();
-    constexpr int kLanes = DKP <= 16 ? 2 : DKP <= 32 ? 4 : DKP <= 64 ? 8 : 16;
     extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, dvp = kept.dvp;
-    const GradLayout lay(DKP, dvp);
+    const GradLayout lay(DKP, dvp, grad_shares<DKP>());
     const long long unit = blockIdx.x / chunks;
     const int n = blockIdx.x % chunks, t0 = n * kChunk, nt = min(kChunk, a.L - t0);
     const long long here = unit * chunks + n, states = unit * (chunks + 1) + n;
     float* const gates = reinterpret_cast<float*>(smem + lay.gates);
-    float *const cy = reinterpret_cast<float*>(smem + lay.cols), *const cyz = cy + dvp, *const red = cyz + dvp;
+    float* const red = reinterpret_cast<float*>(smem + lay.red);
     pdl_wait();
     pdl_launch_dependents();
-    // everything comes in by asynchronous copies at once, and is turned into operands where it lies; rows up to the last strip with tokens
+    // everything comes in by asynchronous copies at once and is an operand as it lies; rows up to the last strip with tokens
     const uint32_t base = smem_u32(smem);
     const int rows = (nt + 15) & ~15;
     const bool before = n > 0 || a.state_in, behind = n + 1 < chunks || a.d_state_out;   // (zeros otherwise, which nothing is read of)
@@ -293,41 +344,26 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
             const bool in = t < nt;   // (rows behind the last token were not written)
             const uint32_t to = t * lay.vp + piece * 2;
             const long long at = (here * kChunk + t) * dvp + piece;
-            cp_async16(base + lay.w + to, kept.w + at, in);
-            cp_async16(base + lay.r + to, kept.du + at, in);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                cp_async16(base + lay.w + m * lay.row_term + to, kept.w + m * kept.row_term + at, in);
+                cp_async16(base + lay.r + m * lay.row_term + to, kept.du + m * kept.row_term + at, in);
+            }
             const bool values = in && piece < a.ldv;
             cp_async16(base + lay.d + to, a.d_out + (values ? a.row(unit, t0 + t) * a.ldv + piece : 0), values);
         }
-    for (int i = tid; i < dvp * (DKP / 8); i += kThreads) {
-        const int j = i / (DKP / 8), e = i % (DKP / 8) * 8;
-        if (before) cp_async16(base + lay.s + j * KP + e * 2, kept.S + (states * dvp + j) * DKP + e, true);
-        if (behind) cp_async16(base + lay.a + j * KP + e * 2, kept.A + (here * dvp + j) * DKP + e, true);
-    }
-    cp_async_commit();
-    // the state behind the chunk, for the gradient that the next chunk's first gate sees
-    constexpr int kBehind = 128 * (DKP / 8) / kThreads;   // pieces of a thread, at most
-    uint4 next[kBehind];
+    auto bring_state = [&](int to, const bf* from, long long term, bool there) {   // (nothing is read of one that is not)
+        if (there)
+            for (int i = tid; i < dvp * (DKP / 8); i += kThreads) {
+                const int j = i / (DKP / 8), e = i % (DKP / 8) * 8;
 #pragma unroll
-    for (int p = 0; p < kBehind; ++p) {
-        const int i = tid + p * kThreads;
-        if (behind && i < dvp * (DKP / 8)) next[p] = *reinterpret_cast<const uint4*>(kept.S + (states + 1) * dvp * DKP + i * 8);
-    }
-    // columns: their powers of two over the largest
-    float Y = 0.f, Z = 0.f;
-    for (int j = lane; j < dvp; j += 32) {
-        Y = fmaxf(Y, kept.y[states * dvp + j]);
-        Z = fmaxf(Z, kept.z[here * dvp + j]);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Y = fmaxf(Y, __shfl_xor_sync(0xffffffffu, Y, o));
-        Z = fmaxf(Z, __shfl_xor_sync(0xffffffffu, Z, o));
-    }
-    for (int j = tid; j < dvp; j += kThreads) {
-        const float y = kept.y[states * dvp + j] / Y;
-        cy[j] = y;
-        cyz[j] = y * (kept.z[here * dvp + j] / Z);
-    }
+                for (int m = 0; m < 2; ++m) cp_async16(base + to + m * lay.state_term + j * KP + e * 2, from + m * term + (long long)i * 8, true);
+            }
+        cp_async_commit();
+    };
+    const bf* const A = kept.A + here * dvp * DKP;
+    if constexpr (!grad_shares<DKP>()) bring_state(lay.a, A, kept.A_term, behind);
+    bring_state(lay.s, kept.S + states * dvp * DKP, kept.S_term, before);
     if (warp == 0) {   // gates, as the walks have them
         float l[2], s[2], be[2];
 #pragma unroll
@@ -354,103 +390,40 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 4 : DKP <= 64
     }
     cp_async_wait<0>();
     __syncthreads();
-    // K, Q to fp16 under their rows' powers of two
+    float anchor = 0.f;   // what the next chunk's first gate sees: the product of A with the state behind the chunk
+    auto meet = [&]() {
+        if (!behind) return;
+        for (int i = tid; i < dvp * (DKP / 8); i += kThreads) {
+            const int j = i / (DKP / 8), e = i % (DKP / 8) * 8;
+            const unsigned char* const x = smem + lay.a + j * KP + e * 2;
+            const bf* const y = kept.S + ((states + 1) * dvp + j) * DKP + e;
+            const uint4 xh = *reinterpret_cast<const uint4*>(x), xl = *reinterpret_cast<const uint4*>(x + lay.state_term), yh = *reinterpret_cast<const uint4*>(y),
+                        yl = *reinterpret_cast<const uint4*>(y + kept.S_term);
+            const uint32_t xs[2][4] = {{xh.x, xh.y, xh.z, xh.w}, {xl.x, xl.y, xl.z, xl.w}}, ys[2][4] = {{yh.x, yh.y, yh.z, yh.w}, {yl.x, yl.y, yl.z, yl.w}};
 #pragma unroll
-    for (int p = 0; p < 2 * kChunk * kLanes / kThreads; ++p) {
-        const int i = tid + p * kThreads, r = i / kLanes, e8 = i % kLanes * 8, t = r & (kChunk - 1);
-        const bool key = r < kChunk;
-        if (p * kThreads / kLanes % kChunk >= rows) continue;   // the first of the pass's rows
-        uint4* const at = reinterpret_cast<uint4*>(smem + (key ? lay.k : lay.q) + t * KP + e8 * 2);
-        const uint4 x = e8 < DKP && t < rows ? *at : make_uint4(0u, 0u, 0u, 0u);
-        uint32_t m = largest_bf16(x);
-#pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        float down, up;
-        power_of(m >> 7, down, up);
-        if (e8 < DKP && t < rows) *at = bf16_to_half(x, down);
-        if (e8 == 0) {
-            gates[(key ? kKu : kQu) * kChunk + t] = up;
-            if (key) {
-                const float gv = gates[kBeta * kChunk + t] * up;
-                gates[kGv * kChunk + t] = gv;
-                gates[kGn * kChunk + t] = gv * up;
+            for (int q = 0; q < 4; ++q) {
+                float u0, u1, v0, v1;
+                unpack2(fadd2(widen_bf16(xs[0][q]), widen_bf16(xs[1][q])), u0, u1);
+                unpack2(fadd2(widen_bf16(ys[0][q]), widen_bf16(ys[1][q])), v0, v1);
+                anchor = fmaf(u0, v0, fmaf(u1, v1, anchor));
             }
         }
-    }
-    // dO under its rows' and its columns' powers of two, dU under its columns'
-    {
-        f32x2 fy[4];
-        __half2 fz[4];
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            fy[p] = piece < dvp ? *reinterpret_cast<const f32x2*>(cy + piece + 2 * p) : 0ull;
-            fz[p] = piece < dvp ? __floats2half2_rn(cyz[piece + 2 * p], cyz[piece + 2 * p + 1]) : __float2half2_rn(0.f);
-        }
-        // (whole warps: a warp's rows, at most sixteen, are either all there or all not)
-        for (int t = tid >> lg; t < rows; t += kThreads >> lg) {
-            uint4* const at = reinterpret_cast<uint4*>(smem + lay.d + t * lay.vp + piece * 2);
-            const uint4 x = piece < dvp ? *at : make_uint4(0u, 0u, 0u, 0u);
-            uint32_t m = largest_bf16(x);
-            for (int o = 1; o < 1 << lg; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-            float down, up;
-            power_of(m >> 7, down, up);
-            if (piece < dvp) {
-                const f32x2 dn = pack2(down, down);
-                *at = make_uint4(pack_half(fmul2(fmul2(widen_bf16(x.x), dn), fy[0])), pack_half(fmul2(fmul2(widen_bf16(x.y), dn), fy[1])),
-                                 pack_half(fmul2(fmul2(widen_bf16(x.z), dn), fy[2])), pack_half(fmul2(fmul2(widen_bf16(x.w), dn), fy[3])));
-                uint4* const ar = reinterpret_cast<uint4*>(smem + lay.r + t * lay.vp + piece * 2);
-                uint4 y = *ar;
-                __half2* const h = reinterpret_cast<__half2*>(&y);
-#pragma unroll
-                for (int p = 0; p < 4; ++p) h[p] = __hmul2(h[p], fz[p]);
-                *ar = y;
-            }
-            if (piece == 0) gates[kH * kChunk + t] = up;
-        }
-    }
-    // A under its columns' powers of two, and its product with the state behind the chunk
-    float anchor = 0.f;
-#pragma unroll
-    for (int p = 0; p < kBehind; ++p) {
-        const int i = tid + p * kThreads, j = i / (DKP / 8), e = i % (DKP / 8) * 8;
-        if (behind && i < dvp * (DKP / 8)) {
-            uint4* const at = reinterpret_cast<uint4*>(smem + lay.a + j * KP + e * 2);
-            const uint4 x = *at;
-            *at = scale_halves(x, cyz[j]);
-            {
-                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ss[4] = {next[p].x, next[p].y, next[p].z, next[p].w};
-                float dot = 0.f;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float2 u = unpack_half(xs[q]), v = unpack_half(ss[q]);
-                    dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
-                }
-                anchor = fmaf(dot * kept.y[(states + 1) * dvp + j], kept.z[here * dvp + j], anchor);
-            }
-        }
-    }
+    };
+    if constexpr (!grad_shares<DKP>()) meet();
+    uint32_t seen = 0u;
+    const int strip = warp & 3, half = warp >> 2, step = kThreads / 128;
+    auto bring_a = [&]() {
+        __syncthreads();
+        bring_state(lay.a, A, kept.A_term, behind);
+        cp_async_wait<0>();
+        __syncthreads();
+        meet();
+    };
+    if (grad_shares<DKP>() || strip * 16 < nt) grad_strip<DKP>(strip, a, smem, lay, dvp, unit, n, before, behind, half, step, lane, seen, bring_a);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) anchor += __shfl_xor_sync(0xffffffffu, anchor, o);
     if (lane == 0) red[warp] = anchor;
-    __syncthreads();
-    // the scales of dO's and q's rows together, over the largest
-    float HF = 0.f;
-    {
-        const float p = lane < rows ? gates[kH * kChunk + lane] * gates[kQu * kChunk + lane] : 0.f,
-                    q = lane + 32 < rows ? gates[kH * kChunk + lane + 32] * gates[kQu * kChunk + lane + 32] : 0.f;
-        HF = fmaxf(p, q);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) HF = fmaxf(HF, __shfl_xor_sync(0xffffffffu, HF, o));
-        if (warp == 0) {
-            gates[kHf * kChunk + lane] = p / HF;
-            gates[kHf * kChunk + lane + 32] = q / HF;
-        }
-    }
-    __syncthreads();
-    Largest seen;
-    const int strip = warp & 3, half = warp >> 2, step = kThreads / 128;
-    if (strip * 16 < nt) grad_strip<DKP>(strip, a, smem, lay, dvp, unit, n, Y, Z, HF, before, behind, half, step, lane, seen);
-    const int lost = __syncthreads_or(seen.lost());
+    const int lost = __syncthreads_or(!within(seen, 3.3e38f));
     if (tid == 0) kept.lost_grad[here] = lost;
     // dlog_alpha: sums from the chunk's end; a gate that leaves nothing, or has nothing to scale, has none, and the sums start anew there
     if (warp == 0) {
@@ -481,8 +454,8 @@ cudaError_t launch_gdr_grad(const Gdr<__nv_bfloat16>& a, const GdrKept& kept, cu
     const int chunks = (a.L + kChunk - 1) / kChunk;
     auto launch = [&](auto D) {
         constexpr int dkp = decltype(D)::value;
-        const int smem = GradLayout(dkp, kept.dvp).total;
-        cudaError_t e = allow_smem<gdr_grad_kernel<dkp>>(GradLayout(dkp, kMostColumns).total);
+        const int smem = GradLayout(dkp, kept.dvp, grad_shares<dkp>()).total;
+        cudaError_t e = allow_smem<gdr_grad_kernel<dkp>>(GradLayout(dkp, kMostColumns, grad_shares<dkp>()).total);
         if (e != cudaSuccess) return e;
         count_launch();
         return launch_pdl(gdr_grad_kernel<dkp>, dim3((unsigned)(a.units * chunks)), dim3(grad_threads<dkp>()), smem, stream, a, kept, chunks);

@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(512) gdr_finish_kernel(Gdr<T> a, Scratch s) {
     finish<T>(a, s, blockIdx.x / borders(a.L), blockIdx.x % borders(a.L));
 }
 
-// Behind the gradient in chunks: units of which something left the range of fp16, whole, a block at a time.  Without any the block ends
+// Behind the gradient in chunks: units that the loop left to the walks (grown too far, or not finite), whole, a block at a time.  Without any the block ends
 // at once.
 constexpr int kRepairR = 32, kRepairG = 4, kRepairOwners = 64;
 __global__ void __launch_bounds__(256) gdr_repair_kernel(Gdr<__nv_bfloat16> a, Scratch s, const int* first, int per, const int* second, int chunks, int* status) {
