@@ -43,9 +43,9 @@ template <int DKP>
 constexpr int key_pitch() { return DKP * 2 + 16; }
 
 // Per token of a chunk, in shared memory: arrays of kChunk floats.
-//   b running sum of log2 alpha; eb 2^b; dl 2^{b_C - b}; beta; and of the whole chunk the largest of K and of Q that each preparing warp met (at 0 and
+//   b, bl running sum of log2 alpha (two floats); eb 2^b; dl 2^{b_C - b}; beta; and of the whole chunk the largest of K and of Q that each preparing warp met (at 0 and
 //   4), and of beta (at 8)
-enum { kB, kEb, kDl, kBeta, kMost, kGateRows };
+enum { kB, kBl, kEb, kDl, kBeta, kMost, kGateRows };
 __device__ __forceinline__ f32x2 gate_pair(const float* gates, int row, int t) { return *reinterpret_cast<const f32x2*>(gates + row * kChunk + t); }
 
 // Terms of what is computed: states that leave the call in fp32 are made of three, bf16 results of two.
@@ -121,27 +121,16 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
         if (it >= 2) named_bar(kBarEmpty + buf, threads);
         float* const gates = reinterpret_cast<float*>(smem + lay.gates(buf));
         if (warp == 0) {   // running sum of log2 alpha, two tokens a lane
-            float l[2], s[2];
+            Sum b[2], all;
+            gate_sums(la, b, all);
+            float step = fmaxf(fabsf(be[0]), fabsf(be[1]));
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                // (below 2^-150 nothing of the state is left in fp32; the bound keeps sums of such gates exact to 2^-11)
-                const float x = la[h] * 1.4426950408889634f;
-                l[h] = x < -160.f ? -160.f : x;
-            }
-            s[0] = l[0];
-            s[1] = l[0] + l[1];
-            float run = s[1], step = fmaxf(fabsf(be[0]), fabsf(be[1]));
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const float y = __shfl_up_sync(0xffffffffu, run, o);
-                if (lane >= o) run += y;
-                step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, o));
-            }
-            const float before = run - s[1], all = __shfl_sync(0xffffffffu, run, 31), b0 = before + s[0], b1 = before + s[1];
+            for (int o = 1; o < 32; o <<= 1) step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, o));
             auto two = [&](int row, float x, float y) { *reinterpret_cast<float2*>(gates + row * kChunk + 2 * lane) = make_float2(x, y); };
-            two(kB, b0, b1);
-            two(kEb, ex2(b0), ex2(b1));
-            two(kDl, ex2(all - b0), ex2(all - b1));
+            two(kB, b[0].h, b[1].h);
+            two(kBl, b[0].l, b[1].l);
+            two(kEb, ex2(b[0].h + b[0].l), ex2(b[1].h + b[1].l));
+            two(kDl, ex2(all.to(b[0])), ex2(all.to(b[1])));
             two(kBeta, be[0], be[1]);
             if (lane == 0) gates[kMost * kChunk + 8] = step;
         }
@@ -189,6 +178,12 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
 #pragma unroll
             for (int m = 0; m < kN; ++m) *reinterpret_cast<uint32_t*>(smem + matrix + m * Lay::kMat + at) = t[m];
         };
+        auto sum_at = [&](int t) { return Sum{gates[kB * kChunk + t], gates[kBl * kChunk + t]}; };
+        auto sums_at = [&](int t, Sum& x, Sum& y) {   // of two neighbours
+            const float2 h = *reinterpret_cast<const float2*>(gates + kB * kChunk + t), l = *reinterpret_cast<const float2*>(gates + kBl * kChunk + t);
+            x = {h.x, l.x};
+            y = {h.y, l.y};
+        };
         const std::integral_constant<int, TERMS> terms_n;
         const std::integral_constant<int, PT> terms_p;
         if (warp < 2) {
@@ -202,12 +197,14 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {   // rows g, g + 8
                     const int tt = g + 8 * h, t = i * 16 + tt;
-                    const float bt = gates[kB * kChunk + t], beta = gates[kBeta * kChunk + t];
+                    const Sum bt = sum_at(t);
+                    const float beta = gates[kBeta * kChunk + t];
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {   // columns 8m + 2c, + 1
                         const int ss = 8 * m + 2 * c, at = block_of(i, i) + in_block(tt, m) + 4 * c;
-                        const float2 bs = *reinterpret_cast<const float2*>(gates + kB * kChunk + i * 16 + ss);
-                        const float e0 = ss <= tt ? ex2(bt - bs.x) : 0.f, e1 = ss + 1 <= tt ? ex2(bt - bs.y) : 0.f;
+                        Sum b0, b1;
+                        sums_at(i * 16 + ss, b0, b1);
+                        const float e0 = ss <= tt ? ex2(bt.to(b0)) : 0.f, e1 = ss + 1 <= tt ? ex2(bt.to(b1)) : 0.f;
                         // (selected, not multiplied: what is not finite stays out of earlier tokens)
                         if constexpr (Q) put(terms_p, lay.p(buf), at, pack2(ss <= tt ? pp[m][2 * h] * e0 : 0.f, ss + 1 <= tt ? pp[m][2 * h + 1] * e1 : 0.f));
                         const float n0 = ss < tt ? nn[m][2 * h] * e0 : 0.f, n1 = ss + 1 < tt ? nn[m][2 * h + 1] * e1 : 0.f;
@@ -256,16 +253,17 @@ __device__ void prepare_chunks(const Gdr<bf>& a, unsigned char* smem, const Layo
                 float nn[2][4] = {}, pp[2][4] = {};
                 products(i, j, nn, pp);
                 // e^{b_t - b_s} by way of the last token of s' sixteen: both factors are at most one
-                const float ref = gates[kB * kChunk + j * 16 + 15];
+                const Sum ref = sum_at(j * 16 + 15);
                 f32x2 ec[2];
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    const float2 bs = *reinterpret_cast<const float2*>(gates + kB * kChunk + j * 16 + 8 * m + 2 * c);
-                    ec[m] = pack2(ex2(ref - bs.x), ex2(ref - bs.y));
+                    Sum b0, b1;
+                    sums_at(j * 16 + 8 * m + 2 * c, b0, b1);
+                    ec[m] = pack2(ex2(ref.to(b0)), ex2(ref.to(b1)));
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float et = ex2(gates[kB * kChunk + i * 16 + g + 8 * h] - ref);
+                    const float et = ex2(sum_at(i * 16 + g + 8 * h).to(ref));
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
                         const int at = block_of(i, j) + in_block(g + 8 * h, m) + 4 * c;

@@ -28,8 +28,8 @@ constexpr int grad_threads() { return DKP > 64 ? 256 : 128; }   // two warps a s
 template <int DKP>
 constexpr bool grad_shares() { return DKP > 96; }
 
-// Per token, arrays of kChunk floats: running sum of log2 alpha, 2^b, 2^{b_C - b}, beta, and e of a strip's first and second warp.
-enum { kB, kEb, kDl, kBeta, kE, kE2, kRows };
+// Per token, arrays of kChunk floats: running sum of log2 alpha (two floats), 2^b, 2^{b_C - b}, beta, and e of a strip's first and second warp.
+enum { kB, kBl, kEb, kDl, kBeta, kE, kE2, kRows };
 
 struct GradLayout {   // W, dU, S and A: two terms, row_term and state_term bytes apart
     int kp, vp, row_term, state_term, k, q, d, r, w, s, a, gates, red, total;
@@ -121,8 +121,14 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
         }
     }
     const int t0 = I * 16 + g;   // rows t0, t0 + 8
-    const float bt[2] = {gates[kB * kChunk + t0], gates[kB * kChunk + t0 + 8]}, beta[2] = {gates[kBeta * kChunk + t0], gates[kBeta * kChunk + t0 + 8]};
-    const float end = gates[kB * kChunk + I * 16 + 15];
+    auto sum_at = [&](int t) { return Sum{gates[kB * kChunk + t], gates[kBl * kChunk + t]}; };
+    auto sums_at = [&](int t, Sum (&x)[2]) {   // of two neighbours
+        const float2 h = row2(gates, kB, t), l = row2(gates, kBl, t);
+        x[0] = {h.x, l.x};
+        x[1] = {h.y, l.y};
+    };
+    const Sum bt[2] = {sum_at(t0), sum_at(t0 + 8)}, end = sum_at(I * 16 + 15);
+    const float beta[2] = {gates[kBeta * kChunk + t0], gates[kBeta * kChunk + t0 + 8]};
     float db[2] = {0.f, 0.f};
     // to operands of two terms, e^{b_t - b_s} by way of the last token of s' sixteen off the diagonal (both factors are at most one)
     uint32_t xa[5][2][4], ea[5][2][4];
@@ -140,18 +146,19 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
 #pragma unroll
             for (int h = 0; h < 4; ++h) xa[p][0][h] = xa[p][1][h] = ea[p][0][h] = ea[p][1][h] = 0u;
         } else if (j != I) {
-            const float ref = low ? gates[kB * kChunk + j * 16 + 15] : end;
+            const Sum ref = low ? sum_at(j * 16 + 15) : end;
             f32x2 er[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float r = ex2(low ? bt[h] - ref : ref - bt[h]);
+                const float r = ex2(low ? bt[h].to(ref) : ref.to(bt[h]));
                 er[h] = pack2(r, r);
             }
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
                 const int col = j * 16 + 8 * m + 2 * c;
-                const float2 bc = row2(gates, kB, col);
-                f32x2 fx = pack2(ex2(low ? ref - bc.x : bc.x - ref), ex2(low ? ref - bc.y : bc.y - ref)), fe = fmul2(fx, row_pair(gates, kBeta, col));
+                Sum bc[2];
+                sums_at(col, bc);
+                f32x2 fx = pack2(ex2(low ? ref.to(bc[0]) : bc[0].to(ref)), ex2(low ? ref.to(bc[1]) : bc[1].to(ref))), fe = fmul2(fx, row_pair(gates, kBeta, col));
                 if (low) fx = fe;                          // columns s: times beta_s
                 else fe = fmul2(fe, pack2(-1.f, -1.f));    // columns t: times - beta_t, X as it is
 #pragma unroll
@@ -170,7 +177,9 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
                 const int cc = 8 * m + 2 * c, col = I * 16 + cc;
-                const float2 bc = row2(gates, kB, col), be = row2(gates, kBeta, col);
+                const float2 be = row2(gates, kBeta, col);
+                Sum bc[2];
+                sums_at(col, bc);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int row = g + 8 * h;
@@ -178,7 +187,7 @@ __device__ __forceinline__ void grad_strip(const int I, const Gdr<bf>& a, unsign
 #pragma unroll
                     for (int f = 0; f < 2; ++f) {
                         const bool in = low ? cc + f <= row : cc + f >= row, strict = in && cc + f != row;
-                        const float gam = in ? ex2(low ? bt[h] - (f ? bc.y : bc.x) : (f ? bc.y : bc.x) - bt[h]) : 0.f, step = f ? be.y : be.x;
+                        const float gam = in ? ex2(low ? bt[h].to(bc[f]) : bc[f].to(bt[h])) : 0.f, step = f ? be.y : be.x;
                         xx[f] = in ? x[p][m][2 * h + f] * gam * (low ? step : 1.f) : 0.f;
                         ee[f] = strict ? e[p][m][2 * h + f] * gam * (low ? step : -step) : 0.f;
                     }
@@ -365,27 +374,20 @@ __global__ void __launch_bounds__(grad_threads<DKP>(), DKP <= 32 ? 3 : DKP <= 64
     if constexpr (!grad_shares<DKP>()) bring_state(lay.a, A, kept.A_term, behind);
     bring_state(lay.s, kept.S + states * dvp * DKP, kept.S_term, before);
     if (warp == 0) {   // gates, as the walks have them
-        float l[2], s[2], be[2];
+        float la[2], be[2];
+        Sum b[2], all;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int t = 2 * lane + h;
-            const float x = t < nt ? __bfloat162float(a.la[a.row(unit, t0 + t)]) * 1.4426950408889634f : 0.f;
-            l[h] = x < -160.f ? -160.f : x;
+            la[h] = t < nt ? __bfloat162float(a.la[a.row(unit, t0 + t)]) : 0.f;
             be[h] = t < nt ? __bfloat162float(a.beta[a.row(unit, t0 + t)]) : 0.f;
         }
-        s[0] = l[0];
-        s[1] = l[0] + l[1];
-        float run = s[1];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const float y = __shfl_up_sync(0xffffffffu, run, o);
-            if (lane >= o) run += y;
-        }
-        const float before = run - s[1], all = __shfl_sync(0xffffffffu, run, 31), b0 = before + s[0], b1 = before + s[1];
+        gate_sums(la, b, all);
         auto two = [&](int row, float x, float y) { *reinterpret_cast<float2*>(gates + row * kChunk + 2 * lane) = make_float2(x, y); };
-        two(kB, b0, b1);
-        two(kEb, ex2(b0), ex2(b1));
-        two(kDl, ex2(all - b0), ex2(all - b1));
+        two(kB, b[0].h, b[1].h);
+        two(kBl, b[0].l, b[1].l);
+        two(kEb, ex2(b[0].h + b[0].l), ex2(b[1].h + b[1].l));
+        two(kDl, ex2(all.to(b[0])), ex2(all.to(b[1])));
         two(kBeta, be[0], be[1]);
     }
     cp_async_wait<0>();

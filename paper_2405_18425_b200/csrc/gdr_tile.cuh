@@ -90,6 +90,38 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// Running sums of log2 alpha of a chunk as two floats: multiples of 2^-8, of which 64 add up exactly (a gate counts down to 2^-160, below which fp32
+// keeps nothing of a state), and what is left, below 2^-3 in sum.  So a difference of two sums is as exact behind gates that forget as anywhere: of
+// one float it had lost up to ten bits.
+struct Sum {
+    float h, l;
+    __device__ __forceinline__ float to(const Sum& s) const { return (h - s.h) + (l - s.l); }   // from s to here
+};
+// The sums at tokens 2 lane and 2 lane + 1, and of the whole chunk, of natural logarithms la.
+__device__ __forceinline__ void gate_sums(const float (&la)[2], Sum (&b)[2], Sum& all) {
+    const int lane = threadIdx.x & 31;
+    float h[2], l[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float x = la[i] * 1.4426950408889634f;
+        x = x < -160.f ? -160.f : x;
+        h[i] = rintf(x * 256.f) * 0x1p-8f;
+        l[i] = x - h[i];
+    }
+    float rh = h[0] + h[1], rl = l[0] + l[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float yh = __shfl_up_sync(0xffffffffu, rh, o), yl = __shfl_up_sync(0xffffffffu, rl, o);
+        if (lane >= o) {
+            rh += yh;
+            rl += yl;
+        }
+    }
+    all = {__shfl_sync(0xffffffffu, rh, 31), __shfl_sync(0xffffffffu, rl, 31)};
+    b[0] = {rh - h[1], rl - l[1]};
+    b[1] = {rh, rl};
+}
+
 // Largest magnitudes of pairs of bf16; a NaN stays.
 __device__ __forceinline__ void see(uint32_t& m, uint32_t x) { asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(x)); }   // (larger magnitude, the signs' product)
 __device__ __forceinline__ bool within(uint32_t m, float limit) {   // false for what is not finite
