@@ -37,24 +37,29 @@ struct Gdr {
 };
 
 #ifdef __CUDACC__
-// Sums from the end of 64 values, two a lane, that start anew at a stop: what the values behind this lane's pair come to, `end` behind the
-// last where nothing stopped it.
-__device__ __forceinline__ float suffix_of_pairs(const float (&x)[2], const bool (&stop)[2], float end) {
+// Of 64 values, two a lane: what is in front of this lane's pair, and what is behind it.  (Nothing is added and taken off again: a small sum beside large
+// values keeps its digits.)
+__device__ __forceinline__ float before_pair(float x0, float x1) {
     const int lane = threadIdx.x & 31;
-    float acc = stop[0] ? 0.f : x[0] + (stop[1] ? 0.f : x[1]);
-    bool cut = stop[0] || stop[1];
+    float run = x0 + x1;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const float y = __shfl_down_sync(0xffffffffu, acc, o);
-        const int z = __shfl_down_sync(0xffffffffu, (int)cut, o);
-        if (lane + o < 32) {
-            if (!cut) acc += y;
-            cut = cut || z;
-        }
+        const float y = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += y;
     }
-    const float later = __shfl_down_sync(0xffffffffu, acc, 1);
-    const int later_cut = __shfl_down_sync(0xffffffffu, (int)cut, 1);
-    return lane == 31 ? end : later + (later_cut ? 0.f : end);
+    run = __shfl_up_sync(0xffffffffu, run, 1);
+    return lane == 0 ? 0.f : run;
+}
+__device__ __forceinline__ float behind_pair(float x0, float x1) {
+    const int lane = threadIdx.x & 31;
+    float run = x0 + x1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float y = __shfl_down_sync(0xffffffffu, run, o);
+        if (lane + o < 32) run += y;
+    }
+    run = __shfl_down_sync(0xffffffffu, run, 1);
+    return lane == 31 ? 0.f : run;
 }
 #endif
 
@@ -87,9 +92,8 @@ cudaError_t launch_gdr_chunk_fwd(const Gdr<__nv_bfloat16>& a, void* scratch, cud
 struct GdrKept {
     __nv_bfloat16* w;      // [2][units][chunks][64][dvp]: W; rows behind a call's last sixteen are not written
     __nv_bfloat16* du;     // [2][units][chunks][64][dvp]: dU
-    __nv_bfloat16 *S, *A;  // transposed, [2][units][chunks + 1][dvp][DKP] before each chunk and, where its gradient is given, behind the
-                           // last; [2][units][chunks][dvp][DKP]: what arrives behind each chunk
-    long long row_term, S_term, A_term;
+    __nv_bfloat16 *S, *A;  // transposed, [2][units][chunks][dvp][DKP]: before each chunk, and what arrives behind it
+    long long row_term, state_term;
     int* lost_grad;        // [units][chunks]: something is not finite
     int dvp;
     // Sixteen columns and sixteen key dimensions of a state, as packed for an A operand; not `there`: a state of zeros, which nothing is read of.

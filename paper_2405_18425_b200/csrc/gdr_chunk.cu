@@ -439,7 +439,7 @@ __device__ __forceinline__ bool forward_chunk(State<DKP>& S, const Gdr<bf>& a, c
         pack_a<TERMS>(S.x[2 * s], S.x[2 * s + 1], sa);
 #pragma unroll
         for (int e = 0; e < 4; ++e) larger(sm[e & 1], sa[0][e]);
-        if constexpr (KEEP) kept.keep_state<DKP>(kept.S, kept.S_term, unit * (chunks + 1) + n, col0, s, sa, g, c, n > 0 || a.state_in);
+        if constexpr (KEEP) kept.keep_state<DKP>(kept.S, kept.state_term, unit * chunks + n, col0, s, sa, g, c, n > 0 || a.state_in);
         state_times_rows<DKP, TERMS, NS>(w, sa, kt, s, ln);
         if constexpr (OUT) state_times_rows<DKP, 2, NS>(o, sa, qt, s, ln);
     }
@@ -560,7 +560,7 @@ __device__ __forceinline__ bool backward_chunk(State<DKP>& A, const Gdr<bf>& a, 
         pack_a<TERMS>(A.x[2 * s], A.x[2 * s + 1], aa);
 #pragma unroll
         for (int e = 0; e < 4; ++e) larger(am[e & 1], aa[0][e]);
-        if constexpr (WAY == Way::kBack) kept.keep_state<DKP>(kept.A, kept.A_term, unit * chunks + n, col0, s, aa, g, c, n + 1 < chunks || a.d_state_out);
+        if constexpr (WAY == Way::kBack) kept.keep_state<DKP>(kept.A, kept.state_term, unit * chunks + n, col0, s, aa, g, c, n + 1 < chunks || a.d_state_out);
         state_times_rows<DKP, TERMS, NS>(r, aa, kt, s, ln);
     }
     A.decay(gates[kEb * kChunk + kChunk - 1]);
@@ -737,16 +737,7 @@ __global__ void __launch_bounds__(32 * kMostWarps + kPrep, two_blocks<DKP, EXACT
             if (WAY == Way::kKeep) *flag = lost;
             else if (lost) *flag = 1;
         }
-        if constexpr (WAY == Way::kKeep) {   // the last state, for the gates' gradient
-            if (ends && a.d_state_out) {
-#pragma unroll
-                for (int s = 0; s < DKP / 16; ++s) {
-                    uint32_t sa[2][4];
-                    pack_a<2>(S.x[2 * s], S.x[2 * s + 1], sa);
-                    kept.keep_state<DKP>(kept.S, kept.S_term, unit * (chunks + 1) + chunks, col0, s, sa, g, c, true);
-                }
-            }
-        } else if (a.d_state_in && ends) S.store(a.d_state_in + unit * plane, a.dk, a.dv, col0 + g, c);
+        if (WAY == Way::kBack && a.d_state_in && ends) S.store(a.d_state_in + unit * plane, a.dk, a.dv, col0 + g, c);
     } else {
         if (lost && lane == 0) segs.lost[unit * segs.slots + segs.n * kMostColumns] = 1;   // (whichever warp of the unit's)
         if (vectors) S.store(segs.trans + at * a.dk * a.dk, a.dk, a.dk, col0 + g, c);
@@ -914,12 +905,11 @@ Kept cut_kept(char* base, long long units, int L, int dk, int dv, size_t* total)
     };
     k.dvp = (int)dvp;
     k.row_term = (long long)(units * chunks * kChunk * dvp);
-    k.S_term = (long long)(units * (chunks + 1) * dvp * dkp);
-    k.A_term = (long long)(units * chunks * dvp * dkp);
+    k.state_term = (long long)(units * chunks * dvp * dkp);
     k.w = (bf*)take(2 * k.row_term * 2);
     k.du = (bf*)take(2 * k.row_term * 2);
-    k.S = (bf*)take(2 * k.S_term * 2);
-    k.A = (bf*)take(2 * k.A_term * 2);
+    k.S = (bf*)take(2 * k.state_term * 2);
+    k.A = (bf*)take(2 * k.state_term * 2);
     k.lost_grad = (int*)take(units * chunks * 4);
     *total = at;
     return k;

@@ -6,17 +6,16 @@
 // of four lanes (eight for vectors of more than 64), the shared vectors come through shared memory, 16 or 32 tokens at a time.  A step's chain bounds
 // it (two exchanges between lanes, two passes over the column): 48 units of 196 tokens, 32 x 64 fp32, 35 us, 340 cycles a token.
 // The gradient is four such walks and nothing else:
-//   columns forwards   w, and S at the end of every 64 tokens (of the last ones where d_state_out meets it)
+//   columns forwards   w, and S at the end of every 64 tokens but the last ones
 //   columns backwards  A = what arrives at S_t from behind;  D = A + q do^T;  du = D^T k;  dv = beta du;  A <- alpha (D - beta k du^T);
 //                      and A at the end of every 64 tokens
 //   rows forwards      dq = S do,  dk'' = - beta S~ du     (S from w: u = beta w)
 //   rows backwards     dk' = D u                           (D from du)
-// and what is left per token:  dk = dk' + dk'';  dbeta = du . w;  dlog_alpha_t = E_t + .. + E_c + <S_c, A_c> with E = q . dq - v . dv and c
-// the end of the 64 tokens (replacing S by its decayed form shows <S~_t, dS~_t> = E_t + <S_t, A_t>, and <S_t, A_t> is the gradient of the
-// next token's gate), so that a long sequence's sums start anew every 64 tokens.
+// and what is left per token (finish):  dk = dk' + dk'';  dbeta = du . w;  and the gates' gradient.
 #include <type_traits>
 
 #include "gdr.h"
+#include "gdr_tile.cuh"
 #include "ptx.cuh"
 
 namespace vig {
@@ -232,7 +231,7 @@ __device__ void walk_columns(const Gdr<T>& a, const Scratch& s, float* sm, long 
             beta = beta1;
             y = y1;
         }
-        if (KEEP && !BACK && (t0 + nt == a.L ? a.d_state_out != nullptr : (t0 + nt) % kBorder == 0)) keep(s.S, (t0 + nt - 1) / kBorder);
+        if (KEEP && !BACK && (t0 + nt) % kBorder == 0 && t0 + nt < a.L) keep(s.S, (t0 + nt - 1) / kBorder);
         staged();   // the next tile
         __syncthreads();
         for (int i = tid; i < nt * owners; i += nth) {
@@ -378,71 +377,282 @@ __global__ void __launch_bounds__(256) gdr_rows_grad_kernel(Gdr<T> a, Scratch s,
     else walk_rows<T, R, G, true>(a, s, sm, blockIdx.x, blockIdx.y * owners, owners);
 }
 
-// ---- what is left per token: a block per 64 tokens of a unit -----------------------------------------------------------------
-template <typename T>
-__device__ void finish(const Gdr<T>& a, const Scratch& s, long long unit, int border) {
-    __shared__ float E[kBorder], part[16];
-    const int threads = blockDim.x, warps = threads >> 5;
-    const int t0 = border * kBorder, nt = min(kBorder, a.L - t0);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const long long plane = (long long)a.dk * a.dv, at = (unit * borders(a.L) + border) * plane;
-    float sum = 0.f;
-    const bool last = t0 + nt == a.L;
-    const float* const behind = last ? a.d_state_out ? a.d_state_out + unit * plane : nullptr : s.A + at;
-    if (behind)
-#pragma unroll 8
-        for (int i = tid; i < plane; i += threads) sum = fmaf(s.S[at + i], behind[i], sum);
+// ---- what is left per token: a block of 256 threads per 64 tokens of a unit ---------------------------------------------------
+// A gate's gradient <dS~_t, S~_t> is the sum over everything that passes through the gate: with S in front of the 64 tokens, A behind them, b the running sum
+// of the log gates in them and Gam_rs = e^{b_r - b_s},
+//   dlog_alpha_t = e^{b_64} <S, A> + sum_{r >= t} F_r + sum_{s < t} G_s + sum_{s < t <= r} H_rs
+//   F_r = e^{b_r} (q_r . S do_r - beta_r k_r . S du_r)     G_s = e^{b_64 - b_s} k_s . A u_s
+//   H_rs = Gam_rs ((q_r . k_s) (do_r . u_s) - beta_r (k_r . k_s) (du_r . u_s))
+// Every term has the gate's own factor in it and nothing is subtracted that it does not contain.  (Running sums of q . dq - v . dv, which is the same
+// by algebra, are differences of terms without that factor: at log_alpha = -12 nothing but their rounding was left.)
+// 64 tokens of 32 x 64 are 0.8 M multiplications, products of 64 x 64 a slice of 32 dimensions at a time, in 256 threads: 48 units
+// of 196 tokens 37 us, the multiplications themselves.
+constexpr int kSlice = 32, kPitch = kBorder + 4;
+struct FinishShared {
+    union {
+        __align__(16) float stage[4][kSlice][kPitch];   // [dimension][token or column]
+        float H[kBorder][kBorder + 1];                  // rows r, columns s
+    };
+    float bh[kBorder], bl[kBorder], beta[kBorder], F[kBorder], G[kBorder], part[8];
+};
+
+// to[dimension][token] of `kSlice` dimensions from e0 on: value(t, e), n tokens of `width` values.
+template <typename F>
+__device__ __forceinline__ void stage_slice(float (&to)[kSlice][kPitch], int n, int e0, int width, F value) {
+    constexpr int kEach = kSlice * kBorder / 256;
+    const int e = threadIdx.x % kSlice, t = threadIdx.x / kSlice;
+    float x[kEach];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) part[warp] = sum;
+    for (int p = 0; p < kEach; ++p) x[p] = value(min(t + p * 8, n - 1), min(e0 + e, width - 1));   // (all of them at once, none behind a branch)
+#pragma unroll
+    for (int p = 0; p < kEach; ++p) to[e][t + p * 8] = t + p * 8 < n && e0 + e < width ? x[p] : 0.f;
+}
+
+// The same of a state [dk][dv] (null: zeros), 64 columns from j0 on.
+__device__ __forceinline__ void stage_state(float (&to)[kSlice][kPitch], const float* S, int e0, int j0, int dk, int dv) {
+    constexpr int kEach = kSlice * kBorder / 256;
+    const int e = threadIdx.x / kBorder, j = threadIdx.x % kBorder;
+    float x[kEach];
+    if (S)
+#pragma unroll
+        for (int p = 0; p < kEach; ++p) x[p] = S[(long long)min(e0 + e + p * 4, dk - 1) * dv + min(j0 + j, dv - 1)];
+#pragma unroll
+    for (int p = 0; p < kEach; ++p) to[e + p * 4][j] = S && e0 + e + p * 4 < dk && j0 + j < dv ? x[p] : 0.f;
+}
+
+// RT: rows of a thread, sixteen of them in a column of the block; tokens in front of 16 RT.
+template <typename T, int RT>
+__device__ void gate_gradient(const Gdr<T>& a, const Scratch& s, FinishShared& m, long long unit, int t0, int nt, const float* S, const float* A) {
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, r0 = ty * RT, s0 = tx * 4;
+    auto at = [&](int t) { return a.row(unit, t0 + t); };
+    auto sum = [&](int t) { return gdr::Sum{m.bh[t], m.bl[t]}; };
+    auto cols = [&](const float (&x)[kSlice][kPitch], int e, f32x2 (&y)[2]) {   // two values an instruction
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&x[e][s0]);
+        y[0] = v.x;
+        y[1] = v.y;
+    };
+    auto add = [&](f32x2 (&acc)[RT][2], const float (&x)[RT], const f32x2 (&y)[2]) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const f32x2 xx = pack2(x[r], x[r]);
+            acc[r][0] = ffma2(xx, y[0], acc[r][0]);
+            acc[r][1] = ffma2(xx, y[1], acc[r][1]);
+        }
+    };
+    auto each = [&](const f32x2 (&acc)[RT][2], float (&y)[RT][4]) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            unpack2(acc[r][0], y[r][0], y[r][1]);
+            unpack2(acc[r][1], y[r][2], y[r][3]);
+        }
+    };
+    auto rows = [&](const float (&x)[kSlice][kPitch], int e, float (&y)[RT]) {
+        if constexpr (RT == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(&x[e][r0]);
+            y[0] = v.x; y[1] = v.y; y[2] = v.z; y[3] = v.w;
+        } else y[0] = x[e][r0];
+    };
+    float f[RT] = {}, g[RT] = {};
+    for (int j0 = 0; j0 < a.dv && (S || A); j0 += kBorder) {   // q S, k S and k A, 64 columns at a time
+        f32x2 qs2[RT][2] = {}, ks2[RT][2] = {}, ka2[RT][2] = {};
+        for (int e0 = 0; e0 < a.dk; e0 += kSlice) {
+            __syncthreads();
+            stage_slice(m.stage[0], nt, e0, a.dk, [&](int t, int e) { return to_f(a.k[at(t) * a.ldk + e]); });
+            stage_slice(m.stage[1], nt, e0, a.dk, [&](int t, int e) { return to_f(a.q[at(t) * a.ldk + e]); });
+            stage_state(m.stage[2], S, e0, j0, a.dk, a.dv);
+            stage_state(m.stage[3], A, e0, j0, a.dk, a.dv);
+            __syncthreads();
+            if (r0 < nt)
 #pragma unroll 2
-    for (int t = warp; t < nt; t += warps) {
-        const long long r = a.row(unit, t0 + t);
-        const float beta = to_f(a.beta[r]);
-        float e = 0.f, db = 0.f;
-        for (int i = lane; i < a.dk; i += 32) {
-            const float dq = s.dq[r * a.dk + i];
-            e = fmaf(to_f(a.q[r * a.ldk + i]), dq, e);
-            if constexpr (sizeof(T) == 2) a.dq[r * a.ldk + i] = from_f<T>(dq);
-            a.dk_out[r * a.ldk + i] = from_f<T>(s.dk1[r * a.dk + i] + s.dk2[r * a.dk + i]);
+                for (int i = 0; i < kSlice; ++i) {
+                    float k[RT], q[RT];
+                    f32x2 c[2], d[2];
+                    rows(m.stage[0], i, k);
+                    rows(m.stage[1], i, q);
+                    cols(m.stage[2], i, c);
+                    cols(m.stage[3], i, d);
+                    add(qs2, q, c);
+                    add(ks2, k, c);
+                    add(ka2, k, d);
+                }
         }
-        for (int i = lane; i < a.dv; i += 32) {
-            const float du = s.du[r * a.dv + i];
-            db = fmaf(du, s.w[r * a.dv + i], db);
-            e = fmaf(-beta * du, to_f(a.v[r * a.ldv + i]), e);
-        }
+        float qs[RT][4], ks[RT][4], ka[RT][4];
+        each(qs2, qs);
+        each(ks2, ks);
+        each(ka2, ka);
+        if (r0 < nt)
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            e += __shfl_xor_sync(0xffffffffu, e, o);
-            db += __shfl_xor_sync(0xffffffffu, db, o);
+            for (int i = 0; i < RT; ++i) {
+                const long long r = at(min(r0 + i, nt - 1));
+                const float beta = m.beta[r0 + i];
+                float o[4], d[4], w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = min(j0 + s0 + j, a.dv - 1);
+                    o[j] = to_f(a.d_out[r * a.ldv + c]);
+                    d[j] = s.du[r * a.dv + c];
+                    w[j] = s.w[r * a.dv + c];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool in = j0 + s0 + j < a.dv;
+                    f[i] = in ? fmaf(qs[i][j], o[j], fmaf(-beta * ks[i][j], d[j], f[i])) : f[i];
+                    g[i] = in ? fmaf(ka[i][j], beta * w[j], g[i]) : g[i];
+                }
+            }
+    }
+    const gdr::Sum end = sum(kBorder - 1);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) {
+            f[i] += __shfl_xor_sync(0xffffffffu, f[i], o);
+            g[i] += __shfl_xor_sync(0xffffffffu, g[i], o);
         }
-        if (lane == 0) {
-            E[t] = e;
-            a.dbeta[r] = from_f<T>(db);
+        if (tx == 0 && r0 + i < nt) {
+            const gdr::Sum b = sum(r0 + i);
+            m.F[r0 + i] = ex2(b.h + b.l) * f[i];
+            m.G[r0 + i] = ex2(end.to(b)) * g[i];
+        }
+    }
+    float meet = 0.f;
+    if (S && A)
+#pragma unroll 8
+        for (int i = tid; i < a.dk * a.dv; i += 256) meet = fmaf(S[i], A[i], meet);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) meet += __shfl_xor_sync(0xffffffffu, meet, o);
+    if ((tid & 31) == 0) m.part[tid >> 5] = meet;
+    // H
+    const bool mine = r0 < nt && s0 < r0 + RT;
+    f32x2 qk2[RT][2] = {}, kk2[RT][2] = {}, x2[RT][2] = {}, e2[RT][2] = {};
+    for (int e0 = 0; e0 < a.dk; e0 += kSlice) {
+        __syncthreads();
+        stage_slice(m.stage[0], nt, e0, a.dk, [&](int t, int e) { return to_f(a.k[at(t) * a.ldk + e]); });
+        stage_slice(m.stage[1], nt, e0, a.dk, [&](int t, int e) { return to_f(a.q[at(t) * a.ldk + e]); });
+        __syncthreads();
+        if (mine)
+#pragma unroll 2
+            for (int i = 0; i < kSlice; ++i) {
+                float k[RT], q[RT];
+                f32x2 c[2];
+                rows(m.stage[0], i, k);
+                rows(m.stage[1], i, q);
+                cols(m.stage[0], i, c);
+                add(qk2, q, c);
+                add(kk2, k, c);
+            }
+    }
+    for (int e0 = 0; e0 < a.dv; e0 += kSlice) {
+        __syncthreads();
+        stage_slice(m.stage[0], nt, e0, a.dv, [&](int t, int e) { return to_f(a.d_out[at(t) * a.ldv + e]); });
+        stage_slice(m.stage[1], nt, e0, a.dv, [&](int t, int e) { return s.du[at(t) * a.dv + e]; });
+        stage_slice(m.stage[2], nt, e0, a.dv, [&](int t, int e) { return s.w[at(t) * a.dv + e]; });
+        __syncthreads();
+        if (mine)
+#pragma unroll 2
+            for (int i = 0; i < kSlice; ++i) {
+                float g[RT], d[RT];
+                f32x2 c[2];
+                rows(m.stage[0], i, g);
+                rows(m.stage[1], i, d);
+                cols(m.stage[2], i, c);
+                add(x2, g, c);
+                add(e2, d, c);
+            }
+    }
+    __syncthreads();
+    float qk[RT][4], kk[RT][4], x[RT][4], e[RT][4];
+    each(qk2, qk);
+    each(kk2, kk);
+    each(x2, x);
+    each(e2, e);
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = r0 + i, c = s0 + j;
+            // (a step of zero has no u, whatever its w)
+            m.H[r][c] = c < r && r < nt && m.beta[c] != 0.f ? ex2(sum(r).to(sum(c))) * m.beta[c] * fmaf(x[i][j], qk[i][j], -m.beta[r] * e[i][j] * kk[i][j]) : 0.f;
+            if (c == r && r < nt) a.dbeta[at(r)] = from_f<T>(e[i][j]);   // du . w
+        }
+    __syncthreads();
+    if (tid < nt) {   // a row's sums up to each of its columns
+        float run = 0.f;
+        for (int c = 0; c <= tid; c += 8) {   // (zeros behind the diagonal)
+            float h[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = m.H[tid][c + i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                m.H[tid][c + i] = run;
+                run += h[i];
+            }
         }
     }
     __syncthreads();
-    // sums from the border; a gate that leaves nothing (what the sums come to there is rounding), or that has nothing to scale (the first of a
-    // sequence without an initial state), has none, and they start anew there
-    if (warp == 0) {
-        float run = 0.f;
-        for (int w = 0; w < warps; ++w) run += part[w];
-        float mine[2];
-        bool stop[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int t = 2 * lane + h;
-            stop[h] = t < nt && (expf(to_f(a.la[a.row(unit, t0 + t)])) == 0.f || (t0 + t == 0 && !a.state_in));
-            mine[h] = t < nt && !stop[h] ? E[t] : 0.f;
-        }
-        run = suffix_of_pairs(mine, stop, run);
-        if (2 * lane + 1 < nt) a.dla[a.row(unit, t0 + 2 * lane + 1)] = from_f<T>(run = stop[1] ? 0.f : mine[1] + run);
-        if (2 * lane < nt) a.dla[a.row(unit, t0 + 2 * lane)] = from_f<T>(stop[0] ? 0.f : mine[0] + run);
+    if (tid < nt) {
+        float through = 0.f, x = 0.f;
+        for (int w = 0; w < 8; ++w) through += m.part[w];
+#pragma unroll 8
+        for (int c = 0; c < tid; ++c) x += m.G[c];
+#pragma unroll 8
+        for (int r = tid; r < nt; ++r) x += m.F[r] + m.H[r][tid];
+        a.dla[at(tid)] = from_f<T>(fmaf(through, ex2(end.h + end.l), x));
     }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(512) gdr_finish_kernel(Gdr<T> a, Scratch s) {
+__device__ void finish(const Gdr<T>& a, const Scratch& s, long long unit, int border) {
+    __shared__ FinishShared m;
+    const int t0 = border * kBorder, nt = min(kBorder, a.L - t0);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const long long plane = (long long)a.dk * a.dv, at = unit * borders(a.L) + border;
+    if (warp == 0) {
+        float la[2], be[2];
+        gdr::Sum b[2], all;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int t = 2 * lane + h;
+            la[h] = t < nt ? to_f(a.la[a.row(unit, t0 + t)]) : 0.f;
+            be[h] = t < nt ? to_f(a.beta[a.row(unit, t0 + t)]) : 0.f;
+        }
+        gdr::gate_sums(la, b, all);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            m.bh[2 * lane + h] = b[h].h;
+            m.bl[2 * lane + h] = b[h].l;
+            m.beta[2 * lane + h] = be[h];
+        }
+    }
+    // dk = dk' + dk'', and dq where it is not the call's own yet: rows of the block in a row, four values a thread at a time
+    const long long first = min(a.row(unit, t0), a.row(unit, t0 + nt - 1));
+    for (int i0 = tid; i0 < nt * a.dk; i0 += 4 * 256) {
+        float x[4], y[4], q[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const long long i = first * a.dk + min(i0 + p * 256, nt * a.dk - 1);
+            x[p] = s.dk1[i];
+            y[p] = s.dk2[i];
+            if constexpr (sizeof(T) == 2) q[p] = s.dq[i];
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const int i = i0 + p * 256, t = i / a.dk;
+            if (i >= nt * a.dk) break;
+            const long long to = (first + t) * a.ldk + i - t * a.dk;
+            a.dk_out[to] = from_f<T>(x[p] + y[p]);
+            if constexpr (sizeof(T) == 2) a.dq[to] = from_f<T>(q[p]);
+        }
+    }
+    __syncthreads();
+    const float* const front = border > 0 ? s.S + (at - 1) * plane : a.state_in ? a.state_in + unit * plane : nullptr;
+    const float* const behind = t0 + nt < a.L ? s.A + at * plane : a.d_state_out ? a.d_state_out + unit * plane : nullptr;
+    if (nt <= 16) gate_gradient<T, 1>(a, s, m, unit, t0, nt, front, behind);
+    else gate_gradient<T, 4>(a, s, m, unit, t0, nt, front, behind);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256, 2) gdr_finish_kernel(Gdr<T> a, Scratch s) {
     pdl_wait();
     pdl_launch_dependents();
     finish<T>(a, s, blockIdx.x / borders(a.L), blockIdx.x % borders(a.L));
@@ -600,7 +810,7 @@ cudaError_t launch_gdr_walk_bwd(const Gdr<T>& a, void* scratch, cudaStream_t str
     });
     if (e != cudaSuccess) return e;
     count_launch(3);
-    return launch_pdl(gdr_finish_kernel<T>, dim3((unsigned)(a.units * borders(a.L))), dim3(512), 0, stream, a, s);
+    return launch_pdl(gdr_finish_kernel<T>, dim3((unsigned)(a.units * borders(a.L))), dim3(256), 0, stream, a, s);
 }
 
 size_t gdr_repair_slot_bytes(int L, int dk, int dv) { return gdr_walk_bwd_scratch_bytes<__nv_bfloat16>(1, L, dk, dv); }
