@@ -181,18 +181,6 @@ __device__ __forceinline__ void over_pairs(int c, int g, int per, F f) {   // g:
 // A warp per group straight away took 3400 cycles of a block's 20000.)
 constexpr size_t on_chip_floats(int lanes, int slab, int groups) { return 2 * ((size_t)lanes * slab + (1 + kMostBlocks) * groups + (slab > kThreads ? slab : kThreads)); }
 
-// (n values, their mean m, their sum of squares about it q) of all lanes, joined.
-__device__ __forceinline__ void join_warp(float& n, float& m, float& q) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const float n2 = __shfl_xor_sync(0xffffffffu, n, o), m2 = __shfl_xor_sync(0xffffffffu, m, o), q2 = __shfl_xor_sync(0xffffffffu, q, o);
-        const float s = n + n2, f = s > 0.f ? n2 / s : 0.f, d = m2 - m;
-        q += fmaf(d * d, n * f, q2);
-        m = fmaf(d, f, m);
-        n = s;
-    }
-}
-
 // A vector's channels in the gradient.
 template <typename T>
 struct Channels {
@@ -586,26 +574,56 @@ __global__ void __launch_bounds__(kThreads) norm_stats_kernel(Norm<T> a) {
         a.part[(long long)blockIdx.x * a.C + c0 + c] = make_float2(m, q);
     }
 }
-// A warp per image and group: joins the chunks' channels.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) norm_join_kernel(Norm<T> a, int chunks, long long total) {
+// Chunks' channels of an image's group joined by W threads: a warp, or a block where the entries (chunks x channels of the group) are many.  (A warp for any
+// number of them, a chain of divisions: 1450 us for 1 x 56 x 56 x 768 in one group, 150000 entries.)
+constexpr int kJoinWide = 1024;
+constexpr long long kJoinWarp = 2048;   // entries that a warp takes
+template <int W>
+__device__ __forceinline__ float join_sum(float x, float* red) {   // over the W threads, in all of them
+    x = warp_sum(x);
+    if constexpr (W > 32) {
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+        __syncthreads();
+        x = warp_sum(red[threadIdx.x & 31]);
+    }
+    return x;
+}
+// f(chunk, channel of the group) for every W-th entry.
+template <int W, typename F>
+__device__ __forceinline__ void over_entries(int chunks, int per, F f) {
+    int chunk = (threadIdx.x % W) / per, c = (threadIdx.x % W) - chunk * per;
+    const int chunk_step = W / per, c_step = W - chunk_step * per;
+#pragma unroll 4
+    while (chunk < chunks) {
+        f(chunk, c);
+        chunk += chunk_step;
+        c += c_step;
+        if (c >= per) {
+            c -= per;
+            ++chunk;
+        }
+    }
+}
+// Mean first, then the squares about it.
+template <typename T, int W>
+__global__ void __launch_bounds__(W > 32 ? W : kThreads) norm_join_kernel(Norm<T> a, int chunks, long long total) {
+    __shared__ float red[32];
     pdl_wait();
     pdl_launch_dependents();
-    const long long at = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    if (at >= total) return;
-    const int lane = threadIdx.x & 31, G = a.C / a.per;
+    const long long at = W > 32 ? blockIdx.x : (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    if (at >= total) return;   // (whole warps; never where a block is at it)
+    const int lane = threadIdx.x % W, G = a.C / a.per;
     const long long b = at / G;
-    const int c0 = (int)(at % G) * a.per;
-    float n = 0.f, m = 0.f, q = 0.f;
-    for (long long i = lane; i < (long long)chunks * a.per; i += 32) {
-        const int chunk = (int)(i / a.per);
-        const float2 p = a.part[(b * chunks + chunk) * a.C + c0 + i % a.per];
-        const float k = (float)min(a.rows, a.HW - chunk * a.rows), dm = p.x - m, share = k / (n + k);
-        q += fmaf(dm * dm, share * n, p.y);
-        m = fmaf(dm, share, m);
-        n += k;
-    }
-    join_warp(n, m, q);
+    const float2* const part = a.part + b * chunks * a.C + at % G * a.per;
+    auto over = [&](auto f) {   // sum of f(values of the entry, the entry)
+        float x = 0.f;
+        over_entries<W>(chunks, a.per, [&](int chunk, int c) { x += f((float)min(a.rows, a.HW - chunk * a.rows), part[(long long)chunk * a.C + c]); });
+        return join_sum<W>(x, red);
+    };
+    const float n = (float)a.HW * a.per;
+    const float m = over([](float k, float2 p) { return k * p.x; }) / n;
+    const float q = over([m](float k, float2 p) { return fmaf(k * (p.x - m), p.x - m, p.y); });
     if (lane == 0) {
         a.mean[at] = m;
         a.rstd[at] = rsqrtf(q / n + a.eps);
@@ -720,26 +738,27 @@ __global__ void __launch_bounds__(kThreads) norm_grad_chunk_kernel(Norm<T> a, co
         }
     }
 }
-// A warp per image and group: means of g w and g w xhat.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) norm_grad_join_kernel(Norm<T> a, float2* means, int chunks, long long total) {
+// Means of g w and g w xhat of an image's group, by W threads as above.
+template <typename T, int W>
+__global__ void __launch_bounds__(W > 32 ? W : kThreads) norm_grad_join_kernel(Norm<T> a, float2* means, int chunks, long long total) {
+    __shared__ float red[32];
     pdl_wait();
     pdl_launch_dependents();
-    const long long at = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const long long at = W > 32 ? blockIdx.x : (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     if (at >= total) return;
-    const int lane = threadIdx.x & 31, G = a.C / a.per;
+    const int lane = threadIdx.x % W, G = a.C / a.per;
     const long long b = at / G;
     const int c0 = (int)(at % G) * a.per;
+    const float2* const part = a.part + b * chunks * a.C + c0;
     float u = 0.f, v = 0.f;
-    for (long long i = lane; i < (long long)chunks * a.per; i += 32) {
-        const int c = c0 + (int)(i % a.per);
-        const float2 p = a.part[(b * chunks + i / a.per) * a.C + c];
-        const float w = one(a.weight, c, 1.f);
+    over_entries<W>(chunks, a.per, [&](int chunk, int c) {
+        const float2 p = part[(long long)chunk * a.C + c];
+        const float w = one(a.weight, c0 + c, 1.f);
         u = fmaf(p.x, w, u);
         v = fmaf(p.y, w, v);
-    }
-    u = warp_sum(u);
-    v = warp_sum(v);
+    });
+    u = join_sum<W>(u, red);
+    v = join_sum<W>(v, red);
     const float inv = 1.f / ((float)a.HW * a.per);
     if (lane == 0) means[at] = make_float2(u * inv, v * inv);
 }
@@ -894,7 +913,9 @@ cudaError_t launch_group_norm(const T* x, const T* weight, const T* bias, T* out
     const dim3 grid((unsigned)((long long)p.chunks * B), 1, p.slabs);
     cudaError_t e = launch_pdl(norm_stats_kernel<T>, grid, dim3(kThreads), 2 * kThreads * V * 4, stream, a);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(norm_join_kernel<T>, dim3((unsigned)((total + 7) / 8)), dim3(kThreads), 0, stream, a, p.chunks, total);
+    e = (long long)p.chunks * a.per > kJoinWarp
+            ? launch_pdl(norm_join_kernel<T, kJoinWide>, dim3((unsigned)total), dim3(kJoinWide), 0, stream, a, p.chunks, total)
+            : launch_pdl(norm_join_kernel<T, 32>, dim3((unsigned)((total + 7) / 8)), dim3(kThreads), 0, stream, a, p.chunks, total);
     if (e != cudaSuccess) return e;
     count_launch(3);
     return with_act(act, [&](auto A) { return launch_pdl(norm_apply_kernel<T, decltype(A)::value>, grid, dim3(kThreads), 0, stream, a); });
@@ -926,7 +947,9 @@ cudaError_t launch_group_norm_bwd(const T* x, const T* weight, const T* bias, co
             constexpr int kAct = decltype(A)::value;
             cudaError_t r = launch_pdl(norm_grad_chunk_kernel<T, kAct, true>, grid, dim3(kThreads), 2 * kThreads * V * 4, stream, a, nullptr);
             if (r == cudaSuccess)
-                r = launch_pdl(norm_grad_join_kernel<T>, dim3((unsigned)((total + 7) / 8)), dim3(kThreads), 0, stream, a, means, p.chunks, total);
+                r = (long long)p.chunks * a.per > kJoinWarp
+                        ? launch_pdl(norm_grad_join_kernel<T, kJoinWide>, dim3((unsigned)total), dim3(kJoinWide), 0, stream, a, means, p.chunks, total)
+                        : launch_pdl(norm_grad_join_kernel<T, 32>, dim3((unsigned)((total + 7) / 8)), dim3(kThreads), 0, stream, a, means, p.chunks, total);
             if (r == cudaSuccess) r = launch_pdl(norm_grad_chunk_kernel<T, kAct, false>, grid, dim3(kThreads), 0, stream, a, means);
             count_launch(3);
             return r;
