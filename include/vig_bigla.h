@@ -242,7 +242,7 @@ int vig_gate_prep_bwd_f32(const void* g_fwd, const void* g_bwd, const void* dlog
  *       Sizes that are no multiples of eight are laid out again in scratch on the way in and out.  Columns of the state
  *       that grow 2^15-fold within a chunk, which needs beta_t |k_t|^2 > 2, or are not finite are computed by fp32 walks inside the call.  Long
  *       sequences of few units are cut into segments that run side by side, with scratch from the library's pool.
- * f32:  fp32 walks on the CUDA cores.  dk <= 128, dv <= 256 for either type.
+ * f32:  fp32 walks on the CUDA cores.  dk <= 128, dv <= 256, L <= 2^31 - 2^16 for either type.
  * L == 0 with a state_out copies state_in (or zeros) there; tensors without elements may be NULL.
  * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
 int vig_gdr_fwd_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
@@ -276,7 +276,7 @@ int vig_gdr_step_f32(const void* q, const void* k, const void* v, const void* lo
  * the population) over Hh x Ww x C / groups,  out = act((x - mean) / sqrt(var + eps) * weight + bias).
  * x, out: [B, Hh, Ww, C]; weight, bias: [C] or NULL (1, 0); all of the call's element type.  mean, rstd: FP32 [B, groups], what the
  * gradient needs, or NULL.  act: a vig_act (GELU is the exact one, by erf).  eps >= 0.  C must be a multiple of 8 (bf16) or 4 (fp32), at
- * most 2^20, and of groups.  out may be x.  Images too large to stay on chip take scratch from the library's pool, stream-ordered.
+ * most 2^20, and of groups; Hh Ww at most 2^31 - 2^16.  out may be x.  Images too large to stay on chip take scratch from the library's pool, stream-ordered.
  * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
 typedef enum vig_act { VIG_ACT_NONE = 0, VIG_ACT_SILU = 1, VIG_ACT_GELU = 2 } vig_act;
 int vig_group_norm_bf16(const void* x, const void* weight, const void* bias, void* out, void* mean, void* rstd,

@@ -23,11 +23,13 @@ int pass_state(const void* in, void* out, long long units, int dk, int dv, cudaS
     return status_of(in ? cudaMemcpyAsync(out, in, bytes, cudaMemcpyDeviceToDevice, stream) : cudaMemsetAsync(out, 0, bytes, stream));
 }
 
+constexpr int kMostRows = 0x7fffffff - 0xffff;   // tokens or pixels
+
 int check_sizes(int B, int H, int L, int dk, int dv) {
     if (B < 0 || H < 0 || L < 0 || dk < 1 || dv < 1) return VIG_ERR_BAD_DIM;
     if (!gdr_supported(dk, dv)) return VIG_ERR_UNSUPPORTED;
-    // grids count units, or units times pieces of 64 tokens
-    if ((long long)B * H * (L / 64 + 1LL) > 0x7fffffffLL) return VIG_ERR_UNSUPPORTED;
+    // grids count units, or units times pieces of 64 tokens; tokens are counted in 32 bits up to the end of their last piece
+    if (L > kMostRows || (long long)B * H * (L / 64 + 1LL) > 0x7fffffffLL) return VIG_ERR_UNSUPPORTED;
     return VIG_OK;
 }
 
@@ -200,7 +202,7 @@ int gdr_step_impl(const void* q, const void* k, const void* v, const void* la, c
 int check_norm(int B, int Hh, int Ww, int C, int groups, int act, size_t elem) {
     if (B < 0 || Hh < 0 || Ww < 0 || C < 1 || groups < 1) return VIG_ERR_BAD_DIM;
     if (act != VIG_ACT_NONE && act != VIG_ACT_SILU && act != VIG_ACT_GELU) return VIG_ERR_UNSUPPORTED;
-    if ((long long)Hh * Ww > 0x7fffffffLL || !group_norm_supported(B, Hh * Ww, C, groups, elem)) return VIG_ERR_UNSUPPORTED;
+    if ((long long)Hh * Ww > kMostRows || !group_norm_supported(B, Hh * Ww, C, groups, elem)) return VIG_ERR_UNSUPPORTED;
     return VIG_OK;
 }
 
