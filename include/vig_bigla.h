@@ -240,7 +240,7 @@ int vig_gate_prep_bwd_f32(const void* g_fwd, const void* g_bwd, const void* dlog
  * bf16: chunks of 64 tokens on the tensor cores (what is computed enters products as sums of bf16 terms: sixteen significant bits, 24 where a final
  *       state is asked for, with the range of fp32; sums and states fp32); a handful of tokens, and the gradient of more than 128 value columns, as fp32 walks on the CUDA cores.
  *       Sizes that are no multiples of eight are laid out again in scratch on the way in and out.  Columns of the state
- *       that grow 2^15-fold within a chunk, which needs beta_t |k_t|^2 > 2, or are not finite are computed by fp32 walks inside the call.  Long
+ *       that outgrow what a chunk takes in 512-fold, which needs beta_t |k_t|^2 > 2, or are not finite are computed by fp32 walks inside the call.  Long
  *       sequences of few units are cut into segments that run side by side, with scratch from the library's pool.
  * f32:  fp32 walks on the CUDA cores.  dk <= 128, dv <= 256, L <= 2^31 - 2^16 for either type.
  * L == 0 with a state_out copies state_in (or zeros) there; tensors without elements may be NULL.

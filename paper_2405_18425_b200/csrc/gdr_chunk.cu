@@ -407,8 +407,8 @@ __device__ __forceinline__ void times_block(float (&acc)[2][4], const uint32_t (
 
 // How far a column's U (backwards dU) may outgrow what goes into the chunk before it is walked step by step instead.  With beta |k|^2 <= 2 a token's
 // transition has norm at most one, which bounds a column's |u| by (129 + dk) beta (|v| + |k| |S|) and its |du| by dk |k| (|A| + 64 |q| |do|), with the chunk's
-// largest elements of each; beyond, the chunk's triangular systems cancel digits that the steps keep.
-constexpr float kGrowth = 32768.f;
+// largest elements of each.  Beyond, later tokens may take off again what has grown: of the sums' sixteen bits (24 for states) nine are given away here.
+constexpr float kGrowth = 512.f;
 
 // One chunk of NS strips forwards.  False where a column of this lane grew too far or is not finite.
 template <int DKP, bool EXACT, Way WAY, int NS>
@@ -570,7 +570,7 @@ __device__ __forceinline__ bool backward_chunk(State<DKP>& A, const Gdr<bf>& a, 
         const float k = fmaxf(fmaxf(k4.x, k4.y), fmaxf(k4.z, k4.w)), q = fmaxf(fmaxf(q4.x, q4.y), fmaxf(q4.z, q4.w));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float x = fmaf(q, largest_of(dm[h]), largest_of(am[h]));
+            float x = fmaf(64.f * q, largest_of(dm[h]), largest_of(am[h]));
 #pragma unroll
             for (int o = 1; o < 4; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
             limit[h] = x * k * kGrowth;

@@ -127,3 +127,28 @@ def test_rows_of_the_state_of_very_different_size(size):
     for t in range(size[2]):
         for name, g, w in zip(GRADS[:3], got, want):
             assert off(g[:, :, t], w[:, :, t]) <= 2.0 ** -7, (name, t)
+
+
+@pytest.mark.parametrize("n", [4, 6, 8, 9])
+@pytest.mark.parametrize("size", [(1, 3, 40, 16, 32), (1, 2, 100, 48, 64), (1, 2, 900, 16, 40)], ids=str)
+def test_growth_that_is_undone(size, n):
+    """n steps with beta |k|^2 = 4 along an axis (a row of the state times -3 each), then one of beta = |k| = 1 that replaces the row by its value exactly: up to
+    2e4 is taken off again.  What the steps leave in fp32 is 2^-24 of that, 1e-3 of the value, and as much for the results' own rounding: 2^-7 as everywhere."""
+    for at in (5, 20):
+        d = gdr_inputs(*size, "bf16", seed=46, gate_mean=4.0, states=True)
+        run = slice(at, at + n + 1)
+        d["k"][:, :, run] = 0
+        d["k"][:, :, run, 0] = 2
+        d["k"][:, :, at + n, 0] = 1
+        d["beta"][:, :, run] = 1
+        d["log_alpha"][:, :, run] = 0
+        d["q"][:, :, at + n:at + n + 4] = 0
+        d["q"][:, :, at + n:at + n + 4, 0] = 1
+        ref, ref_last = gdr_oracle(d)
+        for state_out in (False, True):
+            out, last = gdr_forward(d, state_out=state_out)
+            for t in range(size[2]):
+                assert off(out[:, :, t], ref[:, :, t]) <= 2.0 ** -7, (at, t, state_out, off(out[:, :, t], ref[:, :, t]))
+        got, want = gdr_gradient(d), gdr_oracle_gradient(d)
+        for name, g, w in zip(GRADS, got, want):
+            assert off(g, w) <= 2.0 ** -7, (name, at)
