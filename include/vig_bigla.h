@@ -238,11 +238,14 @@ int vig_gate_prep_bwd_f32(const void* g_fwd, const void* g_bwd, const void* dlog
  * reverse != 0: the same from the last token to the first (state_in comes behind token L, state_out is what stands at token 1), the
  * other direction of a bidirectional mixer over the patch sequence.
  * bf16: chunks of 64 tokens on the tensor cores (what is computed enters products as sums of bf16 terms: sixteen significant bits, 24 where a final
- *       state is asked for, with the range of fp32; sums and states fp32); a handful of tokens, and the gradient of more than 128 value columns, as fp32 walks on the CUDA cores.
+ *       state is asked for, with the range of fp32; sums and states fp32); up to eight tokens (in the gradient two, of few units), and the gradient of more than
+ *       128 value columns, as fp32 walks on the CUDA cores.
  *       Sizes that are no multiples of eight are laid out again in scratch on the way in and out.  Columns of the state
  *       that outgrow what a chunk takes in 512-fold, which needs beta_t |k_t|^2 > 2, or are not finite are computed by fp32 walks inside the call.  Long
  *       sequences of few units are cut into segments that run side by side, with scratch from the library's pool.
  * f32:  fp32 walks on the CUDA cores.  dk <= 128, dv <= 256, L <= 2^31 - 2^16 for either type.
+ * The form (walks, segments) depends on B * H and L too, and with it the last bits of a unit's results: the same call repeats them, a call of other
+ * units beside it may not.
  * L == 0 with a state_out copies state_in (or zeros) there; tensors without elements may be NULL.
  * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
 int vig_gdr_fwd_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
@@ -254,8 +257,8 @@ int vig_gdr_fwd_f32(const void* q, const void* k, const void* v, const void* log
 /* Its gradient.  d_out: [B,H,L,dv]; d_state_out: gradient with respect to state_out (fp32) or NULL for zero.  Writes dq, dk_out
  * [B,H,L,dk], dv_out [B,H,L,dv], dlog_alpha, dbeta [B,H,L] and, unless it is NULL, d_state_in (fp32; may be d_state_out).  Everything is
  * computed anew from the inputs; scratch comes from the library's pool, stream-ordered: about 8 dv + dk dv / 8 bytes a token and head in chunks
- * (sizes to multiples of sixteen; 8 dk + 6 dv more where they are no multiples of eight, and the segments' states), 8 dv + 12 dk + dk dv / 8 as walks, and up to 64 MB (or one unit's walks) for units that the chunks leave to them.  Outputs must not
- * overlap inputs or one another.  Errors: as vig_gdr_fwd_*. */
+ * (sizes to multiples of sixteen; 8 dk + 6 dv more where they are no multiples of eight, and the segments' states), 8 dv + 12 dk + dk dv / 8 as
+ * walks, and up to 64 MB (or one unit's walks) for units that the chunks leave to them.  Outputs must not overlap inputs or one another.  Errors: as vig_gdr_fwd_*. */
 int vig_gdr_bwd_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
                      const void* state_in, const void* d_out, const void* d_state_out,
                      void* dq, void* dk_out, void* dv_out, void* dlog_alpha, void* dbeta, void* d_state_in,
@@ -265,7 +268,7 @@ int vig_gdr_bwd_f32(const void* q, const void* k, const void* v, const void* log
                     void* dq, void* dk_out, void* dv_out, void* dlog_alpha, void* dbeta, void* d_state_in,
                     int B, int H, int L, int dk, int dv, int reverse, void* stream);
 /* One token per unit: q, k [B,H,dk], v, out [B,H,dv], log_alpha, beta [B,H]; state (fp32 [B,H,dk,dv]) is updated in place.
- * The same arithmetic as a call of L = 1 in fp32.  Errors: as vig_gdr_fwd_*. */
+ * In fp32 inside for either type, reading out by alpha q S + (q . k) u, of the state as it was.  Errors: as vig_gdr_fwd_*. */
 int vig_gdr_step_bf16(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,
                       void* state, void* out, int B, int H, int dk, int dv, void* stream);
 int vig_gdr_step_f32(const void* q, const void* k, const void* v, const void* log_alpha, const void* beta,

@@ -34,14 +34,14 @@ int check_sizes(int B, int H, int L, int dk, int dv) {
 }
 
 // bf16: chunks on the tensor cores, or walks.  A chunk costs its set-up whatever it holds, a walk its tokens: 1500 units of 64 x 64, forward, tiles and walks
-// us: 2 tokens 29, 21; 8 tokens 29, 33; 128 x 128: 8 tokens 112, 79, 16 tokens 113, about 125; gradient of 150 units of 64 x 64: 4 tokens 40, 33; 8 tokens
-// 40, 40; of 1500: 2 tokens 148, 143; 4 tokens 149, 162.
+// us: 2 tokens 29, 21; 8 tokens 29, 33; 128 x 128: 8 tokens 96, 93, 12 tokens 98, 122; gradient alone of 150 units of 64 x 64: 2 tokens 28, 28; 4 tokens
+// 28, 32; of 150 of 128 x 128: 2 tokens 58, 54; 4 tokens 58, 62; of 500 of 64 x 64: 1 token 42, 50.
 template <typename T>
 bool takes_tiles(long long units, int L, int dk, int dv, bool gradient) {
     if (sizeof(T) != 2 || (gradient && !gdr_grad_supported(dk, dv))) return false;
     const int pref = kernel_preference();
     if (pref == VIG_TEST_KERNEL_SIMT || pref == VIG_TEST_KERNEL_WARP_TILES) return pref == VIG_TEST_KERNEL_WARP_TILES;
-    return L > (gradient ? (units <= 600 ? 4 : 2) : 8);
+    return L > (gradient ? (units <= 300 ? 2 : 0) : 8);
 }
 
 // Copies of a call's rows with zeros up to multiples of eight, where the sizes are none.

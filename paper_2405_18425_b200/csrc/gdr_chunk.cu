@@ -650,7 +650,7 @@ __device__ __forceinline__ bool backward_chunk(State<DKP>& A, const Gdr<bf>& a, 
 }
 
 // Whether two blocks share an SM: their shared memory must.  Each then has 128 registers a thread.  (Unequal shares, 80 to 104 for the preparing
-// warps and 176 to 152 for the others: 53 to 47 us for 64 x 12 units of 196 tokens, 32 x 64, against 46.)
+// warps and 176 to 152 for the others: 53 to 47 us for 64 x 12 units of 196 tokens, 32 x 64, against 46, with one term an operand.)
 template <int DKP, bool EXACT, Way WAY>
 constexpr bool two_blocks() { return 2 * (Layout<DKP, EXACT, WAY>::total(kMostWarps) + 1024) <= 228 * 1024; }
 
@@ -824,7 +824,7 @@ cudaError_t launch_chunks(const Gdr<bf>& a, const Kept& kept, const Segs& segs, 
     int* status = device_status_ptr();
     if (!status) return cudaErrorUnknown;
     const int sixteens = gdr_padded_columns(a.dv) / 16;
-    const int slabs = (sixteens + kMostWarps - 1) / kMostWarps, warps = sixteens / slabs;   // (narrower blocks for few units: 332 -> 414 us for 2 x 16 x 4096, 128 x 128)
+    const int slabs = (sixteens + kMostWarps - 1) / kMostWarps, warps = sixteens / slabs;   // (narrower blocks for few units: 332 -> 414 us for 2 x 16 x 4096, 128 x 128, with one term an operand)
     const long long blocks = a.units * (WAY == Way::kSum ? segs.sums : WAY == Way::kBackSum ? segs.n - 1 : segs.n) * (slabs + (WAY == Way::kSum ? (a.dk + warps * 16 - 1) / (warps * 16) : 0));
     return with_keys(a.dk, [&](auto D) {
         constexpr int dkp = decltype(D)::value;
@@ -854,10 +854,12 @@ cudaError_t launch_fold(const Gdr<bf>& a, const Segs& segs, bool back, cudaStrea
 
 // Segments of a unit: as many as let the blocks of the launch proper run at once (two an SM), of four chunks and more, from three segments on:
 // below, what the first launch adds is what the second saves.  (A block's time is its chunks' in a row, whether or not another shares its SM:
-// 32 units of 4096 tokens, 24 x 48, 8 segments 49 + 39 us for the two launches, 5 segments, with which the first fits the chip too, 40 + 57.)
+// 32 units of 4096 tokens, 24 x 48, 8 segments 49 + 39 us for the two launches, 5 segments, with which the first fits the chip too, 40 + 57, with one term an
+// operand.)
 int segments(long long units, int L, int dk, int dv) {
-    if (dk % 8 || dv % 8) return 1;   // (the states' copies between segments are whole pieces of sixteen bytes)
-    if (dk > kMostSegmentKeys) return 1;   // (one block an SM, and as many columns for the transition as for the state: 2 x 16 units of 4096 tokens, 128 x 128, gain nothing)
+    if (dk % 8 || dv % 8) return 1;   // (the states' copies between segments are whole pieces of sixteen bytes: other sizes go without)
+    if (dk > kMostSegmentKeys) return 1;   // (one block an SM, and as many columns for the transition as for the state: 2 x 16 units of 4096 tokens, 128 x 128, gain
+                                            // nothing; of fewer units than SMs, where segments may well pay, neither side has been measured)
     const long long blocks = units * ((dv + 16 * kMostWarps - 1) / (16 * kMostWarps)), chunks = (L + kChunk - 1) / kChunk;
     const long long fit = 2LL * 148 / blocks, n = fit < chunks / 4 ? fit : chunks / 4;
     return n < 3 ? 1 : (int)(n < 32 ? n : 32);

@@ -1,4 +1,5 @@
-// The gated delta rule step by step in fp32 on the CUDA cores: fp32 calls, and the head sizes that the tensor-core kernels do not take.
+// The gated delta rule step by step in fp32 on the CUDA cores: fp32 calls; bf16 calls of a handful of tokens, gradients of more than 128 value columns, and
+// units that the chunks leave (grown too far, or not finite); and the single token.
 //
 //   S~_t = alpha_t S_{t-1};  w_t = v_t - S~_t^T k_t;  u_t = beta_t w_t;  S_t = S~_t + k_t u_t^T;  out_t = S_t^T q_t
 //
