@@ -9,7 +9,7 @@
 //
 // A block runs through the chunks of a unit for up to 64 columns.  Four of its warps prepare: they bring the rows of K and Q and make N, P and the
 // inverses of the next chunk while the others, a warp for every sixteen columns (gdr_tile.cuh), work on this one.  Two buffers, handed over by
-// named barriers.  64 x 12 units of 196 tokens, 32 x 64 (58 MB): 55 us, 0.16 of the rate of a copy, bound by instruction issue and a chunk's chain with two
+// named barriers.  64 x 12 units of 196 tokens, 32 x 64 (58 MB): 56 us, 0.16 of the rate of a copy, bound by instruction issue and a chunk's chain with two
 // blocks an SM.  (One term of fp16 an operand under powers of two: 50 us, but see gdr_tile.cuh.  32 units of 4096 tokens, 24 x 48, without segments 448 us,
 // 7 us a chunk.)
 #include <type_traits>

@@ -274,6 +274,7 @@ __global__ void __launch_bounds__(kThreads, 4) norm_kernel(Norm<T> a, int N) {
             unpack2(sq[e], q0, q1);
             mean[2 * e] = fmaf(s0, inv, f0);
             mean[2 * e + 1] = fmaf(s1, inv, f1);
+            // (the product inside does not overflow by itself: not a number only where the mean is not finite either, which carries it)
             m2[2 * e] = fmaxf(fmaf(-s0 * inv, s0, q0), 0.f);
             m2[2 * e + 1] = fmaxf(fmaf(-s1 * inv, s1, q1), 0.f);
         }

@@ -54,3 +54,16 @@ def test_one_unit_by_itself(size, same, dtype):
             else:
                 tol = 2.0 ** -15 if x.dtype == torch.float32 else 2.0 ** -7
                 assert off(x, f64(y)) <= 2 * tol, i
+
+
+@pytest.mark.parametrize("size", [(2, 2, 65, 128, 128), (1, 3, 130, 20, 17), (1, 2, 196, 32, 64), (1, 1, 1100, 24, 48), (2, 1, 515, 64, 64), (1, 2, 1000, 96, 40)], ids=str)
+def test_states_of_bf16_calls_hold_the_bound_of_fp32_calls(size):
+    """Operands of 24 bits and fp32 sums: the roundings that the bound of fp32 calls counts, and the decays' exponentials, 2^-22 each, once a chunk."""
+    d = gdr_inputs(*size, "bf16", seed=63, gate_mean=1.0, states=True)
+    tol = 8 * 2.0 ** -24 * sum(size[2:]) ** 0.5 + 2.0 ** -22 * (size[2] // 64 + 1) ** 0.5
+    for reverse in (False, True):
+        last, ref = gdr_forward(d, reverse)[1], gdr_oracle(d, reverse)[1]
+        assert off(last, ref) <= tol
+        got = gdr_gradient(d, reverse)[5]
+        want = oracle.gdr_bwd(*(f64(d[n]) for n in NAMES), f64(d["d_out"]), f64(d["state"]), f64(d["d_state"]), reverse)[5]
+        assert off(got, want) <= tol
