@@ -296,6 +296,111 @@ int vig_group_norm_bwd_f32(const void* x, const void* weight, const void* bias, 
                            const void* d_out, void* dx, void* dweight, void* dbias,
                            int B, int Hh, int Ww, int C, int groups, int act, void* stream);
 
+/* ---- Selective state space scan: the token mixer with N states a channel ---------------------------------------------
+ * For every sequence, channel c and state n, with step sizes delta_t = softplus(dt_t + dt_bias) (softplus != 0; else dt_t + dt_bias),
+ *
+ *     h_t[n] = exp(delta_t A[c,n]) h_{t-1}[n] + delta_t x_t Bt_t[n]                (t = 1 .. L)
+ *     y_t    = sum_n Ct_t[n] h_t[n] + D_c x_t,     out_t = y_t z_t sigmoid(z_t)    (out_t = y_t without z)
+ *
+ * x, dt, z, out: [B, L, C]; Bt, Ct: [B, L, G, N], shared by the C / G neighbouring channels of a group; all of the call's element type.
+ * A: FP32 [C, N]; D, dt_bias: FP32 [C]; states: FP32 [B, C, N].  D, z, dt_bias: NULL for 0, no gate, 0.  state_in: h_0, or NULL for zero;
+ * state_out: receives h_L, or NULL; may be state_in.  reverse != 0: the same from the last token to the first (state_in comes behind token
+ * L, state_out is what stands at token 1).  out may be z or x or dt where it has that tensor's pitch, and overlaps no other input.
+ * Domain: A, dt, dt_bias finite with delta_t A <= 0 for a state that stays bounded; larger is computed all the same.
+ * ld: the tensors may be slices of wider rows, as one projection writes them side by side: from row to row (token to token) ld[0] .. ld[5]
+ * values of x, dt, z, out, Bt, Ct, sequence b beginning at row b L; NULL: dense rows.  A pitch is at least the row's width.
+ * Alignment: x, dt, z, out 16 bytes, their pitches multiples of 16 bytes too; Bt and Ct that of their type only; fp32 arrays 4 bytes.
+ * C: a multiple of 8 G (bf16) or 4 G (fp32), at most 2^20; N <= 32; L <= 2^31 - 2^16.
+ * fp32 inside for either type, exponentials from the special-function unit (relative error 2^-22).  Long sequences of few channels are cut
+ * into segments that run side by side, with scratch from the library's pool; whether they are depends on B, C and L, and with it the last
+ * bits: the same call repeats them, a call of other sequences beside it may not.  L == 0 with a state_out copies state_in (or zeros) there.
+ * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
+int vig_ssm_fwd_bf16(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z,
+                     const void* dt_bias, const void* state_in, void* out, void* state_out,
+                     int B, int L, int C, int G, int N, const long long* ld, int softplus, int reverse, void* stream);
+int vig_ssm_fwd_f32(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z,
+                    const void* dt_bias, const void* state_in, void* out, void* state_out,
+                    int B, int L, int C, int G, int N, const long long* ld, int softplus, int reverse, void* stream);
+/* Its gradient.  d_out: [B, L, C]; d_state_out: gradient with respect to state_out (fp32) or NULL for zero.  Writes dx, ddt [B, L, C], dA
+ * (FP32 [C, N]), dB, dC ([B, L, G, N], sums over a group's channels in a fixed order) and, unless they are NULL, dD, d_dt_bias (FP32
+ * [C]), dz [B, L, C] and d_state_in (fp32; may be d_state_out).  Everything is computed anew from the inputs.
+ * ld[0] .. ld[10]: pitches of x, dt, z, d_out, Bt, Ct, dx, ddt, dz, dB, dC; NULL: dense rows.  Alignment as above (dB, dC as Bt, Ct).
+ * Scratch from the library's pool, stream-ordered: about 8 G N bytes a token for every 64 channels of a group, and the states of every
+ * eighth token of the blocks that run at a time.  bf16: the products that make up dB and dC enter their sums over the channels with
+ * eleven significant bits (tf32; fp32: as two such terms), the sums are fp32.  An empty call (B or L 0) clears dA, dD and d_dt_bias.
+ * Outputs must not overlap inputs or one another.  Errors: as vig_ssm_fwd_*. */
+int vig_ssm_bwd_bf16(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z,
+                     const void* dt_bias, const void* state_in, const void* d_out, const void* d_state_out,
+                     void* dx, void* ddt, void* dA, void* dB, void* dC, void* dD, void* dz, void* d_dt_bias, void* d_state_in,
+                     int B, int L, int C, int G, int N, const long long* ld, int softplus, int reverse, void* stream);
+int vig_ssm_bwd_f32(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z,
+                    const void* dt_bias, const void* state_in, const void* d_out, const void* d_state_out,
+                    void* dx, void* ddt, void* dA, void* dB, void* dC, void* dD, void* dz, void* d_dt_bias, void* d_state_in,
+                    int B, int L, int C, int G, int N, const long long* ld, int softplus, int reverse, void* stream);
+/* One token of every sequence: x, dt, z, out [B, C]; Bt, Ct [B, G, N]; state (fp32 [B, C, N]) is updated in place.  ld as in
+ * vig_ssm_fwd_*, from sequence to sequence.  C: any multiple of G up to 2^20; alignment of x, dt, z, out that of their type; state 16
+ * bytes.  Errors: as vig_ssm_fwd_*. */
+int vig_ssm_step_bf16(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z,
+                      const void* dt_bias, void* state, void* out,
+                      int B, int C, int G, int N, const long long* ld, int softplus, void* stream);
+int vig_ssm_step_f32(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z,
+                     const void* dt_bias, void* state, void* out,
+                     int B, int C, int G, int N, const long long* ld, int softplus, void* stream);
+
+/* ---- Causal convolution along the tokens: what stands in front of the selective scan ---------------------------------
+ * out_t = act(bias + sum_{k < K} w[c][k] x_{t-K+1+k}): every channel sees its own last K tokens.
+ * x, out: [B, L, C]; w: [C, K], K 2 to 4; bias: [C] or NULL; states: [B, K - 1, C]; all of the call's element type, fp32 inside.  act:
+ * VIG_ACT_NONE or VIG_ACT_SILU.  state_in: the tokens in front of the first one, oldest first, or NULL for zeros; state_out: receives
+ * those that a continuation needs, or NULL; may be state_in.  reverse != 0: tokens are walked from the last to the first.
+ * ld: values from row to row of x and out (NULL: dense rows), as for vig_ssm_fwd_*.  16-byte alignment, of pitches too.  C: a multiple
+ * of 8 (bf16) or 4 (fp32), at most 2^20; L <= 2^31 - 2^16.  out must not overlap x or a state.
+ * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
+int vig_causal_conv_bf16(const void* x, const void* w, const void* bias, const void* state_in, void* out, void* state_out,
+                         int B, int L, int C, int K, const long long* ld, int act, int reverse, void* stream);
+int vig_causal_conv_f32(const void* x, const void* w, const void* bias, const void* state_in, void* out, void* state_out,
+                        int B, int L, int C, int K, const long long* ld, int act, int reverse, void* stream);
+/* Its gradient: dx [B, L, C] and, unless they are NULL, dw [C, K], dbias [C] (sums over all tokens in a fixed order), d_state_in.
+ * d_state_out: gradient with respect to state_out, or NULL for zero.  ld: pitches of x, d_out, dx.  An empty call (B or L 0) clears dw and
+ * dbias (and, with L 0, d_state_in takes d_state_out).  Outputs must not overlap inputs or one another.  Errors: as vig_causal_conv_*. */
+int vig_causal_conv_bwd_bf16(const void* x, const void* w, const void* bias, const void* state_in, const void* d_out,
+                             const void* d_state_out, void* dx, void* dw, void* dbias, void* d_state_in,
+                             int B, int L, int C, int K, const long long* ld, int act, int reverse, void* stream);
+int vig_causal_conv_bwd_f32(const void* x, const void* w, const void* bias, const void* state_in, const void* d_out,
+                            const void* d_state_out, void* dx, void* dw, void* dbias, void* d_state_in,
+                            int B, int L, int C, int K, const long long* ld, int act, int reverse, void* stream);
+/* One token of every sequence: x, out [B, C]; state [B, K - 1, C] moves on by it, in place.  ld: pitches of x and out.  Errors: as
+ * vig_causal_conv_*. */
+int vig_causal_conv_step_bf16(const void* x, const void* w, const void* bias, void* state, void* out,
+                              int B, int C, int K, const long long* ld, int act, void* stream);
+int vig_causal_conv_step_f32(const void* x, const void* w, const void* bias, void* state, void* out,
+                             int B, int C, int K, const long long* ld, int act, void* stream);
+
+/* ---- RMS norm with the residual's addition -----------------------------------------------------------------------------
+ * What a block begins with, over rows of C values:  s = x + residual,  out = s / sqrt(mean(s^2) + eps) * weight.
+ * x, residual (or NULL for 0), out, sum_out (or NULL): [rows, C], weight: [C], all of the call's element type; rstd: FP32 [rows], what the
+ * gradient needs, or NULL.  sum_out receives s, which the next block adds to; the norm is of s before that rounding.  fp32 inside; rows
+ * whose squares leave the range of fp32 are summed over their largest value.  eps >= 0.  C: a multiple of 8 (bf16) or 4 (fp32), at most
+ * 16384.  16-byte alignment (rstd, scales: 4).  sum_out or out (not both) may be x or residual.
+ * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
+int vig_rms_norm_bf16(const void* x, const void* residual, const void* weight, void* out, void* sum_out, void* rstd,
+                      long long rows, int C, float eps, void* stream);
+int vig_rms_norm_f32(const void* x, const void* residual, const void* weight, void* out, void* sum_out, void* rstd,
+                     long long rows, int C, float eps, void* stream);
+/* The same with out in 8 bits (e4m3, [rows, C], 8-byte aligned) for a projection in 8 bits: out / scale rounded to nearest, with an FP32
+ * scale = max |out| / 448, at least 2^-126, for every row (block 0: scales [rows]) or for every 128 values of it (block 128: scales
+ * [rows, ceil(C / 128)]).  A NaN makes its block NaN.  Errors: as vig_rms_norm_*. */
+int vig_rms_norm_e4m3_bf16(const void* x, const void* residual, const void* weight, void* out, void* scales, void* sum_out,
+                           long long rows, int C, int block, float eps, void* stream);
+int vig_rms_norm_e4m3_f32(const void* x, const void* residual, const void* weight, void* out, void* scales, void* sum_out,
+                          long long rows, int C, int block, float eps, void* stream);
+/* Its gradient, from s as it was stored and rstd: dx = d_sum + what comes through the norm, the gradient of x and of the residual alike
+ * (d_sum: what arrives along sum_out, or NULL for zero; dx may be d_sum or d_out), and dweight [C] unless it is NULL (a sum over the rows in a
+ * fixed order).  An empty call clears dweight.  Errors: as vig_rms_norm_*. */
+int vig_rms_norm_bwd_bf16(const void* sum, const void* weight, const void* rstd, const void* d_out, const void* d_sum,
+                          void* dx, void* dweight, long long rows, int C, void* stream);
+int vig_rms_norm_bwd_f32(const void* sum, const void* weight, const void* rstd, const void* d_out, const void* d_sum,
+                         void* dx, void* dweight, long long rows, int C, void* stream);
+
 /* ---- Whole path on HOST buffers -------------------------------------------------------------------
  * Gate preparation followed by the BiGLA forward (Eq. 5 line 1 + Eq. 6) for callers whose data
  * lives in host memory.  All seven pointers are HOST pointers (pinned memory makes the copies

@@ -14,3 +14,4 @@ from .locality import dwconv3x3, gate_blend  # noqa: F401
 from .quadratic import bigla_quadratic  # noqa: F401
 from .delta_rule import gdr_bwd, gdr_fwd  # noqa: F401
 from .group_norm import group_norm, group_norm_bwd  # noqa: F401
+from .ssm import causal_conv, causal_conv_bwd, rms_norm, rms_norm_bwd, ssm_bwd, ssm_fwd  # noqa: F401

@@ -99,7 +99,16 @@ def load() -> ctypes.CDLL:
                 getattr(lib, name).argtypes = [vp] * ptrs + [ci] * ints + [vp]
         for name in ("vig_group_norm_bf16", "vig_group_norm_f32"):
             getattr(lib, name).argtypes = [vp] * 6 + [ci] * 5 + [cf, ci, vp]
-        for stem in ("vig_gdr_fwd", "vig_gdr_bwd", "vig_gdr_step", "vig_group_norm", "vig_group_norm_bwd"):
+        cl = ctypes.c_longlong
+        for stem, types in (("vig_ssm_fwd", [vp] * 11 + [ci] * 5 + [vp, ci, ci, vp]), ("vig_ssm_bwd", [vp] * 20 + [ci] * 5 + [vp, ci, ci, vp]),
+                            ("vig_ssm_step", [vp] * 10 + [ci] * 4 + [vp, ci, vp]), ("vig_causal_conv", [vp] * 6 + [ci] * 4 + [vp, ci, ci, vp]),
+                            ("vig_causal_conv_bwd", [vp] * 10 + [ci] * 4 + [vp, ci, ci, vp]), ("vig_causal_conv_step", [vp] * 5 + [ci] * 3 + [vp, ci, vp]),
+                            ("vig_rms_norm", [vp] * 6 + [cl, ci, cf, vp]), ("vig_rms_norm_e4m3", [vp] * 6 + [cl, ci, ci, cf, vp]),
+                            ("vig_rms_norm_bwd", [vp] * 7 + [cl, ci, vp])):
+            for name in (stem + "_bf16", stem + "_f32"):
+                getattr(lib, name).argtypes = types
+        for stem in ("vig_gdr_fwd", "vig_gdr_bwd", "vig_gdr_step", "vig_group_norm", "vig_group_norm_bwd", "vig_ssm_fwd", "vig_ssm_bwd", "vig_ssm_step",
+                     "vig_causal_conv", "vig_causal_conv_bwd", "vig_causal_conv_step", "vig_rms_norm", "vig_rms_norm_e4m3", "vig_rms_norm_bwd"):
             for name in (stem + "_bf16", stem + "_f32"):
                 getattr(lib, name).restype = ci
                 _addr[name] = ctypes.cast(getattr(lib, name), vp).value
@@ -299,6 +308,69 @@ def vig_group_norm_bwd(x, weight, bias, mean, rstd, d_out, dx, dweight, dbias, g
     """Gradient of vig_group_norm from the mean and rstd it left; dweight, dbias may be None."""
     _layer_call("group_norm_bwd", stream, groups, _act(act), x, weight, bias, mean, rstd, d_out, dx, dweight, dbias)
     return dx, dweight, dbias
+
+
+# ---- selective scan, causal convolution, RMS norm.  Tensors [B, L, ..] may be slices of the last dimension of wider rows ("one pitch") --
+def vig_ssm_fwd(x, dt, A, Bt, Ct, out, D=None, z=None, dt_bias=None, state_in=None, state_out=None, softplus=True, reverse=False, stream=None):
+    """Selective state space scan.  x, dt, z, out: [B,L,C]; Bt, Ct: [B,L,G,N]; one dtype (bf16 or fp32).  A: fp32 [C,N]; D, dt_bias: fp32 [C] or
+    None; state_in, state_out: fp32 [B,C,N] or None.  Step sizes are softplus(dt + dt_bias), or dt + dt_bias without softplus; out is gated
+    by silu(z) where z is given.  reverse: from the last token to the first."""
+    _layer_call("ssm_fwd", stream, softplus, reverse, x, dt, A, Bt, Ct, D, z, dt_bias, state_in, out, state_out)
+    return out
+
+
+def vig_ssm_bwd(x, dt, A, Bt, Ct, d_out, dx, ddt, dA, dB, dC, D=None, z=None, dt_bias=None, dD=None, dz=None, d_dt_bias=None, state_in=None,
+                d_state_out=None, d_state_in=None, softplus=True, reverse=False, stream=None):
+    """Gradient of vig_ssm_fwd for d_out (and d_state_out, of the final state); writes and returns dx, ddt, dA, dB, dC, and writes dD, dz,
+    d_dt_bias and d_state_in where they are given."""
+    _layer_call("ssm_bwd", stream, softplus, reverse, x, dt, A, Bt, Ct, D, z, dt_bias, state_in, d_out, d_state_out, dx, ddt, dA, dB, dC, dD, dz, d_dt_bias,
+                d_state_in)
+    return dx, ddt, dA, dB, dC
+
+
+def vig_ssm_step(x, dt, A, Bt, Ct, state, out, D=None, z=None, dt_bias=None, softplus=True, stream=None):
+    """One token of the selective scan: x, dt, z, out [B,C], Bt, Ct [B,G,N]; state (fp32 [B,C,N]) in place."""
+    _layer_call("ssm_step", stream, softplus, x, dt, A, Bt, Ct, D, z, dt_bias, state, out)
+    return out
+
+
+def vig_causal_conv(x, w, bias, out, act="silu", state_in=None, state_out=None, reverse=False, stream=None):
+    """Depth-wise convolution over the last K tokens with an activation ("none", "silu"): x, out [B,L,C]; w [C,K]; bias [C] or None;
+    state_in, state_out: the K - 1 tokens in front, [B,K-1,C], or None."""
+    _layer_call("causal_conv", stream, _act(act), reverse, x, w, bias, state_in, out, state_out)
+    return out
+
+
+def vig_causal_conv_bwd(x, w, bias, d_out, dx, dw, dbias, act="silu", state_in=None, d_state_out=None, d_state_in=None, reverse=False, stream=None):
+    """Gradient of vig_causal_conv; dw, dbias, d_state_in may be None."""
+    _layer_call("causal_conv_bwd", stream, _act(act), reverse, x, w, bias, state_in, d_out, d_state_out, dx, dw, dbias, d_state_in)
+    return dx, dw, dbias
+
+
+def vig_causal_conv_step(x, w, bias, state, out, act="silu", stream=None):
+    """One token of the causal convolution: x, out [B,C]; state [B,K-1,C] moves on by it, in place."""
+    _layer_call("causal_conv_step", stream, _act(act), x, w, bias, state, out)
+    return out
+
+
+def vig_rms_norm(x, weight, out, residual=None, sum_out=None, rstd=None, eps=1e-5, stream=None):
+    """RMS norm over the last dimension of x + residual; sum_out receives that sum.  x, residual, out, sum_out: [..., C]; weight [C]; rstd: fp32
+    [...] for the gradient, or None."""
+    _layer_call("rms_norm", stream, eps, x, residual, weight, out, sum_out, rstd)
+    return out
+
+
+def vig_rms_norm_e4m3(x, weight, out, scales, residual=None, sum_out=None, eps=1e-5, stream=None):
+    """vig_rms_norm with out in 8 bits (torch.float8_e4m3fn) and fp32 scales [..., 1] of its rows, or [..., ceil(C / 128)] of every 128 values."""
+    _layer_call("rms_norm_e4m3", stream, eps, x, residual, weight, out, scales, sum_out)
+    return out, scales
+
+
+def vig_rms_norm_bwd(sum, weight, rstd, d_out, dx, dweight, d_sum=None, stream=None):
+    """Gradient of vig_rms_norm from the sum and rstd it left (without a residual: x); d_sum: what arrives along sum_out.  dx is the gradient
+    of x and of the residual; dweight may be None."""
+    _layer_call("rms_norm_bwd", stream, sum, weight, rstd, d_out, d_sum, dx, dweight)
+    return dx, dweight
 
 
 def _host_ptr(a) -> int:
