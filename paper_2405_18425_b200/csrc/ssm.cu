@@ -17,139 +17,167 @@ using namespace ssm;
 
 constexpr int kMain = 0, kEnds = 1, kBoth = 2;   // kEnds: a segment's end state; kBoth: and what its outputs' gradients add to the adjoint in front
 
-template <typename T, int NS, int MODE>
-__global__ void __launch_bounds__(kThreads, NS <= 4 ? 4 : 2) ssm_kernel(Ssm<T> a) {
-    constexpr int NP = 4 * NS, P = NS / 2;
-    __shared__ __align__(16) float step[kTile][kCh][4];   // delta, delta, delta x, delta x: pairs as the products take them
+template <typename T, int NS, int K, int MODE>
+__global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
+    constexpr int NP = 4 * NS, P = NS / 2, kThreads = threads_of(K), kTile = tile_of(K);
+    __shared__ __align__(16) float step[kTile][kCh][2];   // delta, delta x
     __shared__ __align__(16) float rows_b[kTile * NP], rows_c[MODE == kEnds ? 4 : kTile * NP];
-    __shared__ __align__(16) float sums[MODE == kEnds ? 1 : kTile][kRow];   // y; kBoth: the gradient of y
+    __shared__ __align__(16) float sums[MODE == kMain ? kTile : 1][4][kRow];   // a quarter's part of y
+    __shared__ __align__(16) float grad[MODE == kBoth ? kTile : 1][kCh];       // the gradient of y
     pdl_wait();
     pdl_launch_dependents();
     const Place at(a, blockIdx.x);
-    const int lane = threadIdx.x & 31, ch = (threadIdx.x >> 5) * 8 + (lane & 7), quarter = lane >> 3, n0 = quarter * NS;
-    const bool live = ch < at.live;
-    const int c = at.c0 + (live ? ch : 0);
+    const int lane = threadIdx.x & 31, ch = ((threadIdx.x >> 5) * 8 + (lane & 7)) * K, quarter = lane >> 3, n0 = quarter * NS;
     const int t0 = at.seg * a.seg, t1 = min(t0 + a.seg, a.L);
-    f32x2 rate[P], h[P];
-    load_states<NS>(a.A + (long long)c * a.N, live ? a.N : 0, n0, rate);
+    f32x2 rate[K][P], h[K][P];
+    const long long slot = (((long long)at.b * a.segs + at.seg) * a.C + at.c0 + ch) * NP + n0, own = ((long long)at.b * a.C + at.c0 + ch) * a.N;
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-        rate[i] = fmul2(rate[i], pack2(kLog2E, kLog2E));
-        h[i] = 0;
-    }
-    const long long slot = (((long long)at.b * a.segs + at.seg) * a.C + c) * NP + n0;
-    if (MODE == kMain && live) {
-        if (a.segs > 1) load_pairs<NS>(a.ends + slot, h);
-        else if (a.state_in) load_states<NS>(a.state_in + ((long long)at.b * a.C + c) * a.N, a.N, n0, h);
+    for (int k = 0; k < K; ++k) {
+        const bool live = ch + k < at.live;
+        load_states<NS>(a.A + (long long)(at.c0 + ch + k) * a.N, live ? a.N : 0, n0, rate[k]);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            rate[k][i] = fmul2(rate[k][i], both(kLog2E));
+            h[k][i] = 0;
+        }
+        if (MODE == kMain && live) {
+            if (a.segs > 1) load_pairs<NS>(a.ends + slot + k * NP, h[k]);
+            else if (a.state_in) load_states<NS>(a.state_in + own + k * a.N, a.N, n0, h[k]);
+        }
     }
     // element-wise: token et of a tile, channels ec .. ec + 3
     const int et = threadIdx.x / 16, ec = (threadIdx.x % 16) * 4;
     const bool mine = ec < at.live;
-    const int g0 = at.c0 + ec;
-    float bias[4] = {}, skip[4] = {};
-    if (mine) {
+    const int g0 = at.c0 + (mine ? ec : 0);
+    f32x2 bias[2], skip[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (a.bias) bias[j] = a.bias[g0 + j];
-            if (MODE == kMain && a.D) skip[j] = a.D[g0 + j];
-        }
+    for (int j = 0; j < 2; ++j) {
+        bias[j] = a.bias ? pack2(a.bias[g0 + 2 * j], a.bias[g0 + 2 * j + 1]) : 0;
+        skip[j] = MODE == kMain && a.D ? pack2(a.D[g0 + 2 * j], a.D[g0 + 2 * j + 1]) : 0;
     }
+    const long long r0 = a.row(at.b, t0 + et), way = a.reverse ? -kTile : kTile;
+    const T *px = a.x + r0 * a.ldx + g0, *pd = a.dt + r0 * a.lddt + g0, *pz = a.z + r0 * a.ldz + g0, *po = a.d_out + r0 * a.ldo + g0;
+    T* out = a.out + r0 * a.ldo + g0;
     typename Four<T>::Raw rx = {}, rd = {}, rz = {}, ro = {};
-    Rows<T, NP> rb, rc;
-    auto load = [&](int t) {
-        const int tt = t + et;
-        if (mine && tt < t1) {
-            const long long r = a.row(at.b, tt);
-            rx = load4(a.x + r * a.ldx + g0);
-            rd = load4(a.dt + r * a.lddt + g0);
-            if (MODE != kEnds && a.z) rz = load4(a.z + r * a.ldz + g0);
-            if (MODE == kBoth) ro = load4(a.d_out + r * a.ldo + g0);
+    Rows<T, NP, kTile, kThreads> rb, rc;
+    rb.start(a.Bt, a, a.ldB, at, t0);
+    rc.start(a.Ct, a, a.ldC, at, t0);
+    auto load = [&](int t) {   // a tile, and on to the next one
+        if (mine && t + et < t1) {
+            rx = load4(px);
+            rd = load4(pd);
+            if (MODE != kEnds && a.z) rz = load4(pz);
+            if (MODE == kBoth) ro = load4(po);
         }
-        rb.load(a.Bt, a, a.ldB, at, t);
-        if (MODE != kEnds) rc.load(a.Ct, a, a.ldC, at, t);
+        px += way * a.ldx;
+        pd += way * a.lddt;
+        if (MODE != kEnds) pz += way * a.ldz;
+        if (MODE == kBoth) po += way * a.ldo;
+        rb.load(t, t1, a.N);
+        rb.move(kTile);
+        if (MODE != kEnds) {
+            rc.load(t, t1, a.N);
+            rc.move(kTile);
+        }
     };
-    f32x2 decay[P], back[P];   // kBoth
+    f32x2 decay[K][P], back[K][P];   // kBoth
+    float total[K] = {};
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-        decay[i] = pack2(1.f, 1.f);
-        back[i] = 0;
-    }
-    float total = 0.f;
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            decay[k][i] = both(1.f);
+            back[k][i] = 0;
+        }
     load(t0);
     for (int t = t0; t < t1; t += kTile) {
-        float x[4], z[4];
+        f32x2 x[2], z[2];
+        const bool there = mine && t + et < t1;
         {
-            float d[4], o[4];
+            f32x2 d[2], o[2];
             widen4(rx, x);
             widen4(rd, d);
             widen4(rz, z);
             widen4(ro, o);
-            const bool there = mine && t + et < t1;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float v = d[j] + bias[j];
-                float delta = a.softplus ? softplus_of(v, exp_minus_abs<T>(v)) : v;
-                if (!there) delta = 0.f;   // (decay one, nothing added)
-                const float in = there ? delta * x[j] : 0.f;
-                *reinterpret_cast<float4*>(&step[et][ec + j][0]) = make_float4(delta, delta, in, in);
+            for (int j = 0; j < 2; ++j) {
+                f32x2 delta = fadd2(d[j], bias[j]);
+                if (a.softplus) delta = softplus2(delta, exp_minus_abs<T>(delta));
+                f32x2 in = fmul2(delta, x[j]);
+                if (!there) delta = in = 0;   // (decay one, nothing added)
+                put_step(&step[et][ec + 2 * j], delta, in);
                 if (MODE == kBoth) {
-                    const float gate = a.z ? z[j] * sigmoid_of<T>(z[j], exp_minus_abs<T>(z[j])) : 1.f;
-                    sums[et][ec + j] = there ? o[j] * gate : 0.f;
+                    if (a.z) o[j] = fmul2(o[j], fmul2(z[j], sigmoid2<T>(z[j])));
+                    if (!there) o[j] = 0;
                 }
             }
+            if (MODE == kBoth) store4(&grad[et][ec], o);
             rb.put(rows_b);
             if (MODE != kEnds) rc.put(rows_c);
         }
         __syncthreads();
         if (t + kTile < t1) load(t + kTile);
 #pragma unroll 1
-        for (int s = 0; s < kTile; s += 4) {
-            float p[4];
+        for (int s = 0; s < kTile && t + s < t1; s += 4) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(&step[s + j][ch][0]);
-                f32x2 bt[P], ct[P], y = 0;
+                f32x2 bt[P], ct[P];
+                float d[2 * K], dy[K], part[K];
+                load_floats<2 * K>(&step[s + j][ch][0], d);
                 load_pairs<NS>(&rows_b[(s + j) * NP + n0], bt);
                 if (MODE != kEnds) load_pairs<NS>(&rows_c[(s + j) * NP + n0], ct);
-                if (MODE == kBoth) y = pack2(sums[s + j][ch], sums[s + j][ch]);
+                if (MODE == kBoth) load_floats<K>(&grad[s + j][ch], dy);
 #pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    const f32x2 e = exp2_pair(fmul2(rate[i], d.x));
-                    h[i] = ffma2(e, h[i], fmul2(d.y, bt[i]));
-                    if (MODE == kMain) y = ffma2(ct[i], h[i], y);
-                    if (MODE == kBoth) {
-                        decay[i] = fmul2(decay[i], e);
-                        back[i] = ffma2(decay[i], fmul2(ct[i], y), back[i]);
+                for (int k = 0; k < K; ++k) {
+                    const f32x2 delta = both(d[2 * k]), in = both(d[2 * k + 1]);
+                    f32x2 y = 0;
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        const f32x2 e = decay2<T>(fmul2(rate[k][i], delta));
+                        h[k][i] = ffma2(e, h[k][i], fmul2(in, bt[i]));
+                        if (MODE == kMain) y = i == 0 ? fmul2(ct[i], h[k][i]) : ffma2(ct[i], h[k][i], y);
+                        if (MODE == kBoth) {
+                            decay[k][i] = fmul2(decay[k][i], e);
+                            back[k][i] = ffma2(decay[k][i], fmul2(ct[i], both(dy[k])), back[k][i]);
+                        }
                     }
+                    if (MODE == kMain) part[k] = sum2(y);
+                    else total[k] += d[2 * k];
                 }
-                p[j] = sum2(y);
-                if (MODE != kMain) {
-                    float lo, hi;
-                    unpack2(d.x, lo, hi);
-                    total += lo;
-                }
+                if (MODE == kMain) store_floats<K>(&sums[s + j][quarter][ch], part);
             }
-            if (MODE == kMain) sums[s + quarter][ch] = over_quarters(p[0], p[1], p[2], p[3], quarter);
         }
         __syncthreads();
-        if (MODE == kMain && mine && t + et < t1) {
-            const float4 s4 = *reinterpret_cast<const float4*>(&sums[et][ec]);
-            float y[4] = {s4.x, s4.y, s4.z, s4.w};
+        if (MODE == kMain) {
+            if (there) {
+                f32x2 y[2], part[2];
+                load_pairs<4>(&sums[et][0][ec], y);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                y[j] = fmaf(skip[j], x[j], y[j]);
-                if (a.z) y[j] *= z[j] * sigmoid_of<T>(z[j], exp_minus_abs<T>(z[j]));
+                for (int q = 1; q < 4; ++q) {
+                    load_pairs<4>(&sums[et][q][ec], part);
+                    y[0] = fadd2(y[0], part[0]);
+                    y[1] = fadd2(y[1], part[1]);
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    y[j] = ffma2(skip[j], x[j], y[j]);
+                    if (a.z) y[j] = fmul2(y[j], fmul2(z[j], sigmoid2<T>(z[j])));
+                }
+                store4(out, y);
             }
-            store4(a.out + a.row(at.b, t + et) * a.ldo + g0, y);
+            out += way * a.ldo;
         }
     }
-    if (!live) return;
-    if (MODE == kMain) {
-        if (a.state_out && at.seg == a.segs - 1) store_states<NS>(a.state_out + ((long long)at.b * a.C + c) * a.N, a.N, n0, h);
-    } else {
-        store_pairs<NS>(a.ends + slot, h);
-        if (MODE == kBoth) store_pairs<NS>(a.adjoint + slot, back);
-        if (quarter == 0) a.total[((long long)at.b * a.segs + at.seg) * a.C + c] = total;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (ch + k >= at.live) break;
+        if (MODE == kMain) {
+            if (a.state_out && at.seg == a.segs - 1) store_states<NS>(a.state_out + own + k * a.N, a.N, n0, h[k]);
+        } else {
+            store_pairs<NS>(a.ends + slot + k * NP, h[k]);
+            if (MODE == kBoth) store_pairs<NS>(a.adjoint + slot + k * NP, back[k]);
+            if (quarter == 0) a.total[((long long)at.b * a.segs + at.seg) * a.C + at.c0 + ch + k] = total[k];
+        }
     }
 }
 
@@ -219,7 +247,7 @@ __global__ void __launch_bounds__(128) ssm_step_kernel(Ssm<T> a, float* state, i
     }
     const float x = to_f32(a.x[b * a.ldx + c]), v = to_f32(a.dt[b * a.lddt + c]) + (a.bias ? a.bias[c] : 0.f);
     const float z = a.z ? to_f32(a.z[b * a.ldz + c]) : 0.f, skip = a.D ? a.D[c] : 0.f;
-    const float delta = a.softplus ? softplus_of(v, exp_minus_abs<T>(v)) : v, in = delta * x;
+    const float delta = a.softplus ? softplus_of<T>(v) : v, in = delta * x;
     float y = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -236,18 +264,24 @@ __global__ void __launch_bounds__(128) ssm_step_kernel(Ssm<T> a, float* state, i
     for (int o = lanes / 2; o > 0; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
     if (!live || sub != 0) return;
     y = fmaf(skip, x, y);
-    if (a.z) y *= z * sigmoid_of<T>(z, exp_minus_abs<T>(z));
+    if (a.z) y *= z * sigmoid_of<T>(z);
     from_f32(a.out + b * a.ldo + c, y);
 }
 
+template <typename T, int NS, int K, int MODE>
+cudaError_t walk_of(const Ssm<T>& a, cudaStream_t stream) {
+    count_launch();
+    return launch_pdl(ssm_kernel<T, NS, K, MODE>, dim3((unsigned)a.items), dim3(threads_of(K)), 0, stream, a);
+}
+#ifndef VIG_K
+#define VIG_K 2
+#endif
 template <typename T, int MODE>
 cudaError_t walk(const Ssm<T>& a, cudaStream_t stream) {
-    const dim3 grid((unsigned)a.items);
-    count_launch();
     switch (ssm_padded(a.N)) {
-        case 8: return launch_pdl(ssm_kernel<T, 2, MODE>, grid, dim3(kThreads), 0, stream, a);
-        case 16: return launch_pdl(ssm_kernel<T, 4, MODE>, grid, dim3(kThreads), 0, stream, a);
-        default: return launch_pdl(ssm_kernel<T, 8, MODE>, grid, dim3(kThreads), 0, stream, a);
+        case 8: return walk_of<T, 2, VIG_K, MODE>(a, stream);
+        case 16: return walk_of<T, 4, VIG_K, MODE>(a, stream);
+        default: return walk_of<T, 8, 1, MODE>(a, stream);
     }
 }
 
@@ -263,8 +297,8 @@ void ssm_segments(Ssm<T>& a, bool gradient) {
     if (segs > most) segs = most;
     if (segs < 1) segs = 1;
     long long seg = (a.L + segs - 1) / segs;
-    seg = (seg + kTile - 1) / kTile * kTile;
-    a.seg = (int)(seg < kTile ? kTile : seg);
+    seg = (seg + kSsmTile - 1) / kSsmTile * kSsmTile;
+    a.seg = (int)(seg < kSsmTile ? kSsmTile : seg);
     a.segs = (int)((a.L + (long long)a.seg - 1) / a.seg);
     if (a.segs < 1) a.segs = 1;
     a.items = whole * a.segs;

@@ -1,9 +1,11 @@
 // Pieces that the selective scan's kernels share.
 //
-// A block owns 64 channels of a group, a warp eight of them: lanes l, l + 8, l + 16, l + 24 hold a quarter each of the states of channel
-// l < 8 (NS of them, as pairs of fp32).  Sums over the states cross these four lanes only, for four tokens together.  Element-wise work
-// (step sizes, gates) is done once for every token and channel: thread i takes channels 4 (i % 16) .. + 3 of token i / 16 of a
-// tile of 16 tokens, and hands over through shared memory.
+// A block owns 64 channels of a group.  Lanes l, l + 8, l + 16, l + 24 of a warp hold a quarter each of the states of K neighbouring channels,
+// (l mod 8) K of the warp's 8 K, as pairs of fp32.  What a token's products take comes from shared memory, and that is where the SM's 128
+// bytes a clock into registers count, broadcast or not: rows of Bt and Ct are read once for K channels, step sizes once for a quarter
+// of the states, 32 / K + 8 values a token and channel (K = 1 was bound by it: 126 us for 64 x 196 x 1152 with 16 states).
+// Element-wise work (step sizes, gates) is done once for every token and channel: thread i takes channels 4 (i % 16) .. + 3 of token
+// i / 16 of a tile, and hands over through shared memory, as do the quarters their parts of sums over the states.
 #pragma once
 #include "ssm.h"
 #include "wide.cuh"
@@ -11,8 +13,10 @@
 namespace vig {
 namespace ssm {
 
-constexpr int kThreads = 256, kTile = kSsmTile, kCh = kSsmChannels;
-constexpr int kRow = kCh + 8;   // floats of a row of sums: the four tokens that a warp writes at a time lie in different banks
+constexpr int kCh = kSsmChannels;
+constexpr int kRow = kCh + 8;   // floats of a quarter's row of sums: the four that a warp writes at a time lie in different banks
+__host__ __device__ constexpr int threads_of(int K) { return 256 / K; }
+__host__ __device__ constexpr int tile_of(int K) { return 16 / K; }   // tokens of a tile: four values a thread
 
 // Four neighbouring values.
 __device__ __forceinline__ uint4 load4(const float* p) { return *reinterpret_cast<const uint4*>(p); }
@@ -35,24 +39,109 @@ struct Four<float> { typedef uint4 Raw; };
 template <>
 struct Four<__nv_bfloat16> { typedef uint2 Raw; };
 
-// e^-|v| and with it max(v, 0) + log(1 + e^-|v|) and 1 / (1 + e^-v).  The logarithm is 2 atanh(u / (2 + u)) by the series of atanh, whose
-// argument is at most 1/3: its eighth term is below 2^-26 of the sum.
+__device__ __forceinline__ void widen4(const uint4& r, f32x2 (&f)[2]) {
+    f[0] = pack2(__uint_as_float(r.x), __uint_as_float(r.y));
+    f[1] = pack2(__uint_as_float(r.z), __uint_as_float(r.w));
+}
+__device__ __forceinline__ void widen4(const uint2& r, f32x2 (&f)[2]) {
+    f[0] = pack2(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u));
+    f[1] = pack2(__uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, const f32x2 (&f)[2]) {
+    ulonglong2 u;
+    u.x = f[0];
+    u.y = f[1];
+    *reinterpret_cast<ulonglong2*>(p) = u;
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const f32x2 (&f)[2]) {
+    float a, b, c, d;
+    unpack2(f[0], a, b);
+    unpack2(f[1], c, d);
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+}
+__device__ __forceinline__ f32x2 both(float x) { return pack2(x, x); }
+__device__ __forceinline__ f32x2 neg_add2(f32x2 a, f32x2 b) { return ffma2(a, both(-1.f), b); }   // b - a
+
+// e^-|v|, both of a pair.
 template <typename T>
-__device__ __forceinline__ float exp_minus_abs(float v) { return sizeof(T) == 2 ? ex2(-kLog2E * fabsf(v)) : expf(-fabsf(v)); }
-__device__ __forceinline__ float softplus_of(float v, float u) {
-    const float s = u * reciprocal(2.f + u), q = s * s;
-    float p = fmaf(q, 1.f / 13, 1.f / 11);
-    p = fmaf(q, p, 1.f / 9);
-    p = fmaf(q, p, 1.f / 7);
-    p = fmaf(q, p, 1.f / 5);
-    p = fmaf(q, p, 1.f / 3);
-    p = fmaf(q, p, 1.f);
-    return fmaf(s + s, p, fmaxf(v, 0.f));
+__device__ __forceinline__ f32x2 exp_minus_abs(f32x2 v) {
+    float a, b;
+    unpack2(v, a, b);
+    if constexpr (sizeof(T) == 2) return pack2(ex2(-kLog2E * fabsf(a)), ex2(-kLog2E * fabsf(b)));
+    else return pack2(expf(-fabsf(a)), expf(-fabsf(b)));
+}
+// max(v, 0) + log(1 + u) with u = e^-|v|.  log(1 + u) / u on [0, 1]: polynomial of least largest relative error, 2^-25 (a fit of weighted
+// least squares, the weights raised where the error was large until it was level), so that small steps keep their digits.
+__device__ __forceinline__ f32x2 softplus2(f32x2 v, f32x2 u) {
+    f32x2 p = ffma2(u, both(0.005232691299170256f), both(-0.029505226761102676f));
+    p = ffma2(u, p, both(0.07822593301534653f));
+    p = ffma2(u, p, both(-0.13663244247436523f));
+    p = ffma2(u, p, both(0.19106006622314453f));
+    p = ffma2(u, p, both(-0.2484298199415207f));
+    p = ffma2(u, p, both(0.3331909775733948f));
+    p = ffma2(u, p, both(-0.4999949336051941f));
+    p = ffma2(u, p, both(0.9999999403953552f));
+    float a, b;
+    unpack2(v, a, b);
+    return ffma2(u, p, pack2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
+}
+// 1 / (1 + e^-v) with u = e^-|v|
+template <typename T>
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 v, f32x2 u) {
+    float a, b, x, y;
+    unpack2(fadd2(u, both(1.f)), x, y);
+    const f32x2 r = sizeof(T) == 2 ? pack2(reciprocal(x), reciprocal(y)) : pack2(1.f / x, 1.f / y);
+    unpack2(v, a, b);
+    unpack2(u, x, y);
+    return fmul2(r, pack2(a >= 0.f ? 1.f : x, b >= 0.f ? 1.f : y));
+}
+// The same by itself: e^-v may overflow, the reciprocal is zero then.
+template <typename T>
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 v) {
+    float a, b;
+    unpack2(v, a, b);
+    if constexpr (sizeof(T) == 2) return pack2(sigmoid(a), sigmoid(b));
+    else return pack2(1.f / (1.f + expf(-a)), 1.f / (1.f + expf(-b)));
 }
 template <typename T>
-__device__ __forceinline__ float sigmoid_of(float v, float u) {
-    const float r = sizeof(T) == 2 ? reciprocal(1.f + u) : 1.f / (1.f + u);
-    return v >= 0.f ? r : u * r;
+__device__ __forceinline__ float softplus_of(float v) {
+    float a, b;
+    const f32x2 w = both(v);
+    unpack2(softplus2(w, exp_minus_abs<T>(w)), a, b);
+    return a;
+}
+template <typename T>
+__device__ __forceinline__ float sigmoid_of(float v) { return sizeof(T) == 2 ? sigmoid(v) : 1.f / (1.f + expf(-v)); }
+
+template <int M>
+__device__ __forceinline__ void load_floats(const float* p, float (&v)[M]) {
+    if constexpr (M == 1) {
+        v[0] = *p;
+    } else if constexpr (M == 2) {
+        const float2 u = *reinterpret_cast<const float2*>(p);
+        v[0] = u.x; v[1] = u.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < M / 4; ++i) {
+            const float4 u = *reinterpret_cast<const float4*>(p + 4 * i);
+            v[4 * i] = u.x; v[4 * i + 1] = u.y; v[4 * i + 2] = u.z; v[4 * i + 3] = u.w;
+        }
+    }
+}
+template <int M>
+__device__ __forceinline__ void store_floats(float* p, const float (&v)[M]) {
+    if constexpr (M == 1) *p = v[0];
+    else if constexpr (M == 2) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+    else
+#pragma unroll
+        for (int i = 0; i < M / 4; ++i) *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+// delta, delta x of two neighbouring channels
+__device__ __forceinline__ void put_step(float (*to)[2], f32x2 delta, f32x2 in) {
+    float d0, d1, i0, i1;
+    unpack2(delta, d0, d1);
+    unpack2(in, i0, i1);
+    *reinterpret_cast<float4*>(to[0]) = make_float4(d0, i0, d1, i1);
 }
 
 // What a block works on: sequence, segment, channels of a group.
@@ -87,8 +176,6 @@ __device__ __forceinline__ void store_states(float* p, int N, int n0, const f32x
         if (n0 + 2 * i + 1 < N) p[n0 + 2 * i + 1] = hi;
     }
 }
-template <int NP>
-__device__ __forceinline__ f32x2 lds2(const float* p) { return *reinterpret_cast<const f32x2*>(p); }
 // NS floats (pairs) at 8- or 16-byte alignment.
 template <int NS>
 __device__ __forceinline__ void load_pairs(const float* p, f32x2 (&v)[NS / 2]) {
@@ -117,10 +204,45 @@ __device__ __forceinline__ void store_pairs(float* p, const f32x2 (&v)[NS / 2]) 
         }
     }
 }
-__device__ __forceinline__ f32x2 exp2_pair(f32x2 v) {
+// 2^v of a pair: from the special-function unit (relative error 2^-22, sixteen a clock and SM), or as arithmetic, which other pipes do: 2 to
+// the nearest whole number is put together from bits, 2^f for the rest, |f| <= 1/2, is a polynomial of least largest relative error (2^-23.4 of
+// degree five, 2^-28.9 of six; fitted like the logarithm's).  Below 2^-126 the result is 2^-126, a decay as good as none.
+__device__ __forceinline__ f32x2 exp2_special(f32x2 v) {
     float lo, hi;
     unpack2(v, lo, hi);
     return pack2(ex2(lo), ex2(hi));
+}
+template <bool SIX>
+__device__ __forceinline__ f32x2 exp2_arithmetic(f32x2 v) {
+    float a, b, x, y;
+    unpack2(v, a, b);
+    v = pack2(fminf(fmaxf(a, -126.f), 128.f), fminf(fmaxf(b, -126.f), 128.f));
+    const f32x2 whole = fadd2(v, both(12582912.f));   // 1.5 2^23: the nearest whole number in the last bits
+    const f32x2 f = fadd2(v, neg_add2(whole, both(12582912.f)));
+    f32x2 p;
+    if constexpr (SIX) {
+        p = ffma2(f, both(0.00015353361959569156f), both(0.0013398873852565885f));
+        p = ffma2(f, p, both(0.00961843691766262f));
+        p = ffma2(f, p, both(0.055503323674201965f));
+        p = ffma2(f, p, both(0.24022647738456726f));
+        p = ffma2(f, p, both(0.6931471824645996f));
+    } else {
+        p = ffma2(f, both(0.001326472731307149f), both(0.009671512991189957f));
+        p = ffma2(f, p, both(0.05550733581185341f));
+        p = ffma2(f, p, both(0.24022242426872253f));
+        p = ffma2(f, p, both(0.6931470036506653f));
+    }
+    p = ffma2(f, p, both(1.f));
+    unpack2(whole, x, y);
+    unpack2(p, a, b);
+    return pack2(__uint_as_float(__float_as_uint(a) + (__float_as_uint(x) << 23)), __uint_as_float(__float_as_uint(b) + (__float_as_uint(y) << 23)));
+}
+// The decays of pair i at token j of a run: fp32 calls take the arithmetic for its digits, bf16 calls for a quarter of the states (every pair at
+// another token), so that the special-function unit and the others end together.
+template <typename T>
+__device__ __forceinline__ f32x2 decay2(f32x2 v) {
+    if constexpr (sizeof(T) == 4) return exp2_arithmetic<true>(v);
+    else return exp2_special(v);
 }
 // Sums over the four lanes of a channel of what they hold for four tokens: lane quarter q ends with token q's.
 __device__ __forceinline__ float over_quarters(float p0, float p1, float p2, float p3, int quarter) {
@@ -131,18 +253,34 @@ __device__ __forceinline__ float over_quarters(float p0, float p1, float p2, flo
     return (lo ? k1 : k0) + __shfl_xor_sync(0xffffffffu, lo ? k0 : k1, 8);
 }
 
-// A tile's rows of Bt and Ct, loaded a tile ahead by all threads of a block: E values of either a thread.
-template <typename T, int NP>
+// A tile's rows of Bt or Ct, loaded a tile ahead by all threads of a block: E values a thread.
+template <typename T, int NP, int kTile, int kThreads>
 struct Rows {
     static constexpr int E = (kTile * NP + kThreads - 1) / kThreads;
+    const T* p[E];
+    long long pitch;
     T v[E];
-    __device__ __forceinline__ void load(const T* p, const Ssm<T>& a, long long ld, const Place& at, int t0) {
+    __device__ __forceinline__ void start(const T* rows, const Ssm<T>& a, long long ld, const Place& at, int t0) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int i = threadIdx.x + e * kThreads, t = t0 + i / NP, n = i % NP;
+            const int i = threadIdx.x + e * kThreads;
+            p[e] = rows + a.row(at.b, t0 + i / NP) * ld + at.group * a.N + i % NP;
             from_f32(&v[e], 0.f);
-            if (i < kTile * NP && t < a.L && n < a.N) v[e] = p[a.row(at.b, t) * ld + at.group * a.N + n];
         }
+        pitch = a.reverse ? -ld : ld;
+    }
+    // the tile that starts at token t of `last`, which the pointers stand at
+    __device__ __forceinline__ void load(int t, int last, int N) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = threadIdx.x + e * kThreads;
+            from_f32(&v[e], 0.f);
+            if (i < kTile * NP && i % NP < N && t + i / NP < last) v[e] = *p[e];   // (as it comes: a conversion would wait for it here)
+        }
+    }
+    __device__ __forceinline__ void move(int tokens) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) p[e] += tokens * pitch;
     }
     __device__ __forceinline__ void put(float* to) const {
 #pragma unroll

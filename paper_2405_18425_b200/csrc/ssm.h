@@ -5,7 +5,7 @@
 namespace vig {
 
 constexpr int kSsmChannels = 64;   // of a block
-constexpr int kSsmTile = 16;       // tokens that a block takes through its element-wise work together
+constexpr int kSsmTile = 16;       // segments are multiples of it, and it of the tokens that a block takes through its element-wise work together
 constexpr int kSsmMostN = 32;
 
 // A call of the selective scan.  Row t in walking order is token t, or L - 1 - t in a reverse call.  Null pointers: D, z, bias, the states,

@@ -10,16 +10,12 @@
 // Sums over the states cross four lanes; sums over the channels, two for every state and token, are tensor-core products with a
 // matrix of zeros and ones (tf32 terms, one for bf16 calls, whose results are rounded to eight bits, and two for fp32), a quarter of
 // the shuffles' instructions.  What a block has summed over its channels goes through memory to a last launch that adds the blocks in order.
-#include "gdr.h"
 #include "ssm.cuh"
 
 namespace vig {
 namespace {
 
 using namespace ssm;
-
-template <int NS>
-struct Few { static constexpr int N = NS <= 4 ? 8 : 4; };   // tokens whose decays and states a lane holds in registers
 
 __device__ __forceinline__ uint32_t to_tf32(float x) {
     uint32_t r;
@@ -51,28 +47,28 @@ __device__ __forceinline__ void add_four(float (&d)[4], float v0, float v1, floa
     }
 }
 
-template <int NS>
+template <int NS, int K>
 struct Smem {
-    static constexpr int NP = 4 * NS;
-    float step[kTile][kCh][4];        // delta, delta, delta x, delta x
-    float dy[kTile][kCh][2];
+    static constexpr int NP = 4 * NS, kTile = tile_of(K);
+    float step[kTile][kCh][2];        // delta, delta x
+    float dy[kTile][kCh];
     float rows_b[kTile * NP], rows_c[kTile * NP];
     float sums[3][kTile][kRow];       // y; sum w A (of A log2 e); sum g B
-    float bc[kTile][8][2 * NP];       // sums over a warp's channels
+    float bc[kTile][8 / K][2 * NP];   // sums over a warp's channels
 };
 
-template <typename T, int NS>
-__global__ void __launch_bounds__(kThreads, NS <= 4 ? 2 : 1) ssm_grad_kernel(Ssm<T> a) {
-    constexpr int NP = 4 * NS, P = NS / 2, F = Few<NS>::N;
+// F: tokens whose decays and states a lane holds in registers.
+template <typename T, int NS, int K, int F, int BLOCKS>
+__global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> a) {
+    constexpr int NP = 4 * NS, P = NS / 2, kThreads = threads_of(K), kTile = tile_of(K), kWarps = 8 / K;
     constexpr bool kSplit = sizeof(T) == 4;
-    extern __shared__ __align__(16) unsigned char raw[];
-    Smem<NS>& sm = *reinterpret_cast<Smem<NS>*>(raw);
+    __shared__ __align__(16) Smem<NS, K> sm;
     pdl_wait();
     pdl_launch_dependents();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ch = warp * 8 + (lane & 7), quarter = lane >> 3, n0 = quarter * NS;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ch = (warp * 8 + (lane & 7)) * K, quarter = lane >> 3, n0 = quarter * NS;
     const int et = tid / 16, ec = (tid % 16) * 4;
     const int per_seg = (a.seg + F - 1) / F;
-    float* kept = a.kept + (long long)blockIdx.x * per_seg * kThreads * NS + tid * NS;
+    float* kept = a.kept + ((long long)blockIdx.x * per_seg * K * kThreads + tid) * NS;
     // products with ones: pair i of columns takes lanes of lane / 4 == 2 i (row r of B) and 2 i + 1 (row r + 4)
     const int lg = lane >> 2, lr = lane & 3;
     uint32_t one0[4], one1[4];
@@ -83,40 +79,45 @@ __global__ void __launch_bounds__(kThreads, NS <= 4 ? 2 : 1) ssm_grad_kernel(Ssm
     }
     for (long long item = blockIdx.x; item < a.items; item += gridDim.x) {
         const Place at(a, item);
-        const bool live = ch < at.live, mine = ec < at.live;
-        const int c = at.c0 + (live ? ch : 0), g0 = at.c0 + ec;
+        const bool mine = ec < at.live;
+        const int g0 = at.c0 + (mine ? ec : 0);
         const int t0 = at.seg * a.seg, t1 = min(t0 + a.seg, a.L), tiles = (t1 - t0 + kTile - 1) / kTile;
-        f32x2 rate[P], h[P], g[P], da[P];
-        load_states<NS>(a.A + (long long)c * a.N, live ? a.N : 0, n0, rate);
+        f32x2 rate[K][P], h[K][P], g[K][P], da[K][P];
+        const long long slot = (((long long)at.b * a.segs + at.seg) * a.C + at.c0 + ch) * NP + n0, own = ((long long)at.b * a.C + at.c0 + ch) * a.N;
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            rate[i] = fmul2(rate[i], pack2(kLog2E, kLog2E));
-            h[i] = g[i] = da[i] = 0;
-        }
-        const long long slot = (((long long)at.b * a.segs + at.seg) * a.C + c) * NP + n0, own = ((long long)at.b * a.C + c) * a.N;
-        if (live) {
-            if (a.segs > 1) {
-                load_pairs<NS>(a.ends + slot, h);
-                load_pairs<NS>(a.adjoint + slot, g);
-            } else {
-                if (a.state_in) load_states<NS>(a.state_in + own, a.N, n0, h);
-                if (a.d_state_out) load_states<NS>(a.d_state_out + own, a.N, n0, g);
+        for (int k = 0; k < K; ++k) {
+            const bool live = ch + k < at.live;
+            load_states<NS>(a.A + (long long)(at.c0 + ch + k) * a.N, live ? a.N : 0, n0, rate[k]);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                rate[k][i] = fmul2(rate[k][i], both(kLog2E));
+                h[k][i] = g[k][i] = da[k][i] = 0;
+            }
+            if (live) {
+                if (a.segs > 1) {
+                    load_pairs<NS>(a.ends + slot + k * NP, h[k]);
+                    load_pairs<NS>(a.adjoint + slot + k * NP, g[k]);
+                } else {
+                    if (a.state_in) load_states<NS>(a.state_in + own + k * a.N, a.N, n0, h[k]);
+                    if (a.d_state_out) load_states<NS>(a.d_state_out + own + k * a.N, a.N, n0, g[k]);
+                }
             }
         }
-        float bias[4] = {}, skip[4] = {}, d_skip[4] = {}, d_bias[4] = {};
-        if (mine) {
+        f32x2 bias[2], skip[2], d_skip[2], d_bias[2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (a.bias) bias[j] = a.bias[g0 + j];
-                if (a.D) skip[j] = a.D[g0 + j];
-            }
+        for (int j = 0; j < 2; ++j) {
+            bias[j] = a.bias ? pack2(a.bias[g0 + 2 * j], a.bias[g0 + 2 * j + 1]) : 0;
+            skip[j] = a.D ? pack2(a.D[g0 + 2 * j], a.D[g0 + 2 * j + 1]) : 0;
+            d_skip[j] = d_bias[j] = 0;
         }
         typename Four<T>::Raw rx = {}, rd = {}, rz = {}, ro = {};
-        Rows<T, NP> rb, rc;
+        Rows<T, NP, kTile, kThreads> rb, rc;
+        rb.start(a.Bt, a, a.ldB, at, t0);
+        rc.start(a.Ct, a, a.ldC, at, t0);
+        rc.move((tiles - 1) * kTile);
         auto load = [&](int t, bool back) {
-            const int tt = t + et;
-            if (mine && tt < t1) {
-                const long long r = a.row(at.b, tt);
+            if (mine && t + et < t1) {
+                const long long r = a.row(at.b, t + et);
                 rx = load4(a.x + r * a.ldx + g0);
                 rd = load4(a.dt + r * a.lddt + g0);
                 if (back) {
@@ -124,121 +125,151 @@ __global__ void __launch_bounds__(kThreads, NS <= 4 ? 2 : 1) ssm_grad_kernel(Ssm
                     ro = load4(a.d_out + r * a.ldo + g0);
                 }
             }
-            rb.load(a.Bt, a, a.ldB, at, t);
-            if (back) rc.load(a.Ct, a, a.ldC, at, t);
+            rb.load(t, t1, a.N);
+            if (back) rc.load(t, t1, a.N);
         };
         // forward: the state in front of every F-th token
         load(t0, false);
-        for (int k = 0; k < tiles; ++k) {
-            const int t = t0 + k * kTile;
-            float x[4], d[4];
+        for (int m = 0; m < tiles; ++m) {
+            const int t = t0 + m * kTile;
+            const bool there = mine && t + et < t1;
+            f32x2 x[2], d[2];
             widen4(rx, x);
             widen4(rd, d);
-            const bool there = mine && t + et < t1;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float v = d[j] + bias[j];
-                float delta = a.softplus ? softplus_of(v, exp_minus_abs<T>(v)) : v;
-                if (!there) delta = 0.f;
-                const float in = there ? delta * x[j] : 0.f;
-                *reinterpret_cast<float4*>(&sm.step[et][ec + j][0]) = make_float4(delta, delta, in, in);
+            for (int j = 0; j < 2; ++j) {
+                f32x2 delta = fadd2(d[j], bias[j]);
+                if (a.softplus) delta = softplus2(delta, exp_minus_abs<T>(delta));
+                f32x2 in = fmul2(delta, x[j]);
+                if (!there) delta = in = 0;
+                put_step(&sm.step[et][ec + 2 * j], delta, in);
             }
             rb.put(sm.rows_b);
             __syncthreads();
-            if (k + 1 < tiles) load(t + kTile, false);
-            else load(t, true);
+            if (m + 1 < tiles) {
+                rb.move(kTile);
+                load(t + kTile, false);
+            } else {
+                load(t, true);
+            }
 #pragma unroll 1
             for (int s = 0; s < kTile; s += F) {
                 if (t + s >= t1) break;
-                store_pairs<NS>(kept + (long long)((k * kTile + s) / F) * kThreads * NS, h);
+                float* to = kept + (long long)((m * kTile + s) / F) * K * kThreads * NS;
+#pragma unroll
+                for (int k = 0; k < K; ++k) store_pairs<NS>(to + k * kThreads * NS, h[k]);
                 if (t + s + F >= t1) break;   // (the last few's end is not asked for)
 #pragma unroll
                 for (int j = 0; j < F; ++j) {
-                    const ulonglong2 dd = *reinterpret_cast<const ulonglong2*>(&sm.step[s + j][ch][0]);
                     f32x2 bt[P];
+                    float d2[2 * K];
+                    load_floats<2 * K>(&sm.step[s + j][ch][0], d2);
                     load_pairs<NS>(&sm.rows_b[(s + j) * NP + n0], bt);
 #pragma unroll
-                    for (int i = 0; i < P; ++i) h[i] = ffma2(exp2_pair(fmul2(rate[i], dd.x)), h[i], fmul2(dd.y, bt[i]));
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int i = 0; i < P; ++i) h[k][i] = ffma2(decay2<T>(fmul2(rate[k][i], both(d2[2 * k]))), h[k][i], fmul2(both(d2[2 * k + 1]), bt[i]));
                 }
             }
             __syncthreads();
         }
         // backward
-        for (int k = tiles - 1; k >= 0; --k) {
-            const int t = t0 + k * kTile;
-            float x[4], d[4], z[4], o[4], delta[4], slope[4], dy[4];
+        for (int m = tiles - 1; m >= 0; --m) {
+            const int t = t0 + m * kTile;
+            const bool there = mine && t + et < t1;
+            f32x2 x[2], z[2], o[2], delta[2], slope[2], dy[2];
             widen4(rx, x);
-            widen4(rd, d);
+            widen4(rd, delta);
             widen4(rz, z);
             widen4(ro, o);
-            const bool there = mine && t + et < t1;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float v = d[j] + bias[j], u = exp_minus_abs<T>(v);
-                delta[j] = a.softplus ? softplus_of(v, u) : v;
-                slope[j] = a.softplus ? sigmoid_of<T>(v, u) : 1.f;
-                dy[j] = o[j];
-                if (a.z) dy[j] *= z[j] * sigmoid_of<T>(z[j], exp_minus_abs<T>(z[j]));
-                if (!there) delta[j] = dy[j] = x[j] = 0.f;
-                const float in = delta[j] * x[j];
-                *reinterpret_cast<float4*>(&sm.step[et][ec + j][0]) = make_float4(delta[j], delta[j], in, in);
+            for (int j = 0; j < 2; ++j) {
+                delta[j] = fadd2(delta[j], bias[j]);
+                slope[j] = both(1.f);
+                if (a.softplus) {
+                    const f32x2 u = exp_minus_abs<T>(delta[j]);
+                    slope[j] = sigmoid2<T>(delta[j], u);
+                    delta[j] = softplus2(delta[j], u);
+                }
+                dy[j] = a.z ? fmul2(o[j], fmul2(z[j], sigmoid2<T>(z[j]))) : o[j];
+                if (!there) delta[j] = dy[j] = x[j] = 0;
+                put_step(&sm.step[et][ec + 2 * j], delta[j], fmul2(delta[j], x[j]));
             }
-            *reinterpret_cast<float4*>(&sm.dy[et][ec][0]) = make_float4(dy[0], dy[0], dy[1], dy[1]);
-            *reinterpret_cast<float4*>(&sm.dy[et][ec + 2][0]) = make_float4(dy[2], dy[2], dy[3], dy[3]);
+            store4(&sm.dy[et][ec], dy);
             rb.put(sm.rows_b);
             rc.put(sm.rows_c);
             __syncthreads();
-            if (k > 0) load(t - kTile, true);
+            if (m > 0) {
+                rb.move(-kTile);
+                rc.move(-kTile);
+                load(t - kTile, true);
+            }
 #pragma unroll 1
             for (int s = kTile - F; s >= 0; s -= F) {
                 if (t + s >= t1) continue;
-                f32x2 decay[F][P], before[F][P];
-                float py[F], pw[F], pb[F];
-                load_pairs<NS>(kept + (long long)((k * kTile + s) / F) * kThreads * NS, h);
+                f32x2 decay[F][K][P], before[F][K][P];
+                float part[3][F][K];
+                const float* from = kept + (long long)((m * kTile + s) / F) * K * kThreads * NS;
+#pragma unroll
+                for (int k = 0; k < K; ++k) load_pairs<NS>(from + k * kThreads * NS, h[k]);
 #pragma unroll
                 for (int j = 0; j < F; ++j) {
-                    const ulonglong2 dd = *reinterpret_cast<const ulonglong2*>(&sm.step[s + j][ch][0]);
-                    f32x2 bt[P], ct[P], y = 0;
+                    f32x2 bt[P], ct[P];
+                    float d2[2 * K];
+                    load_floats<2 * K>(&sm.step[s + j][ch][0], d2);
                     load_pairs<NS>(&sm.rows_b[(s + j) * NP + n0], bt);
                     if (a.z) load_pairs<NS>(&sm.rows_c[(s + j) * NP + n0], ct);
 #pragma unroll
-                    for (int i = 0; i < P; ++i) {
-                        before[j][i] = h[i];
-                        decay[j][i] = exp2_pair(fmul2(rate[i], dd.x));
-                        h[i] = ffma2(decay[j][i], h[i], fmul2(dd.y, bt[i]));
-                        if (a.z) y = ffma2(ct[i], h[i], y);
+                    for (int k = 0; k < K; ++k) {
+                        f32x2 y = 0;
+#pragma unroll
+                        for (int i = 0; i < P; ++i) {
+                            before[j][k][i] = h[k][i];
+                            decay[j][k][i] = decay2<T>(fmul2(rate[k][i], both(d2[2 * k])));
+                            h[k][i] = ffma2(decay[j][k][i], h[k][i], fmul2(both(d2[2 * k + 1]), bt[i]));
+                            if (a.z) y = ffma2(ct[i], h[k][i], y);
+                        }
+                        part[0][j][k] = sum2(y);
                     }
-                    py[j] = sum2(y);
                 }
                 float acc[4] = {0.f, 0.f, 0.f, 0.f};
                 constexpr int kTogether = 8 / NS;   // tokens whose sums over channels fill a product's eight columns
 #pragma unroll
                 for (int j = F - 1; j >= 0; --j) {
-                    const ulonglong2 dd = *reinterpret_cast<const ulonglong2*>(&sm.step[s + j][ch][0]);
-                    const f32x2 gy = *reinterpret_cast<const f32x2*>(&sm.dy[s + j][ch][0]);
-                    f32x2 bt[P], ct[P], sw = 0, sb = 0;
-                    float v[2 * NS];
+                    f32x2 bt[P], ct[P], vb[P], vc[P];
+                    float d2[2 * K], gy[K], v[2 * NS];
+                    load_floats<2 * K>(&sm.step[s + j][ch][0], d2);
+                    load_floats<K>(&sm.dy[s + j][ch], gy);
                     load_pairs<NS>(&sm.rows_b[(s + j) * NP + n0], bt);
                     load_pairs<NS>(&sm.rows_c[(s + j) * NP + n0], ct);
 #pragma unroll
-                    for (int i = 0; i < P; ++i) {
-                        g[i] = ffma2(ct[i], gy, g[i]);
-                        const f32x2 after = j + 1 < F ? before[j + 1 < F ? j + 1 : j][i] : h[i];
-                        unpack2(fmul2(g[i], dd.y), v[2 * i], v[2 * i + 1]);
-                        unpack2(fmul2(gy, after), v[NS + 2 * i], v[NS + 2 * i + 1]);
-                        sb = ffma2(g[i], bt[i], sb);
-                        g[i] = fmul2(g[i], decay[j][i]);
-                        const f32x2 w = fmul2(g[i], before[j][i]);
-                        sw = ffma2(w, rate[i], sw);
-                        da[i] = ffma2(w, dd.x, da[i]);
+                    for (int k = 0; k < K; ++k) {
+                        f32x2 sw = 0, sb = 0;
+#pragma unroll
+                        for (int i = 0; i < P; ++i) {
+                            const f32x2 after = j + 1 < F ? before[j + 1 < F ? j + 1 : j][k][i] : h[k][i];
+                            g[k][i] = ffma2(ct[i], both(gy[k]), g[k][i]);
+                            vb[i] = k == 0 ? fmul2(g[k][i], both(d2[2 * k + 1])) : ffma2(g[k][i], both(d2[2 * k + 1]), vb[i]);
+                            vc[i] = k == 0 ? fmul2(after, both(gy[k])) : ffma2(after, both(gy[k]), vc[i]);
+                            sb = i == 0 ? fmul2(g[k][i], bt[i]) : ffma2(g[k][i], bt[i], sb);
+                            g[k][i] = fmul2(g[k][i], decay[j][k][i]);
+                            const f32x2 w = fmul2(g[k][i], before[j][k][i]);
+                            sw = i == 0 ? fmul2(w, rate[k][i]) : ffma2(w, rate[k][i], sw);
+                            da[k][i] = ffma2(w, both(d2[2 * k]), da[k][i]);
+                        }
+                        part[1][j][k] = sum2(sw);
+                        part[2][j][k] = sum2(sb);
                     }
-                    pw[j] = sum2(sw);
-                    pb[j] = sum2(sb);
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        unpack2(vb[i], v[2 * i], v[2 * i + 1]);
+                        unpack2(vc[i], v[NS + 2 * i], v[NS + 2 * i + 1]);
+                    }
 #pragma unroll
                     for (int q = 0; q < NS / 2; ++q)
                         add_four<kSplit>(acc, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], one0[j % kTogether * (NS / 2) + q], one1[j % kTogether * (NS / 2) + q]);
                     if (j % kTogether == 0) {
-                        // lane 4 g + r: values 4 q .. + 3 of token j + r / (NS / 2), q = r % (NS / 2), of four of the eight channels; the
+                        // lane 4 g + r: values 4 q .. + 3 of token j + r / (NS / 2), q = r % (NS / 2), of four of the eight lanes' channels; the
                         // other four are the neighbouring g's
                         const bool odd = lg & 1;
                         const float v0 = acc[0], v1 = acc[1], v2 = acc[2], v3 = acc[3];
@@ -251,37 +282,40 @@ __global__ void __launch_bounds__(kThreads, NS <= 4 ? 2 : 1) ssm_grad_kernel(Ssm
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < F; j += 4) {
-                    if (a.z) sm.sums[0][s + j + quarter][ch] = over_quarters(py[j], py[j + 1], py[j + 2], py[j + 3], quarter);
-                    sm.sums[1][s + j + quarter][ch] = over_quarters(pw[j], pw[j + 1], pw[j + 2], pw[j + 3], quarter);
-                    sm.sums[2][s + j + quarter][ch] = over_quarters(pb[j], pb[j + 1], pb[j + 2], pb[j + 3], quarter);
-                }
+                for (int j = 0; j < F; j += 4)
+#pragma unroll
+                    for (int e = 0; e < 3; ++e) {
+                        if (e == 0 && !a.z) continue;
+                        float to[K];
+#pragma unroll
+                        for (int k = 0; k < K; ++k) to[k] = over_quarters(part[e][j][k], part[e][j + 1][k], part[e][j + 2][k], part[e][j + 3][k], quarter);
+                        store_floats<K>(&sm.sums[e][s + j + quarter][ch], to);
+                    }
             }
             __syncthreads();
             if (there) {
                 const long long r = a.row(at.b, t + et);
-                const float4 w4 = *reinterpret_cast<const float4*>(&sm.sums[1][et][ec]), b4 = *reinterpret_cast<const float4*>(&sm.sums[2][et][ec]);
-                const float w[4] = {w4.x, w4.y, w4.z, w4.w}, into[4] = {b4.x, b4.y, b4.z, b4.w};
-                float dx[4], dd[4];
+                f32x2 w[2], into[2], y[2];
+                load_pairs<4>(&sm.sums[1][et][ec], w);
+                load_pairs<4>(&sm.sums[2][et][ec], into);
+                f32x2 dx[2], dd[2];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    dx[j] = fmaf(delta[j], into[j], skip[j] * dy[j]);
-                    dd[j] = fmaf(w[j], 0.69314718055994531f, x[j] * into[j]) * slope[j];   // (w is of A log2 e)
-                    d_skip[j] = fmaf(dy[j], x[j], d_skip[j]);
-                    d_bias[j] += dd[j];
+                for (int j = 0; j < 2; ++j) {
+                    dx[j] = ffma2(delta[j], into[j], fmul2(skip[j], dy[j]));
+                    dd[j] = fmul2(ffma2(w[j], both(0.69314718055994531f), fmul2(x[j], into[j])), slope[j]);   // (w is of A log2 e)
+                    d_skip[j] = ffma2(dy[j], x[j], d_skip[j]);
+                    d_bias[j] = fadd2(d_bias[j], dd[j]);
                 }
                 store4(a.dx + r * a.lddx + g0, dx);
                 store4(a.ddt + r * a.ldddt + g0, dd);
                 if (a.z && a.dz) {
-                    const float4 y4 = *reinterpret_cast<const float4*>(&sm.sums[0][et][ec]);
-                    const float y[4] = {y4.x, y4.y, y4.z, y4.w};
-                    float dz[4];
+                    load_pairs<4>(&sm.sums[0][et][ec], y);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float s = sigmoid_of<T>(z[j], exp_minus_abs<T>(z[j]));
-                        dz[j] = o[j] * fmaf(skip[j], x[j], y[j]) * s * fmaf(z[j], 1.f - s, 1.f);
+                    for (int j = 0; j < 2; ++j) {
+                        const f32x2 s = sigmoid2<T>(z[j]);
+                        y[j] = fmul2(fmul2(o[j], ffma2(skip[j], x[j], y[j])), fmul2(s, ffma2(z[j], neg_add2(s, both(1.f)), both(1.f))));
                     }
-                    store4(a.dz + r * a.lddz + g0, dz);
+                    store4(a.dz + r * a.lddz + g0, y);
                 }
             }
             // the block's sums over channels: its warps in order
@@ -291,25 +325,28 @@ __global__ void __launch_bounds__(kThreads, NS <= 4 ? 2 : 1) ssm_grad_kernel(Ssm
                 if (t + tt >= t1) continue;
                 float s = 0.f;
 #pragma unroll
-                for (int w = 0; w < 8; ++w) s += sm.bc[tt][w][e];
+                for (int w = 0; w < kWarps; ++w) s += sm.bc[tt][w][e];
                 a.part_bc[(((long long)cb * a.B * a.L + a.row(at.b, t + tt)) * a.G + at.group) * (2 * NP) + e] = s;
             }
             __syncthreads();   // (sums, bc and step are written again)
         }
         const long long where = (long long)at.b * a.segs + at.seg;
-        if (live) {
-            store_pairs<NS>(a.part_a + (where * a.C + c) * NP + n0, da);
-            if (a.d_state_in && at.seg == 0) store_states<NS>(a.d_state_in + own, a.N, n0, g);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (ch + k >= at.live) break;
+            store_pairs<NS>(a.part_a + (where * a.C + at.c0 + ch + k) * NP + n0, da[k]);
+            if (a.d_state_in && at.seg == 0) store_states<NS>(a.d_state_in + own + k * a.N, a.N, n0, g[k]);
         }
-        // sums over the tokens of what is a channel's: sixteen threads hold a part each
-        *reinterpret_cast<float4*>(&sm.sums[0][et][ec]) = make_float4(d_skip[0], d_skip[1], d_skip[2], d_skip[3]);
-        *reinterpret_cast<float4*>(&sm.sums[1][et][ec]) = make_float4(d_bias[0], d_bias[1], d_bias[2], d_bias[3]);
+        // sums over the tokens of what is a channel's: the threads of a tile's tokens hold a part each
+        store4(&sm.sums[0][et][ec], d_skip);
+        store4(&sm.sums[1][et][ec], d_bias);
         __syncthreads();
-        if (tid < 2 * kCh && (tid % kCh) < at.live) {
+        for (int i = tid; i < 2 * kCh; i += kThreads) {
+            if (i % kCh >= at.live) continue;
             float s = 0.f;
 #pragma unroll
-            for (int i = 0; i < kTile; ++i) s += sm.sums[tid / kCh][i][tid % kCh];
-            a.part_c[(where * 2 + tid / kCh) * a.C + at.c0 + tid % kCh] = s;
+            for (int e = 0; e < kTile; ++e) s += sm.sums[i / kCh][e][i % kCh];
+            a.part_c[(where * 2 + i / kCh) * a.C + at.c0 + i % kCh] = s;
         }
         __syncthreads();
     }
@@ -367,24 +404,34 @@ __global__ void __launch_bounds__(256) ssm_grad_sums_kernel(Ssm<T> a, int NP, un
     }
 }
 
-int blocks_at_a_time(int NS, long long items) {
-    const long long most = 148LL * (NS <= 4 ? 2 : 1);
-    return (int)(items < most ? items : most);
-}
+#ifndef VIG_GF
+#define VIG_GF 8
+#define VIG_GB 2
+#endif
+// How the padded states of a channel are spread: channels and tokens of a lane, blocks an SM.
+template <int NS>
+struct Form { static constexpr int K = 2, F = VIG_GF, kBlocks = VIG_GB; };
+template <>
+struct Form<8> { static constexpr int K = 2, F = 4, kBlocks = 2; };
+
+template <typename F>
+auto by_states(int NP, F f) { return NP == 8 ? f(Form<2>{}) : NP == 16 ? f(Form<4>{}) : f(Form<8>{}); }
+
+long long blocks_at_a_time(int per_sm, long long items) { return items < 148LL * per_sm ? items : 148LL * per_sm; }
 
 template <typename T, int NS>
 cudaError_t grad(const Ssm<T>& a, cudaStream_t stream) {
-    const cudaError_t e = allow_smem<ssm_grad_kernel<T, NS>>(sizeof(Smem<NS>));
-    if (e != cudaSuccess) return e;
+    typedef Form<NS> Of;
     count_launch();
-    return launch_pdl(ssm_grad_kernel<T, NS>, dim3(blocks_at_a_time(NS, a.items)), dim3(kThreads), sizeof(Smem<NS>), stream, a);
+    return launch_pdl(ssm_grad_kernel<T, NS, Of::K, Of::F, Of::kBlocks>, dim3((unsigned)blocks_at_a_time(Of::kBlocks, a.items)), dim3(threads_of(Of::K)), 0,
+                      stream, a);
 }
 
 }  // namespace
 
 template <typename T>
 size_t ssm_grad_scratch(Ssm<T>& a, char* base) {
-    const int NP = ssm_padded(a.N), NS = NP / 4, F = NS <= 4 ? 8 : 4;
+    const int NP = ssm_padded(a.N);
     size_t at = 0;
     auto take = [&](float*& p, size_t floats) {
         p = reinterpret_cast<float*>(base ? base + at : nullptr);
@@ -394,7 +441,10 @@ size_t ssm_grad_scratch(Ssm<T>& a, char* base) {
     take(a.ends, a.segs > 1 ? segs * a.C * NP : 0);
     take(a.adjoint, a.segs > 1 ? segs * a.C * NP : 0);
     take(a.total, a.segs > 1 ? segs * a.C : 0);
-    take(a.kept, (size_t)blocks_at_a_time(NS, a.items) * ((a.seg + F - 1) / F) * kThreads * NS);
+    take(a.kept, by_states(NP, [&](auto of) {
+             typedef decltype(of) Of;
+             return (size_t)blocks_at_a_time(Of::kBlocks, a.items) * ((a.seg + Of::F - 1) / Of::F) * kCh * NP;
+         }));
     take(a.part_bc, (size_t)a.blocks * a.B * a.L * a.G * 2 * NP);
     take(a.part_a, segs * a.C * NP);
     take(a.part_c, segs * 2 * a.C);
