@@ -188,12 +188,15 @@ __global__ void __launch_bounds__(kThreads) conv_bwd_kernel(Conv<T> a) {
     }
     if (!a.part) return;
     float* part = a.part + rest * ((long long)a.C * (K + 1));
+    float line[N * K];   // [N channels][K], as the weights lie
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int k = 0; k < K; ++k) part[(long long)(c + j) * K + k] = dw[k][j];
+        for (int k = 0; k < K; ++k) line[j * K + k] = dw[k][j];
 #pragma unroll
-    for (int j = 0; j < N; ++j) part[(long long)a.C * K + c + j] = db[j];
+    for (int i = 0; i < N * K; i += 4) *reinterpret_cast<float4*>(part + (long long)c * K + i) = make_float4(line[i], line[i + 1], line[i + 2], line[i + 3]);
+#pragma unroll
+    for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(part + (long long)a.C * K + c + j) = make_float4(db[j], db[j + 1], db[j + 2], db[j + 3]);
 }
 
 // One token of each sequence; the window moves on by one.
@@ -270,14 +273,17 @@ struct Step {
 
 }  // namespace
 
-// The longest pieces that still give every SM about a thousand threads: the K - 1 tokens beside a piece are read twice.
+// The longest pieces that still give every SM the threads that its registers hold (640; the gradient, which leaves partial sums of K + 1
+// values a channel and piece too, 256, once and a half): the K - 1 tokens beside a piece are read twice.
 template <typename T>
 void conv_pieces(Conv<T>& a, bool gradient) {
-    const long long one = (long long)a.B * (a.C / Vec<T>::N);
+    const long long one = (long long)a.B * (a.C / Vec<T>::N), want = 148 * (gradient ? 384 : 640);
     int piece = 64;
-    while (piece > (gradient ? 8 : 4) && one * ((a.L + piece - 1LL) / piece) < 148 * 1024) piece /= 2;
-    a.piece = piece;
+    while (piece > (gradient ? 8 : 4) && one * ((a.L + piece - 1LL) / piece) < want) piece /= 2;
+    // as long as one another
     a.pieces = (int)((a.L + (long long)piece - 1) / piece);
+    a.piece = (int)((a.L + (long long)a.pieces - 1) / a.pieces);
+    a.pieces = (int)((a.L + (long long)a.piece - 1) / a.piece);
 }
 template <typename T>
 cudaError_t launch_conv(const Conv<T>& a, int K, int act, cudaStream_t stream) { return by_width(K, act, Forward<T>{a, stream}); }

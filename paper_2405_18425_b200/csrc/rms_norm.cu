@@ -17,14 +17,18 @@ namespace {
 // wherever the threads meet in it).
 constexpr int threads_of_block(int tpr) { return tpr == 32 ? 256 : tpr; }
 
+__device__ __forceinline__ float max_or_nan(float a, float b) {   // (fmaxf would drop a NaN: a block that holds one has it as its scale)
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
 // Sum (or maximum) over the TPR threads of a row, in a fixed order; `red`: 32 floats of shared memory a row of more than one warp.
 template <int TPR, bool MAX>
 __device__ __forceinline__ float over_row(float v, float* red) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         const float u = __shfl_xor_sync(0xffffffffu, v, o);
-        // (fmaxf would drop a NaN: a block that holds one has it as its scale)
-        v = MAX ? (v != v || u != u ? v + u : fmaxf(v, u)) : v + u;
+        v = MAX ? max_or_nan(v, u) : v + u;
     }
     if constexpr (TPR > 32) {
         const int warp = threadIdx.x >> 5;
@@ -33,7 +37,7 @@ __device__ __forceinline__ float over_row(float v, float* red) {
         __syncthreads();
         v = red[0];
 #pragma unroll
-        for (int i = 1; i < TPR / 32; ++i) v = MAX ? (v != v || red[i] != red[i] ? v + red[i] : fmaxf(v, red[i])) : v + red[i];
+        for (int i = 1; i < TPR / 32; ++i) v = MAX ? max_or_nan(v, red[i]) : v + red[i];
     }
     return v;
 }
@@ -129,20 +133,14 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
         for (int i = 0; i < V; ++i) {
             float m = 0.f;
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float u = fabsf(s[i][j]);
-                m = u != u || m != m ? u + m : fmaxf(m, u);
-            }
+            for (int j = 0; j < N; ++j) m = max_or_nan(m, fabsf(s[i][j]));
             if (lane + i * TPR >= nv) m = 0.f;   // (behind the row: zero times a scale that may be infinite)
             if constexpr (OUT == 2) {
 #pragma unroll
-                for (int o = kLanes / 2; o > 0; o >>= 1) {
-                    const float u = __shfl_xor_sync(0xffffffffu, m, o);
-                    m = u != u || m != m ? u + m : fmaxf(m, u);
-                }
+                for (int o = kLanes / 2; o > 0; o >>= 1) m = max_or_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
             }
             each[i] = m;
-            most = m != m || most != most ? m + most : fmaxf(most, m);
+            most = max_or_nan(most, m);
         }
         if constexpr (OUT == 1) most = over_row<TPR, true>(most, red);
 #pragma unroll
@@ -150,11 +148,11 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
             const int v = lane + i * TPR;
             // the smallest normal number at least, so that a block of zeros divides by it too
             const float m = OUT == 1 ? most : each[i];
-            const float scale = m != m ? m : fmaxf(__fdiv_rn(m, 448.f), 1.17549435e-38f);
+            const float scale = max_or_nan(__fdiv_rn(m, 448.f), 1.17549435e-38f), over = __fdiv_rn(1.f, scale);
             if (!live || v >= nv) continue;
-            float q[N];
+            float q[N];   // (a product off by a step of fp32 at most, where divisions took a third of the time)
 #pragma unroll
-            for (int j = 0; j < N; ++j) q[j] = __fdiv_rn(s[i][j], scale);
+            for (int j = 0; j < N; ++j) q[j] = s[i][j] * over;
             unsigned char* p = a.q + at + v * N;
             if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(e4m3x4(q[0], q[1], q[2], q[3]), e4m3x4(q[4], q[5], q[6], q[7]));
             else *reinterpret_cast<uint32_t*>(p) = e4m3x4(q[0], q[1], q[2], q[3]);
@@ -242,14 +240,15 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_bwd_kernel(Rms
     for (int c = threadIdx.x; c < a.C; c += blockDim.x) a.part[(long long)blockIdx.x * a.C + c] = sums[c];
 }
 
+constexpr int kRuns = 32;   // a block is a warp a run
 template <typename T>
-__global__ void __launch_bounds__(256) column_sums_kernel(ColumnSums<T> a) {
-    __shared__ float part[8][33];
+__global__ void __launch_bounds__(32 * kRuns) column_sums_kernel(ColumnSums<T> a) {
+    __shared__ float part[kRuns][33];
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    // eight runs of neighbouring rows, each in order, then the runs in order
-    const long long per = (a.rows + 7) / 8, lo = run * per, hi = lo + per < a.rows ? lo + per : a.rows;
+    // runs of neighbouring rows, each in order, then the runs in order
+    const long long per = (a.rows + kRuns - 1) / kRuns, lo = run * per < a.rows ? run * per : a.rows, hi = lo + per < a.rows ? lo + per : a.rows;
     float s = 0.f;
     if (c < a.columns) {
         long long r = lo;
@@ -265,7 +264,7 @@ __global__ void __launch_bounds__(256) column_sums_kernel(ColumnSums<T> a) {
     part[run][lane] = s;
     __syncthreads();
     if (run != 0 || c >= a.columns) return;
-    for (int i = 1; i < 8; ++i) s += part[i][lane];
+    for (int i = 1; i < kRuns; ++i) s += part[i][lane];
     if (c < a.first) {
         if (a.a) from_f32(a.a + c, s);
     } else if (c < a.second) {
@@ -350,7 +349,7 @@ cudaError_t launch_rms_norm_bwd(const RmsNormGrad<T>& a, T* dweight, cudaStream_
 template <typename T>
 cudaError_t launch_column_sums(const ColumnSums<T>& a, cudaStream_t stream) {
     count_launch();
-    return launch_pdl(column_sums_kernel<T>, dim3((a.columns + 31) / 32), dim3(256), 0, stream, a);
+    return launch_pdl(column_sums_kernel<T>, dim3((a.columns + 31) / 32), dim3(32 * kRuns), 0, stream, a);
 }
 
 #define VIG_INSTANCES(T)                                                                        \

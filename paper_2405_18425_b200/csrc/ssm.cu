@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
         }
     }
     // element-wise: token et of a tile, channels ec .. ec + 3
-    const int et = threadIdx.x / 16, ec = (threadIdx.x % 16) * 4;
+    const int et = threadIdx.x / (kCh / 4), ec = (threadIdx.x % (kCh / 4)) * 4;
     const bool mine = ec < at.live;
     const int g0 = at.c0 + (mine ? ec : 0);
     f32x2 bias[2], skip[2];
@@ -91,10 +91,10 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
         }
     load(t0);
     for (int t = t0; t < t1; t += kTile) {
-        f32x2 x[2], z[2];
+        const typename Four<T>::Raw cx = rx, cz = rz;
         const bool there = mine && t + et < t1;
         {
-            f32x2 d[2], o[2];
+            f32x2 x[2], z[2], d[2], o[2];
             widen4(rx, x);
             widen4(rd, d);
             widen4(rz, z);
@@ -150,7 +150,9 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
         __syncthreads();
         if (MODE == kMain) {
             if (there) {
-                f32x2 y[2], part[2];
+                f32x2 x[2], z[2], y[2], part[2];
+                widen4(cx, x);
+                widen4(cz, z);
                 load_pairs<4>(&sums[et][0][ec], y);
 #pragma unroll
                 for (int q = 1; q < 4; ++q) {
@@ -234,14 +236,14 @@ __global__ void __launch_bounds__(128) ssm_step_kernel(Ssm<T> a, float* state, i
     const float* rate = a.A + (long long)c * a.N + n0;
     const T *pb = a.Bt + b * a.ldB + group * a.N + n0, *pc = a.Ct + b * a.ldC + group * a.N + n0;
     if (WIDE && n0 < a.N) {
-        const float4 u = *reinterpret_cast<const float4*>(s);
-        h[0] = u.x; h[1] = u.y; h[2] = u.z; h[3] = u.w;
+        load_floats<4>(s, h);
+        load_floats<4>(rate, A);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const bool there = n0 + j < a.N;
         if (!WIDE || n0 >= a.N) h[j] = there ? s[j] : 0.f;
-        A[j] = there ? rate[j] * kLog2E : 0.f;
+        if (!WIDE || n0 >= a.N) A[j] = there ? rate[j] : 0.f;
         Bt[j] = there ? to_f32(pb[j]) : 0.f;
         Ct[j] = there ? to_f32(pc[j]) : 0.f;
     }
@@ -251,7 +253,7 @@ __global__ void __launch_bounds__(128) ssm_step_kernel(Ssm<T> a, float* state, i
     float y = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        h[j] = fmaf(ex2(delta * A[j]), h[j], in * Bt[j]);
+        h[j] = fmaf(ex2(delta * (A[j] * kLog2E)), h[j], in * Bt[j]);
         y = fmaf(Ct[j], h[j], y);
     }
     if (live) {
@@ -273,14 +275,11 @@ cudaError_t walk_of(const Ssm<T>& a, cudaStream_t stream) {
     count_launch();
     return launch_pdl(ssm_kernel<T, NS, K, MODE>, dim3((unsigned)a.items), dim3(threads_of(K)), 0, stream, a);
 }
-#ifndef VIG_K
-#define VIG_K 2
-#endif
 template <typename T, int MODE>
 cudaError_t walk(const Ssm<T>& a, cudaStream_t stream) {
     switch (ssm_padded(a.N)) {
-        case 8: return walk_of<T, 2, VIG_K, MODE>(a, stream);
-        case 16: return walk_of<T, 4, VIG_K, MODE>(a, stream);
+        case 8: return walk_of<T, 2, 2, MODE>(a, stream);
+        case 16: return walk_of<T, 4, 2, MODE>(a, stream);
         default: return walk_of<T, 8, 1, MODE>(a, stream);
     }
 }
@@ -291,8 +290,8 @@ cudaError_t walk(const Ssm<T>& a, cudaStream_t stream) {
 template <typename T>
 void ssm_segments(Ssm<T>& a, bool gradient) {
     a.blocks = (a.per + kCh - 1) / kCh;
-    const long long whole = (long long)a.B * a.G * a.blocks, want = 148 * (gradient ? 2 : 4);
-    long long segs = whole >= want / 2 ? 1 : (want + whole - 1) / (whole > 0 ? whole : 1);
+    const long long whole = (long long)a.B * a.G * a.blocks, want = 148 * (gradient ? 2 : 5);
+    long long segs = whole >= want / 2 ? 1 : want / (whole > 0 ? whole : 1);
     const long long most = (a.L + 63LL) / 64;
     if (segs > most) segs = most;
     if (segs < 1) segs = 1;
@@ -327,7 +326,7 @@ cudaError_t launch_ssm_step(const Ssm<T>& a, float* state, cudaStream_t stream) 
     while (4 * lanes < a.N) lanes *= 2;
     const dim3 grid((unsigned)(((long long)a.B * a.C * lanes + 127) / 128));
     count_launch();
-    if (a.N % 4 == 0) return launch_pdl(ssm_step_kernel<T, true>, grid, dim3(128), 0, stream, a, state, lanes);
+    if (a.N % 4 == 0 && (reinterpret_cast<uintptr_t>(a.A) & 15u) == 0) return launch_pdl(ssm_step_kernel<T, true>, grid, dim3(128), 0, stream, a, state, lanes);
     return launch_pdl(ssm_step_kernel<T, false>, grid, dim3(128), 0, stream, a, state, lanes);
 }
 

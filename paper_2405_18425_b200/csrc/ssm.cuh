@@ -15,7 +15,7 @@ namespace ssm {
 
 constexpr int kCh = kSsmChannels;
 constexpr int kRow = kCh + 8;   // floats of a quarter's row of sums: the four that a warp writes at a time lie in different banks
-__host__ __device__ constexpr int threads_of(int K) { return 256 / K; }
+__host__ __device__ constexpr int threads_of(int K) { return 4 * kCh / K; }
 __host__ __device__ constexpr int tile_of(int K) { return 16 / K; }   // tokens of a tile: four values a thread
 
 // Four neighbouring values.
@@ -204,44 +204,34 @@ __device__ __forceinline__ void store_pairs(float* p, const f32x2 (&v)[NS / 2]) 
         }
     }
 }
-// 2^v of a pair: from the special-function unit (relative error 2^-22, sixteen a clock and SM), or as arithmetic, which other pipes do: 2 to
-// the nearest whole number is put together from bits, 2^f for the rest, |f| <= 1/2, is a polynomial of least largest relative error (2^-23.4 of
-// degree five, 2^-28.9 of six; fitted like the logarithm's).  Below 2^-126 the result is 2^-126, a decay as good as none.
+// 2^v of a pair: from the special-function unit (relative error 2^-22, sixteen a clock and SM), or, for fp32 calls, whose sums show that
+// error, as arithmetic: 2 to the nearest whole number is put together from bits, 2^f for the rest, |f| <= 1/2, is a polynomial of least largest
+// relative error, 2^-28.9 (fitted like the logarithm's).  Below 2^-126 the result is 2^-126, a decay as good as none.  (A quarter of the
+// bf16 states this way, to relieve the special-function unit: 95 to 106 us for 64 x 196 x 1152; an eighth: 100.)
 __device__ __forceinline__ f32x2 exp2_special(f32x2 v) {
     float lo, hi;
     unpack2(v, lo, hi);
     return pack2(ex2(lo), ex2(hi));
 }
-template <bool SIX>
 __device__ __forceinline__ f32x2 exp2_arithmetic(f32x2 v) {
     float a, b, x, y;
     unpack2(v, a, b);
     v = pack2(fminf(fmaxf(a, -126.f), 128.f), fminf(fmaxf(b, -126.f), 128.f));
     const f32x2 whole = fadd2(v, both(12582912.f));   // 1.5 2^23: the nearest whole number in the last bits
     const f32x2 f = fadd2(v, neg_add2(whole, both(12582912.f)));
-    f32x2 p;
-    if constexpr (SIX) {
-        p = ffma2(f, both(0.00015353361959569156f), both(0.0013398873852565885f));
-        p = ffma2(f, p, both(0.00961843691766262f));
-        p = ffma2(f, p, both(0.055503323674201965f));
-        p = ffma2(f, p, both(0.24022647738456726f));
-        p = ffma2(f, p, both(0.6931471824645996f));
-    } else {
-        p = ffma2(f, both(0.001326472731307149f), both(0.009671512991189957f));
-        p = ffma2(f, p, both(0.05550733581185341f));
-        p = ffma2(f, p, both(0.24022242426872253f));
-        p = ffma2(f, p, both(0.6931470036506653f));
-    }
+    f32x2 p = ffma2(f, both(0.00015353361959569156f), both(0.0013398873852565885f));
+    p = ffma2(f, p, both(0.00961843691766262f));
+    p = ffma2(f, p, both(0.055503323674201965f));
+    p = ffma2(f, p, both(0.24022647738456726f));
+    p = ffma2(f, p, both(0.6931471824645996f));
     p = ffma2(f, p, both(1.f));
     unpack2(whole, x, y);
     unpack2(p, a, b);
     return pack2(__uint_as_float(__float_as_uint(a) + (__float_as_uint(x) << 23)), __uint_as_float(__float_as_uint(b) + (__float_as_uint(y) << 23)));
 }
-// The decays of pair i at token j of a run: fp32 calls take the arithmetic for its digits, bf16 calls for a quarter of the states (every pair at
-// another token), so that the special-function unit and the others end together.
 template <typename T>
 __device__ __forceinline__ f32x2 decay2(f32x2 v) {
-    if constexpr (sizeof(T) == 4) return exp2_arithmetic<true>(v);
+    if constexpr (sizeof(T) == 4) return exp2_arithmetic(v);
     else return exp2_special(v);
 }
 // Sums over the four lanes of a channel of what they hold for four tokens: lane quarter q ends with token q's.

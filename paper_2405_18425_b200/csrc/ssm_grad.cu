@@ -10,6 +10,7 @@
 // Sums over the states cross four lanes; sums over the channels, two for every state and token, are tensor-core products with a
 // matrix of zeros and ones (tf32 terms, one for bf16 calls, whose results are rounded to eight bits, and two for fp32), a quarter of
 // the shuffles' instructions.  What a block has summed over its channels goes through memory to a last launch that adds the blocks in order.
+#include "gdr.h"
 #include "ssm.cuh"
 
 namespace vig {
@@ -47,7 +48,7 @@ __device__ __forceinline__ void add_four(float (&d)[4], float v0, float v1, floa
     }
 }
 
-template <int NS, int K>
+template <int NS, int K, int F>
 struct Smem {
     static constexpr int NP = 4 * NS, kTile = tile_of(K);
     float step[kTile][kCh][2];        // delta, delta x
@@ -55,6 +56,9 @@ struct Smem {
     float rows_b[kTile * NP], rows_c[kTile * NP];
     float sums[3][kTile][kRow];       // y; sum w A (of A log2 e); sum g B
     float bc[kTile][8 / K][2 * NP];   // sums over a warp's channels
+    float slope[kTile][kCh];          // of the step size
+    float bias[kCh], skip[kCh];
+    float decay[F][K][threads_of(K)][NS];   // a lane's own
 };
 
 // F: tokens whose decays and states a lane holds in registers.
@@ -62,11 +66,12 @@ template <typename T, int NS, int K, int F, int BLOCKS>
 __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> a) {
     constexpr int NP = 4 * NS, P = NS / 2, kThreads = threads_of(K), kTile = tile_of(K), kWarps = 8 / K;
     constexpr bool kSplit = sizeof(T) == 4;
-    __shared__ __align__(16) Smem<NS, K> sm;
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    Smem<NS, K, F>& sm = *reinterpret_cast<Smem<NS, K, F>*>(smem_raw);
     pdl_wait();
     pdl_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ch = (warp * 8 + (lane & 7)) * K, quarter = lane >> 3, n0 = quarter * NS;
-    const int et = tid / 16, ec = (tid % 16) * 4;
+    const int et = tid / (kCh / 4), ec = (tid % (kCh / 4)) * 4;
     const int per_seg = (a.seg + F - 1) / F;
     float* kept = a.kept + ((long long)blockIdx.x * per_seg * K * kThreads + tid) * NS;
     // products with ones: pair i of columns takes lanes of lane / 4 == 2 i (row r of B) and 2 i + 1 (row r + 4)
@@ -103,13 +108,12 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                 }
             }
         }
-        f32x2 bias[2], skip[2], d_skip[2], d_bias[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            bias[j] = a.bias ? pack2(a.bias[g0 + 2 * j], a.bias[g0 + 2 * j + 1]) : 0;
-            skip[j] = a.D ? pack2(a.D[g0 + 2 * j], a.D[g0 + 2 * j + 1]) : 0;
-            d_skip[j] = d_bias[j] = 0;
+        f32x2 d_skip[2] = {0, 0}, d_bias[2] = {0, 0};
+        for (int i = tid; i < kCh; i += kThreads) {
+            sm.bias[i] = a.bias && i < at.live ? a.bias[at.c0 + i] : 0.f;
+            sm.skip[i] = a.D && i < at.live ? a.D[at.c0 + i] : 0.f;
         }
+        __syncthreads();
         typename Four<T>::Raw rx = {}, rd = {}, rz = {}, ro = {};
         Rows<T, NP, kTile, kThreads> rb, rc;
         rb.start(a.Bt, a, a.ldB, at, t0);
@@ -133,9 +137,10 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
         for (int m = 0; m < tiles; ++m) {
             const int t = t0 + m * kTile;
             const bool there = mine && t + et < t1;
-            f32x2 x[2], d[2];
+            f32x2 x[2], d[2], bias[2];
             widen4(rx, x);
             widen4(rd, d);
+            load_pairs<4>(&sm.bias[ec], bias);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 f32x2 delta = fadd2(d[j], bias[j]);
@@ -177,25 +182,36 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
         for (int m = tiles - 1; m >= 0; --m) {
             const int t = t0 + m * kTile;
             const bool there = mine && t + et < t1;
-            f32x2 x[2], z[2], o[2], delta[2], slope[2], dy[2];
-            widen4(rx, x);
-            widen4(rd, delta);
-            widen4(rz, z);
-            widen4(ro, o);
+            const typename Four<T>::Raw cx = rx, cz = rz, co = ro;
+            if constexpr (F == kTile) {   // (on its way while the tile is prepared)
+                const float* from = kept + (long long)m * K * kThreads * NS;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                delta[j] = fadd2(delta[j], bias[j]);
-                slope[j] = both(1.f);
-                if (a.softplus) {
-                    const f32x2 u = exp_minus_abs<T>(delta[j]);
-                    slope[j] = sigmoid2<T>(delta[j], u);
-                    delta[j] = softplus2(delta[j], u);
-                }
-                dy[j] = a.z ? fmul2(o[j], fmul2(z[j], sigmoid2<T>(z[j]))) : o[j];
-                if (!there) delta[j] = dy[j] = x[j] = 0;
-                put_step(&sm.step[et][ec + 2 * j], delta[j], fmul2(delta[j], x[j]));
+                for (int k = 0; k < K; ++k) load_pairs<NS>(from + k * kThreads * NS, h[k]);
             }
-            store4(&sm.dy[et][ec], dy);
+            {
+                f32x2 x[2], z[2], dy[2], delta[2], slope[2], bias[2];
+                widen4(cx, x);
+                widen4(rd, delta);
+                widen4(cz, z);
+                widen4(co, dy);
+                load_pairs<4>(&sm.bias[ec], bias);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    delta[j] = fadd2(delta[j], bias[j]);
+                    slope[j] = both(1.f);
+                    if (a.softplus) {
+                        const f32x2 u = exp_minus_abs<T>(delta[j]);
+                        slope[j] = sigmoid2<T>(delta[j], u);
+                        delta[j] = softplus2(delta[j], u);
+                    }
+                    if (a.z) dy[j] = fmul2(dy[j], fmul2(z[j], sigmoid2<T>(z[j])));
+                    f32x2 in = fmul2(delta[j], x[j]);
+                    if (!there) delta[j] = dy[j] = in = 0;
+                    put_step(&sm.step[et][ec + 2 * j], delta[j], in);
+                }
+                store4(&sm.dy[et][ec], dy);
+                store4(&sm.slope[et][ec], slope);
+            }
             rb.put(sm.rows_b);
             rc.put(sm.rows_c);
             __syncthreads();
@@ -207,11 +223,13 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
 #pragma unroll 1
             for (int s = kTile - F; s >= 0; s -= F) {
                 if (t + s >= t1) continue;
-                f32x2 decay[F][K][P], before[F][K][P];
-                float part[3][F][K];
-                const float* from = kept + (long long)((m * kTile + s) / F) * K * kThreads * NS;
+                f32x2 before[F][K][P];
+                float part[2][4][K];
+                if constexpr (F != kTile) {
+                    const float* from = kept + (long long)((m * kTile + s) / F) * K * kThreads * NS;
 #pragma unroll
-                for (int k = 0; k < K; ++k) load_pairs<NS>(from + k * kThreads * NS, h[k]);
+                    for (int k = 0; k < K; ++k) load_pairs<NS>(from + k * kThreads * NS, h[k]);
+                }
 #pragma unroll
                 for (int j = 0; j < F; ++j) {
                     f32x2 bt[P], ct[P];
@@ -221,15 +239,22 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                     if (a.z) load_pairs<NS>(&sm.rows_c[(s + j) * NP + n0], ct);
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
-                        f32x2 y = 0;
+                        f32x2 y = 0, e[P];
 #pragma unroll
                         for (int i = 0; i < P; ++i) {
                             before[j][k][i] = h[k][i];
-                            decay[j][k][i] = decay2<T>(fmul2(rate[k][i], both(d2[2 * k])));
-                            h[k][i] = ffma2(decay[j][k][i], h[k][i], fmul2(both(d2[2 * k + 1]), bt[i]));
-                            if (a.z) y = ffma2(ct[i], h[k][i], y);
+                            e[i] = decay2<T>(fmul2(rate[k][i], both(d2[2 * k])));
+                            h[k][i] = ffma2(e[i], h[k][i], fmul2(both(d2[2 * k + 1]), bt[i]));
+                            if (a.z) y = i == 0 ? fmul2(ct[i], h[k][i]) : ffma2(ct[i], h[k][i], y);
                         }
-                        part[0][j][k] = sum2(y);
+                        store_pairs<NS>(sm.decay[j][k][tid], e);
+                        part[0][j % 4][k] = sum2(y);
+                    }
+                    if (j % 4 == 3 && a.z) {
+                        float to[K];
+#pragma unroll
+                        for (int k = 0; k < K; ++k) to[k] = over_quarters(part[0][0][k], part[0][1][k], part[0][2][k], part[0][3][k], quarter);
+                        store_floats<K>(&sm.sums[0][s + j - 3 + quarter][ch], to);
                     }
                 }
                 float acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -244,7 +269,8 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                     load_pairs<NS>(&sm.rows_c[(s + j) * NP + n0], ct);
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
-                        f32x2 sw = 0, sb = 0;
+                        f32x2 sw = 0, sb = 0, e[P];
+                        load_pairs<NS>(sm.decay[j][k][tid], e);
 #pragma unroll
                         for (int i = 0; i < P; ++i) {
                             const f32x2 after = j + 1 < F ? before[j + 1 < F ? j + 1 : j][k][i] : h[k][i];
@@ -252,13 +278,13 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                             vb[i] = k == 0 ? fmul2(g[k][i], both(d2[2 * k + 1])) : ffma2(g[k][i], both(d2[2 * k + 1]), vb[i]);
                             vc[i] = k == 0 ? fmul2(after, both(gy[k])) : ffma2(after, both(gy[k]), vc[i]);
                             sb = i == 0 ? fmul2(g[k][i], bt[i]) : ffma2(g[k][i], bt[i], sb);
-                            g[k][i] = fmul2(g[k][i], decay[j][k][i]);
+                            g[k][i] = fmul2(g[k][i], e[i]);
                             const f32x2 w = fmul2(g[k][i], before[j][k][i]);
                             sw = i == 0 ? fmul2(w, rate[k][i]) : ffma2(w, rate[k][i], sw);
                             da[k][i] = ffma2(w, both(d2[2 * k]), da[k][i]);
                         }
-                        part[1][j][k] = sum2(sw);
-                        part[2][j][k] = sum2(sb);
+                        part[0][j % 4][k] = sum2(sw);
+                        part[1][j % 4][k] = sum2(sb);
                     }
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
@@ -280,28 +306,33 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                         *reinterpret_cast<float2*>(&sm.bc[s + j + lr / (NS / 2)][warp][kind * NP + (lg >> 1) * NS + value % NS]) = make_float2(k0, k1);
                         acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
                     }
-                }
+                    if (j % 4 == 0) {
 #pragma unroll
-                for (int j = 0; j < F; j += 4)
+                        for (int e = 0; e < 2; ++e) {
+                            float to[K];
 #pragma unroll
-                    for (int e = 0; e < 3; ++e) {
-                        if (e == 0 && !a.z) continue;
-                        float to[K];
-#pragma unroll
-                        for (int k = 0; k < K; ++k) to[k] = over_quarters(part[e][j][k], part[e][j + 1][k], part[e][j + 2][k], part[e][j + 3][k], quarter);
-                        store_floats<K>(&sm.sums[e][s + j + quarter][ch], to);
+                            for (int k = 0; k < K; ++k) to[k] = over_quarters(part[e][0][k], part[e][1][k], part[e][2][k], part[e][3][k], quarter);
+                            store_floats<K>(&sm.sums[1 + e][s + j + quarter][ch], to);
+                        }
                     }
+                }
             }
             __syncthreads();
             if (there) {
                 const long long r = a.row(at.b, t + et);
-                f32x2 w[2], into[2], y[2];
+                f32x2 w[2], into[2], x[2], dy[2], slope[2], skip[2];
+                widen4(cx, x);
                 load_pairs<4>(&sm.sums[1][et][ec], w);
                 load_pairs<4>(&sm.sums[2][et][ec], into);
+                load_pairs<4>(&sm.dy[et][ec], dy);
+                load_pairs<4>(&sm.slope[et][ec], slope);
+                load_pairs<4>(&sm.skip[ec], skip);
                 f32x2 dx[2], dd[2];
+                float d[8];
+                load_floats<8>(&sm.step[et][ec][0], d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    dx[j] = ffma2(delta[j], into[j], fmul2(skip[j], dy[j]));
+                    dx[j] = ffma2(pack2(d[4 * j], d[4 * j + 2]), into[j], fmul2(skip[j], dy[j]));
                     dd[j] = fmul2(ffma2(w[j], both(0.69314718055994531f), fmul2(x[j], into[j])), slope[j]);   // (w is of A log2 e)
                     d_skip[j] = ffma2(dy[j], x[j], d_skip[j]);
                     d_bias[j] = fadd2(d_bias[j], dd[j]);
@@ -309,6 +340,9 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                 store4(a.dx + r * a.lddx + g0, dx);
                 store4(a.ddt + r * a.ldddt + g0, dd);
                 if (a.z && a.dz) {
+                    f32x2 z[2], o[2], y[2];
+                    widen4(cz, z);
+                    widen4(co, o);
                     load_pairs<4>(&sm.sums[0][et][ec], y);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
@@ -404,13 +438,9 @@ __global__ void __launch_bounds__(256) ssm_grad_sums_kernel(Ssm<T> a, int NP, un
     }
 }
 
-#ifndef VIG_GF
-#define VIG_GF 8
-#define VIG_GB 2
-#endif
 // How the padded states of a channel are spread: channels and tokens of a lane, blocks an SM.
 template <int NS>
-struct Form { static constexpr int K = 2, F = VIG_GF, kBlocks = VIG_GB; };
+struct Form { static constexpr int K = 2, F = 4, kBlocks = 4; };
 template <>
 struct Form<8> { static constexpr int K = 2, F = 4, kBlocks = 2; };
 
@@ -422,8 +452,11 @@ long long blocks_at_a_time(int per_sm, long long items) { return items < 148LL *
 template <typename T, int NS>
 cudaError_t grad(const Ssm<T>& a, cudaStream_t stream) {
     typedef Form<NS> Of;
+    constexpr size_t smem = sizeof(Smem<NS, Of::K, Of::F>);
+    const cudaError_t e = allow_smem<ssm_grad_kernel<T, NS, Of::K, Of::F, Of::kBlocks>>(smem);
+    if (e != cudaSuccess) return e;
     count_launch();
-    return launch_pdl(ssm_grad_kernel<T, NS, Of::K, Of::F, Of::kBlocks>, dim3((unsigned)blocks_at_a_time(Of::kBlocks, a.items)), dim3(threads_of(Of::K)), 0,
+    return launch_pdl(ssm_grad_kernel<T, NS, Of::K, Of::F, Of::kBlocks>, dim3((unsigned)blocks_at_a_time(Of::kBlocks, a.items)), dim3(threads_of(Of::K)), smem,
                       stream, a);
 }
 
