@@ -311,7 +311,7 @@ int vig_group_norm_bwd_f32(const void* x, const void* weight, const void* bias, 
  * values of x, dt, z, out, Bt, Ct, sequence b beginning at row b L; NULL: dense rows.  A pitch is at least the row's width.
  * Alignment: x, dt, z, out 16 bytes, their pitches multiples of 16 bytes too; Bt and Ct that of their type only; fp32 arrays 4 bytes.
  * C: a multiple of 8 G (bf16) or 4 G (fp32), at most 2^20; N <= 32; L <= 2^31 - 2^16.
- * fp32 inside for either type, exponentials from the special-function unit (relative error 2^-22).  Long sequences of few channels are cut
+ * fp32 inside for either type; decays of bf16 calls (and the single token's) from the special-function unit (relative error 2^-22).  Long sequences of few channels are cut
  * into segments that run side by side, with scratch from the library's pool; whether they are depends on B, C and L, and with it the last
  * bits: the same call repeats them, a call of other sequences beside it may not.  L == 0 with a state_out copies state_in (or zeros) there.
  * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
@@ -328,6 +328,7 @@ int vig_ssm_fwd_f32(const void* x, const void* dt, const void* A, const void* Bt
  * Scratch from the library's pool, stream-ordered: about 8 G N bytes a token for every 64 channels of a group, and the states of every
  * eighth token of the blocks that run at a time.  bf16: the products that make up dB and dC enter their sums over the channels with
  * eleven significant bits (tf32; fp32: as two such terms), the sums are fp32.  An empty call (B or L 0) clears dA, dD and d_dt_bias.
+ * A product that is not finite makes dB and dC of its token NaN, and may make those of up to three tokens beside it NaN.
  * Outputs must not overlap inputs or one another.  Errors: as vig_ssm_fwd_*. */
 int vig_ssm_bwd_bf16(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z,
                      const void* dt_bias, const void* state_in, const void* d_out, const void* d_state_out,
@@ -380,7 +381,7 @@ int vig_causal_conv_step_f32(const void* x, const void* w, const void* bias, voi
  * x, residual (or NULL for 0), out, sum_out (or NULL): [rows, C], weight: [C], all of the call's element type; rstd: FP32 [rows], what the
  * gradient needs, or NULL.  sum_out receives s, which the next block adds to; the norm is of s before that rounding.  fp32 inside; rows
  * whose squares leave the range of fp32 are summed over their largest value.  eps >= 0.  C: a multiple of 8 (bf16) or 4 (fp32), at most
- * 16384.  16-byte alignment (rstd, scales: 4).  sum_out or out (not both) may be x or residual.
+ * 16384.  16-byte alignment (rstd, scales: 4).  sum_out and out may each be x or residual, but not the same one.
  * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
 int vig_rms_norm_bf16(const void* x, const void* residual, const void* weight, void* out, void* sum_out, void* rstd,
                       long long rows, int C, float eps, void* stream);

@@ -117,8 +117,8 @@ int ssm_bwd_impl(const void* x, const void* dt, const void* A, const void* Bt, c
         return VIG_ERR_MISALIGNED;
     int st = check_ssm(B, L, C, G, N, 16 / sizeof(T));
     if (st == VIG_OK) st = pitch.status;
-    // the last launch counts values of dB and dC
-    if (st == VIG_OK && (long long)B * L > (0x7fffffffLL * 128) / ((long long)G * ssm_padded(N))) st = VIG_ERR_UNSUPPORTED;
+    // the last launch's grid counts values of dB and dC, and then those of dA
+    if (st == VIG_OK && (long long)B * L > (0x3fffffffLL * 128) / ((long long)G * ssm_padded(N))) st = VIG_ERR_UNSUPPORTED;
     if (st != VIG_OK) return st;
     if (B == 0 || L == 0) {
         if ((st = clear(dA, (size_t)C * N * 4, stream)) != VIG_OK || (st = clear(dD, (size_t)C * 4, stream)) != VIG_OK ||

@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
         for (int j = 0; j < N; ++j) sum = fmaf(s[i][j], s[i][j], sum);
     }
     sum = over_row<TPR, false>(sum, red);
-    float r = rsqrtf(sum * a.inv_C + a.eps);
+    float r = __frsqrt_rn(sum * a.inv_C + a.eps);
     if (!(sum < 0x1p+120f) || sum < 0x1p-80f) {   // squares that overflow, or that underflow beside no eps: of the row over its largest value
         float top = 0.f;
 #pragma unroll
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
                 }
             sum = over_row<TPR, false>(sum, red);
             const float e = a.eps * down * part;   // eps / top^2 in two steps
-            r = rsqrtf(sum * a.inv_C + e * down * part) * part * down;
+            r = __frsqrt_rn(sum * a.inv_C + e * down * part) * part * down;
         }
     }
     if (a.rstd && live && lane == 0) a.rstd[row] = r;
@@ -150,9 +150,12 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
             const float m = OUT == 1 ? most : each[i];
             const float scale = max_or_nan(__fdiv_rn(m, 448.f), 1.17549435e-38f), over = __fdiv_rn(1.f, scale);
             if (!live || v >= nv) continue;
-            float q[N];   // (a product off by a step of fp32 at most, where divisions took a third of the time)
+            float q[N];   // the quotient by a product and a correction of what is left (divisions took a quarter of the time)
 #pragma unroll
-            for (int j = 0; j < N; ++j) q[j] = s[i][j] * over;
+            for (int j = 0; j < N; ++j) {
+                q[j] = s[i][j] * over;
+                if (over > 0.f) q[j] = fmaf(fmaf(-q[j], scale, s[i][j]), over, q[j]);
+            }
             unsigned char* p = a.q + at + v * N;
             if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(e4m3x4(q[0], q[1], q[2], q[3]), e4m3x4(q[4], q[5], q[6], q[7]));
             else *reinterpret_cast<uint32_t*>(p) = e4m3x4(q[0], q[1], q[2], q[3]);

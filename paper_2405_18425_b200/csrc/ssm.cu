@@ -290,7 +290,7 @@ cudaError_t walk(const Ssm<T>& a, cudaStream_t stream) {
 template <typename T>
 void ssm_segments(Ssm<T>& a, bool gradient) {
     a.blocks = (a.per + kCh - 1) / kCh;
-    const long long whole = (long long)a.B * a.G * a.blocks, want = 148 * (gradient ? 2 : 5);
+    const long long whole = (long long)a.B * a.G * a.blocks, want = 148 * (gradient ? 4 : 5);
     long long segs = whole >= want / 2 ? 1 : want / (whole > 0 ? whole : 1);
     const long long most = (a.L + 63LL) / 64;
     if (segs > most) segs = most;
