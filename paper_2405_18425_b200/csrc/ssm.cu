@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
 
 // The states in front of the segments from what each adds, and from behind the adjoint's: a thread a state.
 template <typename T>
-__global__ void __launch_bounds__(128) ssm_carry_kernel(Ssm<T> a, int NP, bool gradient) {
+__global__ void __launch_bounds__(128) ssm_carry_kernel(Ssm<T> a, int NP) {
     pdl_wait();
     pdl_launch_dependents();
     const long long id = (long long)blockIdx.x * 128 + threadIdx.x, each = (long long)a.C * NP;
@@ -312,7 +312,7 @@ cudaError_t launch_ssm_segments(const Ssm<T>& a, bool gradient, cudaStream_t str
     if (e != cudaSuccess) return e;
     const int NP = ssm_padded(a.N);
     count_launch();
-    return launch_pdl(ssm_carry_kernel<T>, dim3((unsigned)(((long long)a.B * a.C * NP + 127) / 128), gradient ? 2 : 1), dim3(128), 0, stream, a, NP, gradient);
+    return launch_pdl(ssm_carry_kernel<T>, dim3((unsigned)(((long long)a.B * a.C * NP + 127) / 128), gradient ? 2 : 1), dim3(128), 0, stream, a, NP);
 }
 template <typename T>
 cudaError_t launch_ssm_fwd(const Ssm<T>& a, cudaStream_t stream) {

@@ -21,17 +21,6 @@ __host__ __device__ constexpr int tile_of(int K) { return 16 / K; }   // tokens 
 // Four neighbouring values.
 __device__ __forceinline__ uint4 load4(const float* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ uint2 load4(const __nv_bfloat16* p) { return *reinterpret_cast<const uint2*>(p); }
-__device__ __forceinline__ void widen4(const uint4& r, float (&f)[4]) {
-    f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
-}
-__device__ __forceinline__ void widen4(const uint2& r, float (&f)[4]) {
-    f[0] = __uint_as_float(r.x << 16); f[1] = __uint_as_float(r.x & 0xffff0000u);
-    f[2] = __uint_as_float(r.y << 16); f[3] = __uint_as_float(r.y & 0xffff0000u);
-}
-__device__ __forceinline__ void store4(float* p, const float (&f)[4]) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&f)[4]) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
-}
 template <typename T>
 struct Four;
 template <>
@@ -213,10 +202,16 @@ __device__ __forceinline__ f32x2 exp2_special(f32x2 v) {
     unpack2(v, lo, hi);
     return pack2(ex2(lo), ex2(hi));
 }
+__device__ __forceinline__ float clamp_exponent(float v) {   // (a NaN stays one)
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(-126.f));
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(y) : "f"(128.f));
+    return y;
+}
 __device__ __forceinline__ f32x2 exp2_arithmetic(f32x2 v) {
-    float a, b, x, y;
+    float a, b;
     unpack2(v, a, b);
-    v = pack2(fminf(fmaxf(a, -126.f), 128.f), fminf(fmaxf(b, -126.f), 128.f));
+    v = pack2(clamp_exponent(a), clamp_exponent(b));
     const f32x2 whole = fadd2(v, both(12582912.f));   // 1.5 2^23: the nearest whole number in the last bits
     const f32x2 f = fadd2(v, neg_add2(whole, both(12582912.f)));
     f32x2 p = ffma2(f, both(0.00015353361959569156f), both(0.0013398873852565885f));
@@ -225,9 +220,8 @@ __device__ __forceinline__ f32x2 exp2_arithmetic(f32x2 v) {
     p = ffma2(f, p, both(0.24022647738456726f));
     p = ffma2(f, p, both(0.6931471824645996f));
     p = ffma2(f, p, both(1.f));
-    unpack2(whole, x, y);
-    unpack2(p, a, b);
-    return pack2(__uint_as_float(__float_as_uint(a) + (__float_as_uint(x) << 23)), __uint_as_float(__float_as_uint(b) + (__float_as_uint(y) << 23)));
+    unpack2(whole, a, b);
+    return fmul2(p, pack2(__uint_as_float((__float_as_uint(a) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(b) << 23) + 0x3f800000u)));
 }
 template <typename T>
 __device__ __forceinline__ f32x2 decay2(f32x2 v) {

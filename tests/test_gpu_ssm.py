@@ -204,3 +204,32 @@ def test_oracle_is_the_definition_on_the_gpu_inputs():
     y = y + f64(d["D"]) * x
     z = f64(d["z"])
     assert abs(oracle.ssm_fwd(x, dt, A, Bt, Ct, f64(d["D"]), z, f64(d["dt_bias"]))[0] - y * z / (1 + np.exp(-z))).max() < 1e-12
+
+
+@pytest.mark.parametrize("L", [40, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_are_not_finite_stay_where_they_belong(dtype, L):
+    """A NaN in x: its channel from its token on, in its sequence; a NaN in A: its channel; neighbours, other sequences and earlier tokens
+    keep their bits."""
+    d = ssm_inputs(2, L, 72, 16, dtype, seed=13, states=True)
+    want = ssm_forward(d)
+    x = d["x"].clone()
+    x[1, 21, 5] = float("nan")
+    got = ssm_forward({**d, "x": x})
+    bad = torch.zeros_like(got["out"], dtype=torch.bool)
+    bad[1, 21:, 5] = True
+    assert torch.isnan(got["out"][bad]).all() and torch.equal(got["out"][~bad], want["out"][~bad])
+    A = d["A"].clone()
+    A[7, 3] = float("nan")
+    got = ssm_forward({**d, "A": A})
+    bad = torch.zeros_like(bad)
+    bad[:, :, 7] = True
+    assert torch.isnan(got["out"][bad]).all() and torch.equal(got["out"][~bad], want["out"][~bad])
+    # the decay of a rate without end: the state is forgotten at every token (a step size of zero aside)
+    A = d["A"].clone()
+    A[9] = -float("inf")
+    got = ssm_forward({**d, "A": A})
+    assert torch.isfinite(got["out"]).all() and torch.equal(got["out"][:, :, 10:], want["out"][:, :, 10:])
+    alone = d["dt"].float()[:, -1, 9] + d["dt_bias"][9]
+    h = torch.nn.functional.softplus(alone)[:, None] * d["x"].float()[:, -1, 9, None] * d["Bt"].float()[:, -1, 0]
+    assert torch.allclose(got["state_out"][:, 9], h, rtol=1e-5, atol=1e-6)
