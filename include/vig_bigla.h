@@ -323,10 +323,10 @@ int vig_ssm_fwd_f32(const void* x, const void* dt, const void* A, const void* Bt
                     int B, int L, int C, int G, int N, const long long* ld, int softplus, int reverse, void* stream);
 /* Its gradient.  d_out: [B, L, C]; d_state_out: gradient with respect to state_out (fp32) or NULL for zero.  Writes dx, ddt [B, L, C], dA
  * (FP32 [C, N]), dB, dC ([B, L, G, N], sums over a group's channels in a fixed order) and, unless they are NULL, dD, d_dt_bias (FP32
- * [C]), dz [B, L, C] and d_state_in (fp32; may be d_state_out).  Everything is computed anew from the inputs.
+ * [C]), dz [B, L, C] (with z only) and d_state_in (fp32; may be d_state_out).  Everything is computed anew from the inputs.
  * ld[0] .. ld[10]: pitches of x, dt, z, d_out, Bt, Ct, dx, ddt, dz, dB, dC; NULL: dense rows.  Alignment as above (dB, dC as Bt, Ct).
  * Scratch from the library's pool, stream-ordered: about 8 G N bytes a token for every 64 channels of a group, and the states of every
- * eighth token of the blocks that run at a time.  bf16: the products that make up dB and dC enter their sums over the channels with
+ * fourth token of the blocks that run at a time.  bf16: the products that make up dB and dC enter their sums over the channels with
  * eleven significant bits (tf32; fp32: as two such terms), the sums are fp32.  An empty call (B or L 0) clears dA, dD and d_dt_bias.
  * A product that is not finite makes dB and dC of its token NaN, and may make those of up to three tokens beside it NaN.
  * Outputs must not overlap inputs or one another.  Errors: as vig_ssm_fwd_*. */

@@ -94,7 +94,7 @@ template <typename T>
 int ssm_bwd_impl(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z, const void* bias,
                  const void* state_in, const void* d_out, const void* d_state_out, void* dx, void* ddt, void* dA, void* dB, void* dC, void* dD, void* dz,
                  void* d_bias, void* d_state_in, int B, int L, int C, int G, int N, const long long* ld, int softplus, int reverse, cudaStream_t stream) {
-    if (any_null(A) || !dA) return VIG_ERR_NULL_POINTER;
+    if (any_null(A) || !dA || (dz && !z)) return VIG_ERR_NULL_POINTER;
     if (B != 0 && L != 0 && (any_null(x, dt, Bt, Ct, d_out) || any_null(dx, ddt, dB, dC))) return VIG_ERR_NULL_POINTER;
     if (bad_sizes(B, L, C, G, N)) return VIG_ERR_BAD_DIM;
     Ssm<T> a = {};

@@ -69,6 +69,9 @@ def test_scan_arguments(lib, t):
     half = {i: e // 2 for i in (3, 4, 14, 15)}
     words = {i: 2 for i in (2, 5, 7, 8, 10, 13, 16, 18, 19)}
     _walk(f, ok, 20, (5, 6, 7, 8, 10, 16, 17, 18, 19), {**half, **words}, up(sizes), up(most))
+    bad = list(ok)
+    bad[6] = None                                      # the gate's gradient without a gate
+    assert f(*bad) == -1
     dense = [64, 64, 64, 64, 32, 32, 64, 64, 64, 32, 32]
     for i in range(11):
         ld = list(dense)
