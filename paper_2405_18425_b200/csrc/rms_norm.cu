@@ -90,7 +90,10 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
     }
     sum = over_row<TPR, false>(sum, red);
     float r = __frsqrt_rn(sum * a.inv_C + a.eps);
-    if (!(sum < 0x1p+120f) || sum < 0x1p-80f) {   // squares that overflow, or that underflow beside no eps: of the row over its largest value
+    // Squares that overflow, or that underflow with no eps beside them: of the row over its largest value or the root of eps, whichever is
+    // larger, so that neither the squares nor eps over its square leave the range.  (From an eps of 2^-60 on, squares that underflow
+    // are nothing beside it.)
+    if (!(sum < 0x1p+120f) || (sum < 0x1p-80f && a.eps < 0x1p-60f)) {
         float top = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -98,8 +101,9 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
             for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(s[i][j]));
         top = over_row<TPR, true>(top, red);
         if (top > 0.f && top < INFINITY && sum == sum) {
-            const float down = top > 1.f ? 0x1p-64f : 0x1p+64f;   // (either way twice, so that neither factor leaves the range)
-            const float in_range = top > 1.f ? top * 0x1p-64f : top * 0x1p+64f, part = 1.f / in_range;
+            const float unit = fmaxf(top, sqrtf(a.eps));
+            const float down = unit > 1.f ? 0x1p-64f : 0x1p+64f;   // (either way twice, so that neither factor leaves the range)
+            const float part = 1.f / (unit * down);
             sum = 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i)
@@ -109,7 +113,7 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
                     sum = fmaf(u, u, sum);
                 }
             sum = over_row<TPR, false>(sum, red);
-            const float e = a.eps * down * part;   // eps / top^2 in two steps
+            const float e = a.eps * down * part;   // eps / unit^2 in two steps
             r = __frsqrt_rn(sum * a.inv_C + e * down * part) * part * down;
         }
     }
