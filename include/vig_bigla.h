@@ -380,8 +380,10 @@ int vig_causal_conv_step_f32(const void* x, const void* w, const void* bias, voi
  * What a block begins with, over rows of C values:  s = x + residual,  out = s / sqrt(mean(s^2) + eps) * weight.
  * x, residual (or NULL for 0), out, sum_out (or NULL): [rows, C], weight: [C], all of the call's element type; rstd: FP32 [rows], what the
  * gradient needs, or NULL.  sum_out receives s, which the next block adds to; the norm is of s before that rounding.  fp32 inside; rows
- * whose squares leave the range of fp32 are summed over their largest value (or the root of eps, if that is larger).  eps >= 0.  C: a multiple of 8 (bf16) or 4 (fp32), at most
- * 16384.  16-byte alignment (rstd, scales: 4).  sum_out and out may each be x or residual, but not the same one.
+ * whose squares leave the range of fp32 are summed over their largest value (or the root of eps, if that is larger).  Without an eps, the
+ * rstd of a row of subnormal values may be beyond fp32 and is infinite then (out is right, the gradient not finite).  eps >= 0.  C: a
+ * multiple of 8 (bf16) or 4 (fp32), at most 16384.  16-byte alignment (rstd, scales: 4).  sum_out and out may each be x or residual, but
+ * not the same one.
  * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
 int vig_rms_norm_bf16(const void* x, const void* residual, const void* weight, void* out, void* sum_out, void* rstd,
                       long long rows, int C, float eps, void* stream);

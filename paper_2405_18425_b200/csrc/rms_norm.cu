@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
         for (int j = 0; j < N; ++j) sum = fmaf(s[i][j], s[i][j], sum);
     }
     sum = over_row<TPR, false>(sum, red);
-    float r = __frsqrt_rn(sum * a.inv_C + a.eps);
+    float r = __frsqrt_rn(sum * a.inv_C + a.eps), rstd = r;
     // Squares that overflow, or that underflow with no eps beside them: of the row over its largest value or the root of eps, whichever is
     // larger, so that neither the squares nor eps over its square leave the range.  (From an eps of 2^-60 on, squares that underflow
     // are nothing beside it.)
@@ -114,10 +114,19 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
                 }
             sum = over_row<TPR, false>(sum, red);
             const float e = a.eps * down * part;   // eps / unit^2 in two steps
-            r = __frsqrt_rn(sum * a.inv_C + e * down * part) * part * down;
+            r = __frsqrt_rn(sum * a.inv_C + e * down * part) * part;
+            rstd = r * down;
+            if (unit > 1.f) {
+                r = rstd;
+            } else {   // 1 / unit may leave the range, the result not: the row takes the other factor
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) s[i][j] *= down;
+            }
         }
     }
-    if (a.rstd && live && lane == 0) a.rstd[row] = r;
+    if (a.rstd && live && lane == 0) a.rstd[row] = rstd;
     float most = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
