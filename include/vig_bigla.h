@@ -306,7 +306,8 @@ int vig_group_norm_bwd_f32(const void* x, const void* weight, const void* bias, 
  * A: FP32 [C, N]; D, dt_bias: FP32 [C]; states: FP32 [B, C, N].  D, z, dt_bias: NULL for 0, no gate, 0.  state_in: h_0, or NULL for zero;
  * state_out: receives h_L, or NULL; may be state_in.  reverse != 0: the same from the last token to the first (state_in comes behind token
  * L, state_out is what stands at token 1).  out may be z or x or dt where it has that tensor's pitch, and overlaps no other input.
- * Domain: A, dt, dt_bias finite with delta_t A <= 0 for a state that stays bounded; larger is computed all the same.
+ * Domain: dt, dt_bias finite with delta_t A <= 0 for a state that stays bounded; larger is computed all the same.  A of minus infinity
+ * forgets the state at every token whose step size is not zero.
  * ld: the tensors may be slices of wider rows, as one projection writes them side by side: from row to row (token to token) ld[0] .. ld[5]
  * values of x, dt, z, out, Bt, Ct, sequence b beginning at row b L; NULL: dense rows.  A pitch is at least the row's width.
  * Alignment: x, dt, z, out 16 bytes, their pitches multiples of 16 bytes too; Bt and Ct that of their type only; fp32 arrays 4 bytes.

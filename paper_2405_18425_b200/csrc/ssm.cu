@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
         load_states<NS>(a.A + (long long)(at.c0 + ch + k) * a.N, live ? a.N : 0, n0, rate[k]);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            rate[k][i] = fmul2(rate[k][i], both(kLog2E));
+            rate[k][i] = rate_of2(rate[k][i]);
             h[k][i] = 0;
         }
         if (MODE == kMain && live) {
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(128) ssm_carry_kernel(Ssm<T> a, int NP) {
     if (b >= a.B) return;
     const int at = (int)(id - b * each), c = at / NP, n = at % NP;
     const bool there = n < a.N;
-    const float rate = there ? a.A[(long long)c * a.N + n] * kLog2E : 0.f;
+    const float rate = there ? rate_of(a.A[(long long)c * a.N + n]) : 0.f;
     const long long own = ((long long)b * a.C + c) * a.N + n;
     float* ends = a.ends + (long long)b * a.segs * each + at;
     const float* total = a.total + (long long)b * a.segs * a.C + c;
@@ -251,9 +251,11 @@ __global__ void __launch_bounds__(128) ssm_step_kernel(Ssm<T> a, float* state, i
     const float z = a.z ? to_f32(a.z[b * a.ldz + c]) : 0.f, skip = a.D ? a.D[c] : 0.f;
     const float delta = a.softplus ? softplus_of<T>(v) : v, in = delta * x;
     float y = 0.f;
+    const bool still = delta == 0.f;   // (keeps the state at any rate, one of minus infinity too)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        h[j] = fmaf(ex2(delta * (A[j] * kLog2E)), h[j], in * Bt[j]);
+        const float e = ex2(delta * (A[j] * kLog2E));
+        h[j] = fmaf(still ? 1.f : e, h[j], in * Bt[j]);
         y = fmaf(Ct[j], h[j], y);
     }
     if (live) {

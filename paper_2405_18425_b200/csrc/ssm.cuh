@@ -149,6 +149,15 @@ struct Place {
     }
 };
 
+// A log2 e, the rate of a decay 2^(rate delta), kept finite: beyond every bound it forgets the state at any step size, but at none (the tokens
+// that fill up a group of four have a step size of zero) it keeps it, instead of being infinity times zero.  A NaN stays one.
+__device__ __forceinline__ float finite_rate(float rate) { return isinf(rate) ? copysignf(3.402823466e+38f, rate) : rate; }
+__device__ __forceinline__ float rate_of(float A) { return finite_rate(A * kLog2E); }
+__device__ __forceinline__ f32x2 rate_of2(f32x2 A) {
+    float a, b;
+    unpack2(fmul2(A, both(kLog2E)), a, b);
+    return pack2(finite_rate(a), finite_rate(b));
+}
 // NS / 2 pairs of a lane's states of channel c; zero behind the last state.
 template <int NS>
 __device__ __forceinline__ void load_states(const float* p, int N, int n0, f32x2 (&h)[NS / 2]) {
@@ -195,7 +204,7 @@ __device__ __forceinline__ void store_pairs(float* p, const f32x2 (&v)[NS / 2]) 
 }
 // 2^v of a pair: from the special-function unit (relative error 2^-22, sixteen a clock and SM), or, for fp32 calls, whose sums show that
 // error, as arithmetic: 2 to the nearest whole number is put together from bits, 2^f for the rest, |f| <= 1/2, is a polynomial of least largest
-// relative error, 2^-28.9 (fitted like the logarithm's).  Below 2^-126 the result is 2^-126, a decay as good as none.  (A quarter of the
+// relative error, 2^-28.9 (fitted like the logarithm's).  Below 2^-126.5 the result is zero.  (A quarter of the
 // bf16 states this way, to relieve the special-function unit: 95 to 106 us for 64 x 196 x 1152; an eighth: 100.)
 __device__ __forceinline__ f32x2 exp2_special(f32x2 v) {
     float lo, hi;
@@ -204,7 +213,7 @@ __device__ __forceinline__ f32x2 exp2_special(f32x2 v) {
 }
 __device__ __forceinline__ float clamp_exponent(float v) {   // (a NaN stays one)
     float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(-126.f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(-127.f));
     asm("min.NaN.f32 %0, %0, %1;" : "+f"(y) : "f"(128.f));
     return y;
 }

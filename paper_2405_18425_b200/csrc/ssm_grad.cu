@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
             load_states<NS>(a.A + (long long)(at.c0 + ch + k) * a.N, live ? a.N : 0, n0, rate[k]);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                rate[k][i] = fmul2(rate[k][i], both(kLog2E));
+                rate[k][i] = rate_of2(rate[k][i]);
                 h[k][i] = g[k][i] = da[k][i] = 0;
             }
             if (live) {
