@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const bool live = ch + k < at.live;
-        load_states<NS>(a.A + (long long)(at.c0 + ch + k) * a.N, live ? a.N : 0, n0, rate[k]);
+        load_states<NS, MODE == kMain>(a.A + (long long)(at.c0 + ch + k) * a.N, live ? a.N : 0, n0, rate[k]);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             rate[k][i] = rate_of2(rate[k][i]);
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
         }
         if (MODE == kMain && live) {
             if (a.segs > 1) load_pairs<NS>(a.ends + slot + k * NP, h[k]);
-            else if (a.state_in) load_states<NS>(a.state_in + own + k * a.N, a.N, n0, h[k]);
+            else if (a.state_in) load_states<NS, false>(a.state_in + own + k * a.N, a.N, n0, h[k]);
         }
     }
     // element-wise: token et of a tile, channels ec .. ec + 3
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
     const T *px = a.x + r0 * a.ldx + g0, *pd = a.dt + r0 * a.lddt + g0, *pz = a.z + r0 * a.ldz + g0, *po = a.d_out + r0 * a.ldo + g0;
     T* out = a.out + r0 * a.ldo + g0;
     typename Four<T>::Raw rx = {}, rd = {}, rz = {}, ro = {};
-    Rows<T, NP, kTile, kThreads> rb, rc;
+    Rows<T, NP, kTile, kThreads, MODE == kMain> rb, rc;
     rb.start(a.Bt, a, a.ldB, at, t0);
     rc.start(a.Ct, a, a.ldC, at, t0);
     auto load = [&](int t) {   // a tile, and on to the next one
@@ -113,7 +113,8 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
             }
             if (MODE == kBoth) store4(&grad[et][ec], o);
             rb.put(rows_b);
-            if (MODE != kEnds) rc.put(rows_c);
+            if (MODE == kMain) rc.put_reduced(rows_c, a.N);
+            if (MODE == kBoth) rc.put(rows_c);
         }
         __syncthreads();
         if (t + kTile < t1) load(t + kTile);
@@ -192,7 +193,7 @@ __global__ void __launch_bounds__(128) ssm_carry_kernel(Ssm<T> a, int NP) {
     const int b = (int)(id / each);
     if (b >= a.B) return;
     const int at = (int)(id - b * each), c = at / NP, n = at % NP;
-    const bool there = n < a.N;
+    const bool there = n < a.N;   // (the others start every segment from zero)
     const float rate = there ? rate_of(a.A[(long long)c * a.N + n]) : 0.f;
     const long long own = ((long long)b * a.C + c) * a.N + n;
     float* ends = a.ends + (long long)b * a.segs * each + at;
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(128) ssm_carry_kernel(Ssm<T> a, int NP) {
         for (int i = 0; i < kAhead; ++i) {
             const int k = back ? a.segs - 1 - s - i : s + i;
             const bool in = s + i < a.segs;
-            add[i] = in ? p[k * each] : 0.f;
+            add[i] = in && there ? p[k * each] : 0.f;
             sum[i] = in ? total[(long long)k * a.C] : 0.f;
         }
 #pragma unroll
@@ -256,8 +257,9 @@ __global__ void __launch_bounds__(128) ssm_step_kernel(Ssm<T> a, float* state, i
     for (int j = 0; j < 4; ++j) {
         const float e = ex2(delta * (A[j] * kLog2E));
         h[j] = fmaf(still ? 1.f : e, h[j], in * Bt[j]);
-        y = fmaf(Ct[j], h[j], y);
+        if (WIDE || n0 + j < a.N) y = fmaf(Ct[j], h[j], y);
     }
+    if (WIDE && n0 >= a.N) y = 0.f;   // (where there is no state, an infinite delta x times zero is NaN)
     if (live) {
         if (WIDE && n0 < a.N) *reinterpret_cast<float4*>(s) = make_float4(h[0], h[1], h[2], h[3]);
         else

@@ -158,11 +158,17 @@ __device__ __forceinline__ f32x2 rate_of2(f32x2 A) {
     unpack2(fmul2(A, both(kLog2E)), a, b);
     return pack2(finite_rate(a), finite_rate(b));
 }
-// NS / 2 pairs of a lane's states of channel c; zero behind the last state.
-template <int NS>
+// NS / 2 pairs of a lane's states of channel c.  Behind the last state: zero, or that one again.
+//
+// Where outputs are read from the states, those that fill up the lanes' have the last one's rate and rows, Ct 2^-60 times as large, so that
+// they add less than a sum's rounding.  With zeros in their rows an infinite delta x (or one that has overflowed) would be NaN in them, and
+// out with it.  (8 x 4096 x 384 with sixteen states: 159 us as before; with a search for infinities and those states cleared, 171.)
+constexpr float kCopies = 0x1p-60f;
+template <int NS, bool COPIES>
 __device__ __forceinline__ void load_states(const float* p, int N, int n0, f32x2 (&h)[NS / 2]) {
+    const auto at = [&](int n) { return n < N ? p[n] : COPIES && N > 0 ? p[N - 1] : 0.f; };
 #pragma unroll
-    for (int i = 0; i < NS / 2; ++i) h[i] = pack2(n0 + 2 * i < N ? p[n0 + 2 * i] : 0.f, n0 + 2 * i + 1 < N ? p[n0 + 2 * i + 1] : 0.f);
+    for (int i = 0; i < NS / 2; ++i) h[i] = pack2(at(n0 + 2 * i), at(n0 + 2 * i + 1));
 }
 template <int NS>
 __device__ __forceinline__ void store_states(float* p, int N, int n0, const f32x2 (&h)[NS / 2]) {
@@ -246,8 +252,8 @@ __device__ __forceinline__ float over_quarters(float p0, float p1, float p2, flo
     return (lo ? k1 : k0) + __shfl_xor_sync(0xffffffffu, lo ? k0 : k1, 8);
 }
 
-// A tile's rows of Bt or Ct, loaded a tile ahead by all threads of a block: E values a thread.
-template <typename T, int NP, int kTile, int kThreads>
+// A tile's rows of Bt or Ct, loaded a tile ahead by all threads of a block: E values a thread.  Behind the last state: COPIES of it, or zero.
+template <typename T, int NP, int kTile, int kThreads, bool COPIES>
 struct Rows {
     static constexpr int E = (kTile * NP + kThreads - 1) / kThreads;
     const T* p[E];
@@ -256,8 +262,8 @@ struct Rows {
     __device__ __forceinline__ void start(const T* rows, const Ssm<T>& a, long long ld, const Place& at, int t0) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int i = threadIdx.x + e * kThreads;
-            p[e] = rows + a.row(at.b, t0 + i / NP) * ld + at.group * a.N + i % NP;
+            const int i = threadIdx.x + e * kThreads, n = i % NP;
+            p[e] = rows + a.row(at.b, t0 + i / NP) * ld + at.group * a.N + (COPIES ? min(n, a.N - 1) : n);
             from_f32(&v[e], 0.f);
         }
         pitch = a.reverse ? -ld : ld;
@@ -268,7 +274,7 @@ struct Rows {
         for (int e = 0; e < E; ++e) {
             const int i = threadIdx.x + e * kThreads;
             from_f32(&v[e], 0.f);
-            if (i < kTile * NP && i % NP < N && t + i / NP < last) v[e] = *p[e];   // (as it comes: a conversion would wait for it here)
+            if (i < kTile * NP && (COPIES || i % NP < N) && t + i / NP < last) v[e] = *p[e];   // (as it comes: a conversion would wait for it here)
         }
     }
     __device__ __forceinline__ void move(int tokens) {
@@ -280,6 +286,14 @@ struct Rows {
         for (int e = 0; e < E; ++e) {
             const int i = threadIdx.x + e * kThreads;
             if (i < kTile * NP) to[i] = to_f32(v[e]);
+        }
+    }
+    // copies reduced to kCopies of the value
+    __device__ __forceinline__ void put_reduced(float* to, int N) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = threadIdx.x + e * kThreads;
+            if (i < kTile * NP) to[i] = to_f32(v[e]) * (i % NP < N ? 1.f : kCopies);
         }
     }
 };

@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const bool live = ch + k < at.live;
-            load_states<NS>(a.A + (long long)(at.c0 + ch + k) * a.N, live ? a.N : 0, n0, rate[k]);
+            load_states<NS, false>(a.A + (long long)(at.c0 + ch + k) * a.N, live ? a.N : 0, n0, rate[k]);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 rate[k][i] = rate_of2(rate[k][i]);
@@ -104,8 +104,8 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                     load_pairs<NS>(a.ends + slot + k * NP, h[k]);
                     load_pairs<NS>(a.adjoint + slot + k * NP, g[k]);
                 } else {
-                    if (a.state_in) load_states<NS>(a.state_in + own + k * a.N, a.N, n0, h[k]);
-                    if (a.d_state_out) load_states<NS>(a.d_state_out + own + k * a.N, a.N, n0, g[k]);
+                    if (a.state_in) load_states<NS, false>(a.state_in + own + k * a.N, a.N, n0, h[k]);
+                    if (a.d_state_out) load_states<NS, false>(a.d_state_out + own + k * a.N, a.N, n0, g[k]);
                 }
             }
         }
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
         }
         __syncthreads();
         typename Four<T>::Raw rx = {}, rd = {}, rz = {}, ro = {};
-        Rows<T, NP, kTile, kThreads> rb, rc;
+        Rows<T, NP, kTile, kThreads, false> rb, rc;
         rb.start(a.Bt, a, a.ldB, at, t0);
         rc.start(a.Ct, a, a.ldC, at, t0);
         rc.move((tiles - 1) * kTile);
