@@ -9,9 +9,11 @@
 // (states in registers, decays in shared memory), and over them from behind.  64 x 196 x 1152 with 16 states, bf16: 454 us, bound by what it
 // issues (565 warp instructions for 32 tokens and channels, an instruction in 54 % of the cycles).  So the exponentials are computed twice, and nothing is divided or taken off again.
 // Sums over the states cross four lanes; sums over the channels, two for every state and token, are tensor-core products with a
-// matrix of zeros and ones (tf32 terms, one for bf16 calls, whose results are rounded to eight bits, and two for fp32), a quarter of
-// the shuffles' instructions.  What a block has summed over its channels goes through memory to a last launch that adds the blocks in order.
+// matrix of zeros and ones, a quarter of the shuffles' instructions: every product enters as two terms, of bf16 in bf16 calls (error 2^-17; a
+// training step of the size above 555 us, 550 with a single term of tf32, 2^-12, which shows where channels cancel), of tf32 in fp32 calls (2^-23).
+// What a block has summed over its channels goes through memory to a last launch that adds the blocks in order.
 #include "gdr.h"
+#include "mma.cuh"
 #include "ssm.cuh"
 
 namespace vig {
@@ -30,22 +32,36 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Adds up four values each over the lanes of equal lane / 4: values 0, 2 to column 2 p of rows g, g + 8, values 1, 3 to column 2 p + 1.
-// ones: 1.0f (as tf32) in lanes of lane / 4 == i.
-template <bool SPLIT>
-__device__ __forceinline__ void add_four(float (&d)[4], float v0, float v1, float v2, float v3, uint32_t b0, uint32_t b1) {
-    if constexpr (SPLIT) {
-        const float v[4] = {v0, v1, v2, v3};
+// Both of a pair as two bf16 terms each, side by side: the upper half of a number, and what is left, rounded (error 2^-17).
+__device__ __forceinline__ void two_terms(f32x2 v, uint32_t& t0, uint32_t& t1) {
+    float v0, v1, rest0, rest1;
+    unpack2(v, v0, v1);
+    const float hi0 = __uint_as_float(__float_as_uint(v0) & 0xffff0000u), hi1 = __uint_as_float(__float_as_uint(v1) & 0xffff0000u);
+    unpack2(neg_add2(pack2(hi0, hi1), v), rest0, rest1);
+    t0 = pack_bf16(hi0, rest0);
+    t1 = pack_bf16(hi1, rest1);
+}
+// Adds up two pairs of values each over the lanes of equal lane / 4: their first values to column 2 p of rows g, g + 8, their second ones to
+// column 2 p + 1.  b0, b1: ones in lanes of lane / 4 == 2 p, 2 p + 1.
+template <bool TF32>
+__device__ __forceinline__ void add_four(float (&d)[4], f32x2 v, f32x2 w, uint32_t b0, uint32_t b1) {
+    if constexpr (TF32) {
+        float f[4];
+        unpack2(v, f[0], f[1]);
+        unpack2(w, f[2], f[3]);
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            hi[i] = to_tf32(v[i]);
-            lo[i] = to_tf32(v[i] - __uint_as_float(hi[i]));
+            hi[i] = to_tf32(f[i]);
+            lo[i] = to_tf32(f[i] - __uint_as_float(hi[i]));
         }
         mma_tf32(d, hi[0], hi[2], hi[1], hi[3], b0, b1);
         mma_tf32(d, lo[0], lo[2], lo[1], lo[3], b0, b1);
     } else {
-        mma_tf32(d, to_tf32(v0), to_tf32(v2), to_tf32(v1), to_tf32(v3), b0, b1);
+        uint32_t t[4];   // (a register's two terms are neighbouring columns of A)
+        two_terms(v, t[0], t[2]);
+        two_terms(w, t[1], t[3]);
+        wmma16::mma_k16(d, t, b0, b1);
     }
 }
 
@@ -66,7 +82,8 @@ struct Smem {
 template <typename T, int NS, int K, int F, int BLOCKS>
 __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> a) {
     constexpr int NP = 4 * NS, P = NS / 2, kThreads = threads_of(K), kTile = tile_of(K), kWarps = 8 / K;
-    constexpr bool kSplit = sizeof(T) == 4;
+    constexpr bool kTf32 = sizeof(T) == 4;
+    constexpr uint32_t kOnes = kTf32 ? 0x3f800000u : 0x3f803f80u;
     extern __shared__ __align__(16) unsigned char smem_raw[];
     Smem<NS, K, F>& sm = *reinterpret_cast<Smem<NS, K, F>*>(smem_raw);
     pdl_wait();
@@ -80,8 +97,8 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
     uint32_t one0[4], one1[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        one0[i] = lg == 2 * i ? 0x3f800000u : 0u;
-        one1[i] = lg == 2 * i + 1 ? 0x3f800000u : 0u;
+        one0[i] = lg == 2 * i ? kOnes : 0u;
+        one1[i] = lg == 2 * i + 1 ? kOnes : 0u;
     }
     for (long long item = blockIdx.x; item < a.items; item += gridDim.x) {
         const Place at(a, item);
@@ -263,7 +280,7 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
 #pragma unroll
                 for (int j = F - 1; j >= 0; --j) {
                     f32x2 bt[P], ct[P], vb[P], vc[P];
-                    float d2[2 * K], gy[K], v[2 * NS];
+                    float d2[2 * K], gy[K];
                     load_floats<2 * K>(&sm.step[s + j][ch][0], d2);
                     load_floats<K>(&sm.dy[s + j][ch], gy);
                     load_pairs<NS>(&sm.rows_b[(s + j) * NP + n0], bt);
@@ -288,13 +305,10 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                         part[1][j % 4][k] = sum2(sb);
                     }
 #pragma unroll
-                    for (int i = 0; i < P; ++i) {
-                        unpack2(vb[i], v[2 * i], v[2 * i + 1]);
-                        unpack2(vc[i], v[NS + 2 * i], v[NS + 2 * i + 1]);
+                    for (int q = 0; q < NS / 2; ++q) {   // (a lane's values: NS of vb, then NS of vc)
+                        const f32x2 v = 2 * q < P ? vb[2 * q % P] : vc[2 * q % P], w = 2 * q + 1 < P ? vb[(2 * q + 1) % P] : vc[(2 * q + 1) % P];
+                        add_four<kTf32>(acc, v, w, one0[j % kTogether * (NS / 2) + q], one1[j % kTogether * (NS / 2) + q]);
                     }
-#pragma unroll
-                    for (int q = 0; q < NS / 2; ++q)
-                        add_four<kSplit>(acc, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], one0[j % kTogether * (NS / 2) + q], one1[j % kTogether * (NS / 2) + q]);
                     if (j % kTogether == 0) {
                         // lane 4 g + r: values 4 q .. + 3 of token j + r / (NS / 2), q = r % (NS / 2), of four of the eight lanes' channels; the
                         // other four are the neighbouring g's
