@@ -312,8 +312,9 @@ int vig_group_norm_bwd_f32(const void* x, const void* weight, const void* bias, 
  * values of x, dt, z, out, Bt, Ct, sequence b beginning at row b L; NULL: dense rows.  A pitch is at least the row's width.
  * Alignment: x, dt, z, out 16 bytes, their pitches multiples of 16 bytes too; Bt and Ct that of their type only; fp32 arrays 4 bytes.
  * C: a multiple of 8 G (bf16) or 4 G (fp32), at most 2^20; N <= 32; L <= 2^31 - 2^16.
- * fp32 inside for either type; decays of bf16 calls (and the single token's) from the special-function unit (relative error 2^-22).  Long sequences of few channels are cut
- * into segments that run side by side, with scratch from the library's pool; whether they are depends on B, C and L, and with it the last
+ * fp32 inside for either type; decays, softplus and sigmoid of bf16 calls, and a single token's decays of either type, from the
+ * special-function unit (decays: relative error 2^-22; elsewhere in fp32 calls 2^-24).  Long sequences of few channels are cut into segments that run side by side, with scratch from the library's pool;
+ * whether they are depends on all the sizes together, and with it the last
  * bits: the same call repeats them, a call of other sequences beside it may not.  L == 0 with a state_out copies state_in (or zeros) there.
  * Errors: NULL_POINTER, BAD_DIM, MISALIGNED, UNSUPPORTED, CUDA. */
 int vig_ssm_fwd_bf16(const void* x, const void* dt, const void* A, const void* Bt, const void* Ct, const void* D, const void* z,

@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(128) ssm_carry_kernel(Ssm<T> a, int NP) {
             if (s + i >= a.segs) break;
             const int k = back ? a.segs - 1 - s - i : s + i;
             p[k * each] = h;
-            h = fmaf(ex2(rate * sum[i]), h, add[i]);
+            h = fmaf(decay_of<T>(rate * sum[i]), h, add[i]);
         }
     }
 }
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(128) ssm_step_kernel(Ssm<T> a, float* state, i
     float y = 0.f;
     const bool still = delta == 0.f;   // (keeps the state at any rate, one of minus infinity too)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 4; ++j) {   // (decays of fp32 calls from the special-function unit too: as arithmetic they take a tenth of the time)
         const float e = ex2(delta * (A[j] * kLog2E));
         h[j] = fmaf(still ? 1.f : e, h[j], in * Bt[j]);
         if (WIDE || n0 + j < a.N) y = fmaf(Ct[j], h[j], y);

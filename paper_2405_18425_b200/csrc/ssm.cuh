@@ -243,6 +243,13 @@ __device__ __forceinline__ f32x2 decay2(f32x2 v) {
     if constexpr (sizeof(T) == 4) return exp2_arithmetic(v);
     else return exp2_special(v);
 }
+template <typename T>
+__device__ __forceinline__ float decay_of(float v) {
+    if constexpr (sizeof(T) == 2) return ex2(v);
+    float lo, hi;
+    unpack2(exp2_arithmetic(both(v)), lo, hi);
+    return lo;
+}
 // Sums over the four lanes of a channel of what they hold for four tokens: lane quarter q ends with token q's.
 __device__ __forceinline__ float over_quarters(float p0, float p1, float p2, float p3, int quarter) {
     const bool hi = quarter & 2, lo = quarter & 1;
