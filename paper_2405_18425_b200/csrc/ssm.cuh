@@ -59,17 +59,18 @@ __device__ __forceinline__ f32x2 exp_minus_abs(f32x2 v) {
     if constexpr (sizeof(T) == 2) return pack2(ex2(-kLog2E * fabsf(a)), ex2(-kLog2E * fabsf(b)));
     else return pack2(expf(-fabsf(a)), expf(-fabsf(b)));
 }
-// max(v, 0) + log(1 + u) with u = e^-|v|.  log(1 + u) / u on [0, 1]: polynomial of least largest relative error, 2^-25 (a fit of weighted
-// least squares, the weights raised where the error was large until it was level), so that small steps keep their digits.
+// max(v, 0) + log(1 + u) with u = e^-|v|.  log(1 + u) / u on [0, 1]: polynomial of least largest relative error among those that are one at zero,
+// so that small steps keep their digits, 2^-24.8 (a fit of weighted least squares, the weights raised where the error was large until it was level;
+// a coefficient rounded to fp32 and the higher ones fitted anew).
 __device__ __forceinline__ f32x2 softplus2(f32x2 v, f32x2 u) {
-    f32x2 p = ffma2(u, both(0.005232691299170256f), both(-0.029505226761102676f));
-    p = ffma2(u, p, both(0.07822593301534653f));
-    p = ffma2(u, p, both(-0.13663244247436523f));
-    p = ffma2(u, p, both(0.19106006622314453f));
-    p = ffma2(u, p, both(-0.2484298199415207f));
-    p = ffma2(u, p, both(0.3331909775733948f));
-    p = ffma2(u, p, both(-0.4999949336051941f));
-    p = ffma2(u, p, both(0.9999999403953552f));
+    f32x2 p = ffma2(u, both(0.005365422461181879f), both(-0.030068300664424896f));
+    p = ffma2(u, p, both(0.07920882850885391f));
+    p = ffma2(u, p, both(-0.13754187524318695f));
+    p = ffma2(u, p, both(0.1915384829044342f));
+    p = ffma2(u, p, both(-0.24857217073440552f));
+    p = ffma2(u, p, both(0.33321329951286316f));
+    p = ffma2(u, p, both(-0.49999648332595825f));
+    p = ffma2(u, p, both(1.f));
     float a, b;
     unpack2(v, a, b);
     return ffma2(u, p, pack2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
@@ -210,7 +211,7 @@ __device__ __forceinline__ void store_pairs(float* p, const f32x2 (&v)[NS / 2]) 
 }
 // 2^v of a pair: from the special-function unit (relative error 2^-22, sixteen a clock and SM), or, for fp32 calls, whose sums show that
 // error, as arithmetic: 2 to the nearest whole number is put together from bits, 2^f for the rest, |f| <= 1/2, is a polynomial of least largest
-// relative error, 2^-28.9 (fitted like the logarithm's).  Below 2^-126.5 the result is zero.  (A quarter of the
+// relative error, 2^-28 (fitted like the logarithm's).  Below 2^-126.5 the result is zero.  (A quarter of the
 // bf16 states this way, to relieve the special-function unit: 95 to 106 us for 64 x 196 x 1152; an eighth: 100.)
 __device__ __forceinline__ f32x2 exp2_special(f32x2 v) {
     float lo, hi;
@@ -229,9 +230,9 @@ __device__ __forceinline__ f32x2 exp2_arithmetic(f32x2 v) {
     v = pack2(clamp_exponent(a), clamp_exponent(b));
     const f32x2 whole = fadd2(v, both(12582912.f));   // 1.5 2^23: the nearest whole number in the last bits
     const f32x2 f = fadd2(v, neg_add2(whole, both(12582912.f)));
-    f32x2 p = ffma2(f, both(0.00015353361959569156f), both(0.0013398873852565885f));
-    p = ffma2(f, p, both(0.00961843691766262f));
-    p = ffma2(f, p, both(0.055503323674201965f));
+    f32x2 p = ffma2(f, both(0.0001532646274426952f), both(0.0013390806270763278f));
+    p = ffma2(f, p, both(0.009618505835533142f));
+    p = ffma2(f, p, both(0.05550359934568405f));
     p = ffma2(f, p, both(0.24022647738456726f));
     p = ffma2(f, p, both(0.6931471824645996f));
     p = ffma2(f, p, both(1.f));

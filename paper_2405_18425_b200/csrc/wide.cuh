@@ -42,7 +42,8 @@ __device__ __forceinline__ float reciprocal(float x) {   // one unit in the last
     return y;
 }
 constexpr float kLog2E = 1.4426950408889634f;
-// 1 / (1 + e^-z), relative error below 2^-20 where the result is a normal number: both steps from the special-function unit.
+// 1 / (1 + e^-z), both steps from the special-function unit: relative error below 2^-21 + |z| 2^-23.6 (the exponent's rounding; |z| counts where z
+// is negative) where the result is a normal number.
 __device__ __forceinline__ float sigmoid(float z) { return reciprocal(1.f + ex2(-kLog2E * z)); }
 
 }  // namespace vig
