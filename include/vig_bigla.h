@@ -327,8 +327,9 @@ int vig_ssm_fwd_f32(const void* x, const void* dt, const void* A, const void* Bt
  * (FP32 [C, N]), dB, dC ([B, L, G, N], sums over a group's channels in a fixed order) and, unless they are NULL, dD, d_dt_bias (FP32
  * [C]), dz [B, L, C] (with z only) and d_state_in (fp32; may be d_state_out).  Everything is computed anew from the inputs.
  * ld[0] .. ld[10]: pitches of x, dt, z, d_out, Bt, Ct, dx, ddt, dz, dB, dC; NULL: dense rows.  Alignment as above (dB, dC as Bt, Ct).
- * Scratch from the library's pool, stream-ordered: about 8 G N bytes a token for every 64 channels of a group, and the states of every
- * fourth token of the blocks that run at a time.  The products that make up dB and dC enter their sums over the channels with sixteen
+ * Scratch from the library's pool, stream-ordered: 8 G bytes a token for every 64 channels of a group and every state (N counts as 8, 16 or
+ * 32, the next one), and the states of every fourth token of the blocks that run at a time, 16 GiB at most (longer sequences are cut).
+ * The products that make up dB and dC enter their sums over the channels with sixteen
  * significant bits (fp32 calls: twenty-two), the sums are fp32.  An empty call (B or L 0) clears dA, dD and d_dt_bias.
  * A product that is not finite makes dB and dC of its token NaN, and may make those of up to three tokens beside it NaN.  What an infinite
  * delta_t x_t makes infinite by these formulas (ddt, dz, dA of its channel from that token on) may be NaN.

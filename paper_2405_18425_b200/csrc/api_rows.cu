@@ -2,6 +2,7 @@
 #include <cmath>
 
 #include "ssm.h"
+#include "test_hooks.h"
 
 namespace vig {
 namespace {
@@ -340,5 +341,12 @@ extern "C" {
 
 VIG_ROWS(__nv_bfloat16, bf16)
 VIG_ROWS(float, f32)
+
+size_t vig_test_ssm_bwd_scratch(int B, int L, int C, int G, int N) {
+    Ssm<float> a = {};   // (the same for either type)
+    a.B = B; a.L = L; a.C = C; a.G = G; a.N = N; a.per = C / G;
+    ssm_segments<float>(a, true);
+    return ssm_grad_scratch<float>(a, nullptr);
+}
 
 }  // extern "C"

@@ -293,6 +293,9 @@ cudaError_t walk(const Ssm<T>& a, cudaStream_t stream) {
 // Segments where whole sequences would leave SMs idle: as many as make one round of blocks (five an SM, in the gradient four), of 64 tokens or
 // more.  Two passes over the exponentials instead of one, so not where whole sequences fill half a round.  8 x 4096 x 384: 160 us, 176 with
 // four fifths of a round and a bit, 192 with four fifths, 167 with six fifths; 1 x 16384 x 768: 157, 189, 188, 163.
+// In the gradient segments are no longer than 16 GiB of kept states allow (28336 tokens with more than eight states where a whole round of blocks
+// runs), a tenth of the memory, at the price of the second pass: 32 x 16384 x 1152 22.5 ms in segments of 7 Ki, 18.7 whole.
+constexpr long long kMostKept = 16LL << 30;
 template <typename T>
 void ssm_segments(Ssm<T>& a, bool gradient) {
     a.blocks = (a.per + kCh - 1) / kCh;
@@ -301,6 +304,13 @@ void ssm_segments(Ssm<T>& a, bool gradient) {
     const long long most = (a.L + 63LL) / 64;
     if (segs > most) segs = most;
     if (segs < 1) segs = 1;
+    if (gradient) {
+        // bytes kept for a token by the blocks that run, were every segment long
+        const int padded = ssm_padded(a.N);
+        const long long each = kSsmChannels * (long long)padded * sizeof(float) / kSsmKept, running = 148LL * ssm_grad_blocks(padded);
+        const long long longest = kMostKept / (each * running) / kSsmTile * kSsmTile;
+        if (whole * a.L > kMostKept / each && (a.L + segs - 1) / segs > longest) segs = (a.L + longest - 1) / longest;
+    }
     long long seg = (a.L + segs - 1) / segs;
     seg = (seg + kSsmTile - 1) / kSsmTile * kSsmTile;
     a.seg = (int)(seg < kSsmTile ? kSsmTile : seg);

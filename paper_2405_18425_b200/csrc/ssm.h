@@ -7,6 +7,9 @@ namespace vig {
 constexpr int kSsmChannels = 64;   // of a block
 constexpr int kSsmTile = 16;       // segments are multiples of it, and it of the tokens that a block takes through its element-wise work together
 constexpr int kSsmMostN = 32;
+// The gradient's blocks of an SM, and how often they keep a channel's states: in front of every kSsmKept-th token.  A block keeps its segment's.
+constexpr int ssm_grad_blocks(int padded) { return padded == 32 ? 2 : 4; }
+constexpr int kSsmKept = 4;
 
 // A call of the selective scan.  Row t in walking order is token t, or L - 1 - t in a reverse call.  Null pointers: D, z, bias, the states,
 // dD, dz, dbias where the caller has none; what the call does not read or write.

@@ -456,9 +456,7 @@ __global__ void __launch_bounds__(256) ssm_grad_sums_kernel(Ssm<T> a, int NP, un
 // How the padded states of a channel are spread: channels of a lane, tokens taken together, blocks an SM.  64 x 196 x 1152, a training step:
 // 550 us; one channel, eight tokens, two blocks 615; two, eight, three 608; two, eight, two 594; two, four, three 592.
 template <int NS>
-struct Form { static constexpr int K = 2, F = 4, kBlocks = 4; };
-template <>
-struct Form<8> { static constexpr int K = 2, F = 4, kBlocks = 2; };
+struct Form { static constexpr int K = 2, F = kSsmKept, kBlocks = ssm_grad_blocks(4 * NS); };
 
 template <typename F>
 auto by_states(int NP, F f) { return NP == 8 ? f(Form<2>{}) : NP == 16 ? f(Form<4>{}) : f(Form<8>{}); }

@@ -44,6 +44,9 @@ void vig_test_expire_next_exchange(void);
  * both ends 16-byte aligned), 0 if it would leave them to a copy engine.  Launches nothing. */
 int vig_test_host_copy_usable(const void* host, size_t bytes);
 
+/* Bytes of scratch that vig_ssm_bwd_* takes from the pool for these sizes (which it accepts).  Launches nothing. */
+size_t vig_test_ssm_bwd_scratch(int B, int L, int C, int G, int N);
+
 #ifdef __cplusplus
 }
 #endif
