@@ -201,11 +201,6 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
             const int t = t0 + m * kTile;
             const bool there = mine && t + et < t1;
             const typename Four<T>::Raw cx = rx, cz = rz, co = ro;
-            if constexpr (F == kTile) {   // (on its way while the tile is prepared)
-                const float* from = kept + (long long)m * K * kThreads * NS;
-#pragma unroll
-                for (int k = 0; k < K; ++k) load_pairs<NS>(from + k * kThreads * NS, h[k]);
-            }
             {
                 f32x2 x[2], z[2], dy[2], delta[2], slope[2], bias[2];
                 widen4(cx, x);
@@ -243,11 +238,9 @@ __global__ void __launch_bounds__(threads_of(K), BLOCKS) ssm_grad_kernel(Ssm<T> 
                 if (t + s >= t1) continue;
                 f32x2 before[F][K][P];
                 float part[2][4][K];
-                if constexpr (F != kTile) {
-                    const float* from = kept + (long long)((m * kTile + s) / F) * K * kThreads * NS;
+                const float* from = kept + (long long)((m * kTile + s) / F) * K * kThreads * NS;
 #pragma unroll
-                    for (int k = 0; k < K; ++k) load_pairs<NS>(from + k * kThreads * NS, h[k]);
-                }
+                for (int k = 0; k < K; ++k) load_pairs<NS>(from + k * kThreads * NS, h[k]);
 #pragma unroll
                 for (int j = 0; j < F; ++j) {
                     f32x2 bt[P], ct[P];
