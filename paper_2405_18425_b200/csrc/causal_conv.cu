@@ -292,7 +292,7 @@ template <typename T>
 cudaError_t launch_conv_bwd(const Conv<T>& a, int K, int act, T* dw, T* dbias, cudaStream_t stream) {
     const cudaError_t e = by_width(K, act, Gradient<T>{a, stream});
     if (e != cudaSuccess || !a.part) return e;
-    return launch_column_sums<T>({a.part, (long long)a.B * a.pieces, a.C * (K + 1), a.C * K, a.C * (K + 1), dw, dbias, nullptr}, stream);
+    return launch_column_sums<T>({a.part, (long long)a.B * a.pieces, a.C * (K + 1), a.C * K, dw, dbias}, stream);
 }
 template <typename T>
 cudaError_t launch_conv_step(const Conv<T>& a, int K, int act, T* state, cudaStream_t stream) { return by_width(K, act, Step<T>{a, state, stream}); }

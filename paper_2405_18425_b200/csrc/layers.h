@@ -4,15 +4,14 @@
 
 namespace vig {
 
-// ---- sums over the rows of `part` [rows][columns] in a fixed order, to up to three results side by side: `first` columns to a, up to
-// `second` to b, the rest to c (each may be null) ----
+// ---- sums over the rows of `part` [rows][columns] in a fixed order, to two results side by side: `first` columns to a, the rest to b (either
+// may be null) ----
 template <typename T>
 struct ColumnSums {
     const float* part;
     long long rows;
-    int columns, first, second;
+    int columns, first;
     T *a, *b;
-    float* c;
 };
 template <typename T>
 cudaError_t launch_column_sums(const ColumnSums<T>& a, cudaStream_t stream);

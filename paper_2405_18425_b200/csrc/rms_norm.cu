@@ -284,10 +284,8 @@ __global__ void __launch_bounds__(32 * kRuns) column_sums_kernel(ColumnSums<T> a
     for (int i = 1; i < kRuns; ++i) s += part[i][lane];
     if (c < a.first) {
         if (a.a) from_f32(a.a + c, s);
-    } else if (c < a.second) {
-        if (a.b) from_f32(a.b + (c - a.first), s);
-    } else if (a.c) {
-        a.c[c - a.second] = s;
+    } else if (a.b) {
+        from_f32(a.b + (c - a.first), s);
     }
 }
 
@@ -360,7 +358,7 @@ cudaError_t launch_rms_norm_bwd(const RmsNormGrad<T>& a, T* dweight, cudaStream_
 #undef VIG_CALL
     }();
     if (e != cudaSuccess || !a.part) return e;
-    return launch_column_sums<T>({a.part, blocks, a.C, a.C, a.C, dweight, nullptr, nullptr}, stream);
+    return launch_column_sums<T>({a.part, blocks, a.C, a.C, dweight, nullptr}, stream);
 }
 
 template <typename T>
