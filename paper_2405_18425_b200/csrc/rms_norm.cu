@@ -291,6 +291,8 @@ __global__ void __launch_bounds__(32 * kRuns) column_sums_kernel(ColumnSums<T> a
 
 // What a row of nv vectors takes: a warp up to 128 of them, then as many threads as hold four each.
 int threads_of_row(int nv) { return nv <= 128 ? 32 : nv <= 512 ? 128 : nv <= 1024 ? 256 : nv <= 2048 ? 512 : 1024; }
+template <typename T>
+constexpr int kMostThreads = kRmsMostC / Vec<T>::N / 4;   // 512 for bf16
 
 template <typename T, int V, int TPR>
 cudaError_t norm_of(const RmsNorm<T>& a, int out, cudaStream_t stream) {
@@ -328,7 +330,7 @@ cudaError_t grad_of(const RmsNormGrad<T>& a, int blocks, cudaStream_t stream) {
             }                                                                   \
         case 256: CALL(4, 256);                                                 \
         case 512: CALL(4, 512);                                                 \
-        default: CALL(4, 1024);                                                 \
+        default: CALL(4, kMostThreads<T>);                                      \
     }
 
 }  // namespace

@@ -120,11 +120,9 @@ __device__ __forceinline__ void load_floats(const float* p, float (&v)[M]) {
 }
 template <int M>
 __device__ __forceinline__ void store_floats(float* p, const float (&v)[M]) {
+    static_assert(M <= 2, "one or two channels a lane");
     if constexpr (M == 1) *p = v[0];
-    else if constexpr (M == 2) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
-    else
-#pragma unroll
-        for (int i = 0; i < M / 4; ++i) *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    else *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
 }
 // delta, delta x of two neighbouring channels
 __device__ __forceinline__ void put_step(float (*to)[2], f32x2 delta, f32x2 in) {
