@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(threads_of(K)) ssm_kernel(Ssm<T> a) {
         }
         if (MODE == kMain && live) {
             if (a.segs > 1) load_pairs<NS>(a.ends + slot + k * NP, h[k]);
-            else if (a.state_in) load_states<NS, false>(a.state_in + own + k * a.N, a.N, n0, h[k]);
+            else if (a.state_in) load_states<NS, true>(a.state_in + own + k * a.N, a.N, n0, h[k]);
         }
     }
     // element-wise: token et of a tile, channels ec .. ec + 3
@@ -193,7 +193,10 @@ __global__ void __launch_bounds__(128) ssm_carry_kernel(Ssm<T> a, int NP) {
     const int b = (int)(id / each);
     if (b >= a.B) return;
     const int at = (int)(id - b * each), c = at / NP, n = at % NP;
-    const bool there = n < a.N;   // (the others start every segment from zero)
+    // behind the last state, the outputs' launch has that one again, and the gradient's zero
+    const bool there = n < a.N, gradient = gridDim.y == 2;
+    if (!there && !gradient) return;
+    const bool last = n == a.N - 1 && n != NP - 1 && !gradient;
     const float rate = there ? rate_of(a.A[(long long)c * a.N + n]) : 0.f;
     const long long own = ((long long)b * a.C + c) * a.N + n;
     float* ends = a.ends + (long long)b * a.segs * each + at;
@@ -217,6 +220,9 @@ __global__ void __launch_bounds__(128) ssm_carry_kernel(Ssm<T> a, int NP) {
             if (s + i >= a.segs) break;
             const int k = back ? a.segs - 1 - s - i : s + i;
             p[k * each] = h;
+            if (last)
+#pragma unroll 1
+                for (int more = 1; more < NP - n; ++more) p[k * each + more] = h;
             h = fmaf(decay_of<T>(rate * sum[i]), h, add[i]);
         }
     }

@@ -159,7 +159,7 @@ __device__ __forceinline__ f32x2 rate_of2(f32x2 A) {
 }
 // NS / 2 pairs of a lane's states of channel c.  Behind the last state: zero, or that one again.
 //
-// Where outputs are read from the states, those that fill up the lanes' have the last one's rate and rows, Ct 2^-60 times as large, so that
+// Where outputs are read from the states, those that fill up the lanes' are the last one again, Ct 2^-60 times as large, so that
 // they add less than a sum's rounding.  With zeros in their rows an infinite delta x (or one that has overflowed) would be NaN in them, and
 // out with it.  (8 x 4096 x 384 with sixteen states: 159 us as before; with a search for infinities and those states cleared, 171.)
 constexpr float kCopies = 0x1p-60f;
