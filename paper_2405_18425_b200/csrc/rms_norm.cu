@@ -6,7 +6,7 @@
 // Memory bounds all of it: a row stays in the registers of its threads (a warp up to 128 vectors of 16 bytes, four vectors a thread at
 // most) between its sum and its use, so every value crosses memory once in and once out.  The sum of squares and the mean of the
 // gradient are fp32; the norm is of the sum before it is rounded to the call's type, and the gradient of the sum as it was stored.
-// 12544 x 768 bf16 with residual, 8 bits: 13.9 us (0.75 of a copy's rate); 32768 x 192 fp32: 16 us, its gradient 18.
+// 12544 x 768 bf16 with residual, 8 bits: 14.5 us (0.72 of a copy's rate); 32768 x 192 fp32: 16 us, its gradient 18.
 #include "gdr.h"
 #include "layers.h"
 #include "wide.cuh"
@@ -127,14 +127,22 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
         }
     }
     if (a.rstd && live && lane == 0) a.rstd[row] = rstd;
-    float most = 0.f;
+    // In 8 bits rstd's own digits fall out of out / scale: the row is multiplied by its power of two, which is exact, and the rest of it goes to
+    // the scale alone, so that a code comes of s w, the largest |s w| and two roundings.
+    float by = r, rest = 1.f;
+    if (OUT != 0) {
+        uint32_t bits = __float_as_uint(r) & 0x7f800000u;   // (infinity of a NaN, which the rest then is)
+        if (bits == 0 && r > 0.f) bits = 0x00800000u;
+        by = __uint_as_float(bits);
+        rest = r * __uint_as_float(0x7f000000u - bits);     // r / by
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int v = lane + i * TPR;
         float w[N];
         widen(v < nv ? load16(a.weight + v * N) : make_uint4(0, 0, 0, 0), w, (const T*)nullptr);
 #pragma unroll
-        for (int j = 0; j < N; ++j) s[i][j] = s[i][j] * r * w[j];
+        for (int j = 0; j < N; ++j) s[i][j] = s[i][j] * by * w[j];
         if constexpr (OUT == 0) {
             if (live && v < nv) store16(a.out + at + v * N, narrow(s[i], (const T*)nullptr));
         }
@@ -142,7 +150,7 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
     if constexpr (OUT != 0) {
         constexpr int kLanes = 128 / N;   // of a block of 128 values
         const int blocks = OUT == 2 ? (a.C + 127) / 128 : 1;
-        float each[V];
+        float each[V], most = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             float m = 0.f;
@@ -161,14 +169,24 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
         for (int i = 0; i < V; ++i) {
             const int v = lane + i * TPR;
             // the smallest normal number at least, so that a block of zeros divides by it too
-            const float m = OUT == 1 ? most : each[i];
-            const float scale = max_or_nan(__fdiv_rn(m, 448.f), 1.17549435e-38f), over = __fdiv_rn(1.f, scale);
+            constexpr float kLeast = 1.17549435e-38f;
+            const float m = OUT == 1 ? most : each[i], scale = max_or_nan(__fdiv_rn(m, 448.f) * rest, kLeast);
+            const float over = scale == kLeast ? rest * 0x1p126f : __fdiv_rn(448.f, m);   // (of a NaN a NaN)
             if (!live || v >= nv) continue;
-            float q[N];   // the quotient by a product and a correction of what is left (divisions took a quarter of the time)
+            // bf16 calls: and what is left of 448 s w behind q m, exactly, so that middles between two codes, which their few digits meet, stay
+            // middles (12544 x 768: 14.5 us instead of 13.8; without it one code in 800 000 was the other of two neighbours)
+            float q[N];
+            const bool exactly = sizeof(T) == 2 && over > 0.f && m < 0x1p+100f;
+            const f32x2 quick = pack2(over, over), small = pack2(over * (1.f / 448.f), over * (1.f / 448.f)), most2 = pack2(m, m), less2 = pack2(-m, -m);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                q[j] = s[i][j] * over;
-                if (over > 0.f) q[j] = fmaf(fmaf(-q[j], scale, s[i][j]), over, q[j]);
+            for (int j = 0; j < N; j += 2) {
+                const f32x2 t = pack2(s[i][j], s[i][j + 1]);
+                f32x2 y = fmul2(t, quick);
+                if (exactly) {
+                    const f32x2 p = fmul2(y, less2), rounded = ffma2(y, most2, p);
+                    y = ffma2(ffma2(rounded, pack2(-1.f, -1.f), ffma2(t, pack2(448.f, 448.f), p)), small, y);
+                }
+                unpack2(y, q[j], q[j + 1]);
             }
             unsigned char* p = a.q + at + v * N;
             if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(e4m3x4(q[0], q[1], q[2], q[3]), e4m3x4(q[4], q[5], q[6], q[7]));
