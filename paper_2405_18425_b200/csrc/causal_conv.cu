@@ -5,7 +5,7 @@
 //
 // Memory bounds it: a thread walks over a piece of a sequence with the 16-byte vectors of its channels, the last K values of x (in the
 // gradient of g too) in registers, so a value is read once, but for the K - 1 tokens beside a piece.  8 x 4096 x 384 bf16, K 4: 17 us (0.45 of a
-// copy's rate); 64 x 196 x 1152: 20 us, its gradient 51 (248 registers, two blocks an SM) and 9 for the filters' last sums.
+// copy's rate); 64 x 196 x 1152: 19 us, its gradient 49 (248 registers, two blocks an SM) and 5 for the filters' last sums.
 #include "layers.h"
 #include "wide.cuh"
 

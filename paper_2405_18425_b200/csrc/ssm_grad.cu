@@ -6,8 +6,9 @@
 //
 // A block walks forward over its tokens and keeps the state in front of every few of them (scratch of its own: the grid is what runs at a
 // time and takes one piece of work after another), then backward: decays and states of those few tokens once more, this time kept on chip
-// (states in registers, decays in shared memory), and over them from behind.  64 x 196 x 1152 with 16 states, bf16: 454 us, bound by what it
-// issues (565 warp instructions for 32 tokens and channels, an instruction in 54 % of the cycles).  So the exponentials are computed twice, and nothing is divided or taken off again.
+// (states in registers, decays in shared memory), and over them from behind.  64 x 196 x 1152 with 16 states, bf16: 459 us, bound by what it
+// issues (570 warp instructions for 32 tokens and channels, an instruction in about 54 % of the cycles).  So the exponentials are computed twice, and
+// nothing is divided or taken off again.
 // Sums over the states cross four lanes; sums over the channels, two for every state and token, are tensor-core products with a
 // matrix of zeros and ones, a quarter of the shuffles' instructions: every product enters as two terms, of bf16 in bf16 calls (error 2^-17; a
 // training step of the size above 555 us, 550 with a single term of tf32, 2^-12, which shows where channels cancel), of tf32 in fp32 calls (2^-23).
@@ -446,8 +447,8 @@ __global__ void __launch_bounds__(256) ssm_grad_sums_kernel(Ssm<T> a, int NP, un
     }
 }
 
-// How the padded states of a channel are spread: channels of a lane, tokens taken together, blocks an SM.  64 x 196 x 1152, a training step:
-// 550 us; one channel, eight tokens, two blocks 615; two, eight, three 608; two, eight, two 594; two, four, three 592.
+// How the padded states of a channel are spread: channels of a lane, tokens taken together, blocks an SM.  64 x 196 x 1152, a training step
+// (with a single term of tf32): 550 us; one channel, eight tokens, two blocks 615; two, eight, three 608; two, eight, two 594; two, four, three 592.
 template <int NS>
 struct Form { static constexpr int K = 2, F = kSsmKept, kBlocks = ssm_grad_blocks(4 * NS); };
 
