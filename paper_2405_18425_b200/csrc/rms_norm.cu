@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(threads_of_block(TPR)) rms_norm_kernel(RmsNorm
             // bf16 calls: and what is left of 448 s w behind q m, exactly, so that middles between two codes, which their few digits meet, stay
             // middles (12544 x 768: 14.5 us instead of 13.8; without it one code in 800 000 was the other of two neighbours)
             float q[N];
-            const bool exactly = sizeof(T) == 2 && over > 0.f && m < 0x1p+100f;
+            const bool exactly = sizeof(T) == 2 && scale != kLeast && over > 0.f && m < 0x1p+100f;
             const f32x2 quick = pack2(over, over), small = pack2(over * (1.f / 448.f), over * (1.f / 448.f)), most2 = pack2(m, m), less2 = pack2(-m, -m);
 #pragma unroll
             for (int j = 0; j < N; j += 2) {
